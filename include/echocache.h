@@ -53,7 +53,8 @@ typedef enum {
     ECHO_ERR_CUDA = 4,         /* a CUDA call or launch failed */
     ECHO_ERR_NONFINITE = 5,    /* device flag: NaN/Inf met in a score or amax */
     ECHO_ERR_TIMEOUT = 6,      /* device flag: a bounded device wait gave up */
-    ECHO_ERR_UNSUPPORTED = 7   /* no sm_103a device */
+    ECHO_ERR_UNSUPPORTED = 7,  /* no sm_103a device */
+    ECHO_ERR_PAGE = 8          /* device flag: a page table does not lead to a page of the pool */
 } echo_status;
 
 typedef enum { ECHO_BF16 = 0, ECHO_F32 = 1 } echo_dtype;
@@ -105,7 +106,7 @@ const char *echo_status_str(echo_status s);
 
 /* Synchronises `stream`, then reads and clears the device error flag shared by
  * every kernel of this library on the current device.  Returns ECHO_OK, the
- * flagged error (ECHO_ERR_NONFINITE, ECHO_ERR_TIMEOUT) or ECHO_ERR_CUDA if the
+ * flagged error (ECHO_ERR_NONFINITE, ECHO_ERR_TIMEOUT, ECHO_ERR_PAGE) or ECHO_ERR_CUDA if the
  * synchronisation itself failed. */
 echo_status echo_get_device_error(echo_stream_t stream);
 
@@ -435,6 +436,85 @@ echo_status echo_cache_dequant(const int8_t *q, const float *scale, const int32_
                                int32_t n_rows, int32_t D, void *dst, echo_dtype dt,
                                echo_stream_t stream);
 
+/* ---- paged key/value cache (this build's addition: generation in chunks) ----
+ *
+ * A clip that is generated chunk by chunk keeps the keys and values of its earlier
+ * tokens.  They stand in pages of page_tokens tokens, taken from one pool that many
+ * sequences share: token p of sequence b is slot p mod page_tokens of page
+ * table[b, p / page_tokens].  A page holds its keys and then its values, head by head,
+ * so that a head's tokens lie side by side.  kind ECHO_CACHE_BF16 keeps the values;
+ * ECHO_CACHE_INT8 keeps codes with one scale per token and head (Q of
+ * echo_cache_quant over a head's d values), for keys and values apart.
+ * Pages need no initial contents: nothing at or past a sequence's length is used. */
+typedef struct {
+    int32_t kind;          /* ECHO_CACHE_INT8 or ECHO_CACHE_BF16 */
+    int32_t n_pages;       /* >= 1; 2 n_pages H < 2^31 - 1 */
+    int32_t page_tokens;   /* 16, 32, 64 or 128 */
+    int32_t H, d;          /* key/value heads; d 64 or 128 */
+    void *pages;           /* int8 or bf16 [n_pages, 2, H, page_tokens, d], 16-byte aligned */
+    float *scale;          /* INT8: f32 [n_pages, 2, H, page_tokens], 16-byte aligned; else unused */
+} echo_kv_pool;
+
+/* The sequences of one call, in device memory (int32, 4-byte aligned).  Rows
+ * row0[b] .. row0[b + 1] - 1 of the call's tensors are sequence b's new rows, n_b of
+ * them (none is allowed), at its last positions: row row0[b] + i at position
+ * len[b] - n_b + i, len counting the new rows.  row0 ascends from 0; rows at or past
+ * row0[n_seqs] belong to no sequence and are neither read nor written. */
+typedef struct {
+    const int32_t *table;  /* [n_seqs, max_pages]; read up to the page of len[b] - 1 */
+    const int32_t *len;    /* [n_seqs], >= 0 */
+    const int32_t *row0;   /* [n_seqs + 1] */
+    int32_t n_seqs, max_pages;
+    int32_t n_rows;        /* rows of the call's tensors, >= row0[n_seqs] */
+    int32_t max_rows;      /* about the most rows of one sequence: it chooses between kernels
+                            * and their orders of sums; the results are right for any value */
+} echo_kv_batch;
+
+/* The new rows' keys and values into the pages: k, v [n_rows, ld] of dtype t (head h at
+ * columns h d ..; ld a multiple of 8), rounded to bf16 (BF16) or quantised (INT8).
+ * Rows at a position below 0 are left out.  A non-finite head's row of an INT8 pool gets
+ * codes 0 and its |maximum| as scale, and sets the NONFINITE device flag; a position
+ * whose table entry is no page of the pool, or lies past max_pages, sets the PAGE flag
+ * and is left out.  No two sequences write the same page slot.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
+echo_status echo_kv_write(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *k,
+                          const void *v, int64_t ld, echo_dtype t, echo_stream_t stream);
+
+/* The cached keys and values of the positions that the batch's rows stand at, into
+ * k, v [n_rows, ld] of dtype t: the bf16 values, or float(code) * scale in fp32, rounded
+ * to nearest even for BF16.  Whole sequences: n_b = len[b].  Rows at a position below 0,
+ * or at one that sets the PAGE flag (echo_kv_write), are zeros.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
+echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, void *k, void *v,
+                         int64_t ld, echo_dtype t, echo_stream_t stream);
+
+/* Attention of the new rows over their sequences' pages.  Head h of row r, at position p
+ * of sequence b, with g = h / (Hq / H):
+ *   out[r, h] = sum_{j < top} softmax_j(q[r, h] . k_b[j, g] / sqrt(d)) v_b[j, g]
+ *   top = len[b]                                                causal_block 0
+ *       = p < 0 ? 0 : min(len[b], (p / causal_block + 1) causal_block)    else
+ * causal_block 1 is token-by-token causality, the tokens of a frame make it causal frame
+ * by frame, and with 0 the rows may be queries of any other kind (cross-attention to n_b
+ * rows of any number).  A row that sees no key gives zeros.
+ *   q bf16 [n_rows, ldq], out bf16 [n_rows, ldo]; Hq a multiple of H, Hq / H <= 128;
+ *   ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
+ *   scales multiply scores and weights in fp32); sums, maxima and rescaling are fp32; the
+ *   softmax weights (INT8: times the value's scale) are rounded to bf16 for the product
+ *   with the values.
+ *   workspace >= echo_kv_attention_workspace_size bytes, 256-byte aligned; it holds
+ *   nothing between calls, and calls that may overlap each need their own.
+ * A page that sets the PAGE flag is read as page 0: its sequence's result means nothing.
+ * The same call gives the same bits every time.
+ * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA, UNSUPPORTED; TIMEOUT, PAGE device flags. */
+echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *q,
+                              int64_t ldq, int32_t Hq, int32_t causal_block, void *out, int64_t ldo,
+                              void *workspace, size_t ws_bytes, echo_stream_t stream);
+
+/* Bytes of device workspace that echo_kv_attention needs with this pool, batch and Hq (by
+ * their sizes alone); 0 for sizes that it refuses. */
+size_t echo_kv_attention_workspace_size(const echo_kv_pool *pool, const echo_kv_batch *batch,
+                                        int32_t Hq);
+
 /* ---- single kernels of echo_block_step, exported so that each can be
  *      checked and timed on its own ---- */
 
@@ -483,7 +563,8 @@ typedef enum {
     ECHO_K_LAYERNORM = 4, ECHO_K_GEMM = 5, ECHO_K_ATTENTION = 6, ECHO_K_QUANT = 7,
     ECHO_K_DEQUANT = 8, ECHO_K_MERGE = 9, ECHO_K_STEP_DELTA = 10, ECHO_K_UNIFORM = 11,
     ECHO_K_REF_SCAN = 12, ECHO_K_REF_ALLOC = 13, ECHO_K_REF_STORE = 14, ECHO_K_CACHE_COPY = 15,
-    ECHO_K_MERGE_QUANT = 16, ECHO_K_COUNT = 17
+    ECHO_K_MERGE_QUANT = 16, ECHO_K_KV_WRITE = 17, ECHO_K_KV_READ = 18,
+    ECHO_K_KV_ATTENTION = 19, ECHO_K_COUNT = 20
 } echo_kernel_kind;
 
 /* Number of kernels this library has launched in this process (all devices). */
@@ -503,7 +584,7 @@ echo_status echo_profile_enable(int32_t on);
  * bytes); QUANT, DEQUANT, MERGE (rows, D, 0); ENERGY (T, frames, n_fft); STEP_DELTA (n, element bytes, 0)
  * for the reduction and (0, 0, blocks) for its final combine; UNIFORM (NT, K, 0);
  * REF_SCAN, REF_ALLOC, REF_STORE, CACHE_COPY (rows, D, 0); MERGE_QUANT (NT, D, K active
- * rows). */
+ * rows); KV_WRITE, KV_READ (rows, H d, 0); KV_ATTENTION (rows, Hq d, sequences). */
 int32_t echo_profile_read(int32_t max, int32_t *kinds, int64_t *m, int64_t *n, int64_t *k,
                           float *ms);
 

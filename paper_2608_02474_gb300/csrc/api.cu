@@ -172,7 +172,7 @@ extern "C" const char *echo_kernel_name(int32_t kind) {
         "layernorm_gather",   "gemm_tcgen05", "attention",    "quant_scatter",
         "dequant_gather",     "dequant_merge", "step_delta",   "uniform_select",
         "ref_scan",           "ref_alloc",     "ref_store",    "cache_copy",
-        "merge_quant"};
+        "merge_quant",        "kv_write",      "kv_read",      "kv_attention"};
     if (kind < 0 || kind >= ECHO_K_COUNT) return "unknown";
     return names[kind];
 }
@@ -187,6 +187,7 @@ extern "C" const char *echo_status_str(echo_status s) {
         case ECHO_ERR_NONFINITE: return "ECHO_ERR_NONFINITE";
         case ECHO_ERR_TIMEOUT: return "ECHO_ERR_TIMEOUT";
         case ECHO_ERR_UNSUPPORTED: return "ECHO_ERR_UNSUPPORTED";
+        case ECHO_ERR_PAGE: return "ECHO_ERR_PAGE";
     }
     return "ECHO_ERR_UNKNOWN";
 }

@@ -1,0 +1,254 @@
+// The paged key/value cache: new rows written into pages (rounded to bf16, or
+// quantised to int8 with a scale per token and head) and cached rows read back.
+//
+// Both are one pass: a value is read once and written once, and the time is that of
+// the bytes.  A warp takes one row's next 32 * U pieces of 16 bytes, so that its loads
+// are all in flight before the first is used, and finds the row's place in the pool
+// meanwhile.  A head's values lie in neighbouring lanes (d / 8 or d / 16 of them), which
+// gives its maximum by that many lanes' shuffles.
+#include "kv_pages.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kUnroll = 4;
+
+template <typename T>
+struct Piece8 {   // 8 values as they are loaded
+    uint4 v[sizeof(T) / 2];
+    ECHO_DEV void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+    }
+    ECHO_DEV void values(float *f) const {
+        if constexpr (sizeof(T) == 2) {
+            unpack8_bf16(v[0], f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f[4 * i] = __uint_as_float(v[i].x);
+                f[4 * i + 1] = __uint_as_float(v[i].y);
+                f[4 * i + 2] = __uint_as_float(v[i].z);
+                f[4 * i + 3] = __uint_as_float(v[i].w);
+            }
+        }
+    }
+};
+
+// rows' keys and values into the pages: piece c of a row is 8 values of head
+// (c mod (H d / 8)) / (d / 8), of the keys first and then of the values
+template <typename T, bool INT8, int D>
+__global__ void __launch_bounds__(kThreads)
+kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, const T *__restrict__ v,
+                int64_t ld, int *err) {
+    pdl_enter();
+    constexpr int LPH = D / 8;                        // lanes of a head
+    const int lane = threadIdx.x & 31;
+    const int half = pool.H * LPH, C = 2 * half;      // pieces of a row
+    const int tasks = (C + 32 * kUnroll - 1) / (32 * kUnroll);
+    PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
+    for (; walk.below(b.n_rows); walk.next()) {
+        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * kUnroll + lane;
+        Piece8<T> in[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + 32 * u;
+            if (c < C) in[u].load((c < half ? k : v) + r * ld + (c < half ? c : c - half) * 8);
+        }
+        const int seq = kv_seq_of_row(b, r);
+        if (seq < 0) continue;
+        const int64_t p = (int64_t)b.len[seq] - b.row0[seq + 1] + r;
+        if (p < 0) continue;
+        const int64_t at = kv_place(pool, b, seq, p, err);
+        if (at < 0) continue;
+        const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + 32 * u;
+            const int kv = c >= half, ch = kv ? c - half : c;
+            const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
+            float f[8];
+            if (c < C) in[u].values(f);
+            if constexpr (INT8) {
+                // the largest |value| as fp32 bits: infinity above every number, NaN above it
+                uint32_t a = 0;
+                if (c < C) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+                }
+#pragma unroll
+                for (int o = LPH / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+                if (c >= C) continue;
+                const bool bad = a >= 0x7F800000u;
+                const float amax = __uint_as_float(a);
+                const float inv = !bad && amax > 0.f ? __fdiv_rn(127.f, amax) : 0.f;
+                *reinterpret_cast<uint2 *>(pool.pages + vec * D + (ch % LPH) * 8) =
+                    bad ? make_uint2(0, 0) : quant8(f, inv);
+                if (ch % LPH == 0) {
+                    pool.scale[vec] = !bad ? __fdiv_rn(amax, 127.f)
+                                           : a > 0x7F800000u ? __int_as_float(0x7fc00000) : INFINITY;
+                    if (bad) echo_flag_error(err, ECHO_ERR_NONFINITE);
+                }
+            } else if (c < C) {
+                *reinterpret_cast<uint4 *>(pool.pages + (vec * D + (ch % LPH) * 8) * 2) =
+                    sizeof(T) == 2 ? in[u].v[0] : pack8_bf16(f);
+            }
+        }
+    }
+}
+
+// cached rows back: piece c of a row is 16 bytes of the cache, EP values
+template <typename T, bool INT8, int D>
+__global__ void __launch_bounds__(kThreads)
+kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restrict__ v, int64_t ld,
+               int *err) {
+    pdl_enter();
+    constexpr int EP = INT8 ? 16 : 8, LPH = D / EP;
+    const int lane = threadIdx.x & 31;
+    const int half = pool.H * LPH, C = 2 * half;
+    const int tasks = (C + 32 * kUnroll - 1) / (32 * kUnroll);
+    PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
+    for (; walk.below(b.n_rows); walk.next()) {
+        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * kUnroll + lane;
+        const int seq = kv_seq_of_row(b, r);
+        if (seq < 0) continue;
+        const int64_t p = (int64_t)b.len[seq] - b.row0[seq + 1] + r;
+        const int64_t at = p < 0 ? -1 : kv_place(pool, b, seq, p, err);   // -1: zeros
+        const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
+        uint4 in[kUnroll];
+        float sc[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + 32 * u;
+            in[u] = make_uint4(0, 0, 0, 0);
+            sc[u] = 0.f;
+            if (c >= C || at < 0) continue;
+            const int kv = c >= half, ch = kv ? c - half : c;
+            const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
+            in[u] = __ldcs(reinterpret_cast<const uint4 *>(pool.pages + vec * D * (INT8 ? 1 : 2)) + ch % LPH);
+            if constexpr (INT8) sc[u] = pool.scale[vec];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + 32 * u;
+            if (c >= C) continue;
+            const int ch = c >= half ? c - half : c;
+            T *out = (c >= half ? v : k) + r * ld + (int64_t)ch * EP;
+            float f[EP];
+            if constexpr (INT8) {
+                const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
+#pragma unroll
+                for (int i = 0; i < 16; ++i) f[i] = __fmul_rn((float)(int8_t)(w[i >> 2] >> (8 * (i & 3))), sc[u]);
+            } else {
+                unpack8_bf16(in[u], f);
+            }
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < EP / 8; ++i) __stcs(reinterpret_cast<uint4 *>(out) + i, pack8_bf16(f + 8 * i));
+            } else {
+#pragma unroll
+                for (int i = 0; i < EP / 4; ++i)
+                    __stcs(reinterpret_cast<float4 *>(out) + i,
+                           make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
+            }
+        }
+    }
+}
+
+// blocks for the warps' tasks of all rows, a few waves at most
+int grid_for(const echo_kv_pool &p, int n_rows, int per_piece) {
+    const int64_t C = 2ll * p.H * p.d / per_piece;
+    const int64_t blocks = ((C + 32 * kUnroll - 1) / (32 * kUnroll) * n_rows + kWarps - 1) / kWarps;
+    return (int)(blocks < 16384 ? blocks : 16384);
+}
+
+template <typename T, bool INT8>
+void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, const void *v,
+                  int64_t ld, cudaStream_t st) {
+    const int grid = grid_for(p, b.n_rows, 8);
+    echo::launch_chained(p.d == 64 ? kv_write_kernel<T, INT8, 64> : kv_write_kernel<T, INT8, 128>,
+                         dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
+                         static_cast<const T *>(k), static_cast<const T *>(v), ld,
+                         echo::device_error_ptr());
+}
+
+template <typename T, bool INT8>
+void launch_read(const echo_kv_pool &p, const echo_kv_batch &b, void *k, void *v, int64_t ld,
+                 cudaStream_t st) {
+    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8);
+    echo::launch_chained(p.d == 64 ? kv_read_kernel<T, INT8, 64> : kv_read_kernel<T, INT8, 128>,
+                         dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
+                         static_cast<T *>(k), static_cast<T *>(v), ld, echo::device_error_ptr());
+}
+
+echo_status check_rows(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *k,
+                       const void *v, int64_t ld, echo_dtype t, bool *empty) {
+    const echo_status s = echo::kv_check(pool, batch, empty);
+    if (s != ECHO_OK) return s;
+    if (t != ECHO_BF16 && t != ECHO_F32) return ECHO_ERR_INVALID_ARG;
+    if (ld < (int64_t)pool->H * pool->d || ld % 8) return ECHO_ERR_SHAPE;
+    if (*empty) return ECHO_OK;
+    if (!k || !v || !echo::aligned16(k) || !echo::aligned16(v)) return ECHO_ERR_INVALID_ARG;
+    return echo::device_supported() ? ECHO_OK : ECHO_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+namespace echo {
+
+echo_status kv_check(const echo_kv_pool *p, const echo_kv_batch *b, bool *empty) {
+    if (!p || !b) return ECHO_ERR_INVALID_ARG;
+    if (p->kind != ECHO_CACHE_INT8 && p->kind != ECHO_CACHE_BF16) return ECHO_ERR_INVALID_ARG;
+    if (p->n_pages < 1 || p->H < 1 || (p->d != 64 && p->d != 128)) return ECHO_ERR_SHAPE;
+    if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128)
+        return ECHO_ERR_SHAPE;
+    // a (page, keys or values, head) is one 32-bit coordinate of the tensor maps
+    if (2ll * p->n_pages * p->H > INT32_MAX - 1) return ECHO_ERR_SHAPE;
+    if (b->n_seqs < 0 || b->max_pages < 0 || b->n_rows < 0 || b->max_rows < 0) return ECHO_ERR_SHAPE;
+    if (!p->pages || !aligned16(p->pages)) return ECHO_ERR_INVALID_ARG;
+    if (p->kind == ECHO_CACHE_INT8 && (!p->scale || !aligned16(p->scale))) return ECHO_ERR_INVALID_ARG;
+    *empty = b->n_seqs == 0 || b->n_rows == 0;
+    if (*empty) return ECHO_OK;
+    auto aligned4 = [](const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3u) == 0; };
+    if (!b->len || !b->row0 || !aligned4(b->len) || !aligned4(b->row0)) return ECHO_ERR_INVALID_ARG;
+    if (b->max_pages > 0 && (!b->table || !aligned4(b->table))) return ECHO_ERR_INVALID_ARG;
+    return ECHO_OK;
+}
+
+}  // namespace echo
+
+extern "C" echo_status echo_kv_write(const echo_kv_pool *pool, const echo_kv_batch *batch,
+                                     const void *k, const void *v, int64_t ld, echo_dtype t,
+                                     echo_stream_t stream) {
+    bool empty;
+    const echo_status s = check_rows(pool, batch, k, v, ld, t, &empty);
+    if (s != ECHO_OK || empty) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    echo::LaunchScope ls(ECHO_K_KV_WRITE, batch->n_rows, (int64_t)pool->H * pool->d, 0, st);
+    const bool q = pool->kind == ECHO_CACHE_INT8;
+    if (t == ECHO_BF16)
+        q ? launch_write<__nv_bfloat16, true>(*pool, *batch, k, v, ld, st)
+          : launch_write<__nv_bfloat16, false>(*pool, *batch, k, v, ld, st);
+    else
+        q ? launch_write<float, true>(*pool, *batch, k, v, ld, st)
+          : launch_write<float, false>(*pool, *batch, k, v, ld, st);
+    return echo::last_launch_status();
+}
+
+extern "C" echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, void *k,
+                                    void *v, int64_t ld, echo_dtype t, echo_stream_t stream) {
+    bool empty;
+    const echo_status s = check_rows(pool, batch, k, v, ld, t, &empty);
+    if (s != ECHO_OK || empty) return s;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    echo::LaunchScope ls(ECHO_K_KV_READ, batch->n_rows, (int64_t)pool->H * pool->d, 0, st);
+    const bool q = pool->kind == ECHO_CACHE_INT8;
+    if (t == ECHO_BF16)
+        q ? launch_read<__nv_bfloat16, true>(*pool, *batch, k, v, ld, st)
+          : launch_read<__nv_bfloat16, false>(*pool, *batch, k, v, ld, st);
+    else
+        q ? launch_read<float, true>(*pool, *batch, k, v, ld, st)
+          : launch_read<float, false>(*pool, *batch, k, v, ld, st);
+    return echo::last_launch_status();
+}

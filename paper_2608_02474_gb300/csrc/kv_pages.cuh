@@ -1,0 +1,63 @@
+// The paged key/value cache (echo_kv_pool, echo_kv_batch of echocache.h) as the
+// kernels see it: where a row's keys and values stand.
+#pragma once
+
+#include "common.cuh"
+#include "internal.h"
+
+// a pool by value: pages [n_pages, 2, H, 1 << shift, d], scale [n_pages, 2, H, 1 << shift]
+struct KvPool {
+    uint8_t *pages;
+    float *scale;
+    int n_pages, shift, H;
+};
+
+struct KvBatch {
+    const int32_t *table, *len, *row0;
+    int n_seqs, max_pages, n_rows;
+};
+
+// The sequence that row r belongs to, -1 where there is none: the last b with row0[b] <= r
+// if row0[b + 1] lies beyond r.  The whole warp searches for one row, 32 entries at a time:
+// two dependent loads for up to 1024 sequences, where a bisection takes ten.
+ECHO_DEV int kv_seq_of_row(const KvBatch &b, int r) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = b.n_seqs;
+    while (n > 1) {
+        const int step = (n + 31) >> 5, i = lane * step;
+        const int below = __popc(__ballot_sync(0xffffffffu, i < n && b.row0[lo + i] <= r));
+        if (below == 0) return -1;
+        const int skip = (below - 1) * step;
+        lo += skip;
+        n = min(step, n - skip);
+    }
+    return b.row0[lo] <= r && r < b.row0[lo + 1] ? lo : -1;
+}
+
+// Place of position p of a sequence in the pool, as page * (1 << shift) + slot; -1 where the
+// sequence's table does not lead to a page of the pool, which sets the device flag.
+ECHO_DEV int64_t kv_place(const KvPool &pool, const KvBatch &b, int seq, int64_t p, int *err) {
+    const int64_t i = p >> pool.shift;
+    const int page = i < b.max_pages ? b.table[(int64_t)seq * b.max_pages + i] : -1;
+    if ((unsigned)page >= (unsigned)pool.n_pages) {
+        echo_flag_error(err, ECHO_ERR_PAGE);
+        return -1;
+    }
+    return ((int64_t)page << pool.shift) + (p & ((1 << pool.shift) - 1));
+}
+
+namespace echo {
+// argument checks of the entry points; ECHO_OK with *empty set: there is nothing to do
+echo_status kv_check(const echo_kv_pool *pool, const echo_kv_batch *batch, bool *empty);
+inline int kv_shift(int page_tokens) {
+    int s = 0;
+    while ((1 << s) < page_tokens) ++s;
+    return s;
+}
+inline KvPool kv_pool(const echo_kv_pool &p) {
+    return {static_cast<uint8_t *>(p.pages), p.scale, p.n_pages, kv_shift(p.page_tokens), p.H};
+}
+inline KvBatch kv_batch(const echo_kv_batch &b) {
+    return {b.table, b.len, b.row0, b.n_seqs, b.max_pages, b.n_rows};
+}
+}  // namespace echo

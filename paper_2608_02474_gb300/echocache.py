@@ -59,6 +59,16 @@ class BlockWeightsC(_c.Structure):
                                    "boc", "W1", "b1", "W2", "b2", "KVc")]
 
 
+class KVPoolC(_c.Structure):
+    _fields_ = [("kind", _i32), ("n_pages", _i32), ("page_tokens", _i32), ("H", _i32), ("d", _i32),
+                ("pages", _vp), ("scale", _vp)]
+
+
+class KVBatchC(_c.Structure):
+    _fields_ = [("table", _vp), ("len", _vp), ("row0", _vp), ("n_seqs", _i32), ("max_pages", _i32),
+                ("n_rows", _i32), ("max_rows", _i32)]
+
+
 _SIGS = {
     "echo_status_str": (_c.c_char_p, [_i32]),
     "echo_get_device_error": (_i32, [_vp]),
@@ -95,6 +105,11 @@ _SIGS = {
                                   _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "echo_cache_quant": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp]),
     "echo_cache_dequant": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp]),
+    "echo_kv_write": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _vp, _i64, _i32, _vp]),
+    "echo_kv_read": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _vp, _i64, _i32, _vp]),
+    "echo_kv_attention_workspace_size": (_sz, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _i32]),
+    "echo_kv_attention": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _i64, _i32, _i32,
+                                 _vp, _i64, _vp, _sz, _vp]),
     "echo_linear": (_i32, [_vp, _i64, _i32, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i64,
                            _i32, _vp]),
     "echo_attention": (_i32, [_vp, _i64, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp]),
@@ -542,3 +557,138 @@ def echo_block_step_cache(weights: DeviceBlock, dims: BlockDims, x, idx, K: int,
         _c.byref(cache.cstruct), _p(y), _p(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)))
     return y
+
+
+# ---------------------------------------------------------------------------
+class KVPool:
+    """A pool of key/value pages (echo_kv_pool) over the caller's tensors: pages int8 or
+    bf16 [n_pages, 2, H, page_tokens, d] (keys, then values), with scale f32 [n_pages, 2,
+    H, page_tokens] where the pages hold int8 codes.  Pages need no initial contents."""
+
+    def __init__(self, pages: torch.Tensor, scale: torch.Tensor | None = None):
+        _dev(pages, "pages")
+        if pages.dim() != 5 or pages.shape[1] != 2:
+            raise ValueError("pages must be [n_pages, 2, H, page_tokens, d]")
+        if pages.dtype not in (torch.int8, torch.bfloat16):
+            raise TypeError(f"unsupported page dtype {pages.dtype}")
+        int8 = pages.dtype == torch.int8
+        if int8 != (scale is not None):
+            raise ValueError("int8 pages need scales, and bf16 pages have none")
+        if int8:
+            _dev(scale, "scale")
+            if scale.dtype != torch.float32 or scale.shape != pages.shape[:4]:
+                raise ValueError("scale must be f32 [n_pages, 2, H, page_tokens]")
+        self.pages, self.scale = pages, scale
+        self.n_pages, _, self.H, self.page_tokens, self.d = pages.shape
+        self.cstruct = KVPoolC(CACHE_INT8 if int8 else CACHE_BF16, self.n_pages, self.page_tokens,
+                               self.H, self.d, _p(pages), _p(scale))
+        self._ref = _c.byref(self.cstruct)
+
+    @staticmethod
+    def empty(kind: int, n_pages: int, page_tokens: int, H: int, d: int,
+              device="cuda") -> "KVPool":
+        """A new pool of CACHE_INT8 or CACHE_BF16 pages."""
+        if kind not in (CACHE_INT8, CACHE_BF16):
+            raise ValueError("a pool holds CACHE_INT8 or CACHE_BF16 pages")
+        int8 = kind == CACHE_INT8
+        shape = (n_pages, 2, H, page_tokens, d)
+        return KVPool(torch.empty(shape, dtype=torch.int8 if int8 else torch.bfloat16, device=device),
+                      torch.empty(shape[:4], dtype=torch.float32, device=device) if int8 else None)
+
+
+class KVBatch:
+    """The sequences of one call (echo_kv_batch) over the caller's device tensors: table
+    int32 [n_seqs, max_pages], lens int32 [n_seqs] (the new rows included), row0 int32
+    [n_seqs + 1].  n_rows: rows of the call's tensors; max_rows: about the most rows of one
+    sequence (n_rows when not given), which only chooses between kernels.  Serves the
+    pools of every layer."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, row0: torch.Tensor, n_rows: int,
+                 max_rows: int | None = None):
+        for t, n in ((table, "table"), (lens, "lens"), (row0, "row0")):
+            _dev(t, n)
+            if t.dtype != torch.int32:
+                raise TypeError(f"{n} must be int32")
+        B = lens.numel()
+        if table.dim() != 2 or table.shape[0] != B or row0.numel() != B + 1:
+            raise ValueError("table must be [n_seqs, max_pages] and row0 [n_seqs + 1]")
+        self.table, self.lens, self.row0 = table, lens, row0
+        self.n_seqs, self.n_rows = B, int(n_rows)
+        self.max_rows = self.n_rows if max_rows is None else int(max_rows)
+        self.cstruct = KVBatchC(_p(table), _p(lens), _p(row0), B, table.shape[1], self.n_rows,
+                                self.max_rows)
+        self._ref = _c.byref(self.cstruct)
+
+
+def _kv_rows(pool: KVPool, batch: KVBatch, k, v):
+    """Row stride of k and v, [n_rows, >= H d] each (columns of a wider tensor, too)."""
+    for t, n in ((k, "k"), (v, "v")):
+        _rows_of(t, n, batch.n_rows, pool.H * pool.d)
+    if k.dtype != v.dtype or (batch.n_rows > 1 and k.stride(0) != v.stride(0)):
+        raise ValueError("k and v must share dtype and row stride")
+    return _ld(k)
+
+
+def _rows_of(t, name, n_rows, cols):
+    if not t.is_cuda or t.dim() != 2 or t.shape[0] != n_rows or t.shape[1] < cols:
+        raise ValueError(f"{name} must be a CUDA tensor of {n_rows} rows and {cols} columns")
+    if t.stride(1) != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+
+
+def _ld(t):
+    # the stride of a single row means nothing, and may be anything
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+
+def _empty(shape, dtype, device, stream):
+    # memory of the stream that the kernels run on
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def echo_kv_write(pool: KVPool, batch: KVBatch, k, v, stream=None):
+    """Keys and values of the batch's new rows, [n_rows, H d] bf16 or f32, into the pages."""
+    ld = _kv_rows(pool, batch, k, v)
+    _check("echo_kv_write", lib().echo_kv_write(pool._ref, batch._ref, _p(k), _p(v), ld, _dtype(k),
+                                                _stream(stream)))
+
+
+def echo_kv_read(pool: KVPool, batch: KVBatch, dtype=torch.bfloat16, k=None, v=None, stream=None):
+    """(k, v), [n_rows, H d] each: the cached rows at the positions of the batch's rows."""
+    dev, shape = pool.pages.device, (batch.n_rows, pool.H * pool.d)
+    k = k if k is not None else _empty(shape, dtype, dev, stream)
+    v = v if v is not None else _empty(shape, k.dtype, dev, stream)
+    ld = _kv_rows(pool, batch, k, v)
+    _check("echo_kv_read", lib().echo_kv_read(pool._ref, batch._ref, _p(k), _p(v), ld, _dtype(k),
+                                              _stream(stream)))
+    return k, v
+
+
+def echo_kv_attention_workspace_size(pool: KVPool, batch: KVBatch, Hq: int) -> int:
+    return lib().echo_kv_attention_workspace_size(pool._ref, batch._ref, Hq)
+
+
+def echo_kv_attention(pool: KVPool, batch: KVBatch, q, Hq: int | None = None, causal_block: int = 0,
+                      out=None, workspace=None, stream=None):
+    """Attention of the batch's rows, q bf16 [n_rows, Hq d], over their sequences' pages;
+    Hq is q's columns over d when not given."""
+    Hq = q.shape[1] // pool.d if Hq is None else Hq
+    _rows_of(q, "q", batch.n_rows, Hq * pool.d)
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"unsupported dtype {q.dtype}")
+    if out is None:
+        out = _empty((batch.n_rows, Hq * pool.d), torch.bfloat16, q.device, stream)
+    else:
+        _rows_of(out, "out", batch.n_rows, Hq * pool.d)
+        if out.dtype != torch.bfloat16:
+            raise TypeError(f"unsupported dtype {out.dtype}")
+    if workspace is None:
+        workspace = _empty(echo_kv_attention_workspace_size(pool, batch, Hq), torch.uint8, q.device,
+                           stream)
+    _check("echo_kv_attention", lib().echo_kv_attention(
+        pool._ref, batch._ref, _p(q), _ld(q), Hq, causal_block, _p(out), _ld(out), _p(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
