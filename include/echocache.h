@@ -497,7 +497,7 @@ echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, v
  * by frame, and with 0 the rows may be queries of any other kind (cross-attention to n_b
  * rows of any number).  A row that sees no key gives zeros.
  *   q bf16 [n_rows, ldq], out bf16 [n_rows, ldo]; Hq a multiple of H, Hq / H <= 128;
- *   ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
+ *   n_rows Hq < 2^31; ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
  *   scales multiply scores and weights in fp32); sums, maxima and rescaling are fp32; the
  *   softmax weights (INT8: times the value's scale) are rounded to bf16 for the product
  *   with the values.
@@ -564,7 +564,7 @@ typedef enum {
     ECHO_K_DEQUANT = 8, ECHO_K_MERGE = 9, ECHO_K_STEP_DELTA = 10, ECHO_K_UNIFORM = 11,
     ECHO_K_REF_SCAN = 12, ECHO_K_REF_ALLOC = 13, ECHO_K_REF_STORE = 14, ECHO_K_CACHE_COPY = 15,
     ECHO_K_MERGE_QUANT = 16, ECHO_K_KV_WRITE = 17, ECHO_K_KV_READ = 18,
-    ECHO_K_KV_ATTENTION = 19, ECHO_K_COUNT = 20
+    ECHO_K_KV_ATTENTION = 19, ECHO_K_KV_JOIN = 20, ECHO_K_COUNT = 21
 } echo_kernel_kind;
 
 /* Number of kernels this library has launched in this process (all devices). */
@@ -584,7 +584,8 @@ echo_status echo_profile_enable(int32_t on);
  * bytes); QUANT, DEQUANT, MERGE (rows, D, 0); ENERGY (T, frames, n_fft); STEP_DELTA (n, element bytes, 0)
  * for the reduction and (0, 0, blocks) for its final combine; UNIFORM (NT, K, 0);
  * REF_SCAN, REF_ALLOC, REF_STORE, CACHE_COPY (rows, D, 0); MERGE_QUANT (NT, D, K active
- * rows); KV_WRITE, KV_READ (rows, H d, 0); KV_ATTENTION (rows, Hq d, sequences). */
+ * rows); KV_WRITE, KV_READ (rows, H d, 0); KV_ATTENTION (rows, Hq d, sequences),
+ * KV_JOIN (rows, Hq d, CTAs that shared the work). */
 int32_t echo_profile_read(int32_t max, int32_t *kinds, int64_t *m, int64_t *n, int64_t *k,
                           float *ms);
 

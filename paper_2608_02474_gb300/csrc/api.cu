@@ -59,8 +59,8 @@ echo_status last_launch_status() {
     return cudaGetLastError() == cudaSuccess ? ECHO_OK : ECHO_ERR_CUDA;
 }
 
-bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
-                    uint32_t box_rows) {
+namespace {
+EncodeTiledFn encode_fn() {
     if (!g_encode) {
         std::lock_guard<std::mutex> lk(g_mu);
         if (!g_encode) {
@@ -69,19 +69,56 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
             if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
                                                  cudaEnableDefault, &q) != cudaSuccess ||
                 q != cudaDriverEntryPointSuccess || !fn)
-                return false;
+                return nullptr;
             g_encode = reinterpret_cast<EncodeTiledFn>(fn);
         }
     }
+    return g_encode;
+}
+}  // namespace
+
+bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
+                    uint32_t box_rows) {
+    const EncodeTiledFn encode = encode_fn();
+    if (!encode) return false;
     cuuint64_t gdim[2] = {cols, rows};
     cuuint64_t gstride[1] = {ld * 2};
     cuuint32_t box[2] = {64, box_rows};
     cuuint32_t estride[2] = {1, 1};
-    CUresult r = g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), gdim,
-                          gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    CUresult r = encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), gdim,
+                        gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
+}
+
+bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows) {
+    const EncodeTiledFn encode = encode_fn();
+    if (!encode) return false;
+    const bool int8 = pool.kind == ECHO_CACHE_INT8;
+    const cuuint64_t d = (cuuint64_t)pool.d, row = int8 ? d : 2 * d;
+    cuuint64_t gdim[3] = {d, (cuuint64_t)pool.page_tokens, 2ull * (cuuint64_t)pool.n_pages * (cuuint64_t)pool.H};
+    cuuint64_t gstride[2] = {row, row * (cuuint64_t)pool.page_tokens};
+    cuuint32_t box[3] = {int8 ? (cuuint32_t)d : 64u, box_rows, 1};
+    cuuint32_t estride[3] = {1, 1, 1};
+    CUresult r = encode(m, int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                        pool.pages, gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        int8 && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
+int num_sms() {
+    static int sms[kMaxDevices] = {};
+    const int dev = current_device();
+    if (dev < 0 || dev >= kMaxDevices) return 152;
+    if (!sms[dev]) {
+        int v = 0;
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1)
+            v = 152;
+        sms[dev] = v;
+    }
+    return sms[dev];
 }
 
 // ---------------------------------------------------------------------------
@@ -172,7 +209,8 @@ extern "C" const char *echo_kernel_name(int32_t kind) {
         "layernorm_gather",   "gemm_tcgen05", "attention",    "quant_scatter",
         "dequant_gather",     "dequant_merge", "step_delta",   "uniform_select",
         "ref_scan",           "ref_alloc",     "ref_store",    "cache_copy",
-        "merge_quant",        "kv_write",      "kv_read",      "kv_attention"};
+        "merge_quant",        "kv_write",      "kv_read",      "kv_attention",
+        "kv_join"};
     if (kind < 0 || kind >= ECHO_K_COUNT) return "unknown";
     return names[kind];
 }

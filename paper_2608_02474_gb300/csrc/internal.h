@@ -73,6 +73,10 @@ inline cudaError_t launch_chained(void (*kernel)(KA...), dim3 grid, dim3 block, 
 bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
                     uint32_t box_rows);
 
+// a pool of key/value pages as [z, page_tokens, d], z = (page, keys or values, head): bf16 in
+// boxes of 64 columns, int8 codes in whole rows, box_rows tokens; swizzled by the box's width
+bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
+
 // layernorm.cu
 void launch_layernorm(const void *in, echo_dtype in_t, const int32_t *rows, int32_t n_rows,
                       int32_t D, void *out, cudaStream_t st);
@@ -118,6 +122,24 @@ void launch_dequant_merge(const int8_t *q, const float *scale, const int32_t *ro
 // q[i], s[i]: the merge and the int8 write of the block step in one pass
 void launch_merge_quant(int8_t *q, float *scale, const int32_t *rowmap, const uint32_t *amax,
                         int32_t NT, int32_t D, int32_t K, void *y, cudaStream_t st);
+
+// SMs of the current device
+int num_sms();
+
+// kv_decode.cu, kv_chunk.cu: attention over a paged cache, arguments checked, for sequences
+// of few packed rows (row x head of a group) each and for any; workspace bytes as asked
+struct KvAttention {
+    const echo_kv_pool *pool;
+    const echo_kv_batch *batch;
+    const void *q;
+    int64_t ldq;
+    int32_t Hq, causal_block;
+    void *out;
+    int64_t ldo;
+    void *ws;
+};
+size_t kv_decode_workspace(const echo_kv_pool &pool);
+echo_status launch_kv_decode(const KvAttention &a, cudaStream_t st);
 
 // refcache.cu: cache forms other than plain int8 (and int8 through the same calls)
 echo_status cache_check(const echo_cache *c);
