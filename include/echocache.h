@@ -495,7 +495,9 @@ echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, v
  *       = p < 0 ? 0 : min(len[b], (p / causal_block + 1) causal_block)    else
  * causal_block 1 is token-by-token causality, the tokens of a frame make it causal frame
  * by frame, and with 0 the rows may be queries of any other kind (cross-attention to n_b
- * rows of any number).  A row that sees no key gives zeros.
+ * rows of any number).  A row that sees no key gives zeros.  A key that a row does not see
+ * changes nothing in it, whatever its page holds there; NaN in a key, or a value that is not
+ * finite, makes the rows that see it not finite.
  *   q bf16 [n_rows, ldq], out bf16 [n_rows, ldo]; Hq a multiple of H, Hq / H <= 128;
  *   n_rows Hq < 2^31; ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
  *   scales multiply scores and weights in fp32); sums, maxima and rescaling are fp32; the

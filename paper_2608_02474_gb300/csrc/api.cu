@@ -108,6 +108,20 @@ bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows
     return r == CUDA_SUCCESS;
 }
 
+bool make_tmap_rows(CUtensorMap *m, const void *base, uint64_t n_rows, uint64_t H, uint64_t d,
+                    uint64_t ld, uint32_t box_heads, uint32_t box_rows) {
+    const EncodeTiledFn encode = encode_fn();
+    if (!encode) return false;
+    cuuint64_t gdim[3] = {d, H, n_rows};
+    cuuint64_t gstride[2] = {d * 2, ld * 2};
+    cuuint32_t box[3] = {64, box_heads, box_rows};
+    cuuint32_t estride[3] = {1, 1, 1};
+    CUresult r = encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), gdim, gstride,
+                        box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 int num_sms() {
     static int sms[kMaxDevices] = {};
     const int dev = current_device();

@@ -77,6 +77,11 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
 // boxes of 64 columns, int8 codes in whole rows, box_rows tokens; swizzled by the box's width
 bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
 
+// bf16 rows of heads [n_rows, H, d] (row stride ld elements) in boxes of box_rows rows and
+// box_heads heads, 64 columns, 128-byte swizzle
+bool make_tmap_rows(CUtensorMap *m, const void *base, uint64_t n_rows, uint64_t H, uint64_t d,
+                    uint64_t ld, uint32_t box_heads, uint32_t box_rows);
+
 // layernorm.cu
 void launch_layernorm(const void *in, echo_dtype in_t, const int32_t *rows, int32_t n_rows,
                       int32_t D, void *out, cudaStream_t st);
@@ -140,6 +145,8 @@ struct KvAttention {
 };
 size_t kv_decode_workspace(const echo_kv_pool &pool);
 echo_status launch_kv_decode(const KvAttention &a, cudaStream_t st);
+size_t kv_chunk_workspace(const echo_kv_pool &pool);
+echo_status launch_kv_chunk(const KvAttention &a, cudaStream_t st);
 
 // refcache.cu: cache forms other than plain int8 (and int8 through the same calls)
 echo_status cache_check(const echo_cache *c);

@@ -5,7 +5,8 @@ extern "C" size_t echo_kv_attention_workspace_size(const echo_kv_pool *pool, con
                                                    int32_t Hq) {
     bool empty;
     if (Hq < 1 || echo::kv_check(pool, batch, &empty) != ECHO_OK) return 0;
-    return echo::kv_decode_workspace(*pool);
+    const size_t few = echo::kv_decode_workspace(*pool), many = echo::kv_chunk_workspace(*pool);
+    return few > many ? few : many;
 }
 
 extern "C" echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv_batch *batch,
@@ -27,5 +28,7 @@ extern "C" echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv
     if (!device_supported()) return ECHO_ERR_UNSUPPORTED;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const KvAttention a{pool, batch, q, ldq, Hq, causal_block, out, ldo, workspace};
-    return launch_kv_decode(a, st);
+    // few packed rows a sequence: 16 at a time on the SMs' own tensor instructions
+    const bool few = (int64_t)batch->max_rows * (Hq / pool->H) <= 16;
+    return few ? launch_kv_decode(a, st) : launch_kv_chunk(a, st);
 }

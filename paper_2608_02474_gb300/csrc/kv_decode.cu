@@ -8,9 +8,7 @@
 // own keys, O += P V.  Nothing passes between the warps until the end of a piece, where
 // the four (maximum, sum, O) are joined in a fixed order.
 //
-// int8 codes become bf16 exactly in registers: with b the byte, 0x4300 | (b & 0x7F) is
-// 128 + (b & 0x7F) and 0x4300 | (b & 0x80) is 128 or 256, and their difference is the
-// signed value.  The keys' scales multiply the scores, the values' scales the weights.
+// int8 codes become bf16 exactly in registers (kv_codes2).  The keys' scales multiply the scores, the values' scales the weights.
 // ldmatrix hands out 16-bit units, so a lane gets neighbouring pairs of codes: Q's columns
 // are taken in the same order, and O's columns come out in it.
 #include <cfloat>
@@ -68,15 +66,6 @@ ECHO_DEV void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// two codes of w, picked into 16-bit halves by the selector, as a bf16 pair
-ECHO_DEV uint32_t codes2(uint32_t w, uint32_t sel) {
-    const uint32_t r = __byte_perm(w, 0x43434343u, sel);
-    const uint32_t lo = r & 0xFF7FFF7Fu, hi = r & 0xFF80FF80u;
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&lo),
-                                     *reinterpret_cast<const __nv_bfloat162 *>(&hi));
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
 // byte offset of 16-byte chunk c of row r of a block's K or V, as the tensor maps lay it out
 template <bool INT8, int D>
 ECHO_DEV uint32_t chunk_at(int r, int c) {
@@ -234,7 +223,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                             ldsm4(kbase + chunk_at<INT8, D>(warp * KPW + nt * 8 + mr, c + mi), r);
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                mma16816(sc[nt], qa[c + i], codes2(r[i], 0x4140), codes2(r[i], 0x4342));
+                                mma16816(sc[nt], qa[c + i], kv_codes2(r[i], 0x4140), kv_codes2(r[i], 0x4342));
                         }
                 } else {
 #pragma unroll
@@ -274,9 +263,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int j = key0 + nt * 8 + 2 * tq + e;
+                            if (INT8 && !(fabsf(vs[nt][e]) < INFINITY)) {   // spoils the rows that see it
+                                sc[nt][e] = sc[nt][2 + e] = NAN;
+                                vs[nt][e] = 0.f;
+                            }
                             if (j >= lim[0]) sc[nt][e] = -INFINITY;
                             if (j >= lim[1]) sc[nt][2 + e] = -INFINITY;
-                            if (INT8 && j >= keys) vs[nt][e] = 0.f;   // not copied: may be anything
                         }
                 }
 #pragma unroll
@@ -316,11 +308,34 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                                             pack_bf16(sc[2 * k2 + 1][2], sc[2 * k2 + 1][3])};
                     const int row = warp * KPW + k2 * 16 + (mi & 1) * 8 + mr;
                     uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+                    if (!INT8 && edge && low < keys) {
+                        // rows that do not see all of these keys: values that are not finite
+                        // become 0, and spoil the rows that do see them (0 times infinity)
+                        uint32_t bad = 0;                    // of the 16 keys
+#pragma unroll
+                        for (int c = 0; c < C::ROW_BYTES / 16; c += 2) {
+                            uint32_t r[4];
+                            ldsm4_t(vbase + chunk_at<INT8, D>(row, c + (mi >> 1)), r);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if ((r[i] & 0x7F80u) == 0x7F80u) bad |= 1u << (8 * (i & 1) + 2 * tq);
+                                if ((r[i] & 0x7F800000u) == 0x7F800000u) bad |= 2u << (8 * (i & 1) + 2 * tq);
+                            }
+                        }
+                        bad = __reduce_or_sync(0xffffffffu, bad);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int seen = lim[i] - (key0 + k2 * 16);
+                            if (bad & (seen >= 16 ? 0xffffu : seen > 0 ? (1u << seen) - 1u : 0u)) l[i] = NAN;
+                            keep[i] = ((bad >> (8 * i + 2 * tq)) & 1 ? 0u : 0xffffu) |
+                                      ((bad >> (8 * i + 2 * tq)) & 2 ? 0u : 0xffff0000u);
+                        }
+                    }
                     if (!INT8 && tail) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const int j = key0 + k2 * 16 + 8 * i + 2 * tq;
-                            keep[i] = (j < keys ? 0xffffu : 0u) | (j + 1 < keys ? 0xffff0000u : 0u);
+                            keep[i] &= (j < keys ? 0xffffu : 0u) | (j + 1 < keys ? 0xffff0000u : 0u);
                         }
                     }
 #pragma unroll
@@ -330,11 +345,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         if constexpr (INT8) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                mma16816(o[2 * (c + i)], pa, codes2(r[2 * i], 0x4240), codes2(r[2 * i + 1], 0x4240));
-                                mma16816(o[2 * (c + i) + 1], pa, codes2(r[2 * i], 0x4341), codes2(r[2 * i + 1], 0x4341));
+                                mma16816(o[2 * (c + i)], pa, kv_codes2(r[2 * i], 0x4240), kv_codes2(r[2 * i + 1], 0x4240));
+                                mma16816(o[2 * (c + i) + 1], pa, kv_codes2(r[2 * i], 0x4341), kv_codes2(r[2 * i + 1], 0x4341));
                             }
                         } else {
-                            if (tail) {
+                            if (edge) {
                                 r[0] &= keep[0];
                                 r[1] &= keep[1];
                                 r[2] &= keep[0];
@@ -436,89 +451,6 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     }
 }
 
-// The items that were done in pieces, joined: block (c, .) the one that begins in worker
-// c's range and goes on beyond it, a warp per row.  With the pieces' maxima m_i and sums
-// l_i: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in the order of the keys.
-constexpr int kJoinRows = 16;
-
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinRows)
-kv_join_kernel(const KvWork w, const float *__restrict__ ws, __nv_bfloat16 *__restrict__ out, int64_t ldo) {
-    __shared__ KvFound found;
-    KvWalk walk;
-    // before the wait: the kernel ahead passed its own, so the lengths are there
-    const bool any = kv_find<32 * kJoinRows, true>(w, blockIdx.x, found, walk);
-    pdl_enter();
-    if (!any) return;
-    const int c = blockIdx.x;
-    const int64_t from = walk.at;
-    const KvSeq &s = walk.s;
-    const int nb = s.blocks(w, walk.ntile);
-    if (from >= walk.end || from < walk.start || nb == 0) return;   // not begun here, or nothing in it
-    // pieces: worker c + i, i = 0 .. n - 1
-    int n = 1;
-    const int64_t upto = from + kFixedUnits + nb;
-    while (walk.unit_of(c + n) < upto) ++n;
-    auto covers = [&](int i, int &kb0, int &kb1) {
-        kb0 = i == 0 ? 0 : KvWalk::block_at(walk.unit_of(c + i), from, nb);
-        kb1 = KvWalk::block_at(walk.unit_of(c + i + 1), from, nb);
-    };
-    for (int i = 0; i < 3 && i < n; ++i) {   // stored whole: no other piece has any key
-        int kb0, kb1;
-        covers(i, kb0, kb1);
-        if (kb0 == 0 && kb1 == nb) return;
-    }
-    const int row = blockIdx.y * kJoinRows + ((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int pr = walk.ntile * w.tile + row;
-    if (row >= w.tile || pr >= s.packed) return;
-    constexpr int E = D / 32;
-    const int64_t stride = (int64_t)2 * w.slot_rows * (D + 2);    // to the next worker's first piece
-    const float *one = ws + stride * c + stride / 2, *more = ws + stride * (c + 1);
-    auto piece = [&](int i) { return i == 0 ? one : more + stride * (i - 1); };
-    float m = -FLT_MAX;
-    for (int i = lane; i < n; i += 32) {
-        int kb0, kb1;
-        covers(i, kb0, kb1);
-        if (kb0 < kb1) m = fmaxf(m, piece(i)[w.slot_rows * D + 2 * row]);
-    }
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    float l = 0.f, acc[E] = {};
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        float f = 0.f, li = 0.f;                                   // of piece i0 + lane
-        if (i0 + lane < n) {
-            int kb0, kb1;
-            covers(i0 + lane, kb0, kb1);
-            if (kb0 < kb1) {
-                const float2 ml = *reinterpret_cast<const float2 *>(piece(i0 + lane) + w.slot_rows * D + 2 * row);
-                f = ex2_approx(ml.x - m);
-                li = f * ml.y;
-            }
-        }
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) li += __shfl_xor_sync(0xffffffffu, li, x);
-        l += li;
-        const unsigned live = __ballot_sync(0xffffffffu, f != 0.f);   // NaN stays in
-        const int most = min(32, n - i0);
-#pragma unroll 8
-        for (int i = 0; i < most; ++i) {
-            const float fi = __shfl_sync(0xffffffffu, f, i);
-            if (!(live >> i & 1)) continue;
-            const float *src = piece(i0 + i) + row * D + lane * E;
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                const float2 v = *reinterpret_cast<const float2 *>(src + e);
-                acc[e] += fi * v.x;
-                acc[e + 1] += fi * v.y;
-            }
-        }
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    __nv_bfloat16 *dst = out + (int64_t)(s.row + pr / w.group) * ldo + (walk.nhead * w.group + pr % w.group) * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-}
-
 template <bool INT8, int D>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     using C = Cfg<INT8, D>;
@@ -546,11 +478,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
         echo::launch_chained(kv_decode_kernel<INT8, D>, dim3(p.work.workers), dim3(THREADS), C::SMEM, st, tm, p);
     }
-    if (p.work.split) {
-        echo::LaunchScope ls(ECHO_K_KV_JOIN, a.batch->n_rows, (int64_t)a.Hq * D, p.work.workers, st);
-        echo::launch_chained(kv_join_kernel<D>, dim3(p.work.workers, ROWS / kJoinRows), dim3(32 * kJoinRows), 0, st,
-                             p.work, static_cast<const float *>(a.ws), p.out, a.ldo);
-    }
+    echo::launch_kv_join(a, p.work, st);
     return echo::last_launch_status();
 }
 

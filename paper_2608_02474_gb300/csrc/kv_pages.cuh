@@ -46,6 +46,17 @@ ECHO_DEV int64_t kv_place(const KvPool &pool, const KvBatch &b, int seq, int64_t
     return ((int64_t)page << pool.shift) + (p & ((1 << pool.shift) - 1));
 }
 
+// two codes of w, picked into 16-bit halves by the selector, as a bf16 pair, exactly:
+// with b the byte, 0x4300 | (b & 0x7F) is 128 + (b & 0x7F) and 0x4300 | (b & 0x80) is 128 or
+// 256, and their difference is the signed value
+ECHO_DEV uint32_t kv_codes2(uint32_t w, uint32_t sel) {
+    const uint32_t r = __byte_perm(w, 0x43434343u, sel);
+    const uint32_t lo = r & 0xFF7FFF7Fu, hi = r & 0xFF80FF80u;
+    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&lo),
+                                     *reinterpret_cast<const __nv_bfloat162 *>(&hi));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
 namespace echo {
 // argument checks of the entry points; ECHO_OK with *empty set: there is nothing to do
 echo_status kv_check(const echo_kv_pool *pool, const echo_kv_batch *batch, bool *empty);

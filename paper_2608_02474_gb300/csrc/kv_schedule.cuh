@@ -240,6 +240,7 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
     w.split = 1;
     return w;
 }
+void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st);
 }  // namespace echo
 inline size_t kv_workspace_bytes(int workers, int rows, int D) {
     return (size_t)workers * 2 * rows * (D + 2) * 4;

@@ -263,3 +263,31 @@ def test_other_stream_graph_and_profile(ec):
         g.replay()
         assert torch.equal(out, ec.echo_kv_attention(pool, batch, q, causal_block=1))
     assert ec.echo_get_device_error() == 0
+
+
+@FORMS
+@HEADS
+@pytest.mark.parametrize("rows,cb", [(3, 1), (8, 4), (40, 1), (200, 1), (200, 64)])
+@pytest.mark.parametrize("what", [0, 1])             # a key, a value
+@pytest.mark.parametrize("value", [np.inf, np.nan])
+def test_not_finite_where_only_later_rows_see_it(ec, form, d, rows, cb, what, value):
+    """Rows that do not see the key are as ever; those that do are not finite (an infinite
+    key may give a score of -infinity, and a weight of 0)."""
+    n, at = 300, 300 - rows // 2
+    c = kv_case.make(form, 16, 2, d, [n], [rows], seed=21)
+    q = kv_case.queries(rows, 4 * d, 21)
+    want, mass = P.attend(c.pages, c.scale, c.table, c.lens, c.row0, q, 4, cb)
+    pg, slot = c.table[0, at // 16], at % 16
+    if form == "int8":
+        c.scale[pg, what, 1, slot] = value
+    else:
+        c.pages[pg, what, 1, slot, 5] = value
+    pool, batch = c.device(ec)
+    got = ec.echo_kv_attention(pool, batch, bf(q), causal_block=cb).float().cpu().numpy()
+    sees = np.array([P.top_of(n - rows + i, n, cb) > at for i in range(rows)])
+    assert sees.any() and not sees.all()
+    close(got[:, :2 * d], want[:, :2 * d], mass[:, :2 * d])      # the other key/value head
+    close(got[~sees], want[~sees], mass[~sees])
+    if what == 1 or np.isnan(value):
+        assert not np.isfinite(got[sees][:, [2 * d + 5, 3 * d + 5]]).any()
+    assert ec.echo_get_device_error() == 0
