@@ -7,18 +7,17 @@
 //               shared-memory tiles (128-byte swizzle, 64-column boxes);
 //   warp 1      one elected lane issues S_t = Q_t K^T (TMEM) and O_t += P_t V (P from
 //               TMEM), in the order PV0_f S0_{f+1} PV1_f S1_{f+1}, across pieces too;
-//   warp 2      tensor memory; bf16: clears the value rows that no row may use (below);
 //   warp 3      walks the pieces, hands them to the other warps, copies the queries;
-//   four warps  (int8) codes to bf16, a key per thread: the copy leaves a row of codes
-//               where the second half of the row's bf16 values goes, so that each thread
-//               overwrites only its own;
+//   four warps  int8: codes to bf16, a key per thread: the copy leaves a row of codes where
+//               the second half of the row's bf16 values goes, so that each thread
+//               overwrites only its own.  bf16: clear values that no row may use (below);
 //   eight warps softmax of the two tiles, a row per thread: the running maximum comes from
 //               the piece's first block and moves only when a block's weights sum to more
 //               than 2^64 (exact after the division by the row sum).
 // A row's weights are 0 where it does not see the key, but 0 times a value that is not
 // finite is not 0: slots past a sequence's length may hold anything, and a later row's
-// values too.  In the blocks that some row does not see whole, warp 2 therefore clears
-// values past the end, clears those that are not finite and names their keys; a row that
+// values too.  In the blocks that some row does not see whole, four warps therefore clear
+// values past the end, clear those that are not finite and name their keys; a row that
 // sees such a key becomes NaN.  For int8 pages only a scale can be non-finite: it then
 // spoils the key's score, and stands as 0 among the values' scales.
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
@@ -29,16 +28,16 @@
 namespace {
 
 constexpr int BM = 128, TILES = 2, BN = 128;
+constexpr int THREADS = 512, SOFT0 = 8;         // warps 0-3, 4-7, and the softmax from SOFT0 on
 constexpr int ATOM = 128 * 128;                 // 128 rows of 64 bf16
 constexpr uint32_t TMEM_COLS = 512, O_COL = 256;
 constexpr int PIECES = 4;                       // handed out ahead
 constexpr int SLOT_ROWS = TILES * BM;
-constexpr int V_AHEAD = 4;                      // value tiles in the ring are fewer
+constexpr int PAIRS = 3;                        // (V_f, K_{f+1}) on their way or in use
+constexpr int SPOILT = 2;                       // blocks whose spoilt keys are kept
 
 template <bool INT8, int D>
 struct Cfg {
-    static constexpr int THREADS = INT8 ? 512 : 384;
-    static constexpr int SOFT0 = THREADS / 32 - 8;             // first softmax warp
     static constexpr int ATOMS = D / 64;
     static constexpr int Q_BYTES = ATOMS * ATOM;               // of a tile
     // int8 codes land at byte ATOM of their tile: for d 128 in its second half
@@ -62,7 +61,8 @@ struct ChunkParams {
 
 struct Piece {
     int64_t shift;
-    int blocks, kb0, keys, low;      // blocks < 0: no more pieces; low: keys that every row sees
+    int blocks, kb0, keys;           // blocks < 0: no more pieces
+    int clear;                       // its first blocks that every row sees whole
     int row, packed, len, head, tile, seq;
     int whole, first;
 };
@@ -71,11 +71,11 @@ struct Piece {
 template <bool INT8, int D>
 struct Side {
     static constexpr int RING = Cfg<INT8, D>::RING;
-    uint64_t q_full, q_empty, full[RING], empty[RING], raw_full[RING], v_ok[V_AHEAD];
+    uint64_t q_full, q_empty, k_first, pair[PAIRS], empty[RING], raw_full[RING], edge_go, v_ok;
     uint64_t s_full[TILES], p_full[TILES], pv_done[TILES], drain;
     uint64_t piece_full[PIECES], piece_empty[PIECES], sc_full[2], sc_empty[2];
     Piece piece[PIECES];
-    uint32_t spoilt[V_AHEAD][4];     // keys of a block with values that are not finite
+    uint32_t spoilt[SPOILT][4];      // keys of a block with values that are not finite
     uint32_t tmem_slot;
     int abort_flag;
     union alignas(16) {              // read 16 bytes at a time
@@ -85,7 +85,7 @@ struct Side {
 };
 
 template <bool INT8, int D>
-__global__ void __launch_bounds__((Cfg<INT8, D>::THREADS), 1)
+__global__ void __launch_bounds__(THREADS, 1)
 kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
                 const ChunkParams p) {
     using C = Cfg<INT8, D>;
@@ -100,12 +100,15 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         // it, and none can be two phases ahead of a waiter
         mbar_init(&sh.q_full, 1);
         mbar_init(&sh.q_empty, 1);
+        // V_f and K_{f+1} share a barrier: two copies, or two tiles from four warps
+        mbar_init(&sh.k_first, INT8 ? 4 : 1);
+        for (int i = 0; i < PAIRS; ++i) mbar_init(&sh.pair[i], INT8 ? 8 : 2);
         for (int i = 0; i < RING; ++i) {
-            mbar_init(&sh.full[i], INT8 ? 4 : 1);
-            mbar_init(&sh.empty[i], INT8 ? 1 : 2);     // the MMAs, and warp 2
+            mbar_init(&sh.empty[i], 1);
             mbar_init(&sh.raw_full[i], 1);
         }
-        for (int i = 0; i < V_AHEAD; ++i) mbar_init(&sh.v_ok[i], 1);
+        mbar_init(&sh.edge_go, 1);
+        mbar_init(&sh.v_ok, 4);
         for (int t = 0; t < TILES; ++t) {
             mbar_init(&sh.s_full[t], 1);
             mbar_init(&sh.p_full[t], 4);
@@ -114,7 +117,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         mbar_init(&sh.drain, 1);
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&sh.piece_full[i], 1);
-            mbar_init(&sh.piece_empty[i], INT8 ? 2 + 4 + 8 : 3 + 8);
+            mbar_init(&sh.piece_empty[i], 2 + 4 + 8);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sc_full[i], 4);
@@ -127,7 +130,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     if (warp == 2) tmem_alloc(&sh.tmem_slot, TMEM_COLS);
     // query rows that no copy reaches (groups that do not divide 128) are zeros
-    for (int i = threadIdx.x; i < (BM - p.tile_rows) * TILES * C::ATOMS * 8; i += C::THREADS) {
+    for (int i = threadIdx.x; i < (BM - p.tile_rows) * TILES * C::ATOMS * 8; i += THREADS) {
         const int r = p.tile_rows + (i >> 3) % (BM - p.tile_rows), a = (i >> 3) / (BM - p.tile_rows);
         *reinterpret_cast<uint4 *>(Qs + a * ATOM + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
     }
@@ -135,11 +138,13 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem_slot;
+    // through a warp-wide reduction, whose result the compiler knows to be the same in every
+    // lane: addresses and descriptors made from it need no transfer to uniform registers
+    const uint32_t tmem = __reduce_max_sync(0xffffffffu, sh.tmem_slot);
     volatile int *abort_v = &sh.abort_flag;
     pdl_enter();
     KvWalk walk;
-    kv_find<C::THREADS, false>(p.work, blockIdx.x, sh.found, walk);
+    kv_find<THREADS>(p.work, blockIdx.x, sh.found, walk);
     __syncthreads();                     // `found` makes room for the scales
     auto wait_all = [&](uint64_t *bar, uint32_t parity) -> bool {
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_v, p.err));
@@ -155,8 +160,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     };
 
     if (warp < 4) {
-        if constexpr (INT8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
+        // registers, of the launch's 512 * 128: 128 * (64 + 32) + 256 * 208, and for the
+        // conversion of int8 codes 128 * (64 + 48) + 256 * 200
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
         bool ok = true;
         if (warp == 3) {
             // ---------------- pieces, and their queries ----------------
@@ -171,7 +177,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         pc.shift = walk.s.shift;
                         pc.kb0 = walk.kb0;
                         pc.keys = walk.s.keys(p.work, walk.tile);
-                        pc.low = min(pc.keys, walk.s.top(p.work, walk.s.row + walk.tile * p.work.tile / p.work.group));
+                        const int low = min(pc.keys, walk.s.top(p.work, walk.s.row + walk.tile * p.work.tile / p.work.group));
+                        pc.clear = min(max(low / BN - walk.kb0, 0), walk.kb1 - walk.kb0);
                         pc.row = walk.s.row;
                         pc.packed = walk.s.packed;
                         pc.len = walk.s.len;
@@ -179,7 +186,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         pc.tile = walk.tile;
                         pc.seq = walk.seq;
                         pc.whole = walk.whole();
-                        pc.first = walk.first;
+                        pc.first = walk.kb0 == 0;
                         if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
                     }
                     mbar_arrive(&sh.piece_full[n % PIECES]);
@@ -199,6 +206,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
                 ++loads;
             }
+            if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
             if (*abort_v && loads > 0)
                 mbar_wait(&sh.q_full, (loads - 1) & 1, abort_v, nullptr, 100000000ull);
         } else if (warp == 0) {
@@ -237,7 +245,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         const int slot = li % RING;
                         ok = wait_all(&sh.empty[slot], ((li / RING) & 1) ^ 1);
                         if (!ok) break;
-                        uint64_t *bar = INT8 ? &sh.raw_full[slot] : &sh.full[slot];
+                        uint64_t *bar = INT8 ? &sh.raw_full[slot] : li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS];
                         uint8_t *dst = Ring + slot * C::SLOT;
                         // int8: both scales come with the keys
                         if (lane == 0)
@@ -269,12 +277,28 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     if (!ok) break;
                 }
             }
-            if (*abort_v && lane == 0)   // let this CTA's copies land before it exits
-                for (int i = max(0, li - RING); i < li; ++i)
-                    mbar_wait(INT8 ? &sh.raw_full[i % RING] : &sh.full[i % RING], (i / RING) & 1, abort_v,
-                              nullptr, 100000000ull);
+            // the last V has no K after it
+            if (!INT8 && li > 0 && lane == 0) mbar_arrive(&sh.pair[((li - 1) >> 1) % PAIRS]);
+            if (*abort_v && lane == 0) {   // let this CTA's copies land before it exits
+                if (INT8) {
+                    for (int i = max(0, li - RING); i < li; ++i)
+                        mbar_wait(&sh.raw_full[i % RING], (i / RING) & 1, abort_v, nullptr, 100000000ull);
+                } else if (li > 0) {
+                    mbar_wait(&sh.k_first, 0, abort_v, nullptr, 100000000ull);
+                    for (int i = max(0, (li - 1) / 2 - PAIRS); i < (li - 1) / 2; ++i)
+                        mbar_wait(&sh.pair[i % PAIRS], (i / PAIRS) & 1, abort_v, nullptr, 100000000ull);
+                }
+            }
         } else if (warp == 1) {
-            // ---------------- MMA issuer (see attn_tc_kernel of attention.cu) ----------------
+            // ---------------- products of both tiles ----------------
+            // The whole warp runs the loop and one elected lane issues (attn_tc_kernel of
+            // attention.cu).  P_t lies over the first half of S_t: MMAs of one thread run in
+            // order, so S of the next block cannot overtake the P V that reads it.  A wait
+            // costs about 130 cycles even when there is nothing to wait for, more than the
+            // tensor cores' queue holds: three a block, the next tiles' in the window of the
+            // first tile's softmax.  Whatever the loop carries comes from votes, which the
+            // compiler knows to be the same in every lane; from values read from memory it
+            // would move every descriptor to the uniform registers one by one.
             const bool leader = elect_one_sync();
             constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
             constexpr uint32_t LO_K = 1u << 16;
@@ -301,56 +325,99 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 for (int kk = 1; kk < BN / 16; ++kk)
                     tc_mma_f16_tmem_a(d, a + 8 * kk, desc(b_lo + (uint32_t)(kk * 2048 >> 4)), C::IDESC_PV, 1u);
             };
-            // the blocks of the next piece that has any, 0 at the end
-            int n = 0, pieces = 0;                            // taken, and those with blocks
-            auto next_blocks = [&]() -> int {
-                for (;;) {
+            auto uniform = [&](int v) -> int { return (int)__ballot_sync(0xffffffffu, (v >> lane) & 1); };
+            int n = 0;                                        // pieces taken
+            int blocks = 0, clear = 0;                        // of the piece that is there
+            // the next piece that has blocks; none: blocks 0
+            auto next_piece = [&]() {
+                for (blocks = 0; ok && blocks == 0; ++n) {
                     const Piece &pc = piece(n, ok);
-                    if (!ok || pc.blocks < 0) return 0;
-                    const int b = pc.blocks;
+                    if (!ok) return;
+                    blocks = uniform(pc.blocks);
+                    clear = uniform(pc.clear);
+                    if (blocks < 0) {
+                        blocks = 0;
+                        return;
+                    }
                     piece_done(n);
-                    ++n;
-                    if (b > 0) return b;
                 }
             };
-            int slot = 0;                                     // of K_f; V_f and K_{f+1} follow
-            uint32_t ph = 0;
-            auto next = [&](int &s, uint32_t &h) { if (++s == RING) { s = 0; h ^= 1u; } };
-            int left = next_blocks();                         // of the piece, block f included
-            if (left > 0 && ok) {
-                ok = wait_all(&sh.q_full, 0) && wait_all(&sh.full[0], 0);
-                if (ok) {
+            auto next2 = [](int s) { return s + 2 >= RING ? s + 2 - RING : s + 2; };
+            int vs = 1, ks = 2;                               // slots of V_f and K_{f+1}
+            int pr = 0;                                       // their barrier, and its parity
+            uint32_t pph = 0, fph = 0, qph = 0, eph = 0;      // parities of P, Q, edges
+            auto wait_pair = [&]() -> bool {
+                const bool there = wait_all(&sh.pair[pr], pph);
+                if (++pr == PAIRS) { pr = 0; pph ^= 1u; }
+                return there;
+            };
+            auto edge_go = [&]() { if (!INT8 && lane == 0) mbar_arrive(&sh.edge_go); };
+            auto edge_wait = [&]() -> bool {
+                if (INT8) return true;
+                const bool there = wait_all(&sh.v_ok, eph);
+                eph ^= 1u;
+                return there;
+            };
+            next_piece();
+            if (ok && blocks > 0 && (ok = wait_all(&sh.q_full, 0) && wait_all(&sh.k_first, 0))) {
+                tc_fence_after();
+                if (leader) {
+                    mma_s(0, 0);
+                    tc_commit(&sh.s_full[0]);
+                    mma_s(1, 0);
+                    tc_commit(&sh.s_full[1]);
+                    tc_commit(&sh.empty[0]);
+                    if (blocks == 1) tc_commit(&sh.q_empty);
+                }
+                __syncwarp();
+                ok = wait_pair();
+                if (clear == 0) edge_go();
+            }
+            while (ok && blocks > 0) {
+                const int nb = blocks, nclear = clear;
+                // all blocks but the last: here V_f and K_{f+1} are there
+                for (int j = 0; ok && j < nb - 1; ++j) {
+                    if (j >= nclear && !edge_wait()) { ok = false; break; }
+                    if (!wait_all(&sh.p_full[0], fph)) { ok = false; break; }
                     tc_fence_after();
                     if (leader) {
-                        mma_s(0, 0);
+                        mma_pv(0, vs, j > 0 ? 1u : 0u);
+                        mma_s(0, ks);
                         tc_commit(&sh.s_full[0]);
-                        mma_s(1, 0);
-                        tc_commit(&sh.s_full[1]);
-                        tc_commit(&sh.empty[0]);
-                        if (left == 1) tc_commit(&sh.q_empty);
                     }
                     __syncwarp();
+                    if (!wait_all(&sh.p_full[1], fph)) { ok = false; break; }
+                    tc_fence_after();
+                    if (leader) {
+                        mma_pv(1, vs, j > 0 ? 1u : 0u);
+                        tc_commit(&sh.empty[vs]);
+                        mma_s(1, ks);
+                        tc_commit(&sh.s_full[1]);
+                        tc_commit(&sh.empty[ks]);
+                        if (j == nb - 2) tc_commit(&sh.q_empty);
+                    }
+                    __syncwarp();
+                    vs = next2(vs);
+                    ks = next2(ks);
+                    fph ^= 1u;
+                    if (!wait_pair()) { ok = false; break; }
+                    if (j + 1 >= nclear) edge_go();
                 }
-            }
-            uint32_t acc = 0;
-            for (int f = 0; ok && left > 0; ++f) {
-                int vs = slot; uint32_t vph = ph; next(vs, vph);
-                int ks = vs; uint32_t kph = vph; next(ks, kph);
-                const bool last = left == 1;
-                // after the last block the next piece's: known before this block's P V
-                const int then = last ? next_blocks() : left - 1;
                 if (!ok) break;
-                if (!wait_all(&sh.p_full[0], f & 1)) { ok = false; break; }
-                if (!(INT8 ? wait_all(&sh.full[vs], vph) : wait_all(&sh.v_ok[f % V_AHEAD], (f / V_AHEAD) & 1))) { ok = false; break; }
+                // the last block, and the next piece's first S
+                const uint32_t acc = nb > 1 ? 1u : 0u;
+                if (nclear < nb && !edge_wait()) { ok = false; break; }
+                next_piece();
+                if (!ok || !wait_all(&sh.p_full[0], fph)) { ok = false; break; }
                 tc_fence_after();
                 if (leader) {
                     mma_pv(0, vs, acc);
-                    if (last) tc_commit(&sh.pv_done[0]);
+                    tc_commit(&sh.pv_done[0]);
                 }
                 __syncwarp();
-                if (then > 0) {
-                    if (last && !wait_all(&sh.q_full, ++pieces & 1)) { ok = false; break; }
-                    if (!wait_all(&sh.full[ks], kph)) { ok = false; break; }
+                if (blocks > 0) {
+                    qph ^= 1u;
+                    if (!wait_all(&sh.q_full, qph)) { ok = false; break; }
                     tc_fence_after();
                     if (leader) {
                         mma_s(0, ks);
@@ -358,53 +425,60 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     }
                     __syncwarp();
                 }
-                if (!wait_all(&sh.p_full[1], f & 1)) { ok = false; break; }
+                if (!wait_all(&sh.p_full[1], fph)) { ok = false; break; }
                 tc_fence_after();
                 if (leader) {
                     mma_pv(1, vs, acc);
                     tc_commit(&sh.empty[vs]);
-                    if (last) tc_commit(&sh.pv_done[1]);
-                    if (then > 0) {
+                    tc_commit(&sh.pv_done[1]);
+                    if (blocks > 0) {
                         mma_s(1, ks);
                         tc_commit(&sh.s_full[1]);
                         tc_commit(&sh.empty[ks]);
-                        if (then == 1) tc_commit(&sh.q_empty);
+                        if (blocks == 1) tc_commit(&sh.q_empty);
                     }
                 }
                 __syncwarp();
-                acc = last ? 0u : 1u;
-                left = then;
-                slot = ks;
-                ph = kph;
+                vs = next2(vs);
+                ks = next2(ks);
+                fph ^= 1u;
+                if (blocks > 0) {
+                    ok = wait_pair();
+                    if (ok && clear == 0) edge_go();
+                }
             }
             if (!ok && leader) {   // the MMAs already issued, before tensor memory is freed
                 tc_commit(&sh.drain);
                 mbar_wait(&sh.drain, 0, abort_v, nullptr, 100000000ull);
             }
             __syncwarp();
-        } else if (!INT8) {
+        }
+    } else if (warp < SOFT0) {
+        if constexpr (INT8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 32;" ::: "memory");
+        bool ok = true;
+        int f = 0;                                            // block
+        if constexpr (!INT8) {
             // ---------------- values that no row may use, cleared ----------------
-            int f = 0;
+            int edge = 0;
             for (int n = 0; ok; ++n) {
                 const Piece &pc = piece(n, ok);
                 if (!ok || pc.blocks < 0) break;
-                const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks, keys = pc.keys, low = pc.low;
+                const int blocks = pc.blocks, clear = pc.clear, keys = pc.keys - pc.kb0 * BN;
                 piece_done(n);
-                for (int kb = kb0; kb < kb1; ++kb, ++f) {
-                    // every copy is seen here before its tile is filled again
-                    ok = wait_all(&sh.full[2 * f % RING], (2 * f / RING) & 1);
+                f += clear;
+                for (int j = clear; j < blocks; ++j, ++f, ++edge) {
+                    // from the warp that issues the products: it has seen V_f's copy
+                    const int slot = (2 * f + 1) % RING;
+                    ok = wait_all(&sh.edge_go, edge & 1);
                     if (!ok) break;
-                    if (lane == 0) mbar_arrive(&sh.empty[2 * f % RING]);
-                    const int li = 2 * f + 1, slot = li % RING;
-                    ok = wait_all(&sh.full[slot], (li / RING) & 1);
-                    if (!ok) break;
-                    if ((kb + 1) * BN > low) {
-                        const int valid = keys - kb * BN;
-                        uint32_t spoilt[4] = {0, 0, 0, 0};
-                        // a lane's chunk of a row, four rows (or eight) at a time
+                    {
+                        const int valid = keys - j * BN;
+                        const int r0 = (warp - 4) * 32;       // this warp's keys
+                        uint32_t spoilt = 0;
 #pragma unroll 4
-                        for (int i = lane; i < BN * C::ATOMS * 8; i += 32) {
-                            const int r = (i >> 3) % BN, a = (i >> 3) / BN;
+                        for (int i = lane; i < 32 * C::ATOMS * 8; i += 32) {
+                            const int r = r0 + ((i >> 3) & 31), a = i >> 8;
                             uint4 *at = reinterpret_cast<uint4 *>(Ring + slot * C::SLOT + a * ATOM + r * 128) + (i & 7);
                             const uint4 v = *at;
                             // a bf16 is not finite if all bits of its exponent are set
@@ -415,32 +489,24 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                 bad |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
                             if (r >= valid || bad) {
                                 *at = make_uint4(0, 0, 0, 0);
-                                if (r < valid) spoilt[r >> 5] |= 1u << (r & 31);
+                                if (r < valid) spoilt |= 1u << (r & 31);
                             }
                         }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t all = __reduce_or_sync(0xffffffffu, spoilt[e]);
-                            if (lane == 0) sh.spoilt[f % V_AHEAD][e] = all;
-                        }
+                        spoilt = __reduce_or_sync(0xffffffffu, spoilt);
+                        if (lane == 0) sh.spoilt[edge % SPOILT][warp - 4] = spoilt;
                         fence_proxy_async_smem();
                     }
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&sh.v_ok[f % V_AHEAD]);
-                        mbar_arrive(&sh.empty[slot]);
-                    }
+                    if (lane == 0) mbar_arrive(&sh.v_ok);
                 }
             }
-        }
-    } else if (INT8 && warp < 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
+        } else {
         // ---------------- codes to bf16, a key per thread ----------------
         const int r = (int)threadIdx.x - 128;                 // key of the block
-        bool ok = true;
-        int f = 0;
         for (int n = 0; ok; ++n) {
             const Piece &pc = piece(n, ok);
+            if (ok && pc.blocks < 0 && f > 0 && lane == 0)    // the last V has no K after it
+                mbar_arrive(&sh.pair[(f - 1) % PAIRS]);
             if (!ok || pc.blocks < 0) break;
             const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks, keys = pc.keys;
             piece_done(n);
@@ -451,19 +517,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     ok = wait_all(&sh.raw_full[slot], (li / RING) & 1);
                     if (!ok) break;
                     uint8_t *tile = Ring + slot * C::SLOT;
+                    float ks = 0.f, vs = 0.f;
                     if (kv == 0) {
                         const float *sc = reinterpret_cast<const float *>(tile + (r & ~31) * 128) + lane;
-                        float ks = sc[0], vs = sc[32];
+                        ks = sc[0];
+                        vs = sc[32];
                         __syncwarp();                         // read before the rows are written
-                        const bool there = kb * BN + r < keys;
                         if (!(fabsf(vs) < INFINITY)) ks = NAN, vs = 0.f;
-                        if (!there) ks = vs = 0.f;            // slots past the end: anything
-                        ok = wait_all(&sh.sc_empty[f & 1], ((f >> 1) & 1) ^ 1);
-                        if (!ok) break;
-                        sh.scales[f & 1][0][r % (INT8 ? BN : 1)] = ks * p.scale_log2;
-                        sh.scales[f & 1][1][r % (INT8 ? BN : 1)] = vs;
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh.sc_full[f & 1]);
+                        if (kb * BN + r >= keys) ks = vs = 0.f;   // slots past the end: anything
                     }
 #pragma unroll
                     for (int a = 0; a < C::ATOMS; ++a) {
@@ -488,21 +549,30 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.full[slot]);
+                    if (lane == 0) mbar_arrive(li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS]);
+                    if (kv == 0) {                            // of block f - 2: done with by now
+                        ok = wait_all(&sh.sc_empty[f & 1], ((f >> 1) & 1) ^ 1);
+                        if (!ok) break;
+                        sh.scales[f & 1][0][r % (INT8 ? BN : 1)] = ks * p.scale_log2;
+                        sh.scales[f & 1][1][r % (INT8 ? BN : 1)] = vs;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.sc_full[f & 1]);
+                    }
                 }
             }
         }
+        }
     } else {
-        if constexpr (INT8) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;" ::: "memory");
+        if constexpr (INT8) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;" ::: "memory");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ---------------- softmax and output of tile t, a row per thread ----------------
-        const int t = (warp - C::SOFT0) >> 2, quad = warp & 3;
+        const int t = (warp - SOFT0) >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_at = tmem + lane_base + (uint32_t)(t * BN);
         const uint32_t o_at = tmem + lane_base + O_COL + (uint32_t)(t * D);
         const int row = quad * 32 + lane;                     // of the tile
         bool ok = true;
-        int f = 0, with_blocks = 0;
+        int f = 0, with_blocks = 0, edge = 0;
         for (int n = 0; ok; ++n) {
             const Piece &pc = piece(n, ok);
             if (!ok || pc.blocks < 0) break;
@@ -516,7 +586,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 lim = s.top(p.work, pc.row + pr / p.work.group);
             }
             const int warp_low = __reduce_min_sync(0xffffffffu, lim);
-            const int kb0 = pc.kb0, blocks = pc.blocks, low = pc.low;
+            const int kb0 = pc.kb0, blocks = pc.blocks, clear = pc.clear;
             float m = -FLT_MAX, l = 0.f;
             for (int j = 0; j < blocks; ++j, ++f) {
                 ok = wait_all(&sh.s_full[t], f & 1);
@@ -621,15 +691,16 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 tmem_st32(s_at, pk);
                 tmem_st32(s_at + 32, pk + 32);
                 tmem_st_wait();
-                if (!INT8 && key0 + BN > low) {                 // keys whose values are not finite
-                    ok = wait_all(&sh.v_ok[f % V_AHEAD], (f / V_AHEAD) & 1);
+                if (!INT8 && j >= clear) {                      // keys whose values are not finite
+                    ok = wait_all(&sh.v_ok, edge & 1);
                     if (!ok) break;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int seen = lim - key0 - 32 * e;
                         const uint32_t mask = seen >= 32 ? 0xffffffffu : seen > 0 ? (1u << seen) - 1u : 0u;
-                        if (sh.spoilt[f % V_AHEAD][e] & mask) l = NAN;
+                        if (sh.spoilt[edge % SPOILT][e] & mask) l = NAN;
                     }
+                    ++edge;
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -726,7 +797,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.err = echo::device_error_ptr();
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
+        echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(THREADS), SMEM, st, tq, tk, p);
     }
     echo::launch_kv_join(a, p.work, st);
     return echo::last_launch_status();

@@ -103,7 +103,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     volatile int *abort_v = &abort_flag;
     pdl_enter();
     KvWalk walk;
-    kv_find<THREADS, false>(p.work, blockIdx.x, found, walk);   // and its barriers
+    kv_find<THREADS>(p.work, blockIdx.x, found, walk);   // and its barriers
 
     if (warp == WARPS) {
         // ---------------- producer: the pieces' blocks, a page or part of one at a time ----
@@ -159,6 +159,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 }
             }
         }
+        if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
         if (*abort_v && lane == 0)   // let this CTA's copies land before it exits
             for (int i = max(0, g - C::RING); i < g; ++i)
                 mbar_wait(&full[i % C::RING], (i / C::RING) & 1, abort_v, nullptr, 100000000ull);
@@ -421,7 +422,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         }
         if (warp != 0) continue;
         const bool whole = walk.whole();
-        float *slot = kv_slot(p.ws, blockIdx.x, walk.first, ROWS, D);
+        float *slot = kv_slot(p.ws, blockIdx.x, walk.kb0 == 0, ROWS, D);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (!real[i]) continue;

@@ -60,7 +60,7 @@ struct KvWalk {
     KvSeq s;
     int seq, head, tile;   // of the current piece's item
     int kb0, kb1, nb;      // its key blocks, and the item's
-    bool first;            // the piece begins at the item's first unit
+    bool some;             // there has been a piece
     int64_t start, end, at;   // the worker's units, and those passed (the next item's first)
     int64_t total;            // units of all items
     int G;                    // workers that have any
@@ -96,16 +96,14 @@ struct KvWalk {
             }
             if (w.split) {
                 if (at <= start) continue;
-                first = from >= start;
                 kb0 = block_at(start, from, nb);
                 kb1 = block_at(end, from, nb);
             } else {
                 if (from < start) continue;
-                first = true;
                 kb0 = 0;
                 kb1 = nb;
             }
-            if (kb0 < kb1 || (nb == 0 && first)) return true;
+            if (kb0 < kb1 || (nb == 0 && from >= start)) return some = true;
         }
     }
 };
@@ -118,12 +116,12 @@ struct KvFound {
     int seq;
 };
 
-// The range of `worker`, and the walk set to the item that holds its first unit (AT_END:
-// the first unit past its range).  Called by every thread of the block.  Thread t looks
+// The range of `worker`, and the walk set to the item that holds its first unit.  Called by
+// every thread of the block.  Thread t looks
 // at sequences [t per, (t + 1) per), or a warp at each where there are no more sequences
-// than warps (a long chunk has many tiles).  False where there is no such item.
-template <int THREADS, bool AT_END>
-ECHO_DEV bool kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
+// than warps (a long chunk has many tiles).
+template <int THREADS>
+ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     constexpr int WARPS = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool by_warp = w.b.n_seqs <= WARPS;
@@ -166,7 +164,7 @@ ECHO_DEV bool kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     walk.G = want < w.workers ? (int)want : w.workers;
     walk.start = walk.unit_of(worker);
     walk.end = walk.unit_of(worker + 1);
-    const int64_t pos = AT_END ? walk.end : walk.start;
+    const int64_t pos = walk.start;
     if (by_warp) {
         const int64_t all = __shfl_sync(0xffffffffu, incl, 31);
         if (lane == 0 && before <= pos && pos < before + all) {
@@ -193,7 +191,8 @@ ECHO_DEV bool kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     walk.seq = -1;
     walk.nseq = w.b.n_seqs;
     walk.nhead = walk.ntile = 0;
-    if (sh.seq < 0 || walk.start >= walk.end) return false;
+    walk.some = false;
+    if (sh.seq < 0 || walk.start >= walk.end) return;
     walk.nseq = sh.seq;
     walk.at = sh.base;
     walk.s.load(w, walk.seq = walk.nseq);
@@ -211,17 +210,42 @@ ECHO_DEV bool kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
         const int i = __popc(__ballot_sync(0xffffffffu, walk.at + upto <= pos));
         walk.at += __shfl_sync(0xffffffffu, upto - u, i);
         walk.ntile = t0 + i;
-        return true;
+        return;
     }
 }
 
 // A slot of the workspace: the sums of one piece, `rows` rows of D unnormalised fp32
 // values and their (maximum, sum of weights) after them; a row's maximum is in the
-// exponent of two.  Slot 2 c: worker c's first piece (not begun at the item's beginning),
-// 2 c + 1: its last.
+// exponent of two.  Slot 2 c: worker c's piece that begins inside its item, 2 c + 1: the
+// one that begins there and ends early.
 ECHO_DEV float *kv_slot(float *ws, int worker, bool first, int rows, int D) {
     return ws + (int64_t)(2 * worker + (first ? 1 : 0)) * rows * (D + 2);
 }
+// What worker c leaves for the joining kernel, after the slots: its last piece, where that
+// begins its item and `more` workers after it go on with it.
+struct KvJoin {
+    int more, row, packed0, rows, head;   // first row of the sequence; packed rows of the item
+};
+ECHO_DEV KvJoin *kv_joins(float *ws, const KvWork &w, int D) {
+    return reinterpret_cast<KvJoin *>(ws + (int64_t)2 * w.workers * w.slot_rows * (D + 2));
+}
+// After the last call of walk.next(), by one thread of each CTA.
+ECHO_DEV void kv_leave_join(const KvWork &w, const KvWalk &walk, float *ws, int D) {
+    if (!w.split) return;
+    KvJoin j = {0, 0, 0, 0, 0};
+    if (walk.some && walk.kb0 == 0 && walk.kb0 < walk.kb1 && walk.kb1 < walk.nb) {   // the last piece, cut short
+        while (walk.unit_of((int)blockIdx.x + 1 + j.more) < walk.at) ++j.more;
+        j.row = walk.s.row;
+        j.packed0 = walk.tile * w.tile;
+        j.rows = min(w.tile, walk.s.packed - j.packed0);
+        j.head = walk.head;
+    }
+    kv_joins(ws, w, D)[blockIdx.x] = j;
+}
+inline size_t kv_workspace_bytes(int workers, int rows, int D) {
+    return (size_t)workers * (2 * rows * (D + 2) * 4 + sizeof(KvJoin));
+}
+
 namespace echo {
 inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_shift, int workers) {
     const echo_kv_pool &p = *a.pool;
@@ -242,6 +266,3 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
 }
 void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st);
 }  // namespace echo
-inline size_t kv_workspace_bytes(int workers, int rows, int D) {
-    return (size_t)workers * 2 * rows * (D + 2) * 4;
-}
