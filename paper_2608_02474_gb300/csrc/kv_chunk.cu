@@ -22,6 +22,7 @@
 // spoils the key's score, and stands as 0 among the values' scales.
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
 #include <cfloat>
+#include <type_traits>
 
 #include "kv_schedule.cuh"
 
@@ -375,10 +376,11 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             while (ok && blocks > 0) {
                 const int nb = blocks, nclear = clear;
-                // all blocks but the last: here V_f and K_{f+1} are there
-                for (int j = 0; ok && j < nb - 1; ++j) {
-                    if (j >= nclear && !edge_wait()) { ok = false; break; }
-                    if (!wait_all(&sh.p_full[0], fph)) { ok = false; break; }
+                // all blocks but the last: here V_f and K_{f+1} are there.  EDGE: some row may
+                // not see the block, or the next one, whole, or the next one is the last
+                auto block = [&](int j, auto EDGE) -> bool {
+                    if (EDGE && j >= nclear && !edge_wait()) return false;
+                    if (!wait_all(&sh.p_full[0], fph)) return false;
                     tc_fence_after();
                     if (leader) {
                         mma_pv(0, vs, j > 0 ? 1u : 0u);
@@ -386,7 +388,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         tc_commit(&sh.s_full[0]);
                     }
                     __syncwarp();
-                    if (!wait_all(&sh.p_full[1], fph)) { ok = false; break; }
+                    if (!wait_all(&sh.p_full[1], fph)) return false;
                     tc_fence_after();
                     if (leader) {
                         mma_pv(1, vs, j > 0 ? 1u : 0u);
@@ -394,15 +396,20 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         mma_s(1, ks);
                         tc_commit(&sh.s_full[1]);
                         tc_commit(&sh.empty[ks]);
-                        if (j == nb - 2) tc_commit(&sh.q_empty);
+                        if (EDGE && j == nb - 2) tc_commit(&sh.q_empty);
                     }
                     __syncwarp();
                     vs = next2(vs);
                     ks = next2(ks);
                     fph ^= 1u;
-                    if (!wait_pair()) { ok = false; break; }
-                    if (j + 1 >= nclear) edge_go();
-                }
+                    if (!wait_pair()) return false;
+                    if (EDGE && j + 1 >= nclear) edge_go();
+                    return true;
+                };
+                const int plain = min(nclear - 1, nb - 2);
+                int j = 0;
+                for (; ok && j < plain; ++j) ok = block(j, std::false_type());
+                for (; ok && j < nb - 1; ++j) ok = block(j, std::true_type());
                 if (!ok) break;
                 // the last block, and the next piece's first S
                 const uint32_t acc = nb > 1 ? 1u : 0u;
