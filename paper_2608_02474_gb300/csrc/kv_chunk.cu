@@ -60,13 +60,8 @@ struct ChunkParams {
     int *err;
 };
 
-struct Piece {
-    int64_t shift;
-    int blocks, kb0, keys;           // blocks < 0: no more pieces
-    int clear;                       // its first blocks that every row sees whole
-    int row, packed, len, head, tile, seq;
-    int whole, first;
-};
+// the first blocks of a piece that every row sees whole
+ECHO_DEV int kv_clear(const KvPiece &pc) { return min(max(pc.low / BN - pc.kb0, 0), max(pc.blocks, 0)); }
 
 // what shared memory holds beside the tiles
 template <bool INT8, int D>
@@ -75,7 +70,7 @@ struct Side {
     uint64_t q_full, q_empty, k_first, pair[PAIRS], empty[RING], raw_full[RING], edge_go, v_ok;
     uint64_t s_full[TILES], p_full[TILES], pv_done[TILES], drain;
     uint64_t piece_full[PIECES], piece_empty[PIECES], sc_full[2], sc_empty[2];
-    Piece piece[PIECES];
+    KvPiece piece[PIECES];
     uint32_t spoilt[SPOILT][4];      // keys of a block with values that are not finite
     uint32_t tmem_slot;
     int abort_flag;
@@ -151,7 +146,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_v, p.err));
     };
     // the n-th piece, once it is there
-    auto piece = [&](int n, bool &ok) -> const Piece & {
+    auto piece = [&](int n, bool &ok) -> const KvPiece & {
         ok = wait_all(&sh.piece_full[n % PIECES], (n / PIECES) & 1);
         return sh.piece[n % PIECES];
     };
@@ -168,27 +163,20 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (warp == 3) {
             // ---------------- pieces, and their queries ----------------
             int n = 0, loads = 0;
+            bool tail = false;
             for (bool more = true; more; ++n) {
                 more = walk.next(p.work);
                 if (n >= PIECES && !wait_all(&sh.piece_empty[n % PIECES], ((n / PIECES) & 1) ^ 1)) break;
-                Piece &pc = sh.piece[n % PIECES];
+                KvPiece &pc = sh.piece[n % PIECES];
                 if (lane == 0) {
-                    pc.blocks = more ? walk.kb1 - walk.kb0 : -1;
                     if (more) {
-                        pc.shift = walk.s.shift;
-                        pc.kb0 = walk.kb0;
-                        pc.keys = walk.s.keys(p.work, walk.tile);
-                        const int low = min(pc.keys, walk.s.top(p.work, walk.s.row + walk.tile * p.work.tile / p.work.group));
-                        pc.clear = min(max(low / BN - walk.kb0, 0), walk.kb1 - walk.kb0);
-                        pc.row = walk.s.row;
-                        pc.packed = walk.s.packed;
-                        pc.len = walk.s.len;
-                        pc.head = walk.head;
-                        pc.tile = walk.tile;
-                        pc.seq = walk.seq;
-                        pc.whole = walk.whole();
-                        pc.first = walk.kb0 == 0;
+                        walk.put(p.work, pc);
                         if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
+                        if (walk.tail()) kv_leave_join(p.work, walk, p.ws, D);
+                        tail |= walk.tail();
+                    } else {
+                        pc.blocks = -1;
+                        if (!tail) kv_leave_join(p.work, walk, p.ws, D);
                     }
                     mbar_arrive(&sh.piece_full[n % PIECES]);
                 }
@@ -207,7 +195,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
                 ++loads;
             }
-            if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
             if (*abort_v && loads > 0)
                 mbar_wait(&sh.q_full, (loads - 1) & 1, abort_v, nullptr, 100000000ull);
         } else if (warp == 0) {
@@ -215,7 +202,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int shift = p.pool.shift, per_block = BN >> shift;
             int li = 0;                                       // copies into the ring so far
             for (int n = 0; ok; ++n) {
-                const Piece &pc = piece(n, ok);
+                const KvPiece &pc = piece(n, ok);
                 if (!ok || pc.blocks < 0) break;
                 const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks, head = pc.head, keys = pc.keys;
                 const int32_t *table = p.work.b.table + (int64_t)pc.seq * p.work.b.max_pages;
@@ -332,10 +319,10 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // the next piece that has blocks; none: blocks 0
             auto next_piece = [&]() {
                 for (blocks = 0; ok && blocks == 0; ++n) {
-                    const Piece &pc = piece(n, ok);
+                    const KvPiece &pc = piece(n, ok);
                     if (!ok) return;
                     blocks = uniform(pc.blocks);
-                    clear = uniform(pc.clear);
+                    clear = uniform(kv_clear(pc));
                     if (blocks < 0) {
                         blocks = 0;
                         return;
@@ -469,9 +456,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // ---------------- values that no row may use, cleared ----------------
             int edge = 0;
             for (int n = 0; ok; ++n) {
-                const Piece &pc = piece(n, ok);
+                const KvPiece &pc = piece(n, ok);
                 if (!ok || pc.blocks < 0) break;
-                const int blocks = pc.blocks, clear = pc.clear, keys = pc.keys - pc.kb0 * BN;
+                const int blocks = pc.blocks, clear = kv_clear(pc), keys = pc.keys - pc.kb0 * BN;
                 piece_done(n);
                 f += clear;
                 for (int j = clear; j < blocks; ++j, ++f, ++edge) {
@@ -511,7 +498,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         // ---------------- codes to bf16, a key per thread ----------------
         const int r = (int)threadIdx.x - 128;                 // key of the block
         for (int n = 0; ok; ++n) {
-            const Piece &pc = piece(n, ok);
+            const KvPiece &pc = piece(n, ok);
             if (ok && pc.blocks < 0 && f > 0 && lane == 0)    // the last V has no K after it
                 mbar_arrive(&sh.pair[(f - 1) % PAIRS]);
             if (!ok || pc.blocks < 0) break;
@@ -581,7 +568,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         bool ok = true;
         int f = 0, with_blocks = 0, edge = 0;
         for (int n = 0; ok; ++n) {
-            const Piece &pc = piece(n, ok);
+            const KvPiece &pc = piece(n, ok);
             if (!ok || pc.blocks < 0) break;
             const int pr = (pc.tile * TILES + t) * p.tile_rows + row;        // packed row
             const bool real = row < p.tile_rows && pr < pc.packed;
@@ -593,7 +580,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 lim = s.top(p.work, pc.row + pr / p.work.group);
             }
             const int warp_low = __reduce_min_sync(0xffffffffu, lim);
-            const int kb0 = pc.kb0, blocks = pc.blocks, clear = pc.clear;
+            const int kb0 = pc.kb0, blocks = pc.blocks, clear = kv_clear(pc);
             float m = -FLT_MAX, l = 0.f;
             for (int j = 0; j < blocks; ++j, ++f) {
                 ok = wait_all(&sh.s_full[t], f & 1);
@@ -732,7 +719,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             const int slot_row = t * p.tile_rows + row;
             if (!whole) {
-                part = kv_slot(p.ws, blockIdx.x, pc.first, SLOT_ROWS, D);
+                part = kv_slot(p.ws, blockIdx.x, pc.tail, SLOT_ROWS, D);
                 if (real) *reinterpret_cast<float2 *>(part + SLOT_ROWS * D + 2 * slot_row) = make_float2(m, l);
                 part += (int64_t)slot_row * D;
             }

@@ -20,6 +20,7 @@ namespace {
 constexpr int WARPS = 4;                       // that compute
 constexpr int THREADS = 32 * (WARPS + 1);
 constexpr int ROWS = 16;
+constexpr int PIECES = 4;                      // handed out ahead
 
 template <bool INT8, int D>
 struct Cfg {
@@ -85,7 +86,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                 ~static_cast<uintptr_t>(1023));
     float *join = reinterpret_cast<float *>(smem + C::RING * C::STAGE);
-    __shared__ __align__(8) uint64_t full[C::RING], empty[C::RING];
+    __shared__ __align__(8) uint64_t full[C::RING], empty[C::RING], piece_full[PIECES], piece_empty[PIECES];
+    __shared__ KvPiece piece[PIECES];
     __shared__ float2 row_ml[WARPS][ROWS];
     __shared__ KvFound found;
     __shared__ int abort_flag;
@@ -95,6 +97,10 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         for (int i = 0; i < C::RING; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], WARPS);
+        }
+        for (int i = 0; i < PIECES; ++i) {
+            mbar_init(&piece_full[i], 1);
+            mbar_init(&piece_empty[i], WARPS);
         }
         abort_flag = 0;
         fence_barrier_init();
@@ -110,8 +116,22 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         const int shift = p.pool.shift, cs = min(shift, C::BSHIFT);   // tokens of a copy: 1 << cs
         const int per_block = BK >> cs;
         int g = 0;
-        bool ok = true;
-        while (ok && walk.next(p.work)) {
+        bool ok = true, tail = false;
+        for (int n = 0; ok; ++n) {
+            const bool more = walk.next(p.work);
+            if (n >= PIECES) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&piece_empty[n % PIECES], ((n / PIECES) & 1) ^ 1, abort_v, p.err));
+                if (!ok) break;
+            }
+            if (lane == 0) {
+                KvPiece &pc = piece[n % PIECES];
+                if (more) walk.put(p.work, pc);
+                else pc.blocks = -1;
+                mbar_arrive(&piece_full[n % PIECES]);
+                if (more ? walk.tail() : !tail) kv_leave_join(p.work, walk, p.ws, D);
+            }
+            if (!more) break;
+            tail |= walk.tail();
             const int keys = walk.s.keys(p.work, walk.tile);
             if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
             const int copies = (keys + (1 << cs) - 1) >> cs;
@@ -159,7 +179,6 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 }
             }
         }
-        if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
         if (*abort_v && lane == 0)   // let this CTA's copies land before it exits
             for (int i = max(0, g - C::RING); i < g; ++i)
                 mbar_wait(&full[i % C::RING], (i / C::RING) & 1, abort_v, nullptr, 100000000ull);
@@ -173,20 +192,28 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     const int mi = lane >> 3, mr = lane & 7;
     int g = 0;
     bool ok = true;
-    while (ok && walk.next(p.work)) {
-        const KvSeq &s = walk.s;
-        const int keys = s.keys(p.work, walk.tile), group = p.work.group;
+    for (int n = 0; ok; ++n) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&piece_full[n % PIECES], (n / PIECES) & 1, abort_v, p.err));
+        ok = !named_bar_or(1, 32 * WARPS, !ok);      // the four warps stay together
+        const KvPiece &pc = piece[n % PIECES];
+        if (!ok || pc.blocks < 0) break;
+        KvSeq s;
+        s.row = pc.row;
+        s.packed = pc.packed;
+        s.len = pc.len;
+        s.shift = pc.shift;
+        const int keys = pc.keys, low = pc.low, group = p.work.group, tile = pc.tile, head = pc.head;
+        const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks;
         // rows gq and gq + 8 of the tile: their queries, and the keys that they see
         uint32_t qa[D / 16][4];
-        int lim[2], low = s.top(p.work, s.row + walk.tile * ROWS / group);
-        low = min(low, keys);
+        int lim[2];
         int64_t at[2];                               // row and first column of the row's head
         bool real[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int pr = walk.tile * ROWS + gq + 8 * i;
+            const int pr = tile * ROWS + gq + 8 * i;
             real[i] = pr < s.packed;
-            const int r = s.row + pr / group, h = walk.head * group + pr % group;
+            const int r = s.row + pr / group, h = head * group + pr % group;
             lim[i] = real[i] ? s.top(p.work, r) : keys;
             at[i] = real[i] ? (int64_t)r * p.ldq + h * D : 0;
 #pragma unroll
@@ -206,7 +233,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             }
         }
         float o[OT][4] = {}, m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};
-        for (int kb = walk.kb0; kb < walk.kb1; ++kb, ++g) {
+        for (int kb = kb0; kb < kb1; ++kb, ++g) {
             const int stage = g % C::RING;
             ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (g / C::RING) & 1, abort_v, p.err));
             if (!ok) break;
@@ -420,15 +447,17 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             }
             named_bar_sync(1, 32 * WARPS);
         }
+        const bool whole = pc.whole;
+        float *slot = kv_slot(p.ws, blockIdx.x, pc.tail, ROWS, D);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&piece_empty[n % PIECES]);
         if (warp != 0) continue;
-        const bool whole = walk.whole();
-        float *slot = kv_slot(p.ws, blockIdx.x, walk.kb0 == 0, ROWS, D);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (!real[i]) continue;
-            const int row = gq + 8 * i, pr = walk.tile * ROWS + row;
+            const int row = gq + 8 * i, pr = tile * ROWS + row;
             const float inv = lt[i] == 0.f ? 0.f : 1.f / lt[i];      // no key: zeros
-            __nv_bfloat16 *dst = p.out + (int64_t)(s.row + pr / group) * p.ldo + (walk.head * group + pr % group) * D;
+            __nv_bfloat16 *dst = p.out + (int64_t)(s.row + pr / group) * p.ldo + (head * group + pr % group) * D;
             float *part = slot + row * D;
             if (!whole && tq == 0) *reinterpret_cast<float2 *>(slot + ROWS * D + 2 * row) = make_float2(mt[i], lt[i]);
             if constexpr (INT8) {

@@ -55,56 +55,121 @@ struct KvSeq {             // one sequence of the batch
     }
 };
 
-// A worker's walk over its pieces; the same in every thread that keeps one.
+// One piece of an item, as the warps of a CTA hand it on.
+struct KvPiece {
+    int64_t shift;           // KvSeq::shift
+    int blocks;              // key blocks from kb0 on; < 0: no more pieces
+    int kb0, keys;           // keys that any row of the tile sees
+    int low;                 // keys that every row sees
+    int row, packed, len, head, tile, seq;
+    int whole, tail;         // all of the item's keys; or the last of them
+};
+
+// A worker's walk over its pieces.  First its whole items, and then the piece that it takes
+// over from the worker before and the one that the worker after goes on with: the whole
+// items of all workers begin together, and those of a head run through its keys in step,
+// so that each key block is read from memory once and from the L2 by the others.  For the
+// same reason the worker that goes on with an item takes its first keys: 1560 rows over
+// 32760 keys (40 heads of 128, bf16) 768 -> 695 us.
 struct KvWalk {
     KvSeq s;
-    int seq, head, tile;   // of the current piece's item
-    int kb0, kb1, nb;      // its key blocks, and the item's
-    bool some;             // there has been a piece
-    int64_t start, end, at;   // the worker's units, and those passed (the next item's first)
+    int seq, head, tile;      // of the current piece's item
+    int kb0, kb1, nb;         // its key blocks, and the item's
+    int64_t start, end;       // the worker's units
     int64_t total;            // units of all items
     int G;                    // workers that have any
-    int nseq, nhead, ntile;   // the next item
+    struct Item {
+        int seq, head, tile;
+        int64_t at;           // its first unit
+    } here, first;            // the next item; the one that holds `start`
+    int64_t from;             // the first unit of the current piece's item
+    int stage;                // 0: whole items, 1: the first, 2: the last, 3: none
+    bool begun;               // `start` lies inside an item
 
     ECHO_DEV int64_t unit_of(int worker) const { return worker < G ? total * worker / G : total; }
-    // the first key block of an item (units from ..) that `unit` or a later one pays for
-    static ECHO_DEV int block_at(int64_t unit, int64_t from, int nb) {
+    // key blocks of an item (units from `from`) that the units before `unit` pay for, the
+    // last ones first
+    static ECHO_DEV int paid(int64_t unit, int64_t from, int nb) {
         return (int)min(max(unit - from - kFixedUnits, (int64_t)0), (int64_t)nb);
     }
     ECHO_DEV bool whole() const { return kb0 == 0 && kb1 == nb; }
+    ECHO_DEV bool tail() const { return kb1 == nb && kb0 > 0; }
 
+    ECHO_DEV void item(const KvWork &w, const Item &it) {
+        if (it.seq != seq) s.load(w, seq = it.seq);
+        head = it.head;
+        tile = it.tile;
+        from = it.at;
+        nb = s.blocks(w, tile);
+    }
+    ECHO_DEV void advance(const KvWork &w) {       // past `here`, which is the current item
+        here.at += kFixedUnits + nb;
+        if (++here.tile == s.tiles(w)) {
+            here.tile = 0;
+            if (++here.head == w.H) {
+                here.head = 0;
+                ++here.seq;
+            }
+        }
+    }
     // the next piece that has something to do; false at the end
     ECHO_DEV bool next(const KvWork &w) {
-        for (;;) {
-            if (nseq >= w.b.n_seqs || at >= end) return false;
-            if (nseq != seq) s.load(w, seq = nseq);
+        while (stage == 0) {
+            if (here.seq >= w.b.n_seqs || here.at >= end) {
+                stage = 1;
+                here.seq = w.b.n_seqs;             // no last piece
+                break;
+            }
+            if (here.seq != seq) s.load(w, seq = here.seq);
             if (s.packed == 0) {
-                ++nseq;
+                ++here.seq;
                 continue;
             }
-            head = nhead;
-            tile = ntile;
-            nb = s.blocks(w, tile);
-            const int64_t from = at;
-            at += kFixedUnits + nb;
-            if (++ntile == s.tiles(w)) {
-                ntile = 0;
-                if (++nhead == w.H) {
-                    nhead = 0;
-                    ++nseq;
-                }
+            item(w, here);
+            if (w.split && here.at + kFixedUnits + nb > end) {
+                stage = 1;
+                break;
             }
-            if (w.split) {
-                if (at <= start) continue;
-                kb0 = block_at(start, from, nb);
-                kb1 = block_at(end, from, nb);
-            } else {
-                if (from < start) continue;
-                kb0 = 0;
-                kb1 = nb;
-            }
-            if (kb0 < kb1 || (nb == 0 && from >= start)) return some = true;
+            kb0 = 0;
+            kb1 = nb;
+            advance(w);
+            return true;
         }
+        if (stage == 1) {
+            stage = 2;
+            if (begun) {
+                item(w, first);
+                kb1 = nb - paid(start, first.at, nb);
+                kb0 = nb - paid(end, first.at, nb);
+                if (kb0 < kb1) return true;
+            }
+        }
+        if (stage == 2) {
+            stage = 3;
+            if (here.seq < w.b.n_seqs) {
+                item(w, here);
+                kb1 = nb;
+                kb0 = nb - paid(end, here.at, nb);
+                if (kb0 < kb1 || nb == 0) return true;
+            }
+        }
+        kb0 = kb1 = 0;
+        return false;
+    }
+    ECHO_DEV void put(const KvWork &w, KvPiece &pc) const {
+        pc.shift = s.shift;
+        pc.blocks = kb1 - kb0;
+        pc.kb0 = kb0;
+        pc.keys = s.keys(w, tile);
+        pc.low = min(pc.keys, s.top(w, s.row + tile * w.tile / w.group));
+        pc.row = s.row;
+        pc.packed = s.packed;
+        pc.len = s.len;
+        pc.head = head;
+        pc.tile = tile;
+        pc.seq = seq;
+        pc.whole = whole();
+        pc.tail = tail();
     }
 };
 
@@ -189,52 +254,63 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     }
     __syncthreads();
     walk.seq = -1;
-    walk.nseq = w.b.n_seqs;
-    walk.nhead = walk.ntile = 0;
-    walk.some = false;
+    walk.here = {w.b.n_seqs, 0, 0, 0};
+    walk.stage = 3;
+    walk.begun = false;
+    walk.kb0 = walk.kb1 = 0;
     if (sh.seq < 0 || walk.start >= walk.end) return;
-    walk.nseq = sh.seq;
-    walk.at = sh.base;
-    walk.s.load(w, walk.seq = walk.nseq);
-    walk.nhead = (int)((pos - walk.at) / sh.per_head);
-    walk.at += walk.nhead * sh.per_head;
+    walk.stage = 0;
+    KvWalk::Item &it = walk.here;
+    it.seq = sh.seq;
+    it.at = sh.base;
+    walk.s.load(w, walk.seq = it.seq);
+    it.head = (int)((pos - it.at) / sh.per_head);
+    it.at += it.head * sh.per_head;
     // the tile, 32 at a time: every warp finds it for itself
     const int tiles = walk.s.tiles(w);
     for (int t0 = 0;; t0 += 32) {
         const int64_t u = t0 + lane < tiles ? kFixedUnits + walk.s.blocks(w, t0 + lane) : 0;
         const int64_t upto = scan(u), all = __shfl_sync(0xffffffffu, upto, 31);
-        if (walk.at + all <= pos && t0 + 32 < tiles) {
-            walk.at += all;
+        if (it.at + all <= pos && t0 + 32 < tiles) {
+            it.at += all;
             continue;
         }
-        const int i = __popc(__ballot_sync(0xffffffffu, walk.at + upto <= pos));
-        walk.at += __shfl_sync(0xffffffffu, upto - u, i);
-        walk.ntile = t0 + i;
-        return;
+        const int i = __popc(__ballot_sync(0xffffffffu, it.at + upto <= pos));
+        it.at += __shfl_sync(0xffffffffu, upto - u, i);
+        it.tile = t0 + i;
+        break;
+    }
+    if (it.at < walk.start) {      // begun by the worker before
+        walk.begun = w.split;
+        walk.first = it;
+        walk.item(w, it);
+        walk.advance(w);
     }
 }
 
 // A slot of the workspace: the sums of one piece, `rows` rows of D unnormalised fp32
 // values and their (maximum, sum of weights) after them; a row's maximum is in the
-// exponent of two.  Slot 2 c: worker c's piece that begins inside its item, 2 c + 1: the
-// one that begins there and ends early.
-ECHO_DEV float *kv_slot(float *ws, int worker, bool first, int rows, int D) {
-    return ws + (int64_t)(2 * worker + (first ? 1 : 0)) * rows * (D + 2);
+// exponent of two.  Slot 2 c + 1: worker c's piece with its item's last keys (and not the
+// first), 2 c: its other piece.
+ECHO_DEV float *kv_slot(float *ws, int worker, bool tail, int rows, int D) {
+    return ws + (int64_t)(2 * worker + (tail ? 1 : 0)) * rows * (D + 2);
 }
-// What worker c leaves for the joining kernel, after the slots: its last piece, where that
-// begins its item and `more` workers after it go on with it.
+// What worker c leaves for the joining kernel, after the slots: the item that it began and
+// `more` workers after it went on with.
 struct KvJoin {
     int more, row, packed0, rows, head;   // first row of the sequence; packed rows of the item
 };
 ECHO_DEV KvJoin *kv_joins(float *ws, const KvWork &w, int D) {
     return reinterpret_cast<KvJoin *>(ws + (int64_t)2 * w.workers * w.slot_rows * (D + 2));
 }
-// After the last call of walk.next(), by one thread of each CTA.
+// With walk at its piece with an item's last keys, or at its end where there was none; by
+// one thread of each CTA.
 ECHO_DEV void kv_leave_join(const KvWork &w, const KvWalk &walk, float *ws, int D) {
     if (!w.split) return;
     KvJoin j = {0, 0, 0, 0, 0};
-    if (walk.some && walk.kb0 == 0 && walk.kb0 < walk.kb1 && walk.kb1 < walk.nb) {   // the last piece, cut short
-        while (walk.unit_of((int)blockIdx.x + 1 + j.more) < walk.at) ++j.more;
+    if (walk.tail()) {
+        const int64_t upto = walk.from + kFixedUnits + walk.nb;
+        while (walk.unit_of((int)blockIdx.x + 1 + j.more) < upto) ++j.more;
         j.row = walk.s.row;
         j.packed0 = walk.tile * w.tile;
         j.rows = min(w.tile, walk.s.packed - j.packed0);
