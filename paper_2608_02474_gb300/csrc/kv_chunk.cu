@@ -29,7 +29,6 @@
 namespace {
 
 constexpr int BM = 128, TILES = 2, BN = 128;
-constexpr int THREADS = 512, SOFT0 = 8;         // warps 0-3, 4-7, and the softmax from SOFT0 on
 constexpr int ATOM = 128 * 128;                 // 128 rows of 64 bf16
 constexpr uint32_t TMEM_COLS = 512, O_COL = 256;
 constexpr int PIECES = 4;                       // handed out ahead
@@ -39,12 +38,20 @@ constexpr int SPOILT = 2;                       // blocks whose spoilt keys are 
 
 template <bool INT8, int D>
 struct Cfg {
+    // warps 0-3, helpers from 4 on, softmax
+    static constexpr int HELP = 4, SOFT0 = 4 + HELP, THREADS = 32 * (SOFT0 + 8);
     static constexpr int ATOMS = D / 64;
     static constexpr int Q_BYTES = ATOMS * ATOM;               // of a tile
     // int8 codes land at byte ATOM of their tile: for d 128 in its second half
     static constexpr int SLOT = INT8 && D == 64 ? ATOM + ATOM / 2 : ATOMS * ATOM;
     static constexpr int RING = D == 128 ? 5 : 6;
     static constexpr int TILES_BYTES = TILES * Q_BYTES + RING * SLOT;
+    // registers of warps 0-3, of four helpers and of four softmax warps: together at most
+    // what the launch gives.  4864 rows over 32768 keys, 8 heads of 128: bf16
+    // 350 us (64, 32, 208: 355; 80, 32, 200: 357), int8 512 us (72, 56, 192: 519)
+    static constexpr int REGS[3] = {INT8 ? 56 : 72, INT8 ? 56 : 24, INT8 ? 200 : 208};
+    static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
+                  "setmaxnreg takes from the launch's registers");
     static constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
     static constexpr uint32_t IDESC_PV = idesc_bf16_f32(BM, D) | (1u << 16);   // B MN-major
 };
@@ -81,7 +88,7 @@ struct Side {
 };
 
 template <bool INT8, int D>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__((Cfg<INT8, D>::THREADS), 1)
 kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
                 const ChunkParams p) {
     using C = Cfg<INT8, D>;
@@ -113,7 +120,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         mbar_init(&sh.drain, 1);
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&sh.piece_full[i], 1);
-            mbar_init(&sh.piece_empty[i], 2 + 4 + 8);
+            mbar_init(&sh.piece_empty[i], 2 + C::HELP + 8);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.sc_full[i], 4);
@@ -126,7 +133,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     if (warp == 2) tmem_alloc(&sh.tmem_slot, TMEM_COLS);
     // query rows that no copy reaches (groups that do not divide 128) are zeros
-    for (int i = threadIdx.x; i < (BM - p.tile_rows) * TILES * C::ATOMS * 8; i += THREADS) {
+    for (int i = threadIdx.x; i < (BM - p.tile_rows) * TILES * C::ATOMS * 8; i += C::THREADS) {
         const int r = p.tile_rows + (i >> 3) % (BM - p.tile_rows), a = (i >> 3) / (BM - p.tile_rows);
         *reinterpret_cast<uint4 *>(Qs + a * ATOM + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
     }
@@ -140,7 +147,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     volatile int *abort_v = &sh.abort_flag;
     pdl_enter();
     KvWalk walk;
-    kv_find<THREADS>(p.work, blockIdx.x, sh.found, walk);
+    kv_find<C::THREADS>(p.work, blockIdx.x, sh.found, walk);
     __syncthreads();                     // `found` makes room for the scales
     auto wait_all = [&](uint64_t *bar, uint32_t parity) -> bool {
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_v, p.err));
@@ -156,9 +163,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     };
 
     if (warp < 4) {
-        // registers, of the launch's 512 * 128: 128 * (64 + 32) + 256 * 208, and for the
-        // conversion of int8 codes 128 * (64 + 48) + 256 * 200
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS[0]) : "memory");
         bool ok = true;
         if (warp == 3) {
             // ---------------- pieces, and their queries ----------------
@@ -447,9 +452,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             __syncwarp();
         }
-    } else if (warp < SOFT0) {
-        if constexpr (INT8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 32;" ::: "memory");
+    } else if (warp < C::SOFT0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS[1]) : "memory");
         bool ok = true;
         int f = 0;                                            // block
         if constexpr (!INT8) {
@@ -496,7 +500,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
         } else {
         // ---------------- codes to bf16, a key per thread ----------------
-        const int r = (int)threadIdx.x - 128;                 // key of the block
+        const int r = threadIdx.x & 127;                      // key of the block
         for (int n = 0; ok; ++n) {
             const KvPiece &pc = piece(n, ok);
             if (ok && pc.blocks < 0 && f > 0 && lane == 0)    // the last V has no K after it
@@ -531,7 +535,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         }
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+                            const uint32_t w[4] = {kv_flip(in[c].x), kv_flip(in[c].y), kv_flip(in[c].z), kv_flip(in[c].w)};
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const uint4 v = make_uint4(kv_codes2(w[2 * h], 0x4140), kv_codes2(w[2 * h], 0x4342),
@@ -548,7 +552,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         ok = wait_all(&sh.sc_empty[f & 1], ((f >> 1) & 1) ^ 1);
                         if (!ok) break;
                         sh.scales[f & 1][0][r % (INT8 ? BN : 1)] = ks * p.scale_log2;
-                        sh.scales[f & 1][1][r % (INT8 ? BN : 1)] = vs;
+                        sh.scales[f & 1][1][r % (INT8 ? BN : 1)] = vs * kCodeUnit;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&sh.sc_full[f & 1]);
                     }
@@ -557,10 +561,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         }
         }
     } else {
-        if constexpr (INT8) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;" ::: "memory");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS[2]) : "memory");
         // ---------------- softmax and output of tile t, a row per thread ----------------
-        const int t = (warp - SOFT0) >> 2, quad = warp & 3;
+        const int t = (warp - C::SOFT0) >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t s_at = tmem + lane_base + (uint32_t)(t * BN);
         const uint32_t o_at = tmem + lane_base + O_COL + (uint32_t)(t * D);
@@ -587,82 +590,97 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 if (!ok) break;
                 tc_fence_after();
                 const int key0 = (kb0 + j) * BN;
-                float sv[BN];
-                const float sl2 = INT8 ? 1.f : p.scale_log2;
-                const float *vsc = sh.scales[f & (INT8 ? 1 : 0)][1];
                 if constexpr (INT8) {
                     ok = wait_all(&sh.sc_full[f & 1], (f >> 1) & 1);
                     if (!ok) break;
                 }
-                // the row's scores; -inf where it does not see the key
-                auto load_s = [&]() {
+                const float4 *ksc = reinterpret_cast<const float4 *>(sh.scales[INT8 ? f & 1 : 0][0]);
+                const float4 *vsc = reinterpret_cast<const float4 *>(sh.scales[INT8 ? f & 1 : 0][1]);
+                const bool edge_block = key0 + BN > warp_low;
+                // the row's scores of 32 keys at a time, the next ones on their way
+                float sv[2][32];
+                auto each32 = [&](auto f32) {
+                    tmem_ld32(s_at, reinterpret_cast<uint32_t *>(sv[0]));
 #pragma unroll
-                    for (int c = 0; c < BN / 32; ++c)
-                        tmem_ld32(s_at + 32 * c, reinterpret_cast<uint32_t *>(sv + 32 * c));
-                    tmem_ld_wait();
-                    if constexpr (INT8) {
-                        const float4 *ksc = reinterpret_cast<const float4 *>(sh.scales[f & 1][0]);
-#pragma unroll
-                        for (int i = 0; i < BN / 4; ++i) {
-                            const float4 k4 = ksc[i];
-                            f2_unpack(f2_mul(f2_pack(sv[4 * i], sv[4 * i + 1]), f2_pack(k4.x, k4.y)),
-                                      sv[4 * i], sv[4 * i + 1]);
-                            f2_unpack(f2_mul(f2_pack(sv[4 * i + 2], sv[4 * i + 3]), f2_pack(k4.z, k4.w)),
-                                      sv[4 * i + 2], sv[4 * i + 3]);
-                        }
-                    }
-                    if (key0 + BN > warp_low) {
-                        const int seen = lim - key0;
-#pragma unroll
-                        for (int i = 0; i < BN; ++i)
-                            if (i >= seen) sv[i] = -INFINITY;
+                    for (int c = 0; c < BN / 32; ++c) {
+                        tmem_ld_wait();
+                        if (c + 1 < BN / 32)
+                            tmem_ld32(s_at + 32 * (c + 1), reinterpret_cast<uint32_t *>(sv[(c + 1) & 1]));
+                        f32(c, sv[c & 1]);
                     }
                 };
-                load_s();
-                auto block_max = [&]() -> float {
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                // -inf where the row does not see the key.  int8: after the keys' scales, which
+                // may be 0 (elsewhere they are part of the exponent's product)
+                auto mask32 = [&](int c, float *v) {
+                    if constexpr (INT8) {
 #pragma unroll
-                    for (int i = 0; i < BN; i += 8) {
-                        m4[0] = fmax3(m4[0], sv[i], sv[i + 1]);
-                        m4[1] = fmax3(m4[1], sv[i + 2], sv[i + 3]);
-                        m4[2] = fmax3(m4[2], sv[i + 4], sv[i + 5]);
-                        m4[3] = fmax3(m4[3], sv[i + 6], sv[i + 7]);
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 k4 = ksc[8 * c + i];
+                            f2_unpack(f2_mul(f2_pack(v[4 * i], v[4 * i + 1]), f2_pack(k4.x, k4.y)), v[4 * i], v[4 * i + 1]);
+                            f2_unpack(f2_mul(f2_pack(v[4 * i + 2], v[4 * i + 3]), f2_pack(k4.z, k4.w)), v[4 * i + 2], v[4 * i + 3]);
+                        }
                     }
-                    return fmaxf(fmax3(m4[0], m4[1], m4[2]), m4[3]);
+                    if (edge_block) {
+                        const int seen = lim - key0 - 32 * c;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i >= seen) v[i] = -INFINITY;
+                    }
+                };
+                // the row's largest score of the block, in the exponent of two
+                auto row_max = [&]() -> float {
+                    float m2[2] = {-INFINITY, -INFINITY};
+                    each32([&](int c, float *v) {
+                        mask32(c, v);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            m2[0] = fmax3(m2[0], v[i], v[i + 1]);
+                            m2[1] = fmax3(m2[1], v[i + 2], v[i + 3]);
+                        }
+                    });
+                    return fmaxf(m2[0], m2[1]) * (INT8 ? 1.f : p.scale_log2);
                 };
                 // P = 2^(s - m) on fp32 pairs, times the values' scales, in bf16 pairs;
                 // returns the row's sum of 2^(s - m)
                 uint32_t pk[BN / 2];
-                auto exp_pass = [&]() -> float {
-                    const uint64_t scale2 = f2_pack(sl2, sl2), negm2 = f2_pack(-m, -m);
+                auto exp_pass = [&](auto EDGE) -> float {
+                    const uint64_t negm2 = f2_pack(-m, -m);
                     uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+                    each32([&](int c, float *v) {
+                        if constexpr (EDGE) mask32(c, v);
 #pragma unroll
-                    for (int i = 0; i < BN / 2; ++i) {
-                        float x0, x1;
-                        if constexpr (INT8) f2_unpack(f2_add(f2_pack(sv[2 * i], sv[2 * i + 1]), negm2), x0, x1);
-                        else f2_unpack(f2_fma(f2_pack(sv[2 * i], sv[2 * i + 1]), scale2, negm2), x0, x1);
-                        float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-                        acc2[i & 3] = f2_add(acc2[i & 3], f2_pack(p0, p1));
-                        if constexpr (INT8) {
-                            const float2 v2 = reinterpret_cast<const float2 *>(vsc)[i];
-                            f2_unpack(f2_mul(f2_pack(p0, p1), f2_pack(v2.x, v2.y)), p0, p1);
+                        for (int i = 0; i < 8; ++i) {
+                            float4 k4 = make_float4(p.scale_log2, p.scale_log2, p.scale_log2, p.scale_log2);
+                            [[maybe_unused]] float4 v4;
+                            if constexpr (INT8 && !EDGE) k4 = ksc[8 * c + i];
+                            if constexpr (INT8) v4 = vsc[8 * c + i];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint64_t s2 = f2_pack(v[4 * i + 2 * h], v[4 * i + 2 * h + 1]);
+                                float x0, x1;
+                                if constexpr (INT8 && EDGE) f2_unpack(f2_add(s2, negm2), x0, x1);
+                                else f2_unpack(f2_fma(s2, h ? f2_pack(k4.z, k4.w) : f2_pack(k4.x, k4.y), negm2), x0, x1);
+                                float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                                acc2[2 * (i & 1) + h] = f2_add(acc2[2 * (i & 1) + h], f2_pack(p0, p1));
+                                if constexpr (INT8)
+                                    f2_unpack(f2_mul(f2_pack(p0, p1), h ? f2_pack(v4.z, v4.w) : f2_pack(v4.x, v4.y)), p0, p1);
+                                pk[16 * c + 2 * i + h] = pack_bf16(p0, p1);
+                            }
                         }
-                        pk[i] = pack_bf16(p0, p1);
-                    }
+                    });
                     float a0, a1;
                     f2_unpack(f2_add(f2_add(acc2[0], acc2[1]), f2_add(acc2[2], acc2[3])), a0, a1);
                     return a0 + a1;
                 };
                 // a first block that shows the row no key leaves the maximum at the lowest
                 // number: P is 0 there, and the first finite score overflows and brings its own
-                if (j == 0) m = fmaxf(block_max() * sl2, -FLT_MAX);
-                float bsum = exp_pass();
+                if (j == 0) m = fmaxf(row_max(), -FLT_MAX);
+                float bsum = edge_block ? exp_pass(std::true_type()) : exp_pass(std::false_type());
                 const bool redo = !(bsum <= 1.8446744e19f);     // > 2^64, inf or NaN
                 if (__any_sync(0xffffffffu, redo)) {
-                    load_s();                                   // its registers hold P
+                    const float m_new = fmaxf(m, row_max());
                     float alpha = 1.f;
                     if (redo) {
-                        const float m_new = fmaxf(m, block_max() * sl2);
                         alpha = ex2_approx(m - m_new);
                         l *= alpha;
                         m = m_new;
@@ -679,7 +697,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         }
                         tmem_st_wait();
                     }
-                    bsum = exp_pass();
+                    bsum = edge_block ? exp_pass(std::true_type()) : exp_pass(std::false_type());
                 }
                 l += bsum;
                 tmem_st32(s_at, pk);
@@ -787,11 +805,11 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.ws = static_cast<float *>(a.ws);
     p.ldo = a.ldo;
-    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(THREADS), SMEM, st, tq, tk, p);
+        echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
     }
     echo::launch_kv_join(a, p.work, st);
     return echo::last_launch_status();

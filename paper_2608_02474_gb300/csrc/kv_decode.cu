@@ -250,8 +250,10 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                             uint32_t r[4];
                             ldsm4(kbase + chunk_at<INT8, D>(warp * KPW + nt * 8 + mr, c + mi), r);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                mma16816(sc[nt], qa[c + i], kv_codes2(r[i], 0x4140), kv_codes2(r[i], 0x4342));
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t w = kv_flip(r[i]);
+                                mma16816(sc[nt], qa[c + i], kv_codes2(w, 0x4140), kv_codes2(w, 0x4342));
+                            }
                         }
                 } else {
 #pragma unroll
@@ -274,10 +276,10 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         const int at2 = warp * KPW + nt * 8 + 2 * tq;
                         const float2 ks = *reinterpret_cast<const float2 *>(scales + at2);
                         const float2 v2 = *reinterpret_cast<const float2 *>(scales + BK + at2);
-                        f.x *= ks.x;
+                        f.x *= ks.x;                 // the codes' unit is in scale_log2
                         f.y *= ks.y;
-                        vs[nt][0] = v2.x;
-                        vs[nt][1] = v2.y;
+                        vs[nt][0] = v2.x * kCodeUnit;
+                        vs[nt][1] = v2.y * kCodeUnit;
                     }
                     sc[nt][0] *= f.x;
                     sc[nt][1] *= f.y;
@@ -373,8 +375,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         if constexpr (INT8) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                mma16816(o[2 * (c + i)], pa, kv_codes2(r[2 * i], 0x4240), kv_codes2(r[2 * i + 1], 0x4240));
-                                mma16816(o[2 * (c + i) + 1], pa, kv_codes2(r[2 * i], 0x4341), kv_codes2(r[2 * i + 1], 0x4341));
+                                const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
+                                mma16816(o[2 * (c + i)], pa, kv_codes2(w0, 0x4240), kv_codes2(w1, 0x4240));
+                                mma16816(o[2 * (c + i) + 1], pa, kv_codes2(w0, 0x4341), kv_codes2(w1, 0x4341));
                             }
                         } else {
                             if (edge) {
@@ -502,7 +505,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.ws = static_cast<float *>(a.ws);
     p.ldq = a.ldq;
     p.ldo = a.ldo;
-    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);

@@ -46,17 +46,20 @@ ECHO_DEV int64_t kv_place(const KvPool &pool, const KvBatch &b, int seq, int64_t
     return ((int64_t)page << pool.shift) + (p & ((1 << pool.shift) - 1));
 }
 
-// two codes of w, picked into 16-bit halves by the selector, as a bf16 pair, exactly:
-// with b the byte, 0x4300 | (b & 0x7F) is 128 + (b & 0x7F) and 0x4300 | (b & 0x80) is 128 or
-// 256, and their difference is the signed value
-ECHO_DEV uint32_t kv_codes2(uint32_t w, uint32_t sel) {
-    const uint32_t r = __byte_perm(w, 0x43434343u, sel);
-    const uint32_t lo = r & 0xFF7FFF7Fu, hi = r & 0xFF80FF80u;
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&lo),
-                                     *reinterpret_cast<const __nv_bfloat162 *>(&hi));
-    return *reinterpret_cast<const uint32_t *>(&v);
+// Four int8 codes as bf16 pairs of code / 64, exactly.  With the sign bit flipped a byte is
+// u = code + 128; a 16-bit half with u in its low byte and 0 above is the bf16 number
+// u 2^-133 (below 128 a subnormal one, and bf16 fma takes those), and
+// u 2^-133 2^127 - 2 = (u - 128) / 64 needs no more than 7 bits.  The selectors pick the two
+// bytes of a pair (4: a zero byte).
+constexpr float kCodeUnit = 64.f;   // what the scales are multiplied by in return
+ECHO_DEV uint32_t kv_flip(uint32_t w) { return w ^ 0x80808080u; }
+ECHO_DEV uint32_t kv_codes2(uint32_t flipped, uint32_t sel) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;"
+        : "=r"(r)
+        : "r"(__byte_perm(flipped, 0u, sel)), "r"(0x7F007F00u), "r"(0xC000C000u));   // 2^127, -2
+    return r;
 }
-
 namespace echo {
 // argument checks of the entry points; ECHO_OK with *empty set: there is nothing to do
 echo_status kv_check(const echo_kv_pool *pool, const echo_kv_batch *batch, bool *empty);
