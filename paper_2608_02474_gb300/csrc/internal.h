@@ -143,8 +143,10 @@ struct KvAttention {
     int64_t ldo;
     void *ws;
 };
+constexpr int kDecodeRows = 32;   // the most packed rows of a tile of launch_kv_decode
 size_t kv_decode_workspace(const echo_kv_pool &pool);
-echo_status launch_kv_decode(const KvAttention &a, cudaStream_t st);
+// `rows`: packed rows of a sequence, about
+echo_status launch_kv_decode(const KvAttention &a, int rows, cudaStream_t st);
 size_t kv_chunk_workspace(const echo_kv_pool &pool);
 echo_status launch_kv_chunk(const KvAttention &a, cudaStream_t st);
 

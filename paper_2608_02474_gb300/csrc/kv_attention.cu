@@ -28,7 +28,6 @@ extern "C" echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv
     if (!device_supported()) return ECHO_ERR_UNSUPPORTED;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const KvAttention a{pool, batch, q, ldq, Hq, causal_block, out, ldo, workspace};
-    // few packed rows a sequence: 16 at a time on the SMs' own tensor instructions
-    const bool few = (int64_t)batch->max_rows * (Hq / pool->H) <= 16;
-    return few ? launch_kv_decode(a, st) : launch_kv_chunk(a, st);
+    const int64_t rows = (int64_t)batch->max_rows * (Hq / pool->H);   // packed, of a sequence
+    return rows <= kDecodeRows ? launch_kv_decode(a, (int)rows, st) : launch_kv_chunk(a, st);
 }

@@ -1,40 +1,51 @@
 // Attention over the paged cache where a sequence has few packed rows (single tokens,
-// drafts): 16 at a time, so that the bytes of the pages bound it.
+// drafts): 8, 16 or 32 at a time, so that the bytes of the pages bound it.
 //
 // One CTA works through its share of the items (kv_schedule.cuh): a producer warp copies
 // key blocks (K and V of one head, and the scales of int8 pages) page by page into a ring
 // in shared memory, ahead by whole stages; four warps take a quarter of a block's keys
-// each, on m16n8k16 tensor-core products: S = Q K^T, the running maximum and sum of its
-// own keys, O += P V.  Nothing passes between the warps until the end of a piece, where
-// the four (maximum, sum, O) are joined in a fixed order.
+// each, and where the registers allow it two such groups take the blocks in turn.  The
+// products run on m16n8k16 tensor instructions with the keys and then the values' columns
+// as the 16 rows of A, so that 8 packed rows fill the 8 columns of B:
+//   S^T = K Q^T,  P^T = 2^(S^T - m) (rounded to bf16, turned round by movmatrix),
+//   O^T += V^T P^T.
+// (With the packed rows as A, padded to 16, 48 sequences of up to 8190 int8 keys, 32/8
+// heads of 128, took 117 us against XXX, one token over 131071 bf16 keys 92 against XXX.)
+// A row's maximum comes from the warp's first block of a piece, and moves only when a
+// weight passes 2^64; nothing passes between the warps until the end of a piece, where
+// their (maximum, sum, O) are joined in a fixed order.
 //
-// int8 codes become bf16 exactly in registers (kv_codes2).  The keys' scales multiply the scores, the values' scales the weights.
-// ldmatrix hands out 16-bit units, so a lane gets neighbouring pairs of codes: Q's columns
-// are taken in the same order, and O's columns come out in it.
+// int8 codes become bf16 exactly in registers (kv_codes2).  The keys' scales multiply the
+// scores, the values' scales the weights.  ldmatrix hands out 16-bit units, so a lane gets
+// neighbouring pairs of codes: Q's columns are taken in the same order, and O's columns
+// come out in it.
 #include <cfloat>
 
 #include "kv_schedule.cuh"
 
 namespace {
 
-constexpr int WARPS = 4;                       // that compute
-constexpr int THREADS = 32 * (WARPS + 1);
-constexpr int ROWS = 16;
 constexpr int PIECES = 4;                      // handed out ahead
 
-template <bool INT8, int D>
+template <bool INT8, int D, int NR>
 struct Cfg {
+    static constexpr int ROWS = 8 * NR;
+    static constexpr int GROUPS = NR * D <= (INT8 ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
+    static constexpr int CTAS = NR * D <= 256 ? 2 : 1;     // on an SM
+    static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
     static constexpr int KPW = INT8 ? 32 : 16;             // keys of a warp
-    static constexpr int BK = WARPS * KPW;                 // keys of a block
+    static constexpr int BK = 4 * KPW;                     // keys of a block
     static constexpr int BSHIFT = INT8 ? 7 : 6;
     static constexpr int ROW_BYTES = INT8 ? D : 2 * D;
     static constexpr int HALF = BK * ROW_BYTES;            // K or V of a block
     static constexpr int SCALES = INT8 ? 2 * BK * 4 : 0;
     static constexpr int STAGE = 2 * HALF + SCALES;        // a multiple of 1024
-    static constexpr int JOIN = ROWS * D * 4;              // two warps' half of O
-    static constexpr int RING = (110 * 1024 - JOIN) / STAGE;   // two CTAs share an SM
-    static constexpr int SMEM = RING * STAGE + JOIN + 1024;
-    static_assert(STAGE % 1024 == 0 && RING >= 3, "");
+    static constexpr int JOIN = WARPS / 4 * ROWS * D * 4;  // half of the warps' half of O
+    static constexpr bool Q_SMEM = NR * D > 256;           // the queries' registers do not suffice
+    static constexpr int Q_BYTES = Q_SMEM ? ROWS * D * 2 : 0;
+    static constexpr int RING = ((CTAS == 2 ? 110 : 220) * 1024 - JOIN - Q_BYTES) / STAGE;
+    static constexpr int SMEM = RING * STAGE + JOIN + Q_BYTES + 1024;
+    static_assert(STAGE % 1024 == 0 && RING >= 2, "");
 };
 
 struct DecodeParams {
@@ -60,35 +71,38 @@ ECHO_DEV void ldsm4_t(uint32_t addr, uint32_t *r) {
                  : "r"(addr)
                  : "memory");
 }
+ECHO_DEV uint32_t turn8x8(uint32_t a) {        // an 8x8 matrix of bf16, transposed
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
 ECHO_DEV void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
         "{%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+
 // byte offset of 16-byte chunk c of row r of a block's K or V, as the tensor maps lay it out
-template <bool INT8, int D>
+template <bool INT8, int D, int BK>
 ECHO_DEV uint32_t chunk_at(int r, int c) {
     if constexpr (INT8 && D == 64) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
-    else {
-        constexpr int BK = Cfg<INT8, D>::BK;
-        return (uint32_t)((c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-    }
+    else return (uint32_t)((c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-template <bool INT8, int D>
-__global__ void __launch_bounds__(THREADS, 2)
+template <bool INT8, int D, int NR>
+__global__ void __launch_bounds__((Cfg<INT8, D, NR>::THREADS), (Cfg<INT8, D, NR>::CTAS))
 kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
-    using C = Cfg<INT8, D>;
-    constexpr int KPW = C::KPW, BK = C::BK, NT = KPW / 8, OT = D / 8;
+    using C = Cfg<INT8, D, NR>;
+    constexpr int KPW = C::KPW, BK = C::BK, KG = KPW / 16, MT = D / 16, ROWS = C::ROWS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                 ~static_cast<uintptr_t>(1023));
     float *join = reinterpret_cast<float *>(smem + C::RING * C::STAGE);
+    uint2 *q_smem = reinterpret_cast<uint2 *>(smem + C::RING * C::STAGE + C::JOIN);
     __shared__ __align__(8) uint64_t full[C::RING], empty[C::RING], piece_full[PIECES], piece_empty[PIECES];
     __shared__ KvPiece piece[PIECES];
-    __shared__ float2 row_ml[WARPS][ROWS];
+    __shared__ float2 row_ml[C::WARPS][ROWS];
     __shared__ KvFound found;
     __shared__ int abort_flag;
 
@@ -96,11 +110,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::RING; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], WARPS);
+            mbar_init(&empty[i], C::WARPS);
         }
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&piece_full[i], 1);
-            mbar_init(&piece_empty[i], WARPS);
+            mbar_init(&piece_empty[i], C::WARPS);
         }
         abort_flag = 0;
         fence_barrier_init();
@@ -109,9 +123,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     volatile int *abort_v = &abort_flag;
     pdl_enter();
     KvWalk walk;
-    kv_find<THREADS>(p.work, blockIdx.x, found, walk);   // and its barriers
+    kv_find<C::THREADS>(p.work, blockIdx.x, found, walk);   // and its barriers
 
-    if (warp == WARPS) {
+    if (warp == C::WARPS) {
         // ---------------- producer: the pieces' blocks, a page or part of one at a time ----
         const int shift = p.pool.shift, cs = min(shift, C::BSHIFT);   // tokens of a copy: 1 << cs
         const int per_block = BK >> cs;
@@ -185,16 +199,16 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         return;
     }
 
-    // ---------------- four warps, a quarter of each block's keys each ----------------
-    const int gq = lane >> 2, tq = lane & 3;        // row group and column pair of a fragment
+    // ---------------- groups of four warps, a quarter of each block's keys each ----------------
+    // a fragment's row group and column pair; lane's row and chunk in four 8x8 matrices
+    const int gq = lane >> 2, tq = lane & 3, mi = lane >> 3, mr = lane & 7;
+    const int wk = (warp & 3) * KPW;                 // this warp's first key of a block
     const uint32_t ring = smem_u32(smem);
-    // lane's row and chunk in a ldmatrix of four 8x8 matrices
-    const int mi = lane >> 3, mr = lane & 7;
     int g = 0;
     bool ok = true;
     for (int n = 0; ok; ++n) {
         ok = __all_sync(0xffffffffu, mbar_wait(&piece_full[n % PIECES], (n / PIECES) & 1, abort_v, p.err));
-        ok = !named_bar_or(1, 32 * WARPS, !ok);      // the four warps stay together
+        ok = !named_bar_or(1, 32 * C::WARPS, !ok);   // the warps stay together
         const KvPiece &pc = piece[n % PIECES];
         if (!ok || pc.blocks < 0) break;
         KvSeq s;
@@ -204,190 +218,244 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         s.shift = pc.shift;
         const int keys = pc.keys, low = pc.low, group = p.work.group, tile = pc.tile, head = pc.head;
         const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks;
-        // rows gq and gq + 8 of the tile: their queries, and the keys that they see
-        uint32_t qa[D / 16][4];
-        int lim[2];
-        int64_t at[2];                               // row and first column of the row's head
-        bool real[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int pr = tile * ROWS + gq + 8 * i;
-            real[i] = pr < s.packed;
-            const int r = s.row + pr / group, h = head * group + pr % group;
-            lim[i] = real[i] ? s.top(p.work, r) : keys;
-            at[i] = real[i] ? (int64_t)r * p.ldq + h * D : 0;
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                uint2 v = make_uint2(0u, 0u);
-                if (real[i]) {
-                    const __nv_bfloat16 *src = p.q + at[i] + 16 * kk;
-                    if constexpr (INT8) {
-                        v = *reinterpret_cast<const uint2 *>(src + 4 * tq);
-                    } else {
-                        v.x = *reinterpret_cast<const uint32_t *>(src + 2 * tq);
-                        v.y = *reinterpret_cast<const uint32_t *>(src + 2 * tq + 8);
-                    }
+        // B of the first product: 8 packed rows a fragment, row gq of them in this lane
+        uint32_t qb[C::Q_SMEM ? 1 : NR][C::Q_SMEM ? 1 : MT][2];
+        auto query = [&](int pr, int kk) -> uint2 {
+            uint2 v = make_uint2(0u, 0u);
+            if (pr < s.packed) {
+                const __nv_bfloat16 *src = p.q + (int64_t)(s.row + pr / group) * p.ldq + (head * group + pr % group) * D + 16 * kk;
+                if constexpr (INT8) {
+                    v = *reinterpret_cast<const uint2 *>(src + 4 * tq);
+                } else {
+                    v.x = *reinterpret_cast<const uint32_t *>(src + 2 * tq);
+                    v.y = *reinterpret_cast<const uint32_t *>(src + 2 * tq + 8);
                 }
-                qa[kk][i] = v.x;
-                qa[kk][i + 2] = v.y;
             }
+            return v;
+        };
+        if constexpr (C::Q_SMEM) {                   // the fragments as they are, lane by lane
+            for (int i = warp; i < NR * MT; i += C::WARPS) q_smem[i * 32 + lane] = query(tile * ROWS + (i / MT) * 8 + gq, i % MT);
+            named_bar_sync(1, 32 * C::WARPS);
+        } else {
+#pragma unroll
+            for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+                for (int kk = 0; kk < MT; ++kk) {
+                    const uint2 v = query(tile * ROWS + nt * 8 + gq, kk);
+                    qb[nt][kk][0] = v.x;
+                    qb[nt][kk][1] = v.y;
+                }
         }
-        float o[OT][4] = {}, m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};
+        // rows 8 nt + 2 tq + e of the tile, in S^T's and O^T's columns: the keys that they see
+        int lim[NR][2];
+#pragma unroll
+        for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int pr = tile * ROWS + nt * 8 + 2 * tq + e;
+                lim[nt][e] = pr < s.packed ? s.top(p.work, s.row + pr / group) : keys;
+            }
+        float o[NR][MT][4] = {}, m[NR][2], l[NR][2];
+#pragma unroll
+        for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) m[nt][e] = -FLT_MAX, l[nt][e] = 0.f;
+        bool fresh = true;                           // no maximum yet
         for (int kb = kb0; kb < kb1; ++kb, ++g) {
+            // every warp sees every stage fill, its own or not, before the stage is filled again:
+            // a barrier's phases are told apart by their parity only
             const int stage = g % C::RING;
             ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (g / C::RING) & 1, abort_v, p.err));
             if (!ok) break;
-            const int key0 = kb * BK + warp * KPW;       // this warp's first key
+            const int key0 = kb * BK + wk;               // this warp's first key
             const uint32_t kbase = ring + stage * C::STAGE, vbase = kbase + C::HALF;
-            if (key0 < keys) {
-                // S = Q K^T
-                float sc[NT][4] = {};
-                if constexpr (INT8) {
+            if (key0 < keys && (C::GROUPS == 1 || (g & 1) == warp >> 2)) {
+                // S^T = K Q^T, 16 keys at a time
+                float sc[KG][NR][4] = {};
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
-                        for (int c = 0; c < D / 16; c += 4) {
-                            uint32_t r[4];
-                            ldsm4(kbase + chunk_at<INT8, D>(warp * KPW + nt * 8 + mr, c + mi), r);
+                    for (int kk = 0; kk < MT; kk += INT8 ? 2 : 1) {
+                        uint32_t r[4];
+                        const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
+                        ldsm4(kbase + chunk_at<INT8, D, BK>(row, INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t w = kv_flip(r[i]);
-                                mma16816(sc[nt], qa[c + i], kv_codes2(w, 0x4140), kv_codes2(w, 0x4342));
+                        for (int i = 0; i < (INT8 ? 2 : 1); ++i) {
+                            uint32_t a[4] = {r[0], r[1], r[2], r[3]};
+                            if constexpr (INT8) {
+                                const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
+                                a[0] = kv_codes2(w0, 0x4140);
+                                a[1] = kv_codes2(w1, 0x4140);
+                                a[2] = kv_codes2(w0, 0x4342);
+                                a[3] = kv_codes2(w1, 0x4342);
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < NR; ++nt) {
+                                if constexpr (C::Q_SMEM) {
+                                    const uint2 b = q_smem[(nt * MT + kk + i) * 32 + lane];
+                                    mma16816(sc[kg][nt], a, b.x, b.y);
+                                } else {
+                                    mma16816(sc[kg][nt], a, qb[nt][kk + i][0], qb[nt][kk + i][1]);
+                                }
                             }
                         }
-                } else {
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-                        for (int nt = 0; nt < NT; nt += 2) {
-                            uint32_t r[4];
-                            ldsm4(kbase + chunk_at<INT8, D>(warp * KPW + nt * 8 + (mi >> 1) * 8 + mr,
-                                                            2 * kk + (mi & 1)), r);
-                            mma16816(sc[nt], qa[kk], r[0], r[1]);
-                            mma16816(sc[nt + 1], qa[kk], r[2], r[3]);
-                        }
-                }
-                float vs[NT][2];
-                const float *scales = reinterpret_cast<const float *>(smem + stage * C::STAGE + 2 * C::HALF);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float2 f = make_float2(p.scale_log2, p.scale_log2);
-                    if constexpr (INT8) {
-                        const int at2 = warp * KPW + nt * 8 + 2 * tq;
-                        const float2 ks = *reinterpret_cast<const float2 *>(scales + at2);
-                        const float2 v2 = *reinterpret_cast<const float2 *>(scales + BK + at2);
-                        f.x *= ks.x;                 // the codes' unit is in scale_log2
-                        f.y *= ks.y;
-                        vs[nt][0] = v2.x * kCodeUnit;
-                        vs[nt][1] = v2.y * kCodeUnit;
                     }
-                    sc[nt][0] *= f.x;
-                    sc[nt][1] *= f.y;
-                    sc[nt][2] *= f.x;
-                    sc[nt][3] *= f.y;
-                }
+                // in the exponent of two: keys gq and gq + 8 of each 16, rows 2 tq and 2 tq + 1
+                const float *scales = reinterpret_cast<const float *>(smem + stage * C::STAGE + 2 * C::HALF) + wk + gq;
                 const bool edge = key0 + KPW > low;      // some row does not see all of these keys
-                if (edge) {
+                float vs[KG][2];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int j = key0 + nt * 8 + 2 * tq + e;
-                            if (INT8 && !(fabsf(vs[nt][e]) < INFINITY)) {   // spoils the rows that see it
-                                sc[nt][e] = sc[nt][2 + e] = NAN;
-                                vs[nt][e] = 0.f;
-                            }
-                            if (j >= lim[0]) sc[nt][e] = -INFINITY;
-                            if (j >= lim[1]) sc[nt][2 + e] = -INFINITY;
+                    for (int h = 0; h < 2; ++h) {
+                        float f = p.scale_log2;
+                        if constexpr (INT8) {
+                            f *= scales[kg * 16 + 8 * h];   // the codes' unit is in scale_log2
+                            vs[kg][h] = scales[BK + kg * 16 + 8 * h] * kCodeUnit;
                         }
-                }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float mx = -INFINITY;
+                        for (int nt = 0; nt < NR; ++nt) {
+                            sc[kg][nt][2 * h] *= f;
+                            sc[kg][nt][2 * h + 1] *= f;
+                        }
+                        if (edge) {
+                            const int j = key0 + kg * 16 + 8 * h + gq;
+                            const bool bad = INT8 && !(fabsf(vs[kg][h]) < INFINITY);   // spoils the rows that see it
+                            if (bad) vs[kg][h] = 0.f;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mx = fmax3(mx, sc[nt][2 * i], sc[nt][2 * i + 1]);
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    const float m2 = fmaxf(m[i], mx);
-                    if (__any_sync(0xffffffffu, m2 > m[i])) {
-                        const float a = ex2_approx(m[i] - m2);
-                        m[i] = m2;
-                        l[i] *= a;
+                            for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
-                        for (int t = 0; t < OT; ++t) {
-                            o[t][2 * i] *= a;
-                            o[t][2 * i + 1] *= a;
+                                for (int e = 0; e < 2; ++e) {
+                                    float &x = sc[kg][nt][2 * h + e];
+                                    if (bad) x = NAN;
+                                    if (j >= lim[nt][e]) x = -INFINITY;
+                                }
                         }
                     }
+                // the rows' maxima over this warp's keys
+                auto raise = [&]() {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float w = ex2_approx(sc[nt][2 * i + e] - m[i]);
-                            l[i] += w;
-                            sc[nt][2 * i + e] = INT8 ? w * vs[nt][e] : w;
+                            float mx = -INFINITY;
+#pragma unroll
+                            for (int kg = 0; kg < KG; ++kg) mx = fmax3(mx, sc[kg][nt][e], sc[kg][nt][2 + e]);
+#pragma unroll
+                            for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+                            const float m2 = fmaxf(m[nt][e], mx), a = ex2_approx(m[nt][e] - m2);
+                            m[nt][e] = m2;
+                            l[nt][e] *= a;
+#pragma unroll
+                            for (int t = 0; t < MT; ++t) {
+                                o[nt][t][e] *= a;
+                                o[nt][t][2 + e] *= a;
+                            }
                         }
+                };
+                // P^T in fragments of B; the largest weight, NaN included
+                uint32_t pb[KG][NR][2];
+                float add[NR][2];
+                auto weights = [&]() -> bool {
+                    bool high = false;
+#pragma unroll
+                    for (int nt = 0; nt < NR; ++nt) {
+                        add[nt][0] = add[nt][1] = 0.f;
+#pragma unroll
+                        for (int kg = 0; kg < KG; ++kg)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float w0 = ex2_approx(sc[kg][nt][2 * h] - m[nt][0]);
+                                float w1 = ex2_approx(sc[kg][nt][2 * h + 1] - m[nt][1]);
+                                add[nt][0] += w0;
+                                add[nt][1] += w1;
+                                if constexpr (INT8) w0 *= vs[kg][h], w1 *= vs[kg][h];
+                                pb[kg][nt][h] = pack_bf16(w0, w1);
+                            }
+                        high |= !(add[nt][0] <= 1.8446744e19f) || !(add[nt][1] <= 1.8446744e19f);
+                    }
+                    return __any_sync(0xffffffffu, high);
+                };
+                if (fresh) raise();
+                fresh = false;
+                if (weights()) {
+                    raise();
+                    weights();
                 }
-                // O += P V, 16 keys at a time
+#pragma unroll
+                for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) l[nt][e] += add[nt][e];
+                // O^T += V^T P^T
                 const bool tail = key0 + KPW > keys;     // V rows past the last key: not copied
 #pragma unroll
-                for (int k2 = 0; k2 < NT / 2; ++k2) {
-                    const uint32_t pa[4] = {pack_bf16(sc[2 * k2][0], sc[2 * k2][1]),
-                                            pack_bf16(sc[2 * k2][2], sc[2 * k2][3]),
-                                            pack_bf16(sc[2 * k2 + 1][0], sc[2 * k2 + 1][1]),
-                                            pack_bf16(sc[2 * k2 + 1][2], sc[2 * k2 + 1][3])};
-                    const int row = warp * KPW + k2 * 16 + (mi & 1) * 8 + mr;
+                for (int kg = 0; kg < KG; ++kg) {
+                    uint32_t b[NR][2];
+#pragma unroll
+                    for (int nt = 0; nt < NR; ++nt) {
+                        b[nt][0] = turn8x8(pb[kg][nt][0]);
+                        b[nt][1] = turn8x8(pb[kg][nt][1]);
+                    }
+                    // a matrix of 8 keys and 16 bytes: bf16 keys, then columns; int8 the other way
+                    const int row = wk + kg * 16 + (INT8 ? (mi & 1) : (mi >> 1)) * 8 + mr;
+                    const int col = INT8 ? mi >> 1 : mi & 1;
                     uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
                     if (!INT8 && edge && low < keys) {
                         // rows that do not see all of these keys: values that are not finite
                         // become 0, and spoil the rows that do see them (0 times infinity)
                         uint32_t bad = 0;                    // of the 16 keys
 #pragma unroll
-                        for (int c = 0; c < C::ROW_BYTES / 16; c += 2) {
+                        for (int t = 0; t < MT; ++t) {
                             uint32_t r[4];
-                            ldsm4_t(vbase + chunk_at<INT8, D>(row, c + (mi >> 1)), r);
+                            ldsm4_t(vbase + chunk_at<INT8, D, BK>(row, 2 * t + col), r);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                if ((r[i] & 0x7F80u) == 0x7F80u) bad |= 1u << (8 * (i & 1) + 2 * tq);
-                                if ((r[i] & 0x7F800000u) == 0x7F800000u) bad |= 2u << (8 * (i & 1) + 2 * tq);
+                                if ((r[i] & 0x7F80u) == 0x7F80u) bad |= 1u << (8 * (i >> 1) + 2 * tq);
+                                if ((r[i] & 0x7F800000u) == 0x7F800000u) bad |= 2u << (8 * (i >> 1) + 2 * tq);
                             }
                         }
                         bad = __reduce_or_sync(0xffffffffu, bad);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int seen = lim[i] - (key0 + k2 * 16);
-                            if (bad & (seen >= 16 ? 0xffffu : seen > 0 ? (1u << seen) - 1u : 0u)) l[i] = NAN;
-                            keep[i] = ((bad >> (8 * i + 2 * tq)) & 1 ? 0u : 0xffffu) |
-                                      ((bad >> (8 * i + 2 * tq)) & 2 ? 0u : 0xffff0000u);
-                        }
+                        for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int seen = lim[nt][e] - (key0 + kg * 16);
+                                if (bad & (seen >= 16 ? 0xffffu : seen > 0 ? (1u << seen) - 1u : 0u)) l[nt][e] = NAN;
+                            }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            keep[h] = ((bad >> (8 * h + 2 * tq)) & 1 ? 0u : 0xffffu) |
+                                      ((bad >> (8 * h + 2 * tq)) & 2 ? 0u : 0xffff0000u);
                     }
                     if (!INT8 && tail) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int j = key0 + k2 * 16 + 8 * i + 2 * tq;
-                            keep[i] &= (j < keys ? 0xffffu : 0u) | (j + 1 < keys ? 0xffff0000u : 0u);
+                        for (int h = 0; h < 2; ++h) {
+                            const int j = key0 + kg * 16 + 8 * h + 2 * tq;
+                            keep[h] &= (j < keys ? 0xffffu : 0u) | (j + 1 < keys ? 0xffff0000u : 0u);
                         }
                     }
 #pragma unroll
-                    for (int c = 0; c < C::ROW_BYTES / 16; c += 2) {
+                    for (int t = 0; t < MT; t += INT8 ? 2 : 1) {
                         uint32_t r[4];
-                        ldsm4_t(vbase + chunk_at<INT8, D>(row, c + (mi >> 1)), r);
+                        ldsm4_t(vbase + chunk_at<INT8, D, BK>(row, INT8 ? t + col : 2 * t + col), r);
                         if constexpr (INT8) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
                                 const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
-                                mma16816(o[2 * (c + i)], pa, kv_codes2(w0, 0x4240), kv_codes2(w1, 0x4240));
-                                mma16816(o[2 * (c + i) + 1], pa, kv_codes2(w0, 0x4341), kv_codes2(w1, 0x4341));
+                                const uint32_t a[4] = {kv_codes2(w0, 0x4240), kv_codes2(w0, 0x4341),
+                                                       kv_codes2(w1, 0x4240), kv_codes2(w1, 0x4341)};
+#pragma unroll
+                                for (int nt = 0; nt < NR; ++nt) mma16816(o[nt][t + i], a, b[nt][0], b[nt][1]);
                             }
                         } else {
                             if (edge) {
                                 r[0] &= keep[0];
-                                r[1] &= keep[1];
-                                r[2] &= keep[0];
+                                r[1] &= keep[0];
+                                r[2] &= keep[1];
                                 r[3] &= keep[1];
                             }
-                            mma16816(o[c], pa, r[0], r[1]);
-                            mma16816(o[c + 1], pa, r[2], r[3]);
+#pragma unroll
+                            for (int nt = 0; nt < NR; ++nt) mma16816(o[nt][t], r, b[nt][0], b[nt][1]);
                         }
                     }
                 }
@@ -395,103 +463,114 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty[stage]);
         }
-        // ---- the four warps' sums, joined in warp order; warp 0 stores ----
-        // a wait that gave up is told to all four warps, which leave together
-        ok = !named_bar_or(1, 32 * WARPS, !ok);
+        // ---- the warps' sums, joined in a fixed order; warp 0 stores ----
+        // a wait that gave up is told to all warps, which leave together
+        ok = !named_bar_or(1, 32 * C::WARPS, !ok);
         if (!ok) break;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if (tq == 0) row_ml[warp][gq + 8 * i] = make_float2(m[i], l[i]);
-        }
-        named_bar_sync(1, 32 * WARPS);
-        float mt[2], lt[2];
+        for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            mt[i] = -FLT_MAX;
-            lt[i] = 0.f;
+            for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) mt[i] = fmaxf(mt[i], row_ml[w][gq + 8 * i].x);
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float2 v = row_ml[w][gq + 8 * i];
-                lt[i] += ex2_approx(v.x - mt[i]) * v.y;
+                for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
+                if (gq == 0) row_ml[warp][nt * 8 + 2 * tq + e] = make_float2(m[nt][e], l[nt][e]);
             }
-            const float f = ex2_approx(m[i] - mt[i]);
+        named_bar_sync(1, 32 * C::WARPS);
+        float mt[NR][2], lt[NR][2];
 #pragma unroll
-            for (int t = 0; t < OT; ++t) {
-                o[t][2 * i] *= f;
-                o[t][2 * i + 1] *= f;
-            }
-        }
-        // (0 + 2) + (1 + 3), half the columns at a time through two buffers
+        for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            float *mine = join + (warp & 1) * (OT / 2 * 4 * 32) + lane;
-            if (warp >= 2) {
+            for (int e = 0; e < 2; ++e) {
+                mt[nt][e] = -FLT_MAX;
+                lt[nt][e] = 0.f;
 #pragma unroll
-                for (int t = 0; t < OT / 2 * 4; ++t) mine[t * 32] = o[hf * OT / 2 + t / 4][t % 4];
-            }
-            named_bar_sync(1, 32 * WARPS);
-            if (warp < 2) {
+                for (int w = 0; w < C::WARPS; ++w) mt[nt][e] = fmaxf(mt[nt][e], row_ml[w][nt * 8 + 2 * tq + e].x);
 #pragma unroll
-                for (int t = 0; t < OT / 2 * 4; ++t) o[hf * OT / 2 + t / 4][t % 4] += mine[t * 32];
-                if (warp == 1) {
+                for (int w = 0; w < C::WARPS; ++w) {
+                    const float2 v = row_ml[w][nt * 8 + 2 * tq + e];
+                    lt[nt][e] += ex2_approx(v.x - mt[nt][e]) * v.y;
+                }
+                const float f = ex2_approx(m[nt][e] - mt[nt][e]);
 #pragma unroll
-                    for (int t = 0; t < OT / 2 * 4; ++t) mine[t * 32] = o[hf * OT / 2 + t / 4][t % 4];
+                for (int t = 0; t < MT; ++t) {
+                    o[nt][t][e] *= f;
+                    o[nt][t][2 + e] *= f;
                 }
             }
-            named_bar_sync(1, 32 * WARPS);
-            if (warp == 0) {
-                const float *other = mine + OT / 2 * 4 * 32;
+        // warp w takes over warp w + W/2, W/4, ...: half the columns at a time
+        float *const flat = &o[0][0][0];
+        constexpr int HALF_O = NR * MT * 2;
 #pragma unroll
-                for (int t = 0; t < OT / 2 * 4; ++t) o[hf * OT / 2 + t / 4][t % 4] += other[t * 32];
+        for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+            for (int k = C::WARPS / 2; k >= 1; k >>= 1) {
+                float *at = join + (warp & (k - 1)) * (HALF_O * 32) + lane;
+                if (warp >= k && warp < 2 * k) {
+#pragma unroll
+                    for (int i = 0; i < HALF_O; ++i) at[i * 32] = flat[hf * HALF_O + i];
+                }
+                named_bar_sync(1, 32 * C::WARPS);
+                if (warp < k) {
+#pragma unroll
+                    for (int i = 0; i < HALF_O; ++i) flat[hf * HALF_O + i] += at[i * 32];
+                }
+                named_bar_sync(1, 32 * C::WARPS);
             }
-            named_bar_sync(1, 32 * WARPS);
         }
         const bool whole = pc.whole;
         float *slot = kv_slot(p.ws, blockIdx.x, pc.tail, ROWS, D);
         __syncwarp();
         if (lane == 0) mbar_arrive(&piece_empty[n % PIECES]);
         if (warp != 0) continue;
+        // Columns in pairs: int8 has 2 gq and 2 gq + 1 of each 16.  bf16 has gq and gq + 8:
+        // lanes of even gq trade row 2 tq + 1 for row 2 tq of the lane after them.
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (!real[i]) continue;
-            const int row = gq + 8 * i, pr = tile * ROWS + row;
-            const float inv = lt[i] == 0.f ? 0.f : 1.f / lt[i];      // no key: zeros
-            __nv_bfloat16 *dst = p.out + (int64_t)(s.row + pr / group) * p.ldo + (head * group + pr % group) * D;
-            float *part = slot + row * D;
-            if (!whole && tq == 0) *reinterpret_cast<float2 *>(slot + ROWS * D + 2 * row) = make_float2(mt[i], lt[i]);
-            if constexpr (INT8) {
+        for (int nt = 0; nt < NR; ++nt) {
+            float inv[2];
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    const float v[4] = {o[2 * c][2 * i], o[2 * c + 1][2 * i], o[2 * c][2 * i + 1], o[2 * c + 1][2 * i + 1]};
-                    if (whole)
-                        *reinterpret_cast<uint2 *>(dst + 16 * c + 4 * tq) =
-                            make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
-                    else *reinterpret_cast<float4 *>(part + 16 * c + 4 * tq) = make_float4(v[0], v[1], v[2], v[3]);
-                }
-            } else {
+            for (int e = 0; e < 2; ++e) inv[e] = !whole ? 1.f : lt[nt][e] == 0.f ? 0.f : 1.f / lt[nt][e];   // no key: zeros
 #pragma unroll
-                for (int t = 0; t < OT; ++t) {
-                    const float a = o[t][2 * i], b = o[t][2 * i + 1];
-                    if (whole) *reinterpret_cast<uint32_t *>(dst + 8 * t + 2 * tq) = pack_bf16(a * inv, b * inv);
-                    else *reinterpret_cast<float2 *>(part + 8 * t + 2 * tq) = make_float2(a, b);
-                }
+            for (int e = 0; e < 2; ++e) {
+                const int row = nt * 8 + 2 * tq + e;
+                if (!whole && gq == 0 && tile * ROWS + row < s.packed)
+                    *reinterpret_cast<float2 *>(slot + ROWS * D + 2 * row) = make_float2(mt[nt][e], lt[nt][e]);
             }
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {            // int8: a row; bf16: a column of gq
+                    const int e = INT8 ? u : gq & 1;
+                    float a, b;
+                    if constexpr (INT8) {
+                        a = o[nt][t][u] * inv[u];
+                        b = o[nt][t][2 + u] * inv[u];
+                    } else {
+                        const float x0 = o[nt][t][2 * u] * inv[0], x1 = o[nt][t][2 * u + 1] * inv[1];
+                        const float got = __shfl_xor_sync(0xffffffffu, e ? x0 : x1, 4);
+                        a = e ? got : x0;
+                        b = e ? x1 : got;
+                    }
+                    const int row = nt * 8 + 2 * tq + e, pr = tile * ROWS + row;
+                    const int col = 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
+                    if (pr >= s.packed) continue;
+                    if (whole)
+                        *reinterpret_cast<uint32_t *>(p.out + (int64_t)(s.row + pr / group) * p.ldo +
+                                                      (head * group + pr % group) * D + col) = pack_bf16(a, b);
+                    else *reinterpret_cast<float2 *>(slot + row * D + col) = make_float2(a, b);
+                }
+            __syncwarp();
         }
     }
 }
 
-template <bool INT8, int D>
+template <bool INT8, int D, int NR>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
-    using C = Cfg<INT8, D>;
+    using C = Cfg<INT8, D, NR>;
     static int attr_done[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(kv_decode_kernel<INT8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        cudaFuncSetAttribute(kv_decode_kernel<INT8, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         attr_done[dev] = 1;
     }
     CUtensorMap tm;
@@ -499,7 +578,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
         return ECHO_ERR_CUDA;
     DecodeParams p;
     p.pool = echo::kv_pool(*a.pool);
-    p.work = echo::kv_work(a, ROWS, ROWS, C::BSHIFT, 2 * echo::num_sms());
+    p.work = echo::kv_work(a, C::ROWS, C::ROWS, C::BSHIFT, C::CTAS * echo::num_sms());
     p.q = static_cast<const __nv_bfloat16 *>(a.q);
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.ws = static_cast<float *>(a.ws);
@@ -509,10 +588,17 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.err = echo::device_error_ptr();
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        echo::launch_chained(kv_decode_kernel<INT8, D>, dim3(p.work.workers), dim3(THREADS), C::SMEM, st, tm, p);
+        echo::launch_chained(kv_decode_kernel<INT8, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
     }
     echo::launch_kv_join(a, p.work, st);
     return echo::last_launch_status();
+}
+
+template <bool INT8, int D>
+echo_status launch_rows(const echo::KvAttention &a, int rows, cudaStream_t st) {
+    if (rows <= 8) return launch<INT8, D, 1>(a, st);
+    if (rows <= 16) return launch<INT8, D, 2>(a, st);
+    return launch<INT8, D, 4>(a, st);
 }
 
 }  // namespace
@@ -520,13 +606,13 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
 namespace echo {
 
 size_t kv_decode_workspace(const echo_kv_pool &pool) {
-    return kv_workspace_bytes(2 * num_sms(), ROWS, pool.d);
+    return kv_workspace_bytes(2 * num_sms(), kDecodeRows, pool.d);
 }
 
-echo_status launch_kv_decode(const KvAttention &a, cudaStream_t st) {
+echo_status launch_kv_decode(const KvAttention &a, int rows, cudaStream_t st) {
     const bool i8 = a.pool->kind == ECHO_CACHE_INT8;
-    if (a.pool->d == 64) return i8 ? launch<true, 64>(a, st) : launch<false, 64>(a, st);
-    return i8 ? launch<true, 128>(a, st) : launch<false, 128>(a, st);
+    if (a.pool->d == 64) return i8 ? launch_rows<true, 64>(a, rows, st) : launch_rows<false, 64>(a, rows, st);
+    return i8 ? launch_rows<true, 128>(a, rows, st) : launch_rows<false, 128>(a, rows, st);
 }
 
 }  // namespace echo

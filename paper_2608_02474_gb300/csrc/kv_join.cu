@@ -113,7 +113,7 @@ namespace echo {
 void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st) {
     if (!w.split) return;
     LaunchScope ls(ECHO_K_KV_JOIN, a.batch->n_rows, (int64_t)a.Hq * a.pool->d, w.workers, st);
-    if (w.tile <= 16) launch<1, 4>(a, w, st);
+    if (w.tile <= kDecodeRows) launch<1, 4>(a, w, st);
     else launch<4, 1>(a, w, st);
 }
 
