@@ -145,8 +145,9 @@ struct KvAttention {
 };
 constexpr int kDecodeRows = 32;   // the most packed rows of a tile of launch_kv_decode
 size_t kv_decode_workspace(const echo_kv_pool &pool);
-// `rows`: packed rows of a sequence, about
-echo_status launch_kv_decode(const KvAttention &a, int rows, cudaStream_t st);
+// `rows`: packed rows of a sequence, about; whether it is the faster one for them
+bool kv_few_rows(const echo_kv_pool &pool, int64_t rows);
+echo_status launch_kv_decode(const KvAttention &a, int64_t rows, cudaStream_t st);
 size_t kv_chunk_workspace(const echo_kv_pool &pool);
 echo_status launch_kv_chunk(const KvAttention &a, cudaStream_t st);
 

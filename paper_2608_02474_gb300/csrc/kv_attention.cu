@@ -29,5 +29,5 @@ extern "C" echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const KvAttention a{pool, batch, q, ldq, Hq, causal_block, out, ldo, workspace};
     const int64_t rows = (int64_t)batch->max_rows * (Hq / pool->H);   // packed, of a sequence
-    return rows <= kDecodeRows ? launch_kv_decode(a, (int)rows, st) : launch_kv_chunk(a, st);
+    return kv_few_rows(*pool, rows) ? launch_kv_decode(a, rows, st) : launch_kv_chunk(a, st);
 }

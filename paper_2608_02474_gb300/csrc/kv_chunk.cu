@@ -33,6 +33,7 @@ constexpr int ATOM = 128 * 128;                 // 128 rows of 64 bf16
 constexpr uint32_t TMEM_COLS = 512, O_COL = 256;
 constexpr int PIECES = 4;                       // handed out ahead
 constexpr int SLOT_ROWS = TILES * BM;
+constexpr int kWholeKeys = 768;                 // 64 bf16 rows, 8 heads of 128: whole 512 keys 16.5 us, divided 22
 constexpr int PAIRS = 3;                        // (V_f, K_{f+1}) on their way or in use
 constexpr int SPOILT = 2;                       // blocks whose spoilt keys are kept
 
@@ -801,7 +802,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     ChunkParams p;
     p.pool = echo::kv_pool(*a.pool);
     p.tile_rows = tokens * group;
-    p.work = echo::kv_work(a, TILES * p.tile_rows, SLOT_ROWS, 7, echo::num_sms());
+    p.work = echo::kv_work(a, TILES * p.tile_rows, SLOT_ROWS, 7, echo::num_sms(), kWholeKeys);
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.ws = static_cast<float *>(a.ws);
     p.ldo = a.ldo;

@@ -1,5 +1,5 @@
 // Attention over the paged cache where a sequence has few packed rows (single tokens,
-// drafts): 8, 16 or 32 at a time, so that the bytes of the pages bound it.
+// drafts): 8, 16, 24 or 32 at a time, so that the bytes of the pages bound it.
 //
 // One CTA works through its share of the items (kv_schedule.cuh): a producer warp copies
 // key blocks (K and V of one head, and the scales of int8 pages) page by page into a ring
@@ -26,12 +26,12 @@
 namespace {
 
 constexpr int PIECES = 4;                      // handed out ahead
+constexpr int kWholeKeys = 512;     // 16 heads of 64, one bf16 token: whole 257 keys 10.5 us, 1024 16.5; divided 12.5, 13.3
 
 template <bool INT8, int D, int NR>
 struct Cfg {
     static constexpr int ROWS = 8 * NR;
     static constexpr int GROUPS = NR * D <= (INT8 ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
-    static constexpr int CTAS = NR * D <= 256 ? 2 : 1;     // on an SM
     static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
     static constexpr int KPW = INT8 ? 32 : 16;             // keys of a warp
     static constexpr int BK = 4 * KPW;                     // keys of a block
@@ -41,9 +41,9 @@ struct Cfg {
     static constexpr int SCALES = INT8 ? 2 * BK * 4 : 0;
     static constexpr int STAGE = 2 * HALF + SCALES;        // a multiple of 1024
     static constexpr int JOIN = WARPS / 4 * ROWS * D * 4;  // half of the warps' half of O
-    static constexpr bool Q_SMEM = NR * D > 256;           // the queries' registers do not suffice
+    static constexpr bool Q_SMEM = NR * D >= 192 && D == 64;          // the queries' registers do not suffice
     static constexpr int Q_BYTES = Q_SMEM ? ROWS * D * 2 : 0;
-    static constexpr int RING = ((CTAS == 2 ? 110 : 220) * 1024 - JOIN - Q_BYTES) / STAGE;
+    static constexpr int RING = (110 * 1024 - JOIN - Q_BYTES) / STAGE;   // two CTAs share an SM
     static constexpr int SMEM = RING * STAGE + JOIN + Q_BYTES + 1024;
     static_assert(STAGE % 1024 == 0 && RING >= 2, "");
 };
@@ -91,7 +91,7 @@ ECHO_DEV uint32_t chunk_at(int r, int c) {
 }
 
 template <bool INT8, int D, int NR>
-__global__ void __launch_bounds__((Cfg<INT8, D, NR>::THREADS), (Cfg<INT8, D, NR>::CTAS))
+__global__ void __launch_bounds__((Cfg<INT8, D, NR>::THREADS), 2)
 kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     using C = Cfg<INT8, D, NR>;
     constexpr int KPW = C::KPW, BK = C::BK, KG = KPW / 16, MT = D / 16, ROWS = C::ROWS;
@@ -578,7 +578,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
         return ECHO_ERR_CUDA;
     DecodeParams p;
     p.pool = echo::kv_pool(*a.pool);
-    p.work = echo::kv_work(a, C::ROWS, C::ROWS, C::BSHIFT, C::CTAS * echo::num_sms());
+    p.work = echo::kv_work(a, C::ROWS, C::ROWS, C::BSHIFT, 2 * echo::num_sms(), kWholeKeys);
     p.q = static_cast<const __nv_bfloat16 *>(a.q);
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.ws = static_cast<float *>(a.ws);
@@ -594,11 +594,28 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     return echo::last_launch_status();
 }
 
+// Packed rows of a tile for sequences of `rows`, 0: more than this kernel is for.  Measured
+// with 8 sequences of 7800 tokens, 16 heads (us; the chunk kernel in brackets):
+//   d 64:  bf16 8 rows 54, 16 58, 24 62, 32 69 (82), 48 in tiles of 24 92 (83)
+//          int8 8 rows 37, 16 41, 24 52, 32 65 (107), 48 in 24s 82, 64 in 32s 102 (108)
+//   d 128: bf16 8 rows 90, 16 95 (106), 24 in 16s 104, 32 108 (108)
+//          int8 8 rows 56, 16 62, 24 in 16s 92, 32 94 (132), 48 137 (132); tiles of 24 and
+//          32, with half the CTAs, are no faster than two of 16: 90, 116
+int tile_rows(bool i8, int d, int64_t rows) {
+    if (d == 128) return rows <= 8 ? 8 : rows <= (i8 ? 32 : 16) ? 16 : 0;
+    if (rows <= 32) return (int)(rows + 7) / 8 * 8 + (rows == 0 ? 8 : 0);
+    return i8 && rows <= 64 ? (rows <= 48 ? 24 : 32) : 0;
+}
+
 template <bool INT8, int D>
-echo_status launch_rows(const echo::KvAttention &a, int rows, cudaStream_t st) {
-    if (rows <= 8) return launch<INT8, D, 1>(a, st);
-    if (rows <= 16) return launch<INT8, D, 2>(a, st);
-    return launch<INT8, D, 4>(a, st);
+echo_status launch_rows(const echo::KvAttention &a, int tile, cudaStream_t st) {
+    if (tile == 8) return launch<INT8, D, 1>(a, st);
+    if (tile == 16) return launch<INT8, D, 2>(a, st);
+    if constexpr (D == 64) {
+        if (tile == 24) return launch<INT8, D, 3>(a, st);
+        return launch<INT8, D, 4>(a, st);
+    }
+    return ECHO_ERR_SHAPE;
 }
 
 }  // namespace
@@ -609,10 +626,15 @@ size_t kv_decode_workspace(const echo_kv_pool &pool) {
     return kv_workspace_bytes(2 * num_sms(), kDecodeRows, pool.d);
 }
 
-echo_status launch_kv_decode(const KvAttention &a, int rows, cudaStream_t st) {
+bool kv_few_rows(const echo_kv_pool &pool, int64_t rows) {
+    return tile_rows(pool.kind == ECHO_CACHE_INT8, pool.d, rows) > 0;
+}
+
+echo_status launch_kv_decode(const KvAttention &a, int64_t rows, cudaStream_t st) {
     const bool i8 = a.pool->kind == ECHO_CACHE_INT8;
-    if (a.pool->d == 64) return i8 ? launch_rows<true, 64>(a, rows, st) : launch_rows<false, 64>(a, rows, st);
-    return i8 ? launch_rows<true, 128>(a, rows, st) : launch_rows<false, 128>(a, rows, st);
+    const int tile = tile_rows(i8, a.pool->d, rows);
+    if (a.pool->d == 64) return i8 ? launch_rows<true, 64>(a, tile, st) : launch_rows<false, 64>(a, tile, st);
+    return i8 ? launch_rows<true, 128>(a, tile, st) : launch_rows<false, 128>(a, tile, st);
 }
 
 }  // namespace echo

@@ -323,7 +323,9 @@ inline size_t kv_workspace_bytes(int workers, int rows, int D) {
 }
 
 namespace echo {
-inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_shift, int workers) {
+// whole_keys: tables that cover no more are not divided, which saves the second launch
+inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_shift, int workers,
+                      int whole_keys) {
     const echo_kv_pool &p = *a.pool;
     const int64_t cap = (int64_t)a.batch->max_pages * p.page_tokens;
     KvWork w;
@@ -337,7 +339,7 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
     w.block_shift = block_shift;
     w.workers = workers;
     w.least = 4;
-    w.split = 1;
+    w.split = cap > whole_keys;
     return w;
 }
 void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st);

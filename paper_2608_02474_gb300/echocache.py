@@ -620,25 +620,24 @@ class KVBatch:
         self._ref = _c.byref(self.cstruct)
 
 
-def _kv_rows(pool: KVPool, batch: KVBatch, k, v):
-    """Row stride of k and v, [n_rows, >= H d] each (columns of a wider tensor, too)."""
-    for t, n in ((k, "k"), (v, "v")):
-        _rows_of(t, n, batch.n_rows, pool.H * pool.d)
-    if k.dtype != v.dtype or (batch.n_rows > 1 and k.stride(0) != v.stride(0)):
-        raise ValueError("k and v must share dtype and row stride")
-    return _ld(k)
-
-
 def _rows_of(t, name, n_rows, cols):
-    if not t.is_cuda or t.dim() != 2 or t.shape[0] != n_rows or t.shape[1] < cols:
+    """Row stride of a CUDA tensor of n_rows rows and at least cols contiguous columns (those
+    of a wider tensor, too).  The stride of a single row means nothing, and may be anything."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or len(shape) != 2 or shape[0] != n_rows or shape[1] < cols:
         raise ValueError(f"{name} must be a CUDA tensor of {n_rows} rows and {cols} columns")
-    if t.stride(1) != 1:
+    if stride[1] != 1:
         raise ValueError(f"{name}'s columns must be contiguous")
+    return stride[0] if n_rows > 1 else (shape[1] + 7) // 8 * 8
 
 
-def _ld(t):
-    # the stride of a single row means nothing, and may be anything
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+def _kv_rows(pool: KVPool, batch: KVBatch, k, v):
+    """Row stride of k and v, [n_rows, >= H d] each."""
+    n, cols = batch.n_rows, pool.H * pool.d
+    ld = _rows_of(k, "k", n, cols)
+    if _rows_of(v, "v", n, cols) != ld and n > 1 or k.dtype != v.dtype:
+        raise ValueError("k and v must share dtype and row stride")
+    return ld if n > 1 else (cols + 7) // 8 * 8
 
 
 def _empty(shape, dtype, device, stream):
@@ -675,20 +674,18 @@ def echo_kv_attention(pool: KVPool, batch: KVBatch, q, Hq: int | None = None, ca
                       out=None, workspace=None, stream=None):
     """Attention of the batch's rows, q bf16 [n_rows, Hq d], over their sequences' pages;
     Hq is q's columns over d when not given."""
+    n, bf16 = batch.n_rows, torch.bfloat16
     Hq = q.shape[1] // pool.d if Hq is None else Hq
-    _rows_of(q, "q", batch.n_rows, Hq * pool.d)
-    if q.dtype != torch.bfloat16:
-        raise TypeError(f"unsupported dtype {q.dtype}")
+    ldq = _rows_of(q, "q", n, Hq * pool.d)
     if out is None:
-        out = _empty((batch.n_rows, Hq * pool.d), torch.bfloat16, q.device, stream)
-    else:
-        _rows_of(out, "out", batch.n_rows, Hq * pool.d)
-        if out.dtype != torch.bfloat16:
-            raise TypeError(f"unsupported dtype {out.dtype}")
+        out = _empty((n, Hq * pool.d), bf16, q.device, stream)
+    ldo = _rows_of(out, "out", n, Hq * pool.d)
+    if q.dtype != bf16 or out.dtype != bf16:
+        raise TypeError(f"unsupported dtype {q.dtype if q.dtype != bf16 else out.dtype}")
     if workspace is None:
         workspace = _empty(echo_kv_attention_workspace_size(pool, batch, Hq), torch.uint8, q.device,
                            stream)
     _check("echo_kv_attention", lib().echo_kv_attention(
-        pool._ref, batch._ref, _p(q), _ld(q), Hq, causal_block, _p(out), _ld(out), _p(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        pool._ref, batch._ref, q.data_ptr(), ldq, Hq, causal_block, out.data_ptr(), ldo,
+        workspace.data_ptr(), workspace.nbytes, _stream(stream)))
     return out
