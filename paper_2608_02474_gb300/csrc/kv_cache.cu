@@ -36,46 +36,64 @@ struct Piece8 {   // 8 values as they are loaded
     }
 };
 
-// rows' keys and values into the pages: piece c of a row is 8 values of head
-// (c mod (H d / 8)) / (d / 8), of the keys first and then of the values
+// Codes without conversions, which run at an eighth of the rate of additions:
+// 1.5 2^23 + t, |t| < 2^22, is 1.5 2^23 + rint(t) (half to even), with rint(t) in two's
+// complement in its low bits; |v inv| stays below 127.5, so that nothing is clamped.
+ECHO_DEV uint32_t codes4(const float *f, float inv) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(f[i], inv), 12582912.f));
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+}
+
+// rows' keys and values into the pages: piece c of a row is EP values of its keys first and
+// then of its values.  int8: 16, so that a division and the head's maximum (by shuffles) are
+// few beside the values, and codes leave 16 bytes at a time; with 8, rintf and casts, 32760
+// rows of 40 heads of 128 took 272 us, now XXX.
 template <typename T, bool INT8, int D>
 __global__ void __launch_bounds__(kThreads)
 kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, const T *__restrict__ v,
                 int64_t ld, int *err) {
     pdl_enter();
-    constexpr int LPH = D / 8;                        // lanes of a head
+    constexpr int EP = INT8 ? 16 : 8, LPH = D / EP;   // lanes of a head
+    constexpr int U = INT8 ? kUnroll / 2 : kUnroll;
     const int lane = threadIdx.x & 31;
     const int half = pool.H * LPH, C = 2 * half;      // pieces of a row
-    const int tasks = (C + 32 * kUnroll - 1) / (32 * kUnroll);
+    const int tasks = (C + 32 * U - 1) / (32 * U);
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
-        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * kUnroll + lane;
-        Piece8<T> in[kUnroll];
+        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
+        Piece8<T> in[U][EP / 8];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
-            if (c < C) in[u].load((c < half ? k : v) + r * ld + (c < half ? c : c - half) * 8);
+            if (c < C) {
+#pragma unroll
+                for (int h = 0; h < EP / 8; ++h)
+                    in[u][h].load((c < half ? k : v) + r * ld + (c < half ? c : c - half) * EP + 8 * h);
+            }
         }
-        const int seq = kv_seq_of_row(b, r);
-        if (seq < 0) continue;
-        const int64_t p = (int64_t)b.len[seq] - b.row0[seq + 1] + r;
-        if (p < 0) continue;
-        const int64_t at = kv_place(pool, b, seq, p, err);
+        const KvRow row = kv_find_row(b, r);
+        if (row.seq < 0 || row.p < 0) continue;
+        const int64_t at = kv_place(pool, b, row.seq, row.p, err);
         if (at < 0) continue;
         const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
             const int kv = c >= half, ch = kv ? c - half : c;
             const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            float f[8];
-            if (c < C) in[u].values(f);
+            float f[EP];
+            if (c < C) {
+#pragma unroll
+                for (int h = 0; h < EP / 8; ++h) in[u][h].values(f + 8 * h);
+            }
             if constexpr (INT8) {
                 // the largest |value| as fp32 bits: infinity above every number, NaN above it
                 uint32_t a = 0;
                 if (c < C) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+                    for (int i = 0; i < EP; ++i) a = max(a, __float_as_uint(f[i]) & 0x7FFFFFFFu);
                 }
 #pragma unroll
                 for (int o = LPH / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
@@ -83,8 +101,9 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
                 const bool bad = a >= 0x7F800000u;
                 const float amax = __uint_as_float(a);
                 const float inv = !bad && amax > 0.f ? __fdiv_rn(127.f, amax) : 0.f;
-                *reinterpret_cast<uint2 *>(pool.pages + vec * D + (ch % LPH) * 8) =
-                    bad ? make_uint2(0, 0) : quant8(f, inv);
+                *reinterpret_cast<uint4 *>(pool.pages + vec * D + (ch % LPH) * 16) =
+                    bad ? make_uint4(0, 0, 0, 0)
+                        : make_uint4(codes4(f, inv), codes4(f + 4, inv), codes4(f + 8, inv), codes4(f + 12, inv));
                 if (ch % LPH == 0) {
                     pool.scale[vec] = !bad ? __fdiv_rn(amax, 127.f)
                                            : a > 0x7F800000u ? __int_as_float(0x7fc00000) : INFINITY;
@@ -92,7 +111,7 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
                 }
             } else if (c < C) {
                 *reinterpret_cast<uint4 *>(pool.pages + (vec * D + (ch % LPH) * 8) * 2) =
-                    sizeof(T) == 2 ? in[u].v[0] : pack8_bf16(f);
+                    sizeof(T) == 2 ? in[u][0].v[0] : pack8_bf16(f);
             }
         }
     }
@@ -111,10 +130,9 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
         const int r = (int)walk.row, c0 = (int)walk.piece * 32 * kUnroll + lane;
-        const int seq = kv_seq_of_row(b, r);
-        if (seq < 0) continue;
-        const int64_t p = (int64_t)b.len[seq] - b.row0[seq + 1] + r;
-        const int64_t at = p < 0 ? -1 : kv_place(pool, b, seq, p, err);   // -1: zeros
+        const KvRow row = kv_find_row(b, r);
+        if (row.seq < 0) continue;
+        const int64_t at = row.p < 0 ? -1 : kv_place(pool, b, row.seq, row.p, err);   // -1: zeros
         const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
         uint4 in[kUnroll];
         float sc[kUnroll];
@@ -157,16 +175,16 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
 }
 
 // blocks for the warps' tasks of all rows, a few waves at most
-int grid_for(const echo_kv_pool &p, int n_rows, int per_piece) {
+int grid_for(const echo_kv_pool &p, int n_rows, int per_piece, int unroll) {
     const int64_t C = 2ll * p.H * p.d / per_piece;
-    const int64_t blocks = ((C + 32 * kUnroll - 1) / (32 * kUnroll) * n_rows + kWarps - 1) / kWarps;
+    const int64_t blocks = ((C + 32 * unroll - 1) / (32 * unroll) * n_rows + kWarps - 1) / kWarps;
     return (int)(blocks < 16384 ? blocks : 16384);
 }
 
 template <typename T, bool INT8>
 void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, const void *v,
                   int64_t ld, cudaStream_t st) {
-    const int grid = grid_for(p, b.n_rows, 8);
+    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8, INT8 ? kUnroll / 2 : kUnroll);
     echo::launch_chained(p.d == 64 ? kv_write_kernel<T, INT8, 64> : kv_write_kernel<T, INT8, 128>,
                          dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
                          static_cast<const T *>(k), static_cast<const T *>(v), ld,
@@ -176,7 +194,7 @@ void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, 
 template <typename T, bool INT8>
 void launch_read(const echo_kv_pool &p, const echo_kv_batch &b, void *k, void *v, int64_t ld,
                  cudaStream_t st) {
-    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8);
+    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8, kUnroll);
     echo::launch_chained(p.d == 64 ? kv_read_kernel<T, INT8, 64> : kv_read_kernel<T, INT8, 128>,
                          dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
                          static_cast<T *>(k), static_cast<T *>(v), ld, echo::device_error_ptr());

@@ -17,21 +17,27 @@ struct KvBatch {
     int n_seqs, max_pages, n_rows;
 };
 
-// The sequence that row r belongs to, -1 where there is none: the last b with row0[b] <= r
-// if row0[b + 1] lies beyond r.  The whole warp searches for one row, 32 entries at a time:
-// two dependent loads for up to 1024 sequences, where a bisection takes ten.
-ECHO_DEV int kv_seq_of_row(const KvBatch &b, int r) {
+// The sequence that row r belongs to and the row's position in it; seq -1 where there is
+// none.  It is the last b with row0[b] <= r if row0[b + 1] lies beyond r.  The whole warp
+// searches for one row, 32 entries at a time: two dependent loads for up to 1024 sequences,
+// where a bisection takes ten.
+struct KvRow {
+    int seq;
+    int64_t p;
+};
+ECHO_DEV KvRow kv_find_row(const KvBatch &b, int r) {
     const int lane = threadIdx.x & 31;
     int lo = 0, n = b.n_seqs;
     while (n > 1) {
         const int step = (n + 31) >> 5, i = lane * step;
         const int below = __popc(__ballot_sync(0xffffffffu, i < n && b.row0[lo + i] <= r));
-        if (below == 0) return -1;
+        if (below == 0) return {-1, 0};
         const int skip = (below - 1) * step;
         lo += skip;
         n = min(step, n - skip);
     }
-    return b.row0[lo] <= r && r < b.row0[lo + 1] ? lo : -1;
+    const int first = b.row0[lo], end = b.row0[lo + 1], len = b.len[lo];   // at once
+    return {first <= r && r < end ? lo : -1, (int64_t)len - end + r};
 }
 
 // Place of position p of a sequence in the pool, as page * (1 << shift) + slot; -1 where the
