@@ -2,39 +2,36 @@
 // quantised to int8 with a scale per token and head) and cached rows read back.
 //
 // Both are one pass: a value is read once and written once, and the time is that of
-// the bytes.  A warp takes one row's next 32 * U pieces of 16 bytes, so that its loads
-// are all in flight before the first is used, and finds the row's place in the pool
-// meanwhile.  A head's values lie in neighbouring lanes (d / 8 or d / 16 of them), which
-// gives its maximum by that many lanes' shuffles.
+// the bytes.  A warp takes some of one row's pieces, so that its loads are all in flight
+// before the first is used, and finds the row's place in the pool meanwhile.  A head's
+// values lie in neighbouring lanes, which gives its maximum by their shuffles.
 #include "kv_pages.cuh"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kUnroll = 4;
+constexpr int kLoads = 4;   // 16-byte loads of a lane on their way at once
 
+// 16 bytes of a row: 8 bf16 values, or 4 of fp32
 template <typename T>
-struct Piece8 {   // 8 values as they are loaded
-    uint4 v[sizeof(T) / 2];
-    ECHO_DEV void load(const T *p) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+constexpr int kPer16 = 16 / (int)sizeof(T);
+template <typename T>
+ECHO_DEV void values16(const uint4 &v, float *f) {
+    if constexpr (sizeof(T) == 2) {
+        unpack8_bf16(v, f);
+    } else {
+        f[0] = __uint_as_float(v.x);
+        f[1] = __uint_as_float(v.y);
+        f[2] = __uint_as_float(v.z);
+        f[3] = __uint_as_float(v.w);
     }
-    ECHO_DEV void values(float *f) const {
-        if constexpr (sizeof(T) == 2) {
-            unpack8_bf16(v[0], f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                f[4 * i] = __uint_as_float(v[i].x);
-                f[4 * i + 1] = __uint_as_float(v[i].y);
-                f[4 * i + 2] = __uint_as_float(v[i].z);
-                f[4 * i + 3] = __uint_as_float(v[i].w);
-            }
-        }
-    }
-};
+}
+template <typename T>
+ECHO_DEV void store16(T *p, const float *f) {
+    if constexpr (sizeof(T) == 2) __stcs(reinterpret_cast<uint4 *>(p), pack8_bf16(f));
+    else __stcs(reinterpret_cast<float4 *>(p), make_float4(f[0], f[1], f[2], f[3]));
+}
 
 // Codes without conversions, which run at an eighth of the rate of additions:
 // 1.5 2^23 + t, |t| < 2^22, is 1.5 2^23 + rint(t) (half to even), with rint(t) in two's
@@ -48,29 +45,30 @@ ECHO_DEV uint32_t codes4(const float *f, float inv) {
 
 // rows' keys and values into the pages: piece c of a row is EP values of its keys first and
 // then of its values.  int8: 16, so that a division and the head's maximum (by shuffles) are
-// few beside the values, and codes leave 16 bytes at a time; with 8, rintf and casts, 32760
-// rows of 40 heads of 128 took 272 us, now XXX.
+// few beside the values; with 8, rintf and casts, 32760 rows of 40 heads of 128 took 272 us,
+// now XXX.  A lane's values are 16-byte groups apart by the head's lanes, so that a warp
+// reads and writes whole stretches.
 template <typename T, bool INT8, int D>
 __global__ void __launch_bounds__(kThreads)
 kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, const T *__restrict__ v,
                 int64_t ld, int *err) {
     pdl_enter();
-    constexpr int EP = INT8 ? 16 : 8, LPH = D / EP;   // lanes of a head
-    constexpr int U = INT8 ? kUnroll / 2 : kUnroll;
+    constexpr int GE = kPer16<T>, EP = INT8 ? 16 : 8, NG = EP / GE, LPH = D / EP;   // lanes of a head
+    constexpr int U = kLoads / NG;
     const int lane = threadIdx.x & 31;
     const int half = pool.H * LPH, C = 2 * half;      // pieces of a row
     const int tasks = (C + 32 * U - 1) / (32 * U);
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
         const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
-        Piece8<T> in[U][EP / 8];
+        uint4 in[U][NG];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + 32 * u;
+            const int c = c0 + 32 * u, ch = c < half ? c : c - half;
             if (c < C) {
+                const T *src = (c < half ? k : v) + r * ld + (ch / LPH) * D + (ch % LPH) * GE;
 #pragma unroll
-                for (int h = 0; h < EP / 8; ++h)
-                    in[u][h].load((c < half ? k : v) + r * ld + (c < half ? c : c - half) * EP + 8 * h);
+                for (int h = 0; h < NG; ++h) in[u][h] = __ldcs(reinterpret_cast<const uint4 *>(src + h * (D / NG)));
             }
         }
         const KvRow row = kv_find_row(b, r);
@@ -83,100 +81,113 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
             const int c = c0 + 32 * u;
             const int kv = c >= half, ch = kv ? c - half : c;
             const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            float f[EP];
+            float f[EP] = {};
             if (c < C) {
 #pragma unroll
-                for (int h = 0; h < EP / 8; ++h) in[u][h].values(f + 8 * h);
+                for (int h = 0; h < NG; ++h) values16<T>(in[u][h], f + h * GE);
             }
             if constexpr (INT8) {
                 // the largest |value| as fp32 bits: infinity above every number, NaN above it
                 uint32_t a = 0;
-                if (c < C) {
 #pragma unroll
-                    for (int i = 0; i < EP; ++i) a = max(a, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-                }
+                for (int i = 0; i < EP; ++i) a = max(a, __float_as_uint(f[i]) & 0x7FFFFFFFu);
 #pragma unroll
                 for (int o = LPH / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
                 if (c >= C) continue;
                 const bool bad = a >= 0x7F800000u;
                 const float amax = __uint_as_float(a);
                 const float inv = !bad && amax > 0.f ? __fdiv_rn(127.f, amax) : 0.f;
-                *reinterpret_cast<uint4 *>(pool.pages + vec * D + (ch % LPH) * 16) =
-                    bad ? make_uint4(0, 0, 0, 0)
-                        : make_uint4(codes4(f, inv), codes4(f + 4, inv), codes4(f + 8, inv), codes4(f + 12, inv));
+                uint8_t *dst = pool.pages + vec * D + (ch % LPH) * GE;
+#pragma unroll
+                for (int h = 0; h < NG; ++h) {
+                    const uint32_t lo = bad ? 0u : codes4(f + h * GE, inv);
+                    if constexpr (GE == 4) {
+                        *reinterpret_cast<uint32_t *>(dst + h * (D / NG)) = lo;
+                    } else {
+                        *reinterpret_cast<uint2 *>(dst + h * (D / NG)) =
+                            make_uint2(lo, bad ? 0u : codes4(f + h * GE + 4, inv));
+                    }
+                }
                 if (ch % LPH == 0) {
                     pool.scale[vec] = !bad ? __fdiv_rn(amax, 127.f)
                                            : a > 0x7F800000u ? __int_as_float(0x7fc00000) : INFINITY;
                     if (bad) echo_flag_error(err, ECHO_ERR_NONFINITE);
                 }
             } else if (c < C) {
-                *reinterpret_cast<uint4 *>(pool.pages + (vec * D + (ch % LPH) * 8) * 2) =
-                    sizeof(T) == 2 ? in[u][0].v[0] : pack8_bf16(f);
+                uint8_t *dst = pool.pages + (vec * D + (ch % LPH) * GE) * 2;
+#pragma unroll
+                for (int h = 0; h < NG; ++h) {
+                    if constexpr (GE == 8) {
+                        *reinterpret_cast<uint4 *>(dst) = in[u][0];
+                    } else {
+                        *reinterpret_cast<uint2 *>(dst + h * D) =
+                            make_uint2(pack_bf16(f[4 * h], f[4 * h + 1]), pack_bf16(f[4 * h + 2], f[4 * h + 3]));
+                    }
+                }
             }
         }
     }
 }
 
-// cached rows back: piece c of a row is 16 bytes of the cache, EP values
+// cached rows back: piece c of a row is 16 bytes of what is stored, so that a warp stores
+// whole stretches
 template <typename T, bool INT8, int D>
 __global__ void __launch_bounds__(kThreads)
 kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restrict__ v, int64_t ld,
                int *err) {
     pdl_enter();
-    constexpr int EP = INT8 ? 16 : 8, LPH = D / EP;
+    constexpr int EP = kPer16<T>, BYTES = EP * (INT8 ? 1 : 2), LPH = D / EP, U = BYTES == 16 ? kLoads : 2 * kLoads;
     const int lane = threadIdx.x & 31;
     const int half = pool.H * LPH, C = 2 * half;
-    const int tasks = (C + 32 * kUnroll - 1) / (32 * kUnroll);
+    const int tasks = (C + 32 * U - 1) / (32 * U);
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
-        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * kUnroll + lane;
+        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
         const KvRow row = kv_find_row(b, r);
         if (row.seq < 0) continue;
         const int64_t at = row.p < 0 ? -1 : kv_place(pool, b, row.seq, row.p, err);   // -1: zeros
         const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
-        uint4 in[kUnroll];
-        float sc[kUnroll];
+        uint32_t in[U][BYTES / 4];
+        float sc[U];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
-            in[u] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < BYTES / 4; ++i) in[u][i] = 0u;
             sc[u] = 0.f;
             if (c >= C || at < 0) continue;
             const int kv = c >= half, ch = kv ? c - half : c;
             const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            in[u] = __ldcs(reinterpret_cast<const uint4 *>(pool.pages + vec * D * (INT8 ? 1 : 2)) + ch % LPH);
+            const uint8_t *src = pool.pages + vec * D * (INT8 ? 1 : 2) + ch % LPH * BYTES;
+            if constexpr (BYTES == 16) {
+                const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(src));
+                in[u][0] = w.x, in[u][1] = w.y, in[u][2] = w.z, in[u][3] = w.w;
+            } else if constexpr (BYTES == 8) {
+                const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(src));
+                in[u][0] = w.x, in[u][1] = w.y;
+            } else {
+                in[u][0] = __ldcs(reinterpret_cast<const uint32_t *>(src));
+            }
             if constexpr (INT8) sc[u] = pool.scale[vec];
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
             if (c >= C) continue;
-            const int ch = c >= half ? c - half : c;
-            T *out = (c >= half ? v : k) + r * ld + (int64_t)ch * EP;
             float f[EP];
-            if constexpr (INT8) {
-                const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] = __fmul_rn((float)(int8_t)(w[i >> 2] >> (8 * (i & 3))), sc[u]);
-            } else {
-                unpack8_bf16(in[u], f);
+            for (int i = 0; i < EP; ++i) {
+                if constexpr (INT8) f[i] = __fmul_rn((float)(int8_t)(in[u][i >> 2] >> (8 * (i & 3))), sc[u]);
+                else f[i] = i & 1 ? bf16hi(in[u][i >> 1]) : bf16lo(in[u][i >> 1]);
             }
-            if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int i = 0; i < EP / 8; ++i) __stcs(reinterpret_cast<uint4 *>(out) + i, pack8_bf16(f + 8 * i));
-            } else {
-#pragma unroll
-                for (int i = 0; i < EP / 4; ++i)
-                    __stcs(reinterpret_cast<float4 *>(out) + i,
-                           make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]));
-            }
+            store16<T>((c >= half ? v : k) + r * ld + (int64_t)(c >= half ? c - half : c) * EP, f);
         }
     }
 }
 
-// blocks for the warps' tasks of all rows, a few waves at most
-int grid_for(const echo_kv_pool &p, int n_rows, int per_piece, int unroll) {
-    const int64_t C = 2ll * p.H * p.d / per_piece;
+// blocks for the warps' tasks of all rows: `unroll` pieces of `values` a lane; a few waves at most
+int grid_for(const echo_kv_pool &p, int n_rows, int values, int unroll) {
+    const int64_t C = 2ll * p.H * p.d / values;
     const int64_t blocks = ((C + 32 * unroll - 1) / (32 * unroll) * n_rows + kWarps - 1) / kWarps;
     return (int)(blocks < 16384 ? blocks : 16384);
 }
@@ -184,7 +195,8 @@ int grid_for(const echo_kv_pool &p, int n_rows, int per_piece, int unroll) {
 template <typename T, bool INT8>
 void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, const void *v,
                   int64_t ld, cudaStream_t st) {
-    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8, INT8 ? kUnroll / 2 : kUnroll);
+    constexpr int EP = INT8 ? 16 : 8;
+    const int grid = grid_for(p, b.n_rows, EP, kLoads * kPer16<T> / EP);
     echo::launch_chained(p.d == 64 ? kv_write_kernel<T, INT8, 64> : kv_write_kernel<T, INT8, 128>,
                          dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
                          static_cast<const T *>(k), static_cast<const T *>(v), ld,
@@ -194,7 +206,7 @@ void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, 
 template <typename T, bool INT8>
 void launch_read(const echo_kv_pool &p, const echo_kv_batch &b, void *k, void *v, int64_t ld,
                  cudaStream_t st) {
-    const int grid = grid_for(p, b.n_rows, INT8 ? 16 : 8, kUnroll);
+    const int grid = grid_for(p, b.n_rows, kPer16<T>, !INT8 && sizeof(T) == 2 ? kLoads : 2 * kLoads);
     echo::launch_chained(p.d == 64 ? kv_read_kernel<T, INT8, 64> : kv_read_kernel<T, INT8, 128>,
                          dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
                          static_cast<T *>(k), static_cast<T *>(v), ld, echo::device_error_ptr());
