@@ -409,3 +409,118 @@ class CachedStack:
                 hy.copy_(self._yd[b], non_blocking=True)
                 ev["y_copied"][b].record(self._d2h)
         comp.wait_event(ev["y_copied"][(len(host_x) - 1) % 2])
+
+
+class PageTable:
+    """Host bookkeeping of a pool of key/value pages that clips share: which pages are free,
+    which a clip has, in order.  The same numbers serve the pools of every layer."""
+
+    def __init__(self, n_pages: int, page_tokens: int):
+        self.n_pages, self.page_tokens = n_pages, page_tokens
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.pages: dict[int, list[int]] = {}
+        self.lens: dict[int, int] = {}
+
+    def open(self, clip: int):
+        if clip in self.lens:
+            raise ValueError(f"clip {clip} is open already")
+        self.pages[clip], self.lens[clip] = [], 0
+
+    def close(self, clip: int):
+        """Give the clip's pages back.  Work already enqueued may still read them: whoever
+        gets them next writes them on the same stream."""
+        del self.lens[clip]
+        self.free.extend(reversed(self.pages.pop(clip)))
+
+    def extend(self, rows: dict[int, int]):
+        """Room for rows[clip] more tokens of each clip; all of them or none."""
+        need = {c: -(-(self.lens[c] + n) // self.page_tokens) - len(self.pages[c])
+                for c, n in rows.items()}
+        if sum(need.values()) > len(self.free):
+            raise MemoryError(f"{sum(need.values())} pages needed, {len(self.free)} free")
+        for c, n in rows.items():
+            self.pages[c].extend(self.free.pop() for _ in range(need[c]))
+            self.lens[c] += n
+
+    def batch(self, rows: dict[int, int], device="cuda") -> ec.KVBatch:
+        """The clips of one call with their new rows (rows[clip] each, in the dict's order),
+        copied to the device."""
+        clips = list(rows)
+        width = max([len(self.pages[c]) for c in clips] + [1])
+        host = [self.pages[c] + [-1] * (width - len(self.pages[c])) for c in clips]
+        row0 = [0]
+        for n in rows.values():
+            row0.append(row0[-1] + n)
+        flat = torch.tensor([p for h in host for p in h] + [self.lens[c] for c in clips] + row0,
+                            dtype=torch.int32).pin_memory().to(device, non_blocking=True)
+        B = len(clips)
+        return ec.KVBatch(flat[:B * width].view(B, width), flat[B * width:B * width + B],
+                          flat[B * width + B:], row0[-1], max(rows.values(), default=0))
+
+
+class ChunkStream:
+    """Blocks run chunk by chunk over several clips at once, each clip's earlier keys and
+    values in pages of one pool per layer.
+
+    step({clip: x}) takes the new latent tokens of each clip (any number of frames, or a
+    single token), appends their keys and values to the clip's pages, and returns the last
+    layer's outputs.  Self-attention is causal frame by frame (frame_tokens = 1: token by
+    token): a token sees its own frame and all earlier ones.  The audio condition of a clip,
+    of any length, is written into pages of its own when the clip is opened, and the
+    cross-attention reads it from there.  The block is that of echo_block_step on these rows:
+      h1 = x + MHA(LN(x)) Wo + bo,  h2 = h1 + MHA(LN(h1) Wqc; audio) Woc + boc,
+      y = h2 + GELU(LN(h2) W1 + b1) W2 + b2.
+    kind: ec.CACHE_BF16 or ec.CACHE_INT8 pages."""
+
+    def __init__(self, blocks: list, H: int, d: int, frame_tokens: int, n_pages: int,
+                 cond_pages: int, page_tokens: int = 64, kind: int = ec.CACHE_INT8, device="cuda"):
+        self.blocks, self.H, self.d, self.frame_tokens = blocks, H, d, frame_tokens
+        self.device = torch.device(device)
+        pool = lambda n: [ec.KVPool.empty(kind, n, page_tokens, H, d, device) for _ in blocks]
+        self.self_pools, self.cond_pools = pool(n_pages), pool(cond_pages)
+        self.self_table = PageTable(n_pages, page_tokens)
+        self.cond_table = PageTable(cond_pages, page_tokens)
+
+    def open(self, clip: int, cond_kv: list):
+        """A new clip with its audio condition: per layer the keys and values bf16 [Lc, 2 D]
+        of echo_precompute_cross_kv."""
+        Lc, D = cond_kv[0].shape[0], self.H * self.d
+        self.cond_table.open(clip)
+        try:
+            self.cond_table.extend({clip: Lc})
+        except MemoryError:
+            self.cond_table.close(clip)
+            raise
+        self.self_table.open(clip)
+        batch = self.cond_table.batch({clip: Lc}, self.device)
+        for pool, kv in zip(self.cond_pools, cond_kv):
+            ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
+
+    def close(self, clip: int):
+        self.self_table.close(clip)
+        self.cond_table.close(clip)
+
+    def step(self, chunks: dict[int, torch.Tensor]) -> dict[int, torch.Tensor]:
+        """chunks: bf16 [n, D] per clip; returns bf16 [n, D] per clip."""
+        rows = {c: x.shape[0] for c, x in chunks.items()}
+        if any(c not in self.self_table.lens for c in rows):
+            raise ValueError("a clip is not open")
+        D = self.H * self.d
+        x = torch.cat(list(chunks.values())) if len(chunks) > 1 else next(iter(chunks.values()))
+        self.self_table.extend(rows)
+        batch = self.self_table.batch(rows, self.device)
+        cond = self.cond_table.batch(rows, self.device)   # the same rows, over the audio's pages
+        for blk, pool, cond_pool in zip(self.blocks, self.self_pools, self.cond_pools):
+            w = blk.tensors
+            n1 = ec.echo_layernorm(x)
+            kv = ec.echo_linear(n1, w["Wkv"], w["bkv"])
+            ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
+            a = ec.echo_kv_attention(pool, batch, ec.echo_linear(n1, w["Wq"], w["bq"]),
+                                     causal_block=self.frame_tokens)
+            h1 = ec.echo_linear(a, w["Wo"], w["bo"], resid=x, out_dtype=torch.float32)
+            q = ec.echo_linear(ec.echo_layernorm(h1), w["Wqc"], w["bqc"])
+            a = ec.echo_kv_attention(cond_pool, cond, q)
+            h2 = ec.echo_linear(a, w["Woc"], w["boc"], resid=h1, out_dtype=torch.float32)
+            u = ec.echo_linear(ec.echo_layernorm(h2), w["W1"], w["b1"], act=1)
+            x = ec.echo_linear(u, w["W2"], w["b2"], resid=h2)
+        return dict(zip(rows, x.split(list(rows.values()))))
