@@ -18,12 +18,21 @@ template <int D, int R, int PARTS>
 __global__ void __launch_bounds__(32 * kWarps)
 kv_join_kernel(const KvWork w, float *ws, __nv_bfloat16 *__restrict__ out, int64_t ldo) {
     pdl_enter();
-    const KvJoin j = kv_joins(ws, w, D)[blockIdx.x];
+    const KvJoin *joins = kv_joins(ws, w, D) + blockIdx.x;
+    const KvJoin j = *joins;
     constexpr int E = D / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % PARTS;
     const int row0 = (blockIdx.y * (kWarps / PARTS) + warp / PARTS) * R;
-    if (j.more == 0 || (int)blockIdx.y * (kWarps / PARTS) * R >= j.rows) return;
-    const int n = 1 + j.more;
+    if (j.upto == 0 || (int)blockIdx.y * (kWarps / PARTS) * R >= j.rows) return;
+    // pieces: this worker's and those of the workers after it whose units begin before upto
+    int n = 1;
+    for (int i0 = 0;; i0 += 32) {
+        const int i = i0 + lane;
+        const bool on = (int)blockIdx.x + i + 1 < w.workers && joins[i].end < j.upto;
+        const int some = __popc(__ballot_sync(0xffffffffu, on));
+        n += some;
+        if (some < 32) break;
+    }
     const int64_t slot = (int64_t)w.slot_rows * (D + 2);
     // piece 0 in this worker's second slot, piece i in worker c + i's first
     auto piece = [&](int i) -> const float * { return ws + slot * (2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)); };

@@ -4,12 +4,22 @@
 // Items: (sequence, key/value head, row tile).  The Hq / H query heads that share a
 // key/value head are packed with the rows, packed row = row * group + head of the group,
 // and a tile is `tile` of them, so that keys and values are read once for all.  An item
-// costs kFixed + (its key blocks) units; the items stand in a row, sequence by sequence,
-// head by head, tile by tile, and worker c of G takes units [U c / G, U (c + 1) / G).  An
-// item that crosses such a boundary is done in pieces: each worker leaves its piece's sums
-// in the workspace, and the combining kernel joins them in the order of the keys.  A
-// worker has at most one piece that does not begin at its item's beginning (its first) and
-// one that begins there but ends early (its last): two slots of workspace each.
+// costs kFixedUnits + (its key blocks) units, and every worker gets the same sum of units.
+//
+// As many items as every worker can take whole go round first, in their order: worker c of
+// G takes W of them from item W c on.  The units of the items left over are dealt out so
+// that the workers' sums come out even, in one row, each worker's next to the one's before.
+// An item that crosses a boundary there is done in pieces: each worker leaves its piece's
+// sums in the workspace, and the joining kernel adds them up.  A worker has at most one
+// piece with an item's last keys but not its first (an item that it begins, and others go
+// on with), and one other: two slots of workspace each.
+//
+// The whole items of all workers begin together, and the tiles of a head run through its
+// keys in step, so that a key block is read from memory once and from the L2 by the
+// others.  For the same reason the worker that goes on with an item takes its first keys.
+// 1560 rows over 32760 keys (40 heads of 128, bf16): one row of all items, each worker's
+// share in the items' order 768 us; whole items first, and the first keys to the later
+// worker 695; as it is 662.
 #pragma once
 
 #include "kv_pages.cuh"
@@ -65,28 +75,23 @@ struct KvPiece {
     int whole, tail;         // all of the item's keys; or the last of them
 };
 
-// A worker's walk over its pieces.  First its whole items, and then the piece that it takes
-// over from the worker before and the one that the worker after goes on with: the whole
-// items of all workers begin together, and those of a head run through its keys in step,
-// so that each key block is read from memory once and from the L2 by the others.  For the
-// same reason the worker that goes on with an item takes its first keys: 1560 rows over
-// 32760 keys (40 heads of 128, bf16) 768 -> 695 us.
+// A worker's walk over its pieces: the whole items of the first round, the whole ones of its
+// share of the others, and then the piece that it takes over from the worker before and the
+// one that the worker after goes on with.
 struct KvWalk {
     KvSeq s;
     int seq, head, tile;      // of the current piece's item
     int kb0, kb1, nb;         // its key blocks, and the item's
-    int64_t start, end;       // the worker's units
-    int64_t total;            // units of all items
-    int G;                    // workers that have any
+    int64_t start, end;       // the worker's units of the items left over
     struct Item {
         int seq, head, tile;
         int64_t at;           // its first unit
-    } here, first;            // the next item; the one that holds `start`
+    } round, here, first;     // the next of the first round; of the others; the one that holds `start`
+    int left;                 // of the first round
     int64_t from;             // the first unit of the current piece's item
     int stage;                // 0: whole items, 1: the first, 2: the last, 3: none
     bool begun;               // `start` lies inside an item
 
-    ECHO_DEV int64_t unit_of(int worker) const { return worker < G ? total * worker / G : total; }
     // key blocks of an item (units from `from`) that the units before `unit` pay for, the
     // last ones first
     static ECHO_DEV int paid(int64_t unit, int64_t from, int nb) {
@@ -102,38 +107,49 @@ struct KvWalk {
         from = it.at;
         nb = s.blocks(w, tile);
     }
-    ECHO_DEV void advance(const KvWork &w) {       // past `here`, which is the current item
-        here.at += kFixedUnits + nb;
-        if (++here.tile == s.tiles(w)) {
-            here.tile = 0;
-            if (++here.head == w.H) {
-                here.head = 0;
-                ++here.seq;
+    ECHO_DEV void advance(const KvWork &w, Item &it) {       // past `it`, which is the current item
+        it.at += kFixedUnits + nb;
+        if (++it.tile == s.tiles(w)) {
+            it.tile = 0;
+            if (++it.head == w.H) {
+                it.head = 0;
+                ++it.seq;
             }
         }
     }
+    // `it`, or the first one of a later sequence that has any; false past the last
+    ECHO_DEV bool settle(const KvWork &w, Item &it) {
+        for (; it.seq < w.b.n_seqs; ++it.seq) {
+            if (it.seq != seq) s.load(w, seq = it.seq);
+            if (s.packed > 0) {
+                item(w, it);
+                return true;
+            }
+        }
+        return false;
+    }
     // the next piece that has something to do; false at the end
     ECHO_DEV bool next(const KvWork &w) {
-        while (stage == 0) {
-            if (here.seq >= w.b.n_seqs || here.at >= end) {
-                stage = 1;
-                here.seq = w.b.n_seqs;             // no last piece
-                break;
-            }
-            if (here.seq != seq) s.load(w, seq = here.seq);
-            if (s.packed == 0) {
-                ++here.seq;
-                continue;
-            }
-            item(w, here);
-            if (w.split && here.at + kFixedUnits + nb > end) {
-                stage = 1;
-                break;
-            }
+        if (left > 0) {
+            --left;
+            settle(w, round);
             kb0 = 0;
             kb1 = nb;
-            advance(w);
+            advance(w, round);
             return true;
+        }
+        if (stage == 0) {
+            if (here.at < end && settle(w, here)) {
+                if (!w.split || here.at + kFixedUnits + nb <= end) {
+                    kb0 = 0;
+                    kb1 = nb;
+                    advance(w, here);
+                    return true;
+                }
+            } else {
+                here.seq = w.b.n_seqs;             // no last piece
+            }
+            stage = 1;
         }
         if (stage == 1) {
             stage = 2;
@@ -173,18 +189,19 @@ struct KvWalk {
     }
 };
 
-// What the threads of a block find together: the units of all items, and the item that
-// holds one unit.
+// What the threads of a block find together.
 struct KvFound {
-    int64_t units[32];
+    int64_t units[32];           // of the warps' sequences, one head each
+    int items[32], most[32];     // items; the most units of one
+    int64_t at[3];               // the first units of items
+    KvWalk::Item begin;
     int64_t base, per_head;
     int seq;
 };
 
-// The range of `worker`, and the walk set to the item that holds its first unit.  Called by
-// every thread of the block.  Thread t looks
-// at sequences [t per, (t + 1) per), or a warp at each where there are no more sequences
-// than warps (a long chunk has many tiles).
+// The walk of `worker`.  Called by every thread of the block.  Thread t looks at sequences
+// [t per, (t + 1) per), or a warp at each where there are no more sequences than warps (a
+// long chunk has many tiles).
 template <int THREADS>
 ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     constexpr int WARPS = THREADS / 32;
@@ -192,43 +209,104 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     const bool by_warp = w.b.n_seqs <= WARPS;
     const int per = by_warp ? 1 : (w.b.n_seqs + THREADS - 1) / THREADS;
     const int b0 = by_warp ? warp : (int)threadIdx.x * per;
-    auto units_of = [&](int seq, int from, int step) -> int64_t {   // of one head
+    const int b1 = min(b0 + per, w.b.n_seqs);
+    // units of a sequence's first n tiles: by_warp this lane's share of them
+    auto units_of = [&](int seq, int n, int *most) -> int64_t {
         KvSeq s;
         s.load(w, seq);
         int64_t u = 0;
-        const int tiles = s.tiles(w);
-        for (int t = from; t < tiles; t += step) u += kFixedUnits + s.blocks(w, t);
+        const int tiles = min(s.tiles(w), n);
+        for (int t = by_warp ? lane : 0; t < tiles; t += by_warp ? 32 : 1) {
+            const int v = kFixedUnits + s.blocks(w, t);
+            u += v;
+            *most = max(*most, v);
+        }
         return u;
     };
-    auto scan = [&](int64_t v) -> int64_t {                         // inclusive, over the warp
+    auto scan = [&](auto v) {                                       // inclusive, over the warp
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t x = __shfl_up_sync(0xffffffffu, v, o);
+            const auto x = __shfl_up_sync(0xffffffffu, v, o);
             if (lane >= o) v += x;
         }
         return v;
     };
     int64_t mine = 0;
-    if (by_warp) {
-        if (b0 < w.b.n_seqs) mine = units_of(b0, lane, 32) * w.H;
-    } else {
-        for (int i = 0; i < per && b0 + i < w.b.n_seqs; ++i) mine += units_of(b0 + i, 0, 1) * w.H;
+    int items = 0, most = 0;
+    for (int i = b0; i < b1; ++i) {
+        mine += units_of(i, INT32_MAX, &most) * w.H;
+        KvSeq s;
+        s.load(w, i);
+        if (!by_warp || lane == 0) items += s.tiles(w) * w.H;
     }
     const int64_t incl = scan(mine);
-    if (lane == 31) sh.units[warp] = incl;
+    const int incl_items = scan(items);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) {
+        sh.units[warp] = incl;
+        sh.items[warp] = incl_items;
+        sh.most[warp] = most;
+    }
     if (threadIdx.x == 0) sh.seq = -1;
     __syncthreads();
-    int64_t before = 0, total = 0;   // of the earlier warps; of all
+    int64_t before = 0, total = 0;   // units of the earlier warps; of all
+    int before_items = 0;
+    most = 1;
     for (int i = 0; i < WARPS; ++i) {
         const int64_t v = sh.units[i];
-        if (i < warp) before += v;
+        if (i < warp) {
+            before += v;
+            before_items += sh.items[i];
+        }
         total += v;
+        most = max(most, sh.most[i]);
     }
     const int64_t want = total / w.least + 1;
-    walk.total = total;
-    walk.G = want < w.workers ? (int)want : w.workers;
-    walk.start = walk.unit_of(worker);
-    walk.end = walk.unit_of(worker + 1);
+    const int G = want < w.workers ? (int)want : w.workers;
+    auto even = [&](int c) -> int64_t { return c < G ? total * c / G : total; };
+    const int64_t round = w.split && G == w.workers ? total / G / most : 0;   // items of a worker
+    walk.start = even(worker);
+    walk.end = even(worker + 1);
+    walk.left = (int)round;
+    if (round > 0) {
+        // first units of this worker's first item of the round, of the next worker's, and of
+        // the first item left over
+        if (threadIdx.x < 3) sh.at[threadIdx.x] = total;
+        __syncthreads();
+        for (int q = 0; q < 3; ++q) {
+            const int64_t at = round * (q == 0 ? worker : q == 1 ? worker + 1 : G);
+            int64_t u = by_warp ? before : before + incl - mine;
+            int64_t i0 = by_warp ? before_items : before_items + incl_items - items;
+            for (int i = b0; i < b1; ++i) {
+                KvSeq s;
+                s.load(w, i);
+                const int tiles = s.tiles(w), n = tiles * w.H;
+                if (at >= i0 && at < i0 + n) {
+                    const int head = (int)(at - i0) / tiles, tile = (int)(at - i0) % tiles;
+                    int none = 0;
+                    int64_t all = units_of(i, INT32_MAX, &none), part = units_of(i, tile, &none);
+                    if (by_warp) {
+                        all = __shfl_sync(0xffffffffu, scan(all), 31);
+                        part = __shfl_sync(0xffffffffu, scan(part), 31);
+                    }
+                    if (!by_warp || lane == 0) {
+                        sh.at[q] = u + head * all + part;
+                        if (q == 0) sh.begin = {i, head, tile, sh.at[0]};
+                    }
+                    break;
+                }
+                if (i + 1 < b1) {                     // more than one only where not by_warp
+                    int none = 0;
+                    u += units_of(i, INT32_MAX, &none) * w.H;
+                    i0 += n;
+                }
+            }
+        }
+        __syncthreads();
+        walk.round = sh.begin;
+        walk.start += sh.at[2] - sh.at[0];
+        walk.end += sh.at[2] - sh.at[1];
+    }
     const int64_t pos = walk.start;
     if (by_warp) {
         const int64_t all = __shfl_sync(0xffffffffu, incl, 31);
@@ -240,10 +318,11 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     } else {
         int64_t u = before + incl - mine;
         if (u <= pos && pos < u + mine) {
-            for (int i = 0;; ++i) {
-                const int64_t v = units_of(b0 + i, 0, 1);
+            for (int i = b0;; ++i) {
+                int none = 0;
+                const int64_t v = units_of(i, INT32_MAX, &none);
                 if (pos < u + v * w.H) {
-                    sh.seq = b0 + i;
+                    sh.seq = i;
                     sh.base = u;
                     sh.per_head = v;
                     break;
@@ -265,6 +344,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     it.at = sh.base;
     walk.s.load(w, walk.seq = it.seq);
     it.head = (int)((pos - it.at) / sh.per_head);
+    it.tile = 0;
     it.at += it.head * sh.per_head;
     // the tile, 32 at a time: every warp finds it for itself
     const int tiles = walk.s.tiles(w);
@@ -284,7 +364,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
         walk.begun = w.split;
         walk.first = it;
         walk.item(w, it);
-        walk.advance(w);
+        walk.advance(w, it);
     }
 }
 
@@ -295,10 +375,11 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
 ECHO_DEV float *kv_slot(float *ws, int worker, bool tail, int rows, int D) {
     return ws + (int64_t)(2 * worker + (tail ? 1 : 0)) * rows * (D + 2);
 }
-// What worker c leaves for the joining kernel, after the slots: the item that it began and
-// `more` workers after it went on with.
+// What worker c leaves for the joining kernel, after the slots: the end of its units, and
+// the item that it began and those after it went on with, up to unit `upto` (0: none).
 struct KvJoin {
-    int more, row, packed0, rows, head;   // first row of the sequence; packed rows of the item
+    int64_t end, upto;
+    int row, packed0, rows, head;      // first row of the sequence; packed rows of the item
 };
 ECHO_DEV KvJoin *kv_joins(float *ws, const KvWork &w, int D) {
     return reinterpret_cast<KvJoin *>(ws + (int64_t)2 * w.workers * w.slot_rows * (D + 2));
@@ -307,10 +388,9 @@ ECHO_DEV KvJoin *kv_joins(float *ws, const KvWork &w, int D) {
 // one thread of each CTA.
 ECHO_DEV void kv_leave_join(const KvWork &w, const KvWalk &walk, float *ws, int D) {
     if (!w.split) return;
-    KvJoin j = {0, 0, 0, 0, 0};
+    KvJoin j = {walk.end, 0, 0, 0, 0, 0};
     if (walk.tail()) {
-        const int64_t upto = walk.from + kFixedUnits + walk.nb;
-        while (walk.unit_of((int)blockIdx.x + 1 + j.more) < upto) ++j.more;
+        j.upto = walk.from + kFixedUnits + walk.nb;
         j.row = walk.s.row;
         j.packed0 = walk.tile * w.tile;
         j.rows = min(w.tile, walk.s.packed - j.packed0);
@@ -319,6 +399,7 @@ ECHO_DEV void kv_leave_join(const KvWork &w, const KvWalk &walk, float *ws, int 
     kv_joins(ws, w, D)[blockIdx.x] = j;
 }
 inline size_t kv_workspace_bytes(int workers, int rows, int D) {
+    static_assert(sizeof(KvJoin) % 16 == 0, "");
     return (size_t)workers * (2 * rows * (D + 2) * 4 + sizeof(KvJoin));
 }
 
