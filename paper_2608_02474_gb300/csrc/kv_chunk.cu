@@ -11,7 +11,7 @@
 //   four warps  int8: codes to bf16, a key per thread: the copy leaves a row of codes where
 //               the second half of the row's bf16 values goes, so that each thread
 //               overwrites only its own.  bf16: clear values that no row may use (below);
-//   eight warps softmax of the two tiles, a row per thread: the running maximum comes from
+//   eight warps softmax of the two tiles: a row's running maximum comes from
 //               the piece's first block and moves only when a block's weights sum to more
 //               than 2^64 (exact after the division by the row sum).
 // A row's weights are 0 where it does not see the key, but 0 times a value that is not
@@ -48,9 +48,11 @@ struct Cfg {
     static constexpr int RING = D == 128 ? 5 : 6;
     static constexpr int TILES_BYTES = TILES * Q_BYTES + RING * SLOT;
     // registers of warps 0-3, of four helpers and of four softmax warps: together at most
-    // what the launch gives.  4864 rows over 32768 keys, 8 heads of 128: bf16
-    // 350 us (64, 32, 208: 355; 80, 32, 200: 357), int8 512 us (72, 56, 192: 519)
-    static constexpr int REGS[3] = {INT8 ? 56 : 72, INT8 ? 56 : 24, INT8 ? 200 : 208};
+    // what the launch gives; the splits that were fastest.  4864 rows over 32768
+    // keys, 8 heads of 128: bf16 352 us (96, 48, 184: 352); 8192 keys, heads of 64: bf16 80
+    // (72, 24, 208: 87); int8 451 (80, 80, 176: 471)
+    static constexpr int REGS[3] = {INT8 ? 56 : D == 64 ? 96 : 72, INT8 ? 56 : D == 64 ? 48 : 24,
+                                    INT8 ? 200 : D == 64 ? 184 : 208};
     static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
                   "setmaxnreg takes from the launch's registers");
     static constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
@@ -172,6 +174,19 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             bool tail = false;
             for (bool more = true; more; ++n) {
                 more = walk.next(p.work);
+                // Items that see no key become zeros here: the other warps get pieces with
+                // blocks only.  (They look one piece ahead, and a row of empty ones longer
+                // than the pieces handed out would keep each waiting for the other.)
+                while (more && walk.kb0 == walk.kb1) {
+                    const int first = walk.tile * p.work.tile, rows = min(p.work.tile, walk.s.packed - first);
+                    for (int i = lane; i < rows * (D / 8); i += 32) {
+                        const int pr = first + i / (D / 8);
+                        *reinterpret_cast<uint4 *>(p.out + (int64_t)(walk.s.row + pr / p.work.group) * p.ldo +
+                                                   (walk.head * p.work.group + pr % p.work.group) * D + i % (D / 8) * 8) =
+                            make_uint4(0, 0, 0, 0);
+                    }
+                    more = walk.next(p.work);
+                }
                 if (n >= PIECES && !wait_all(&sh.piece_empty[n % PIECES], ((n / PIECES) & 1) ^ 1)) break;
                 KvPiece &pc = sh.piece[n % PIECES];
                 if (lane == 0) {
@@ -187,7 +202,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     mbar_arrive(&sh.piece_full[n % PIECES]);
                 }
                 __syncwarp();
-                if (!more || walk.kb0 == walk.kb1) continue;
+                if (!more) continue;
                 // the queries' buffer is free once the last S of the piece before is done
                 if (loads > 0 && !wait_all(&sh.q_empty, (loads - 1) & 1)) break;
                 if (lane == 0) {
@@ -221,7 +236,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     echo_flag_error(p.err, ECHO_ERR_PAGE);
                     return 0;
                 };
-                if (kb0 == kb1) continue;
                 // 32 pages in the lanes, the next 32 on their way
                 int c0 = kb0 * per_block;
                 int now = page_of(c0 + lane), then = page_of(c0 + 32 + lane);
@@ -322,19 +336,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             auto uniform = [&](int v) -> int { return (int)__ballot_sync(0xffffffffu, (v >> lane) & 1); };
             int n = 0;                                        // pieces taken
             int blocks = 0, clear = 0;                        // of the piece that is there
-            // the next piece that has blocks; none: blocks 0
+            // the next piece; none: blocks 0
             auto next_piece = [&]() {
-                for (blocks = 0; ok && blocks == 0; ++n) {
-                    const KvPiece &pc = piece(n, ok);
-                    if (!ok) return;
-                    blocks = uniform(pc.blocks);
-                    clear = uniform(kv_clear(pc));
-                    if (blocks < 0) {
-                        blocks = 0;
-                        return;
-                    }
-                    piece_done(n);
-                }
+                const KvPiece &pc = piece(n, ok);
+                blocks = 0;
+                if (!ok) return;
+                blocks = max(uniform(pc.blocks), 0);
+                clear = uniform(kv_clear(pc));
+                if (blocks > 0) piece_done(n++);
             };
             auto next2 = [](int s) { return s + 2 >= RING ? s + 2 - RING : s + 2; };
             int vs = 1, ks = 2;                               // slots of V_f and K_{f+1}
@@ -570,7 +579,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         const uint32_t o_at = tmem + lane_base + O_COL + (uint32_t)(t * D);
         const int row = quad * 32 + lane;                     // of the tile
         bool ok = true;
-        int f = 0, with_blocks = 0, edge = 0;
+        int f = 0, edge = 0;
         for (int n = 0; ok; ++n) {
             const KvPiece &pc = piece(n, ok);
             if (!ok || pc.blocks < 0) break;
@@ -585,7 +594,31 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             const int warp_low = __reduce_min_sync(0xffffffffu, lim);
             const int kb0 = pc.kb0, blocks = pc.blocks, clear = kv_clear(pc);
-            float m = -FLT_MAX, l = 0.f;
+            // Rows of a lane: its own, a whole row of S per thread.  int8: rows gq + 8 x of the
+            // warp's 32, every fourth pair of columns, as the fragments of a product lie, so
+            // that a lane needs only a quarter of the scales (a whole row per thread loads all
+            // 256 of a block: 487 against XXX us, 4864 rows over 32768 keys, 8 heads of 128)
+            constexpr int NX = INT8 ? 4 : 1;
+            const int gq = lane >> 2, tq = lane & 3;
+            float m[NX], l[NX];
+            int seen[NX];                                     // keys that the rows see
+#pragma unroll
+            for (int x = 0; x < NX; ++x) {
+                m[x] = -FLT_MAX;
+                l[x] = 0.f;
+                seen[x] = INT8 ? __shfl_sync(0xffffffffu, lim, gq + 8 * x) : lim;
+            }
+            // the value of this thread's own row
+            auto own = [&](const float *v) -> float {
+                if constexpr (!INT8) return v[0];
+                float r = 0.f;
+#pragma unroll
+                for (int x = 0; x < NX; ++x) {
+                    const float y = __shfl_sync(0xffffffffu, v[x], (lane & 7) * 4);
+                    if (lane >> 3 == x) r = y;
+                }
+                return r;
+            };
             for (int j = 0; j < blocks; ++j, ++f) {
                 ok = wait_all(&sh.s_full[t], f & 1);
                 if (!ok) break;
@@ -595,97 +628,130 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     ok = wait_all(&sh.sc_full[f & 1], (f >> 1) & 1);
                     if (!ok) break;
                 }
-                const float4 *ksc = reinterpret_cast<const float4 *>(sh.scales[INT8 ? f & 1 : 0][0]);
-                const float4 *vsc = reinterpret_cast<const float4 *>(sh.scales[INT8 ? f & 1 : 0][1]);
                 const bool edge_block = key0 + BN > warp_low;
-                // the row's scores of 32 keys at a time, the next ones on their way
+                // the scores of 32 keys at a time, the next ones on their way
                 float sv[2][32];
+                auto load32 = [&](int c) {
+                    uint32_t *to = reinterpret_cast<uint32_t *>(sv[c & 1]);
+                    if constexpr (INT8) {
+                        tmem_ld_frag32(s_at + 32 * c, to);
+                        tmem_ld_frag32(s_at + 32 * c + (16u << 16), to + 16);
+                    } else {
+                        tmem_ld32(s_at + 32 * c, to);
+                    }
+                };
                 auto each32 = [&](auto f32) {
-                    tmem_ld32(s_at, reinterpret_cast<uint32_t *>(sv[0]));
+                    load32(0);
 #pragma unroll
                     for (int c = 0; c < BN / 32; ++c) {
                         tmem_ld_wait();
-                        if (c + 1 < BN / 32)
-                            tmem_ld32(s_at + 32 * (c + 1), reinterpret_cast<uint32_t *>(sv[(c + 1) & 1]));
+                        if (c + 1 < BN / 32) load32(c + 1);
                         f32(c, sv[c & 1]);
                     }
                 };
+                // pair i of the 32 keys' in v[2 i], v[2 i + 1]: whose row, and its first key;
+                // the scales of keys 2 k and 2 k + 1 of the block
+                auto row_of = [](int i) { return INT8 ? 2 * (i >> 3) + (i & 1) : 0; };
+                auto key_of = [&](int i) { return INT8 ? 8 * ((i >> 1) & 3) + 2 * tq : 2 * i; };
+                auto scale2 = [&](int kv, int key) -> uint64_t {
+                    const float2 s2 = *reinterpret_cast<const float2 *>(&sh.scales[INT8 ? f & 1 : 0][kv][key]);
+                    return f2_pack(s2.x, s2.y);
+                };
+                const uint64_t unit2 = f2_pack(p.scale_log2, p.scale_log2);
                 // -inf where the row does not see the key.  int8: after the keys' scales, which
                 // may be 0 (elsewhere they are part of the exponent's product)
                 auto mask32 = [&](int c, float *v) {
-                    if constexpr (INT8) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 k4 = ksc[8 * c + i];
-                            f2_unpack(f2_mul(f2_pack(v[4 * i], v[4 * i + 1]), f2_pack(k4.x, k4.y)), v[4 * i], v[4 * i + 1]);
-                            f2_unpack(f2_mul(f2_pack(v[4 * i + 2], v[4 * i + 3]), f2_pack(k4.z, k4.w)), v[4 * i + 2], v[4 * i + 3]);
+                    for (int i = 0; i < 16; ++i) {
+                        if constexpr (INT8)
+                            f2_unpack(f2_mul(f2_pack(v[2 * i], v[2 * i + 1]), scale2(0, 32 * c + key_of(i))), v[2 * i], v[2 * i + 1]);
+                        if (edge_block) {
+                            const int k = key0 + 32 * c + key_of(i);
+                            if (k >= seen[row_of(i)]) v[2 * i] = -INFINITY;
+                            if (k + 1 >= seen[row_of(i)]) v[2 * i + 1] = -INFINITY;
                         }
                     }
-                    if (edge_block) {
-                        const int seen = lim - key0 - 32 * c;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i >= seen) v[i] = -INFINITY;
-                    }
                 };
-                // the row's largest score of the block, in the exponent of two
-                auto row_max = [&]() -> float {
-                    float m2[2] = {-INFINITY, -INFINITY};
+                // the rows' largest scores of the block, in the exponent of two
+                auto row_max = [&](float *mx) {
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) mx[x] = -INFINITY;
                     each32([&](int c, float *v) {
                         mask32(c, v);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            m2[0] = fmax3(m2[0], v[i], v[i + 1]);
-                            m2[1] = fmax3(m2[1], v[i + 2], v[i + 3]);
-                        }
+                        for (int i = 0; i < 16; ++i) mx[row_of(i)] = fmax3(mx[row_of(i)], v[2 * i], v[2 * i + 1]);
                     });
-                    return fmaxf(m2[0], m2[1]) * (INT8 ? 1.f : p.scale_log2);
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) {
+                        if constexpr (INT8) {
+                            mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], 1));
+                            mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], 2));
+                        } else {
+                            mx[x] *= p.scale_log2;
+                        }
+                    }
                 };
-                // P = 2^(s - m) on fp32 pairs, times the values' scales, in bf16 pairs;
-                // returns the row's sum of 2^(s - m)
+                // P = 2^(s - m) on fp32 pairs, times the values' scales, in bf16 pairs; this
+                // lane's part of the rows' sums of 2^(s - m); whether one is above 2^64 or NaN
                 uint32_t pk[BN / 2];
-                auto exp_pass = [&](auto EDGE) -> float {
-                    const uint64_t negm2 = f2_pack(-m, -m);
-                    uint64_t acc2[4] = {0ull, 0ull, 0ull, 0ull};
+                float bsum[NX];
+                auto exp_pass = [&](auto EDGE) -> bool {
+                    uint64_t negm2[NX], acc2[4];
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) negm2[x] = f2_pack(-m[x], -m[x]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) acc2[x] = 0ull;
                     each32([&](int c, float *v) {
                         if constexpr (EDGE) mask32(c, v);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float4 k4 = make_float4(p.scale_log2, p.scale_log2, p.scale_log2, p.scale_log2);
-                            [[maybe_unused]] float4 v4;
-                            if constexpr (INT8 && !EDGE) k4 = ksc[8 * c + i];
-                            if constexpr (INT8) v4 = vsc[8 * c + i];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint64_t s2 = f2_pack(v[4 * i + 2 * h], v[4 * i + 2 * h + 1]);
-                                float x0, x1;
-                                if constexpr (INT8 && EDGE) f2_unpack(f2_add(s2, negm2), x0, x1);
-                                else f2_unpack(f2_fma(s2, h ? f2_pack(k4.z, k4.w) : f2_pack(k4.x, k4.y), negm2), x0, x1);
-                                float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-                                acc2[2 * (i & 1) + h] = f2_add(acc2[2 * (i & 1) + h], f2_pack(p0, p1));
-                                if constexpr (INT8)
-                                    f2_unpack(f2_mul(f2_pack(p0, p1), h ? f2_pack(v4.z, v4.w) : f2_pack(v4.x, v4.y)), p0, p1);
-                                pk[16 * c + 2 * i + h] = pack_bf16(p0, p1);
+                        for (int i = 0; i < 16; ++i) {
+                            const uint64_t s2 = f2_pack(v[2 * i], v[2 * i + 1]);
+                            uint64_t k2 = unit2;
+                            if constexpr (INT8 && !EDGE) k2 = scale2(0, 32 * c + key_of(i));
+                            float x0, x1;
+                            if constexpr (INT8 && EDGE) f2_unpack(f2_add(s2, negm2[row_of(i)]), x0, x1);
+                            else f2_unpack(f2_fma(s2, k2, negm2[row_of(i)]), x0, x1);
+                            float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                            const int to = INT8 ? row_of(i) : i & 3;
+                            acc2[to] = f2_add(acc2[to], f2_pack(p0, p1));
+                            if constexpr (INT8) {
+                                f2_unpack(f2_mul(f2_pack(p0, p1), scale2(1, 32 * c + key_of(i))), p0, p1);
+                                pk[32 * (i >> 3) + 2 * (4 * c + ((i >> 1) & 3)) + (i & 1)] = pack_bf16(p0, p1);
+                            } else {
+                                pk[16 * c + i] = pack_bf16(p0, p1);
                             }
                         }
                     });
-                    float a0, a1;
-                    f2_unpack(f2_add(f2_add(acc2[0], acc2[1]), f2_add(acc2[2], acc2[3])), a0, a1);
-                    return a0 + a1;
+                    bool high = false;
+                    if constexpr (!INT8) acc2[0] = f2_add(f2_add(acc2[0], acc2[1]), f2_add(acc2[2], acc2[3]));
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) {
+                        float a0, a1;
+                        f2_unpack(acc2[x], a0, a1);
+                        bsum[x] = a0 + a1;
+                        high |= !(bsum[x] <= 1.8446744e19f);
+                    }
+                    return __any_sync(0xffffffffu, high);
                 };
+                float mx[NX];
                 // a first block that shows the row no key leaves the maximum at the lowest
                 // number: P is 0 there, and the first finite score overflows and brings its own
-                if (j == 0) m = fmaxf(row_max(), -FLT_MAX);
-                float bsum = edge_block ? exp_pass(std::true_type()) : exp_pass(std::false_type());
-                const bool redo = !(bsum <= 1.8446744e19f);     // > 2^64, inf or NaN
-                if (__any_sync(0xffffffffu, redo)) {
-                    const float m_new = fmaxf(m, row_max());
-                    float alpha = 1.f;
-                    if (redo) {
-                        alpha = ex2_approx(m - m_new);
-                        l *= alpha;
-                        m = m_new;
+                if (j == 0) {
+                    row_max(mx);
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) m[x] = fmaxf(mx[x], -FLT_MAX);
+                }
+                if (edge_block ? exp_pass(std::true_type()) : exp_pass(std::false_type())) {
+                    row_max(mx);
+                    float a[NX];
+#pragma unroll
+                    for (int x = 0; x < NX; ++x) {
+                        const float high = fmaxf(m[x], mx[x]);
+                        a[x] = ex2_approx(m[x] - high);
+                        l[x] *= a[x];
+                        m[x] = high;
                     }
+                    const float alpha = own(a);
                     if (j > 0) {   // S of this block completed after P V of the one before
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c) {
@@ -698,20 +764,27 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         }
                         tmem_st_wait();
                     }
-                    bsum = edge_block ? exp_pass(std::true_type()) : exp_pass(std::false_type());
+                    if (edge_block) exp_pass(std::true_type());
+                    else exp_pass(std::false_type());
                 }
-                l += bsum;
-                tmem_st32(s_at, pk);
-                tmem_st32(s_at + 32, pk + 32);
+#pragma unroll
+                for (int x = 0; x < NX; ++x) l[x] += bsum[x];
+                if constexpr (INT8) {
+                    tmem_st_frag64(s_at, pk);
+                    tmem_st_frag64(s_at + (16u << 16), pk + 32);
+                } else {
+                    tmem_st32(s_at, pk);
+                    tmem_st32(s_at + 32, pk + 32);
+                }
                 tmem_st_wait();
                 if (!INT8 && j >= clear) {                      // keys whose values are not finite
                     ok = wait_all(&sh.v_ok, edge & 1);
                     if (!ok) break;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int seen = lim - key0 - 32 * e;
-                        const uint32_t mask = seen >= 32 ? 0xffffffffu : seen > 0 ? (1u << seen) - 1u : 0u;
-                        if (sh.spoilt[edge % SPOILT][e] & mask) l = NAN;
+                        const int some = lim - key0 - 32 * e;
+                        const uint32_t mask = some >= 32 ? 0xffffffffu : some > 0 ? (1u << some) - 1u : 0u;
+                        if (sh.spoilt[edge % SPOILT][e] & mask) l[0] = NAN;
                     }
                     ++edge;
                 }
@@ -723,13 +796,19 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
             }
             if (!ok) break;
-            if (blocks > 0) {
-                ok = wait_all(&sh.pv_done[t], with_blocks++ & 1);
-                if (!ok) break;
-                tc_fence_after();
+            ok = wait_all(&sh.pv_done[t], n & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if constexpr (INT8) {
+#pragma unroll
+                for (int x = 0; x < NX; ++x) {
+                    l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+                    l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+                }
             }
             const bool whole = pc.whole;
-            const float inv = l == 0.f ? 0.f : 1.f / l;          // no key: zeros
+            const float m_row = own(m), l_row = own(l);
+            const float inv = l_row == 0.f ? 0.f : 1.f / l_row;  // no key: zeros
             __nv_bfloat16 *dst = nullptr;
             float *part = nullptr;
             if (real) {
@@ -739,19 +818,14 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int slot_row = t * p.tile_rows + row;
             if (!whole) {
                 part = kv_slot(p.ws, blockIdx.x, pc.tail, SLOT_ROWS, D);
-                if (real) *reinterpret_cast<float2 *>(part + SLOT_ROWS * D + 2 * slot_row) = make_float2(m, l);
+                if (real) *reinterpret_cast<float2 *>(part + SLOT_ROWS * D + 2 * slot_row) = make_float2(m_row, l_row);
                 part += (int64_t)slot_row * D;
             }
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
-                if (blocks > 0) {
-                    tmem_ld32(o_at + 32 * c, o);
-                    tmem_ld_wait();
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0u;
-                }
+                tmem_ld32(o_at + 32 * c, o);
+                tmem_ld_wait();
                 if (real && whole) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {

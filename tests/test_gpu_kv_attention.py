@@ -291,3 +291,14 @@ def test_not_finite_where_only_later_rows_see_it(ec, form, d, rows, cb, what, va
     if what == 1 or np.isnan(value):
         assert not np.isfinite(got[sees][:, [2 * d + 5, 3 * d + 5]]).any()
     assert ec.echo_get_device_error() == 0
+
+
+@FORMS
+@HEADS
+@pytest.mark.parametrize("group", [1, 40])
+def test_many_items_without_keys(ec, form, d, group):
+    """More of them in a row than a CTA hands out at once, before, between and after others."""
+    lens = [0] * 30 + [200] + [0] * 25 + [3, 400] + [0] * 17
+    rows = [3] * len(lens)
+    check(ec, kv_case.make(form, 16, 2, d, lens, rows, seed=23), group, 0)
+    check(ec, kv_case.make(form, 16, 2, d, lens, rows, seed=24), group, 2)
