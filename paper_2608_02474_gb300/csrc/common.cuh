@@ -148,19 +148,6 @@ ECHO_DEV bool mbar_try_wait(uint32_t bar_addr, uint32_t parity) {
     return ok != 0;
 }
 
-// Whether the phase of `parity` is complete, without waiting for it.
-ECHO_DEV bool mbar_test_wait(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
 // Bounded wait for the phase of `parity` to complete.  Gives up after
 // `limit_ns` or as soon as *abort is set by another role of the CTA; a timeout
 // sets *abort and the device flag ECHO_ERR_TIMEOUT.  Returns true on success.

@@ -6,7 +6,8 @@
 //   warp 0      copies key blocks page by page (K_0, V_0, K_1, V_1, ...) into a ring of
 //               shared-memory tiles (128-byte swizzle, 64-column boxes);
 //   warp 1      one elected lane issues S_t = Q_t K^T (TMEM) and O_t += P_t V (P from
-//               TMEM), in the order PV0_f S0_{f+1} PV1_f S1_{f+1}, across pieces too;
+//               TMEM), in the order PV0_f S0_{f+1} PV1_f S1_{f+1}, across pieces too; for
+//               heads of 64 S is half a block further ahead;
 //   warp 3      walks the pieces, hands them to the other warps, copies the queries;
 //   four warps  int8: codes to bf16, a key per thread: the copy leaves a row of codes where
 //               the second half of the row's bf16 values goes, so that each thread
@@ -30,7 +31,7 @@ namespace {
 
 constexpr int BM = 128, TILES = 2, BN = 128;
 constexpr int ATOM = 128 * 128;                 // 128 rows of 64 bf16
-constexpr uint32_t TMEM_COLS = 512, O_COL = 256;
+constexpr uint32_t TMEM_COLS = 512;
 constexpr int PIECES = 4;                       // handed out ahead
 constexpr int SLOT_ROWS = TILES * BM;
 constexpr int kWholeKeys = 768;                 // 64 bf16 rows, 8 heads of 128: whole 512 keys 16.5 us, divided 22
@@ -45,14 +46,18 @@ struct Cfg {
     static constexpr int Q_BYTES = ATOMS * ATOM;               // of a tile
     // int8 codes land at byte ATOM of their tile: for d 128 in its second half
     static constexpr int SLOT = INT8 && D == 64 ? ATOM + ATOM / 2 : ATOMS * ATOM;
-    static constexpr int RING = D == 128 ? 5 : 6;
-    static constexpr int TILES_BYTES = TILES * Q_BYTES + RING * SLOT;
+    static constexpr int RING = D == 128 ? 5 : 6;              // d 64: of three blocks, below
+    // tensor memory: S buffers of 128 columns, then O of both tiles.  d 64 leaves room for a
+    // third S, and for the queries of two pieces (below, at the products)
+    static constexpr int S_BUFS = D == 64 ? 3 : 2, Q_BUFS = D == 64 ? 2 : 1;
+    static constexpr int S_BARS = D == 64 ? 6 : 2;   // full: one per buffer and tile that uses it
+    static constexpr uint32_t O_COL = S_BUFS * BN;
+    static constexpr int Q_BUF = TILES * Q_BYTES, TILES_BYTES = Q_BUFS * Q_BUF + RING * SLOT;
     // registers of warps 0-3, of four helpers and of four softmax warps: together at most
-    // what the launch gives; the splits that were fastest.  4864 rows over 32768
-    // keys, 8 heads of 128: bf16 352 us (96, 48, 184: 352); 8192 keys, heads of 64: bf16 80
-    // (72, 24, 208: 87); int8 451 (80, 80, 176: 471)
-    static constexpr int REGS[3] = {INT8 ? 56 : D == 64 ? 96 : 72, INT8 ? 56 : D == 64 ? 48 : 24,
-                                    INT8 ? 200 : D == 64 ? 184 : 208};
+    // what the launch gives; the splits that were fastest.  4864 rows, 8 heads, bf16: 32768
+    // keys of 128 354 us (72, 24, 208: 358), 8192 keys of 64 70 us (96, 48, 184: 73); int8
+    // 440 and 100 us (96, 48, 184: 477 and 112)
+    static constexpr int REGS[3] = {INT8 ? 56 : 88, INT8 ? 56 : 40, INT8 ? 200 : 192};
     static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
                   "setmaxnreg takes from the launch's registers");
     static constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
@@ -77,8 +82,9 @@ ECHO_DEV int kv_clear(const KvPiece &pc) { return min(max(pc.low / BN - pc.kb0, 
 template <bool INT8, int D>
 struct Side {
     static constexpr int RING = Cfg<INT8, D>::RING;
-    uint64_t q_full, q_empty, k_first, pair[PAIRS], empty[RING], raw_full[RING], edge_go, v_ok;
-    uint64_t s_full[TILES], p_full[TILES], pv_done[TILES], drain;
+    using C = Cfg<INT8, D>;
+    uint64_t q_full[C::Q_BUFS], q_empty[C::Q_BUFS], k_first, pair[PAIRS], empty[RING], raw_full[RING], edge_go, v_ok;
+    uint64_t s_full[C::S_BARS], p_full[C::S_BUFS], pv_done[TILES], drain;
     uint64_t piece_full[PIECES], piece_empty[PIECES], sc_full[2], sc_empty[2];
     KvPiece piece[PIECES];
     uint32_t spoilt[SPOILT][4];      // keys of a block with values that are not finite
@@ -97,15 +103,17 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     using C = Cfg<INT8, D>;
     constexpr int RING = C::RING;
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint8_t *Qs = smem, *Ring = smem + TILES * C::Q_BYTES;
+    uint8_t *Qs = smem, *Ring = smem + C::Q_BUFS * C::Q_BUF;
     Side<INT8, D> &sh = *reinterpret_cast<Side<INT8, D> *>(smem + C::TILES_BYTES);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         // every barrier is waited for in each of its phases, in order, by whoever waits on
         // it, and none can be two phases ahead of a waiter
-        mbar_init(&sh.q_full, 1);
-        mbar_init(&sh.q_empty, 1);
+        for (int i = 0; i < C::Q_BUFS; ++i) {
+            mbar_init(&sh.q_full[i], 1);
+            mbar_init(&sh.q_empty[i], 1);
+        }
         // V_f and K_{f+1} share a barrier: two copies, or two tiles from four warps
         mbar_init(&sh.k_first, INT8 ? 4 : 1);
         for (int i = 0; i < PAIRS; ++i) mbar_init(&sh.pair[i], INT8 ? 8 : 2);
@@ -116,10 +124,10 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         mbar_init(&sh.edge_go, 1);
         mbar_init(&sh.v_ok, 4);
         for (int t = 0; t < TILES; ++t) {
-            mbar_init(&sh.s_full[t], 1);
-            mbar_init(&sh.p_full[t], 4);
             mbar_init(&sh.pv_done[t], 1);
         }
+        for (int i = 0; i < C::S_BARS; ++i) mbar_init(&sh.s_full[i], 1);
+        for (int i = 0; i < C::S_BUFS; ++i) mbar_init(&sh.p_full[i], 4);
         mbar_init(&sh.drain, 1);
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&sh.piece_full[i], 1);
@@ -136,7 +144,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     if (warp == 2) tmem_alloc(&sh.tmem_slot, TMEM_COLS);
     // query rows that no copy reaches (groups that do not divide 128) are zeros
-    for (int i = threadIdx.x; i < (BM - p.tile_rows) * TILES * C::ATOMS * 8; i += C::THREADS) {
+    for (int i = threadIdx.x; i < (BM - p.tile_rows) * C::Q_BUFS * TILES * C::ATOMS * 8; i += C::THREADS) {
         const int r = p.tile_rows + (i >> 3) % (BM - p.tile_rows), a = (i >> 3) / (BM - p.tile_rows);
         *reinterpret_cast<uint4 *>(Qs + a * ATOM + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
     }
@@ -203,21 +211,23 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
                 __syncwarp();
                 if (!more) continue;
-                // the queries' buffer is free once the last S of the piece before is done
-                if (loads > 0 && !wait_all(&sh.q_empty, (loads - 1) & 1)) break;
+                // the queries' buffer is free once the last S of its piece before is done
+                const int qb = loads % C::Q_BUFS, use = loads / C::Q_BUFS;
+                if (use > 0 && !wait_all(&sh.q_empty[qb], (use - 1) & 1)) break;
                 if (lane == 0) {
-                    mbar_arrive_expect_tx(&sh.q_full, TILES * C::ATOMS * p.tile_rows * 128);
+                    mbar_arrive_expect_tx(&sh.q_full[qb], TILES * C::ATOMS * p.tile_rows * 128);
                     const int tokens = p.tile_rows / p.work.group;
                     for (int t = 0; t < TILES; ++t)
                         for (int a = 0; a < C::ATOMS; ++a)
-                            tma_load_3d(Qs + t * C::Q_BYTES + a * ATOM, &tm_q, &sh.q_full, 64 * a,
+                            tma_load_3d(Qs + qb * C::Q_BUF + t * C::Q_BYTES + a * ATOM, &tm_q, &sh.q_full[qb], 64 * a,
                                         walk.head * p.work.group,
                                         walk.s.row + (walk.tile * TILES + t) * tokens);
                 }
                 ++loads;
             }
-            if (*abort_v && loads > 0)
-                mbar_wait(&sh.q_full, (loads - 1) & 1, abort_v, nullptr, 100000000ull);
+            if (*abort_v)   // let this CTA's copies land before it exits
+                for (int i = max(0, loads - C::Q_BUFS); i < loads; ++i)
+                    mbar_wait(&sh.q_full[i % C::Q_BUFS], (i / C::Q_BUFS) & 1, abort_v, nullptr, 100000000ull);
         } else if (warp == 0) {
             // ---------------- keys and values, a page at a time ----------------
             const int shift = p.pool.shift, per_block = BN >> shift;
@@ -251,7 +261,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv, ++li) {
                         const int slot = li % RING;
-                        ok = wait_all(&sh.empty[slot], ((li / RING) & 1) ^ 1);
+                        // d 128: a slot; 64: those of V_f and K_{f+1}
+                        if (D == 128) ok = wait_all(&sh.empty[slot], ((li / RING) & 1) ^ 1);
+                        else if (kv == 1) ok = wait_all(&sh.empty[((li >> 1) + 1) % 3], ((((li >> 1) + 1) / 3) & 1) ^ 1);
                         if (!ok) break;
                         uint64_t *bar = INT8 ? &sh.raw_full[slot] : li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS];
                         uint8_t *dst = Ring + slot * C::SLOT;
@@ -314,41 +326,30 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const uint32_t q_lo = ((smem_u32(Qs) & 0x3FFFFu) >> 4) | LO_K;
             const uint32_t ring_lo = (smem_u32(Ring) & 0x3FFFFu) >> 4;
             auto desc = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI << 32) | lo; };
-            auto mma_s = [&](int t, int slot) {
-                const uint32_t a_lo = q_lo + (uint32_t)t * (C::Q_BYTES >> 4);
+            auto mma_s = [&](int t, int slot, int buf, int qb) {
+                const uint32_t a_lo = q_lo + (uint32_t)(qb * (C::Q_BUF >> 4) + t * (C::Q_BYTES >> 4));
                 const uint32_t b_lo = (ring_lo + (uint32_t)slot * (C::SLOT >> 4)) | LO_K;
-                const uint32_t d = tmem + (uint32_t)(t * BN);
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) {
                     const uint32_t off = (uint32_t)(((kk >> 2) * ATOM + (kk & 3) * 32) >> 4);
                     tc_mma_f16(d, desc(a_lo + off), desc(b_lo + off), C::IDESC_S, kk > 0);
                 }
             };
-            auto mma_pv = [&](int t, int slot, uint32_t acc0) {
+            auto mma_pv = [&](int t, int slot, int buf, uint32_t acc0) {
                 const uint32_t b_lo = (ring_lo + (uint32_t)slot * (C::SLOT >> 4)) | LO_MN;
-                const uint32_t d = tmem + O_COL + (uint32_t)(t * D);
-                const uint32_t a = tmem + (uint32_t)(t * BN);
+                const uint32_t d = tmem + C::O_COL + (uint32_t)(t * D);
+                const uint32_t a = tmem + (uint32_t)(buf * BN);
                 tc_mma_f16_tmem_a(d, a, desc(b_lo), C::IDESC_PV, acc0);
 #pragma unroll
                 for (int kk = 1; kk < BN / 16; ++kk)
                     tc_mma_f16_tmem_a(d, a + 8 * kk, desc(b_lo + (uint32_t)(kk * 2048 >> 4)), C::IDESC_PV, 1u);
             };
             auto uniform = [&](int v) -> int { return (int)__ballot_sync(0xffffffffu, (v >> lane) & 1); };
-            int n = 0;                                        // pieces taken
-            int blocks = 0, clear = 0;                        // of the piece that is there
-            // the next piece; none: blocks 0
-            auto next_piece = [&]() {
-                const KvPiece &pc = piece(n, ok);
-                blocks = 0;
-                if (!ok) return;
-                blocks = max(uniform(pc.blocks), 0);
-                clear = uniform(kv_clear(pc));
-                if (blocks > 0) piece_done(n++);
-            };
             auto next2 = [](int s) { return s + 2 >= RING ? s + 2 - RING : s + 2; };
-            int vs = 1, ks = 2;                               // slots of V_f and K_{f+1}
-            int pr = 0;                                       // their barrier, and its parity
-            uint32_t pph = 0, fph = 0, qph = 0, eph = 0;      // parities of P, Q, edges
+            int pr = 0;                                       // barrier of the next pair, and its parity
+            uint32_t pph = 0, eph = 0;                        // and that of edges
+            [[maybe_unused]] uint32_t fph = 0, qph = 0;       // of P, of Q
             auto wait_pair = [&]() -> bool {
                 const bool there = wait_all(&sh.pair[pr], pph);
                 if (++pr == PAIRS) { pr = 0; pph ^= 1u; }
@@ -361,99 +362,262 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 eph ^= 1u;
                 return there;
             };
-            next_piece();
-            if (ok && blocks > 0 && (ok = wait_all(&sh.q_full, 0) && wait_all(&sh.k_first, 0))) {
-                tc_fence_after();
-                if (leader) {
-                    mma_s(0, 0);
-                    tc_commit(&sh.s_full[0]);
-                    mma_s(1, 0);
-                    tc_commit(&sh.s_full[1]);
-                    tc_commit(&sh.empty[0]);
-                    if (blocks == 1) tc_commit(&sh.q_empty);
-                }
-                __syncwarp();
-                ok = wait_pair();
-                if (clear == 0) edge_go();
-            }
-            while (ok && blocks > 0) {
-                const int nb = blocks, nclear = clear;
-                // all blocks but the last: here V_f and K_{f+1} are there.  EDGE: some row may
-                // not see the block, or the next one, whole, or the next one is the last
-                auto block = [&](int j, auto EDGE) -> bool {
-                    if (EDGE && j >= nclear && !edge_wait()) return false;
-                    if (!wait_all(&sh.p_full[0], fph)) return false;
-                    tc_fence_after();
+            if constexpr (D == 64) {
+                // Work items k = 2 f + t (block f, tile t) in S buffer k mod 3, in the order
+                //   S(0) S(1) S(2) | PV(0) S(3) | PV(1) S(4) | ...
+                // S(k + 3) goes over P(k) right after P V of item k has been issued, and
+                // S(k + 2), the tile's next block, is done while its softmax still works on
+                // item k.  With two buffers each tile's softmax waited for its products
+                // (4864 rows, 8192 keys, 8 heads of 64: 82 us, so 70); d 128, whose products
+                // take twice as long, has them at the tensor cores' rate with two.  S runs
+                // ahead across pieces, whose queries have two buffers.  Issuing must not cost
+                // more than the 1024 cycles of a block's products: a commit takes about 80
+                // cycles and a wait 130, so V_f and K_{f+1} are freed by one commit, and
+                // blocks without an edge have a loop of their own (without either: 103 us).
+                int n_s = 0, s_left = 0, s_j = 0, s_clear = 0;   // piece that S is in, its blocks
+                int ks = 0, s_bar = 0, s_blocks = 0, pairs = 0;  // slot of S's K; blocks begun, pairs seen
+                bool s_end = false, edge = false;             // no more; the last block begun is an edge
+                auto see_pair = [&]() -> bool {
+                    if (!wait_pair()) return false;
+                    if (edge) edge_go();
+                    ++pairs;
+                    return true;
+                };
+                // S of tile t of the next block: before it, what the block needs
+                auto next_s = [&]() -> bool {
+                    if (s_left == 0) {
+                        const KvPiece &pc = piece(n_s, ok);
+                        if (!ok) return false;
+                        s_left = uniform(pc.blocks);
+                        s_clear = uniform(kv_clear(pc));
+                        s_j = 0;
+                        s_end = s_left < 0;
+                        if (s_end) return true;
+                        if (!wait_all(&sh.q_full[n_s & 1], (n_s >> 1) & 1)) return false;
+                        ++n_s;
+                    }
+                    // K_f comes with V_{f-1}
+                    if (!(s_blocks == 0 ? wait_all(&sh.k_first, 0) : see_pair())) return false;
+                    ++s_blocks;
+                    edge = s_j >= s_clear;
+                    return true;
+                };
+                auto issue_s = [&](int t, int buf) {
+                    const int qb = (n_s - 1) & 1;
                     if (leader) {
-                        mma_pv(0, vs, j > 0 ? 1u : 0u);
-                        mma_s(0, ks);
-                        tc_commit(&sh.s_full[0]);
+                        mma_s(t, ks, buf, qb);
+                        tc_commit(&sh.s_full[s_bar]);
+                        if (t == 1) {
+                            if (s_blocks == 1) tc_commit(&sh.empty[0]);   // K_0
+                            if (s_left == 1) tc_commit(&sh.q_empty[qb]);
+                        }
                     }
                     __syncwarp();
-                    if (!wait_all(&sh.p_full[1], fph)) return false;
+                    if (++s_bar == C::S_BARS) s_bar = 0;
+                    if (t == 1) {
+                        ks = next2(ks);
+                        --s_left;
+                        ++s_j;
+                    }
+                };
+                int n = 0, f = 0, j = 0, nb = 0, nclear = 0;  // piece and block that P V is in
+                int vs = 1, rel = 1, t = 1, buf = 0;          // rel: of V_f and K_{f+1}
+                uint32_t pbuf = 0;                            // parity of the S buffers' P
+                // two S before the first P V; from then on P V of an item, S of the third after it
+                for (int item = -3; ok; ++item) {
+                    if (item >= 0) {
+                        if (t == 1) {                         // next: the tile 0 of a block
+                            if (j == nb) {
+                                const KvPiece &pc = piece(n, ok);
+                                if (!ok) break;
+                                nb = uniform(pc.blocks);
+                                nclear = uniform(kv_clear(pc));
+                                if (nb < 0) break;
+                                piece_done(n++);              // S has been here
+                                j = 0;
+                            }
+                            // blocks without an edge, S in the same piece
+                            const int plain = min(nclear - 1, nb - 2);
+                            if (j < plain) {
+                                const int some = plain - j, qb = (n_s - 1) & 1;
+                                for (; ok && j < plain; ++j) {
+                                    const int buf1 = buf + 1 == C::S_BUFS ? 0 : buf + 1;
+                                    ok = wait_all(&sh.p_full[buf], pbuf);
+                                    if (!ok) break;
+                                    tc_fence_after();
+                                    if (leader) {
+                                        mma_pv(0, vs, buf, j > 0 ? 1u : 0u);
+                                        mma_s(1, ks, buf, qb);
+                                        tc_commit(&sh.s_full[s_bar]);
+                                    }
+                                    __syncwarp();
+                                    if (buf == 2) pbuf ^= 1u;
+                                    ks = next2(ks);
+                                    if (++s_bar == C::S_BARS) s_bar = 0;
+                                    ok = wait_pair() && wait_all(&sh.p_full[buf1], pbuf);
+                                    if (!ok) break;
+                                    tc_fence_after();
+                                    if (leader) {
+                                        mma_pv(1, vs, buf1, j > 0 ? 1u : 0u);
+                                        tc_commit(&sh.empty[rel]);
+                                        mma_s(0, ks, buf1, qb);
+                                        tc_commit(&sh.s_full[s_bar]);
+                                    }
+                                    __syncwarp();
+                                    if (buf1 == 2) pbuf ^= 1u;
+                                    if (++s_bar == C::S_BARS) s_bar = 0;
+                                    vs = next2(vs);
+                                    if (++rel == 3) rel = 0;
+                                    buf = buf1 + 1 == C::S_BUFS ? 0 : buf1 + 1;
+                                }
+                                if (!ok) break;
+                                f += some;
+                                pairs += some;
+                                s_left -= some;
+                                s_j += some;
+                                s_blocks += some;
+                                edge = s_j >= s_clear;
+                            }
+                            if (pairs <= f) ok = see_pair();  // the last block's V comes alone
+                            if (ok && j >= nclear) ok = edge_wait();
+                            if (!ok) break;
+                        }
+                        t ^= 1;
+                        ok = wait_all(&sh.p_full[buf], pbuf);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (leader) {
+                            mma_pv(t, vs, buf, j > 0 ? 1u : 0u);
+                            if (t == 1) tc_commit(&sh.empty[rel]);
+                            if (j == nb - 1) tc_commit(&sh.pv_done[t]);
+                        }
+                        __syncwarp();
+                        if (t == 1) {
+                            vs = next2(vs);
+                            if (++rel == 3) rel = 0;
+                            ++j;
+                            ++f;
+                        }
+                    }
+                    const int ts = (item + 3) & 1;
+                    if (!s_end && ts == 0) ok = next_s();
+                    if (!ok) break;
+                    if (!s_end) {
+                        tc_fence_after();
+                        issue_s(ts, buf);
+                    }
+                    if (++buf == C::S_BUFS) {
+                        buf = 0;
+                        if (item >= 0) pbuf ^= 1u;
+                    }
+                }
+            } else {
+                int n = 0;                                        // pieces taken
+                int blocks = 0, clear = 0;                        // of the piece that is there
+                // the next piece; none: blocks 0
+                auto next_piece = [&]() {
+                    const KvPiece &pc = piece(n, ok);
+                    blocks = 0;
+                    if (!ok) return;
+                    blocks = max(uniform(pc.blocks), 0);
+                    clear = uniform(kv_clear(pc));
+                    if (blocks > 0) piece_done(n++);
+                };
+                int vs = 1, ks = 2;                               // slots of V_f and K_{f+1}
+                next_piece();
+                if (ok && blocks > 0 && (ok = wait_all(&sh.q_full[0], 0) && wait_all(&sh.k_first, 0))) {
                     tc_fence_after();
                     if (leader) {
-                        mma_pv(1, vs, j > 0 ? 1u : 0u);
-                        tc_commit(&sh.empty[vs]);
-                        mma_s(1, ks);
+                        mma_s(0, 0, 0, 0);
+                        tc_commit(&sh.s_full[0]);
+                        mma_s(1, 0, 1, 0);
                         tc_commit(&sh.s_full[1]);
-                        tc_commit(&sh.empty[ks]);
-                        if (EDGE && j == nb - 2) tc_commit(&sh.q_empty);
+                        tc_commit(&sh.empty[0]);
+                        if (blocks == 1) tc_commit(&sh.q_empty[0]);
+                    }
+                    __syncwarp();
+                    ok = wait_pair();
+                    if (clear == 0) edge_go();
+                }
+                while (ok && blocks > 0) {
+                    const int nb = blocks, nclear = clear;
+                    // all blocks but the last: here V_f and K_{f+1} are there.  EDGE: some row may
+                    // not see the block, or the next one, whole, or the next one is the last
+                    auto block = [&](int j, auto EDGE) -> bool {
+                        if (EDGE && j >= nclear && !edge_wait()) return false;
+                        if (!wait_all(&sh.p_full[0], fph)) return false;
+                        tc_fence_after();
+                        if (leader) {
+                            mma_pv(0, vs, 0, j > 0 ? 1u : 0u);
+                            mma_s(0, ks, 0, 0);
+                            tc_commit(&sh.s_full[0]);
+                        }
+                        __syncwarp();
+                        if (!wait_all(&sh.p_full[1], fph)) return false;
+                        tc_fence_after();
+                        if (leader) {
+                            mma_pv(1, vs, 1, j > 0 ? 1u : 0u);
+                            tc_commit(&sh.empty[vs]);
+                            mma_s(1, ks, 1, 0);
+                            tc_commit(&sh.s_full[1]);
+                            tc_commit(&sh.empty[ks]);
+                            if (EDGE && j == nb - 2) tc_commit(&sh.q_empty[0]);
+                        }
+                        __syncwarp();
+                        vs = next2(vs);
+                        ks = next2(ks);
+                        fph ^= 1u;
+                        if (!wait_pair()) return false;
+                        if (EDGE && j + 1 >= nclear) edge_go();
+                        return true;
+                    };
+                    const int plain = min(nclear - 1, nb - 2);
+                    int j = 0;
+                    for (; ok && j < plain; ++j) ok = block(j, std::false_type());
+                    for (; ok && j < nb - 1; ++j) ok = block(j, std::true_type());
+                    if (!ok) break;
+                    // the last block, and the next piece's first S
+                    const uint32_t acc = nb > 1 ? 1u : 0u;
+                    if (nclear < nb && !edge_wait()) { ok = false; break; }
+                    next_piece();
+                    if (!ok || !wait_all(&sh.p_full[0], fph)) { ok = false; break; }
+                    tc_fence_after();
+                    if (leader) {
+                        mma_pv(0, vs, 0, acc);
+                        tc_commit(&sh.pv_done[0]);
+                    }
+                    __syncwarp();
+                    if (blocks > 0) {
+                        qph ^= 1u;
+                        if (!wait_all(&sh.q_full[0], qph)) { ok = false; break; }
+                        tc_fence_after();
+                        if (leader) {
+                            mma_s(0, ks, 0, 0);
+                            tc_commit(&sh.s_full[0]);
+                        }
+                        __syncwarp();
+                    }
+                    if (!wait_all(&sh.p_full[1], fph)) { ok = false; break; }
+                    tc_fence_after();
+                    if (leader) {
+                        mma_pv(1, vs, 1, acc);
+                        tc_commit(&sh.empty[vs]);
+                        tc_commit(&sh.pv_done[1]);
+                        if (blocks > 0) {
+                            mma_s(1, ks, 1, 0);
+                            tc_commit(&sh.s_full[1]);
+                            tc_commit(&sh.empty[ks]);
+                            if (blocks == 1) tc_commit(&sh.q_empty[0]);
+                        }
                     }
                     __syncwarp();
                     vs = next2(vs);
                     ks = next2(ks);
                     fph ^= 1u;
-                    if (!wait_pair()) return false;
-                    if (EDGE && j + 1 >= nclear) edge_go();
-                    return true;
-                };
-                const int plain = min(nclear - 1, nb - 2);
-                int j = 0;
-                for (; ok && j < plain; ++j) ok = block(j, std::false_type());
-                for (; ok && j < nb - 1; ++j) ok = block(j, std::true_type());
-                if (!ok) break;
-                // the last block, and the next piece's first S
-                const uint32_t acc = nb > 1 ? 1u : 0u;
-                if (nclear < nb && !edge_wait()) { ok = false; break; }
-                next_piece();
-                if (!ok || !wait_all(&sh.p_full[0], fph)) { ok = false; break; }
-                tc_fence_after();
-                if (leader) {
-                    mma_pv(0, vs, acc);
-                    tc_commit(&sh.pv_done[0]);
-                }
-                __syncwarp();
-                if (blocks > 0) {
-                    qph ^= 1u;
-                    if (!wait_all(&sh.q_full, qph)) { ok = false; break; }
-                    tc_fence_after();
-                    if (leader) {
-                        mma_s(0, ks);
-                        tc_commit(&sh.s_full[0]);
-                    }
-                    __syncwarp();
-                }
-                if (!wait_all(&sh.p_full[1], fph)) { ok = false; break; }
-                tc_fence_after();
-                if (leader) {
-                    mma_pv(1, vs, acc);
-                    tc_commit(&sh.empty[vs]);
-                    tc_commit(&sh.pv_done[1]);
                     if (blocks > 0) {
-                        mma_s(1, ks);
-                        tc_commit(&sh.s_full[1]);
-                        tc_commit(&sh.empty[ks]);
-                        if (blocks == 1) tc_commit(&sh.q_empty);
+                        ok = wait_pair();
+                        if (ok && clear == 0) edge_go();
                     }
-                }
-                __syncwarp();
-                vs = next2(vs);
-                ks = next2(ks);
-                fph ^= 1u;
-                if (blocks > 0) {
-                    ok = wait_pair();
-                    if (ok && clear == 0) edge_go();
                 }
             }
             if (!ok && leader) {   // the MMAs already issued, before tensor memory is freed
@@ -575,8 +739,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         // ---------------- softmax and output of tile t, a row per thread ----------------
         const int t = (warp - C::SOFT0) >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t s_at = tmem + lane_base + (uint32_t)(t * BN);
-        const uint32_t o_at = tmem + lane_base + O_COL + (uint32_t)(t * D);
+        const uint32_t o_at = tmem + lane_base + C::O_COL + (uint32_t)(t * D);
+        int s_bar = t;                                        // of S of this block, and its parity
+        uint32_t sph = 0;
         const int row = quad * 32 + lane;                     // of the tile
         bool ok = true;
         int f = 0, edge = 0;
@@ -597,7 +762,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // Rows of a lane: its own, a whole row of S per thread.  int8: rows gq + 8 x of the
             // warp's 32, every fourth pair of columns, as the fragments of a product lie, so
             // that a lane needs only a quarter of the scales (a whole row per thread loads all
-            // 256 of a block: 487 against XXX us, 4864 rows over 32768 keys, 8 heads of 128)
+            // 256 of a block: 487 against 450 us, 4864 rows over 32768 keys, 8 heads of 128)
             constexpr int NX = INT8 ? 4 : 1;
             const int gq = lane >> 2, tq = lane & 3;
             float m[NX], l[NX];
@@ -620,9 +785,11 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 return r;
             };
             for (int j = 0; j < blocks; ++j, ++f) {
-                ok = wait_all(&sh.s_full[t], f & 1);
+                ok = wait_all(&sh.s_full[s_bar], sph);
                 if (!ok) break;
                 tc_fence_after();
+                const int buf = s_bar >= C::S_BUFS ? s_bar - C::S_BUFS : s_bar;
+                const uint32_t s_at = tmem + lane_base + (uint32_t)(buf * BN);
                 const int key0 = (kb0 + j) * BN;
                 if constexpr (INT8) {
                     ok = wait_all(&sh.sc_full[f & 1], (f >> 1) & 1);
@@ -752,7 +919,16 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         m[x] = high;
                     }
                     const float alpha = own(a);
-                    if (j > 0) {   // S of this block completed after P V of the one before
+                    if (j > 0) {
+                        // two S buffers: S of this block completed after P V of the one before
+                        // (three: the next item's S did, or for the piece's last P V, tile 0's)
+                        if constexpr (D == 64) {
+                            const int next = 2 * f + t + 1;
+                            ok = t == 1 && j == blocks - 1 ? wait_all(&sh.pv_done[0], n & 1)
+                                                           : wait_all(&sh.s_full[next % 6], (next / 6) & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c) {
                             uint32_t o[32];
@@ -791,8 +967,13 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&sh.p_full[t]);
+                    mbar_arrive(&sh.p_full[buf]);
                     if constexpr (INT8) mbar_arrive(&sh.sc_empty[f & 1]);
+                }
+                s_bar += TILES;
+                if (s_bar >= C::S_BARS) {
+                    s_bar = t;
+                    sph ^= 1u;
                 }
             }
             if (!ok) break;
