@@ -189,8 +189,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     const int first = walk.tile * p.work.tile, rows = min(p.work.tile, walk.s.packed - first);
                     for (int i = lane; i < rows * (D / 8); i += 32) {
                         const int pr = first + i / (D / 8);
-                        *reinterpret_cast<uint4 *>(p.out + (int64_t)(walk.s.row + pr / p.work.group) * p.ldo +
-                                                   (walk.head * p.work.group + pr % p.work.group) * D + i % (D / 8) * 8) =
+                        const int r = p.work.by_group(pr), h = pr - r * p.work.group;
+                        *reinterpret_cast<uint4 *>(p.out + (int64_t)(walk.s.row + r) * p.ldo +
+                                                   (walk.head * p.work.group + h) * D + i % (D / 8) * 8) =
                             make_uint4(0, 0, 0, 0);
                     }
                     more = walk.next(p.work);
@@ -216,7 +217,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 if (use > 0 && !wait_all(&sh.q_empty[qb], (use - 1) & 1)) break;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(&sh.q_full[qb], TILES * C::ATOMS * p.tile_rows * 128);
-                    const int tokens = p.tile_rows / p.work.group;
+                    const int tokens = p.work.by_group(p.tile_rows);
                     for (int t = 0; t < TILES; ++t)
                         for (int a = 0; a < C::ATOMS; ++a)
                             tma_load_3d(Qs + qb * C::Q_BUF + t * C::Q_BYTES + a * ATOM, &tm_q, &sh.q_full[qb], 64 * a,
@@ -755,7 +756,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 KvSeq s;
                 s.len = pc.len;
                 s.shift = pc.shift;
-                lim = s.top(p.work, pc.row + pr / p.work.group);
+                lim = s.top(p.work, pc.row + p.work.by_group(pr));
             }
             const int warp_low = __reduce_min_sync(0xffffffffu, lim);
             const int kb0 = pc.kb0, blocks = pc.blocks, clear = kv_clear(pc);
@@ -993,8 +994,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             __nv_bfloat16 *dst = nullptr;
             float *part = nullptr;
             if (real) {
-                const int g = p.work.group;
-                dst = p.out + (int64_t)(pc.row + pr / g) * p.ldo + (pc.head * g + pr % g) * D;
+                const int g = p.work.group, r = p.work.by_group(pr);
+                dst = p.out + (int64_t)(pc.row + r) * p.ldo + (pc.head * g + pr - r * g) * D;
             }
             const int slot_row = t * p.tile_rows + row;
             if (!whole) {

@@ -133,6 +133,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         bool ok = true, tail = false;
         for (int n = 0; ok; ++n) {
             const bool more = walk.next(p.work);
+            const int keys = more ? walk.s.keys(p.work, walk.tile) : 0;
             if (n >= PIECES) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&piece_empty[n % PIECES], ((n / PIECES) & 1) ^ 1, abort_v, p.err));
                 if (!ok) break;
@@ -146,7 +147,6 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             }
             if (!more) break;
             tail |= walk.tail();
-            const int keys = walk.s.keys(p.work, walk.tile);
             if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
             const int copies = (keys + (1 << cs) - 1) >> cs;
             const int32_t *table = p.work.b.table + (int64_t)walk.seq * p.work.b.max_pages;
@@ -223,7 +223,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         auto query = [&](int pr, int kk) -> uint2 {
             uint2 v = make_uint2(0u, 0u);
             if (pr < s.packed) {
-                const __nv_bfloat16 *src = p.q + (int64_t)(s.row + pr / group) * p.ldq + (head * group + pr % group) * D + 16 * kk;
+                const int r = p.work.by_group(pr);
+                const __nv_bfloat16 *src = p.q + (int64_t)(s.row + r) * p.ldq + (head * group + pr - r * group) * D + 16 * kk;
                 if constexpr (INT8) {
                     v = *reinterpret_cast<const uint2 *>(src + 4 * tq);
                 } else {
@@ -234,7 +235,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             return v;
         };
         if constexpr (C::Q_SMEM) {                   // the fragments as they are, lane by lane
-            for (int i = warp; i < NR * MT; i += C::WARPS) q_smem[i * 32 + lane] = query(tile * ROWS + (i / MT) * 8 + gq, i % MT);
+#pragma unroll
+            for (int i0 = 0; i0 < NR * MT; i0 += C::WARPS) {
+                const int i = i0 + warp;             // WARPS divides NR * MT
+                q_smem[i * 32 + lane] = query(tile * ROWS + (i / MT) * 8 + gq, i % MT);
+            }
             named_bar_sync(1, 32 * C::WARPS);
         } else {
 #pragma unroll
@@ -253,7 +258,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int pr = tile * ROWS + nt * 8 + 2 * tq + e;
-                lim[nt][e] = pr < s.packed ? s.top(p.work, s.row + pr / group) : keys;
+                lim[nt][e] = pr < s.packed ? s.top(p.work, s.row + p.work.by_group(pr)) : keys;
             }
         float o[NR][MT][4] = {}, m[NR][2], l[NR][2];
 #pragma unroll
@@ -553,9 +558,10 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                     const int row = nt * 8 + 2 * tq + e, pr = tile * ROWS + row;
                     const int col = 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
                     if (pr >= s.packed) continue;
+                    const int r = pr / group;
                     if (whole)
-                        *reinterpret_cast<uint32_t *>(p.out + (int64_t)(s.row + pr / group) * p.ldo +
-                                                      (head * group + pr % group) * D + col) = pack_bf16(a, b);
+                        *reinterpret_cast<uint32_t *>(p.out + (int64_t)(s.row + r) * p.ldo +
+                                                      (head * group + pr - r * group) * D + col) = pack_bf16(a, b);
                     else *reinterpret_cast<float2 *>(slot + row * D + col) = make_float2(a, b);
                 }
             __syncwarp();

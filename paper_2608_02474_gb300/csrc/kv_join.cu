@@ -11,7 +11,7 @@ namespace {
 // in the order of the workers.  It waits for memory a few times in a row and does little
 // else, so that what counts is how much of an item is on its way at once: R rows of it per
 // warp (many rows, few pieces: chunks), or a row's pieces dealt to PARTS warps (few rows,
-// many pieces: tokens), added up at the end in the order of the parts.
+// many pieces), added up at the end in the order of the parts.
 constexpr int kWarps = 8;
 
 template <int D, int R, int PARTS>
@@ -19,17 +19,19 @@ __global__ void __launch_bounds__(32 * kWarps)
 kv_join_kernel(const KvWork w, float *ws, __nv_bfloat16 *__restrict__ out, int64_t ldo) {
     pdl_enter();
     const KvJoin *joins = kv_joins(ws, w, D) + blockIdx.x;
-    const KvJoin j = *joins;
     constexpr int E = D / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % PARTS;
+    // the ends of worker c + 1 + lane, on their way before it is known whether they are needed
+    int64_t end = (int)blockIdx.x + lane + 1 < w.workers ? joins[lane].end : INT64_MAX;
+    const KvJoin j = *joins;
     const int row0 = (blockIdx.y * (kWarps / PARTS) + warp / PARTS) * R;
     if (j.upto == 0 || (int)blockIdx.y * (kWarps / PARTS) * R >= j.rows) return;
     // pieces: this worker's and those of the workers after it whose units begin before upto
     int n = 1;
     for (int i0 = 0;; i0 += 32) {
         const int i = i0 + lane;
-        const bool on = (int)blockIdx.x + i + 1 < w.workers && joins[i].end < j.upto;
-        const int some = __popc(__ballot_sync(0xffffffffu, on));
+        if (i0 > 0) end = (int)blockIdx.x + i + 1 < w.workers ? joins[i].end : INT64_MAX;
+        const int some = __popc(__ballot_sync(0xffffffffu, end < j.upto));
         n += some;
         if (some < 32) break;
     }
@@ -63,7 +65,7 @@ kv_join_kernel(const KvWork w, float *ws, __nv_bfloat16 *__restrict__ out, int64
             l[r] += li;
         }
         const int some = min(32, n - i0);
-#pragma unroll 4
+#pragma unroll 8
         for (int i = part; i < some; i += PARTS) {
             const float *src = piece(i0 + i) + row0 * D + lane * E;
 #pragma unroll
@@ -99,8 +101,8 @@ kv_join_kernel(const KvWork w, float *ws, __nv_bfloat16 *__restrict__ out, int64
         if (row0 + r >= j.rows) continue;
         const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
         const int pr = j.packed0 + row0 + r;
-        __nv_bfloat16 *dst = out + (int64_t)(j.row + pr / w.group) * ldo +
-                             (j.head * w.group + pr % w.group) * D + lane * E;
+        const int at = w.by_group(pr);
+        __nv_bfloat16 *dst = out + (int64_t)(j.row + at) * ldo + (j.head * w.group + pr - at * w.group) * D + lane * E;
 #pragma unroll
         for (int e = 0; e < E; e += 2)
             *reinterpret_cast<uint32_t *>(dst + e) = pack_bf16(acc[r][e] * inv, acc[r][e + 1] * inv);
@@ -122,8 +124,15 @@ namespace echo {
 void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st) {
     if (!w.split) return;
     LaunchScope ls(ECHO_K_KV_JOIN, a.batch->n_rows, (int64_t)a.Hq * a.pool->d, w.workers, st);
-    if (w.tile <= kDecodeRows) launch<1, 4>(a, w, st);
-    else launch<4, 1>(a, w, st);
+    // Few rows: a row's pieces dealt to four warps where there are many of them, or to so many
+    // that all rows of all items are in one wave of blocks (128 items in 304 pieces, 32 rows:
+    // 25.7 us a call with four warps a row, 22.4 with one; one item in 304 pieces, 24 rows:
+    // 36.7, 56.7)
+    const int64_t items = (int64_t)a.batch->n_seqs * w.H;
+    if (w.tile > kDecodeRows) launch<4, 1>(a, w, st);
+    else if (w.tile <= 8 || items * 16 < w.workers) launch<1, 4>(a, w, st);
+    else if (w.tile <= 16) launch<1, 2>(a, w, st);
+    else launch<1, 1>(a, w, st);
 }
 
 }  // namespace echo

@@ -24,17 +24,36 @@
 
 #include "kv_pages.cuh"
 
+// Division of 0 .. 2^31 - 1 by a number known to the host, as a product: with s = ceil(log2 d)
+// and m = ceil(2^(31 + s) / d), m d exceeds 2^(31 + s) by less than 2^s, so that n m / 2^(31 + s)
+// exceeds n / d by less than 1 / d.
+struct KvDiv {
+    uint32_t m;
+    int s, d;
+    explicit KvDiv(int by = 1) : m(0), s(0), d(by) {
+        while ((1ll << s) < by) ++s;
+        if (s > 0) m = (uint32_t)(((1ull << (31 + s)) + by - 1) / by);
+    }
+    ECHO_DEV int operator()(int n) const { return s == 0 ? n : (int)(__umulhi((uint32_t)n, m) >> (s - 1)); }
+};
+// as 32-bit numbers where they are: a division of 64 bits takes several hundred cycles
+ECHO_DEV int64_t kv_div64(int64_t a, int64_t b) {
+    return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 struct KvWork {
     KvBatch b;
     int H, group, causal_block;
+    KvDiv by_group, by_tile, by_block;
     int tile, slot_rows;   // packed rows of a tile, and rows of a workspace slot
     int cap;               // positions that a table row covers
     int block_shift;       // keys of a block, as a power of two
-    int workers, least;    // workers, and the fewest units for one
+    int workers;
     int split;             // 0: items are not divided; each goes to the worker of its first unit
 };
 
 constexpr int kFixedUnits = 2;   // set-up and end of a piece, in key-block times
+constexpr int kLeast = 4;        // the fewest units for a worker
 
 struct KvSeq {             // one sequence of the batch
     int row, packed, len;  // its first row, its packed rows, its length
@@ -46,19 +65,19 @@ struct KvSeq {             // one sequence of the batch
         len = max(w.b.len[seq], 0);
         shift = (int64_t)len - e;
     }
-    ECHO_DEV int tiles(const KvWork &w) const { return (packed + w.tile - 1) / w.tile; }
+    ECHO_DEV int tiles(const KvWork &w) const { return w.by_tile(packed + w.tile - 1); }
     // keys that row r sees
     ECHO_DEV int top(const KvWork &w, int r) const {
         if (w.causal_block == 0) return min(len, w.cap);
         const int64_t p = shift + r;
         if (p < 0) return 0;
-        const unsigned cb = (unsigned)w.causal_block;
-        return (int)min((unsigned)min(len, w.cap), ((unsigned)min(p, (int64_t)INT32_MAX) / cb + 1u) * cb);
+        const unsigned i = (unsigned)w.by_block((int)min(p, (int64_t)INT32_MAX));
+        return (int)min((unsigned)min(len, w.cap), (i + 1u) * (unsigned)w.causal_block);
     }
     // keys that any row of tile t sees: those of its last row
     ECHO_DEV int keys(const KvWork &w, int t) const {
         const int last = min((t + 1) * w.tile, packed) - 1;
-        return top(w, row + last / w.group);
+        return top(w, row + w.by_group(last));
     }
     ECHO_DEV int blocks(const KvWork &w, int t) const {
         return (keys(w, t) + (1 << w.block_shift) - 1) >> w.block_shift;
@@ -177,7 +196,7 @@ struct KvWalk {
         pc.blocks = kb1 - kb0;
         pc.kb0 = kb0;
         pc.keys = s.keys(w, tile);
-        pc.low = min(pc.keys, s.top(w, s.row + tile * w.tile / w.group));
+        pc.low = min(pc.keys, s.top(w, s.row + w.by_group(tile * w.tile)));
         pc.row = s.row;
         pc.packed = s.packed;
         pc.len = s.len;
@@ -231,10 +250,10 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
         }
         return v;
     };
-    int64_t mine = 0;
+    int64_t mine = 0;                                               // of one head
     int items = 0, most = 0;
     for (int i = b0; i < b1; ++i) {
-        mine += units_of(i, INT32_MAX, &most) * w.H;
+        mine += units_of(i, INT32_MAX, &most);
         KvSeq s;
         s.load(w, i);
         if (!by_warp || lane == 0) items += s.tiles(w) * w.H;
@@ -243,7 +262,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     const int incl_items = scan(items);
     most = __reduce_max_sync(0xffffffffu, most);
     if (lane == 31) {
-        sh.units[warp] = incl;
+        sh.units[warp] = incl * w.H;
         sh.items[warp] = incl_items;
         sh.most[warp] = most;
     }
@@ -261,10 +280,12 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
         total += v;
         most = max(most, sh.most[i]);
     }
-    const int64_t want = total / w.least + 1;
+    const int64_t want = total / kLeast + 1;
     const int G = want < w.workers ? (int)want : w.workers;
-    auto even = [&](int c) -> int64_t { return c < G ? total * c / G : total; };
-    const int64_t round = w.split && G == w.workers ? total / G / most : 0;   // items of a worker
+    const int64_t per_worker = kv_div64(total, G);
+    const unsigned rest = (unsigned)(total - per_worker * G);       // < G, a few hundred
+    auto even = [&](int c) -> int64_t { return c < G ? per_worker * c + rest * (unsigned)c / (unsigned)G : total; };
+    const int64_t round = w.split && G == w.workers ? kv_div64(per_worker, most) : 0;   // items of a worker
     walk.start = even(worker);
     walk.end = even(worker + 1);
     walk.left = (int)round;
@@ -275,7 +296,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
         __syncthreads();
         for (int q = 0; q < 3; ++q) {
             const int64_t at = round * (q == 0 ? worker : q == 1 ? worker + 1 : G);
-            int64_t u = by_warp ? before : before + incl - mine;
+            int64_t u = by_warp ? before : before + (incl - mine) * w.H;
             int64_t i0 = by_warp ? before_items : before_items + incl_items - items;
             for (int i = b0; i < b1; ++i) {
                 KvSeq s;
@@ -310,17 +331,17 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     const int64_t pos = walk.start;
     if (by_warp) {
         const int64_t all = __shfl_sync(0xffffffffu, incl, 31);
-        if (lane == 0 && before <= pos && pos < before + all) {
+        if (lane == 0 && before <= pos && pos < before + all * w.H) {
             sh.seq = b0;
             sh.base = before;
-            sh.per_head = all / w.H;
+            sh.per_head = all;
         }
     } else {
-        int64_t u = before + incl - mine;
-        if (u <= pos && pos < u + mine) {
+        int64_t u = before + (incl - mine) * w.H;
+        if (u <= pos && pos < u + mine * w.H) {
             for (int i = b0;; ++i) {
                 int none = 0;
-                const int64_t v = units_of(i, INT32_MAX, &none);
+                const int64_t v = per == 1 ? mine : units_of(i, INT32_MAX, &none);
                 if (pos < u + v * w.H) {
                     sh.seq = i;
                     sh.base = u;
@@ -343,12 +364,12 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     it.seq = sh.seq;
     it.at = sh.base;
     walk.s.load(w, walk.seq = it.seq);
-    it.head = (int)((pos - it.at) / sh.per_head);
+    it.head = (int)kv_div64(pos - it.at, sh.per_head);
     it.tile = 0;
     it.at += it.head * sh.per_head;
     // the tile, 32 at a time: every warp finds it for itself
     const int tiles = walk.s.tiles(w);
-    for (int t0 = 0;; t0 += 32) {
+    for (int t0 = 0; tiles > 1; t0 += 32) {
         const int64_t u = t0 + lane < tiles ? kFixedUnits + walk.s.blocks(w, t0 + lane) : 0;
         const int64_t upto = scan(u), all = __shfl_sync(0xffffffffu, upto, 31);
         if (it.at + all <= pos && t0 + 32 < tiles) {
@@ -415,11 +436,13 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
     w.group = a.Hq / p.H;
     w.causal_block = a.causal_block;
     w.tile = tile;
+    w.by_group = KvDiv(w.group);
+    w.by_tile = KvDiv(tile);
+    w.by_block = KvDiv(a.causal_block > 0 ? a.causal_block : 1);
     w.slot_rows = slot_rows;
     w.cap = (int)(cap < INT32_MAX ? cap : INT32_MAX);
     w.block_shift = block_shift;
     w.workers = workers;
-    w.least = 4;
     w.split = cap > whole_keys;
     return w;
 }
