@@ -1313,7 +1313,19 @@ int items_block(int L) {
     return best;
 }
 
-using echo::num_sms;
+int num_sms() {
+    static int sms[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64) return 152;
+    if (!sms[dev]) {
+        int v = 0;
+        if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1)
+            v = 152;
+        sms[dev] = v;
+    }
+    return sms[dev];
+}
 
 template <int DH, int BN>
 echo_status launch_items(const void *Q, int64_t ldq, const void *K, const void *V, int64_t ldkv,

@@ -56,8 +56,8 @@ struct Cfg {
     // registers of warps 0-3, of four helpers and of four softmax warps: together at most
     // what the launch gives; the splits that were fastest.  4864 rows, 8 heads, bf16: 32768
     // keys of 128 354 us (72, 24, 208: 358), 8192 keys of 64 70 us (96, 48, 184: 73); int8
-    // 440 and 100 us (96, 48, 184: 477 and 112)
-    static constexpr int REGS[3] = {INT8 ? 56 : 88, INT8 ? 56 : 40, INT8 ? 200 : 192};
+    // 464 and 98 us (88, 40, 192: 524 and 114; 56, 56, 200: 472 and 101)
+    static constexpr int REGS[3] = {INT8 ? 64 : 88, INT8 ? 64 : 40, 192};
     static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
                   "setmaxnreg takes from the launch's registers");
     static constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
@@ -763,7 +763,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // Rows of a lane: its own, a whole row of S per thread.  int8: rows gq + 8 x of the
             // warp's 32, every fourth pair of columns, as the fragments of a product lie, so
             // that a lane needs only a quarter of the scales (a whole row per thread loads all
-            // 256 of a block: 487 against 450 us, 4864 rows over 32768 keys, 8 heads of 128)
+            // 256 of a block: 487 us where this took 450, 4864 rows over 32768 keys, 8 heads of 128)
             constexpr int NX = INT8 ? 4 : 1;
             const int gq = lane >> 2, tq = lane & 3;
             float m[NX], l[NX];

@@ -6,6 +6,8 @@
     python -m paper_2608_02474_gb300.kernel_bench --kernel merge --T 21 --N 1560 --D 5120 --K 6552
     python -m paper_2608_02474_gb300.kernel_bench --kernel step_delta --T 21 --N 1560 --D 5120
     python -m paper_2608_02474_gb300.kernel_bench --kernel block --T 21 --N 1560 --D 5120 --K 6552
+    python -m paper_2608_02474_gb300.kernel_bench --kernel kv_attention --M 1560 --L 32760 --H 40 --d 128
+    python -m paper_2608_02474_gb300.kernel_bench --kernel kv_attention --M 1 --L 8190 --seqs 48 --H 8 --group 4 --int8
 
 Inputs are seeded random device tensors of the right shapes (values do not
 change the work of these kernels).  Prints the mean time per launch over
@@ -26,7 +28,8 @@ def make_parser() -> argparse.ArgumentParser:
     ap = argparse.ArgumentParser()
     ap.add_argument("--kernel", required=True,
                     choices=["gemm", "attention", "drift", "select", "merge", "quant", "layernorm",
-                             "energy", "step_delta", "ref_write", "block"])
+                             "energy", "step_delta", "ref_write", "block", "kv_write", "kv_read",
+                             "kv_attention"])
     ap.add_argument("--M", type=int, default=6552)
     ap.add_argument("--N", type=int, default=5120)
     ap.add_argument("--K", type=int, default=5120)
@@ -41,6 +44,11 @@ def make_parser() -> argparse.ArgumentParser:
     ap.add_argument("--samples", type=int, default=80960, help="energy: audio samples")
     ap.add_argument("--F", type=int, default=13824, help="block: FFN width")
     ap.add_argument("--Lc", type=int, default=672, help="block: audio condition tokens")
+    ap.add_argument("--seqs", type=int, default=1, help="kv_*: sequences of L tokens, M rows each")
+    ap.add_argument("--group", type=int, default=1, help="kv_attention: query heads of a key/value head")
+    ap.add_argument("--page", type=int, default=64, help="kv_*: tokens of a page")
+    ap.add_argument("--int8", action="store_true", help="kv_*: int8 pages")
+    ap.add_argument("--cb", type=int, default=0, help="kv_attention: causal_block")
     ap.add_argument("--iters", type=int, default=3)
     ap.add_argument("--warmup", type=int, default=1)
     return ap
@@ -127,6 +135,33 @@ def main():
         ws = torch.empty(cache.write_workspace_size(a.K), dtype=torch.uint8, device=dev)
         run = lambda: cache.write(src, rows, workspace=ws)
         work, unit = a.K * (3.0 * D + 8), "GB/s"
+    elif a.kernel.startswith("kv_"):
+        # a batch whose M rows of every sequence are its L tokens' last, pages in random order
+        per, n = -(-a.L // a.page), a.seqs * a.M
+        pool = ec.KVPool.empty(ec.CACHE_INT8 if a.int8 else ec.CACHE_BF16, per * a.seqs, a.page, a.H, a.d)
+        for page in pool.pages:
+            page.copy_(torch.randint(-127, 128, page.shape, generator=g, device=dev) if a.int8 else rn(*page.shape))
+        if a.int8:
+            pool.scale.copy_(torch.rand(pool.scale.shape, generator=g, device=dev) / 64)
+        batch = ec.KVBatch(torch.randperm(per * a.seqs, generator=g, device=dev).to(torch.int32).view(a.seqs, per),
+                           torch.full((a.seqs,), a.L, dtype=torch.int32, device=dev),
+                           torch.arange(0, n + 1, a.M, dtype=torch.int32, device=dev), n, a.M)
+        token = 2.0 * a.H * (a.d + 4 if a.int8 else 2 * a.d)       # bytes of a token in the pages
+        if a.kernel == "kv_attention":
+            q = rn(n, a.H * a.group * a.d).to(torch.bfloat16)
+            out = torch.empty_like(q)
+            ws = torch.empty(ec.echo_kv_attention_workspace_size(pool, batch, a.H * a.group), dtype=torch.uint8, device=dev)
+            run = lambda: ec.echo_kv_attention(pool, batch, q, causal_block=a.cb, out=out, workspace=ws)
+            if a.M * a.group <= 32:
+                work, unit = a.seqs * a.L * token + 4.0 * n * a.H * a.group * a.d, "GB/s"
+            else:
+                work, unit = 4.0 * n * a.L * a.H * a.group * a.d, "TFLOP/s"       # of all keys
+        else:
+            kv = rn(n, 2 * a.H * a.d).to(torch.bfloat16)
+            k, v = kv[:, :a.H * a.d], kv[:, a.H * a.d:]
+            run = (lambda: ec.echo_kv_write(pool, batch, k, v)) if a.kernel == "kv_write" else \
+                (lambda: ec.echo_kv_read(pool, batch, k=k, v=v))
+            work, unit = n * (token + 4.0 * a.H * a.d), "GB/s"
     elif a.kernel == "block":
         # one cached layer step (echo_block_step) on K of T*N tokens with
         # random weights: every kernel of the block, for captures of any of them
