@@ -149,6 +149,40 @@ def test_late_maxima(ec, form, d, rows):
 
 @FORMS
 @HEADS
+@pytest.mark.parametrize("lens,rows", [([1300], [150]), ([129, 128, 300], [128, 200, 129])])
+def test_maxima_in_every_block(ec, form, d, lens, rows):
+    """One key of every 64, and the last, whose score exceeds the earlier ones by far more
+    than 2^64, up for even rows and down for odd ones: the maximum moves in every block of
+    every tile, the last one too."""
+    c = kv_case.make(form, 64, 1, d, lens, rows, seed=13, amplitude=0.1)
+    q = kv_case.queries(sum(rows), 2 * d, 14, 0.3) + F32(2.0)
+    q[::2] *= -1
+    q = kv_case.G.to_bf16_values(q)
+    for b, n in enumerate(lens):
+        for i, p in enumerate([*range(37, n, 64), n - 1]):
+            a, pg = (1.0 + 3 * i) * (-1) ** i, c.table[b, p // 64]
+            if form == "int8":
+                c.pages[pg, 0, 0, p % 64] = 127 if a > 0 else -127
+                c.scale[pg, 0, 0, p % 64] = abs(a) / 127
+            else:
+                c.pages[pg, 0, 0, p % 64] = a
+    want, mass = P.attend(c.pages, c.scale, c.table, c.lens, c.row0, q, 2, 0)
+    close(run(ec, c, q, 2, 0, max_rows=1000), want, mass)
+
+
+@FORMS
+@HEADS
+@pytest.mark.parametrize("cb", [0, 1])
+def test_many_short_items_of_the_chunk_kernel(ec, form, d, cb):
+    """More items of one to four key blocks than CTAs, by the kernel for many rows."""
+    g = np.random.default_rng(15)
+    lens = [int(n) for n in g.integers(1, 450, 260)]
+    rows = [int(r) for r in g.integers(0, 4, 260)]
+    check(ec, kv_case.make(form, 16, 3, d, lens, rows, seed=16), 2, cb, max_rows=1000)
+
+
+@FORMS
+@HEADS
 @pytest.mark.parametrize("rows", [1, 40])
 def test_strided_rows_and_columns_beyond(ec, form, d, rows):
     """q as columns of a wider tensor, out into one: nothing beyond its columns changes."""
