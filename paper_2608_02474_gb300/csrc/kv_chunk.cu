@@ -34,7 +34,7 @@ constexpr int ATOM = 128 * 128;                 // 128 rows of 64 bf16
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int PIECES = 4;                       // handed out ahead
 constexpr int SLOT_ROWS = TILES * BM;
-constexpr int kWholeKeys = 768;                 // 64 bf16 rows, 8 heads of 128: whole 512 keys 16.5 us, divided 22
+constexpr int kWholeKeys = 1024;                // 64 bf16 rows, 8 heads of 128: whole 512 keys 16.5 us, 1024 21.5; divided 19.8, 21.8
 constexpr int PAIRS = 3;                        // (V_f, K_{f+1}) on their way or in use
 constexpr int SPOILT = 2;                       // blocks whose spoilt keys are kept
 

@@ -26,7 +26,7 @@
 namespace {
 
 constexpr int PIECES = 4;                      // handed out ahead
-constexpr int kWholeKeys = 512;     // 16 heads of 64, one bf16 token: whole 257 keys 10.5 us, 1024 16.5; divided 12.5, 13.3
+constexpr int kWholeKeys = 768;     // 16 heads of 64, one bf16 token: whole 256 keys 9.2 us, 1024 13.4; divided 11.6, 12.1
 
 template <bool INT8, int D, int NR>
 struct Cfg {
