@@ -602,11 +602,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
 
 // Packed rows of a tile for sequences of `rows`, 0: more than this kernel is for.  Measured
 // with 8 sequences of 7800 tokens, 16 heads (us; the chunk kernel in brackets):
-//   d 64:  bf16 8 rows 54, 16 58, 24 62, 32 69 (82), 48 in tiles of 24 92 (83)
-//          int8 8 rows 37, 16 41, 24 52, 32 65 (107), 48 in 24s 82, 64 in 32s 102 (108)
-//   d 128: bf16 8 rows 90, 16 95 (106), 24 in 16s 104, 32 108 (108)
-//          int8 8 rows 56, 16 62, 24 in 16s 92, 32 94 (132), 48 137 (132); tiles of 24 and
-//          32, with half the CTAs, are no faster than two of 16: 90, 116
+//   d 64:  bf16 8 rows 56, 16 56, 24 59, 32 64 (74), 48 in tiles of 24 84 (75)
+//          int8 8 rows 35, 16 39, 24 47, 32 58 (100), 48 in 24s 75, 64 in 32s 92 (102)
+//   d 128: bf16 8 rows 89, 16 90 (108), 24 in 16s 104, 32 103 (108, 110; one sequence of
+//          32760 tokens, 40 heads: 32 in 16s 190, 133)
+//          int8 8 rows 56, 16 60, 24 in 16s 89, 32 90 (128), 48 131 (129); three CTAs of an
+//          SM, with two thirds of the registers, are slower: d 64 int8 24 rows 60
 int tile_rows(bool i8, int d, int64_t rows) {
     if (d == 128) return rows <= 8 ? 8 : rows <= (i8 ? 32 : 16) ? 16 : 0;
     if (rows <= 32) return (int)(rows + 7) / 8 * 8 + (rows == 0 ? 8 : 0);
