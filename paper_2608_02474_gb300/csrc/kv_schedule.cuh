@@ -8,7 +8,8 @@
 //
 // As many items as every worker can take whole go round first, in their order: worker c of
 // G takes W of them from item W c on.  The units of the items left over are dealt out so
-// that the workers' sums come out even, in one row, each worker's next to the one's before.
+// that the workers' sums come out even, in one row, each worker's next to the one's before
+// and no worker between two others without any (the joining kernel relies on it).
 // An item that crosses a boundary there is done in pieces: each worker leaves its piece's
 // sums in the workspace, and the joining kernel adds them up.  A worker has at most one
 // piece with an item's last keys but not its first (an item that it begins, and others go
@@ -269,7 +270,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     if (threadIdx.x == 0) sh.seq = -1;
     __syncthreads();
     int64_t before = 0, total = 0;   // units of the earlier warps; of all
-    int before_items = 0;
+    int before_items = 0, all_items = 0;
     most = 1;
     for (int i = 0; i < WARPS; ++i) {
         const int64_t v = sh.units[i];
@@ -278,14 +279,19 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
             before_items += sh.items[i];
         }
         total += v;
+        all_items += sh.items[i];
         most = max(most, sh.most[i]);
     }
     const int64_t want = total / kLeast + 1;
     const int G = want < w.workers ? (int)want : w.workers;
     const int64_t per_worker = kv_div64(total, G);
     const unsigned rest = (unsigned)(total - per_worker * G);       // < G, a few hundred
-    auto even = [&](int c) -> int64_t { return c < G ? per_worker * c + rest * (unsigned)c / (unsigned)G : total; };
-    const int64_t round = w.split && G == w.workers ? kv_div64(per_worker, most) : 0;   // items of a worker
+    auto even = [&](int c) -> int64_t { return c < G ? per_worker * c + min((unsigned)c, rest) : total; };
+    // Items of a worker.  Every worker keeps a unit of those left over, since the joining kernel
+    // takes the pieces of an item from workers that follow one another.  Where all items have
+    // the same units, the ones without any come after the last unit.
+    int64_t round = w.split && G == w.workers ? kv_div64(per_worker, most) : 0;
+    if (round > 0 && round * most == per_worker && total != (int64_t)all_items * most) --round;
     walk.start = even(worker);
     walk.end = even(worker + 1);
     walk.left = (int)round;
