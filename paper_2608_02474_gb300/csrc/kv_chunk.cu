@@ -179,7 +179,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (warp == 3) {
             // ---------------- pieces, and their queries ----------------
             int n = 0, loads = 0;
-            bool tail = false;
+            if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
             for (bool more = true; more; ++n) {
                 more = walk.next(p.work);
                 // Items that see no key become zeros here: the other warps get pieces with
@@ -203,10 +203,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         walk.put(p.work, pc);
                         if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
                         if (walk.tail()) kv_leave_join(p.work, walk, p.ws, D);
-                        tail |= walk.tail();
                     } else {
                         pc.blocks = -1;
-                        if (!tail) kv_leave_join(p.work, walk, p.ws, D);
                     }
                     mbar_arrive(&sh.piece_full[n % PIECES]);
                 }
@@ -1064,11 +1062,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.ldo = a.ldo;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
+    cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
+        launched = echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
     }
-    echo::launch_kv_join(a, p.work, st);
+    if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
 }
 

@@ -130,7 +130,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         const int shift = p.pool.shift, cs = min(shift, C::BSHIFT);   // tokens of a copy: 1 << cs
         const int per_block = BK >> cs;
         int g = 0;
-        bool ok = true, tail = false;
+        bool ok = true;
+        if (lane == 0) kv_leave_join(p.work, walk, p.ws, D);
         for (int n = 0; ok; ++n) {
             const bool more = walk.next(p.work);
             const int keys = more ? walk.s.keys(p.work, walk.tile) : 0;
@@ -143,10 +144,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 if (more) walk.put(p.work, pc);
                 else pc.blocks = -1;
                 mbar_arrive(&piece_full[n % PIECES]);
-                if (more ? walk.tail() : !tail) kv_leave_join(p.work, walk, p.ws, D);
+                if (more && walk.tail()) kv_leave_join(p.work, walk, p.ws, D);
             }
             if (!more) break;
-            tail |= walk.tail();
             if (walk.s.len > p.work.cap) echo_flag_error(p.err, ECHO_ERR_PAGE);
             const int copies = (keys + (1 << cs) - 1) >> cs;
             const int32_t *table = p.work.b.table + (int64_t)walk.seq * p.work.b.max_pages;
@@ -592,11 +592,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.ldo = a.ldo;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
+    cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        echo::launch_chained(kv_decode_kernel<INT8, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
+        launched = echo::launch_chained(kv_decode_kernel<INT8, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
     }
-    echo::launch_kv_join(a, p.work, st);
+    if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
 }
 

@@ -363,7 +363,7 @@ ECHO_DEV void kv_find(const KvWork &w, int worker, KvFound &sh, KvWalk &walk) {
     walk.here = {w.b.n_seqs, 0, 0, 0};
     walk.stage = 3;
     walk.begun = false;
-    walk.kb0 = walk.kb1 = 0;
+    walk.kb0 = walk.kb1 = walk.nb = 0;
     if (sh.seq < 0 || walk.start >= walk.end) return;
     walk.stage = 0;
     KvWalk::Item &it = walk.here;
@@ -411,8 +411,9 @@ struct KvJoin {
 ECHO_DEV KvJoin *kv_joins(float *ws, const KvWork &w, int D) {
     return reinterpret_cast<KvJoin *>(ws + (int64_t)2 * w.workers * w.slot_rows * (D + 2));
 }
-// With walk at its piece with an item's last keys, or at its end where there was none; by
-// one thread of each CTA.
+// By one thread of each CTA, before the first wait that may give up (the joining kernel runs
+// all the same, and takes its addresses from here), and again with walk at its piece with an
+// item's last keys.
 ECHO_DEV void kv_leave_join(const KvWork &w, const KvWalk &walk, float *ws, int D) {
     if (!w.split) return;
     KvJoin j = {walk.end, 0, 0, 0, 0, 0};
