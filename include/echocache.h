@@ -444,7 +444,8 @@ echo_status echo_cache_dequant(const int8_t *q, const float *scale, const int32_
  * table[b, p / page_tokens].  A page holds its keys and then its values, head by head,
  * so that a head's tokens lie side by side.  kind ECHO_CACHE_BF16 keeps the values;
  * ECHO_CACHE_INT8 keeps codes with one scale per token and head (Q of
- * echo_cache_quant over a head's d values), for keys and values apart.
+ * echo_cache_quant over a head's d values; a value of 0 has code 0 where 127 / a is
+ * infinite, too), for keys and values apart.
  * Pages need no initial contents: nothing at or past a sequence's length is used. */
 typedef struct {
     int32_t kind;          /* ECHO_CACHE_INT8 or ECHO_CACHE_BF16 */

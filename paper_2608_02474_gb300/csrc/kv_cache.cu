@@ -35,7 +35,8 @@ ECHO_DEV void store16(T *p, const float *f) {
 
 // Codes without conversions, which run at an eighth of the rate of additions:
 // 1.5 2^23 + t, |t| < 2^22, is 1.5 2^23 + rint(t) (half to even), with rint(t) in two's
-// complement in its low bits; |v inv| stays below 127.5, so that nothing is clamped.
+// complement in its low bits; |v inv| stays below 127.5 for a finite inv, so that nothing is
+// clamped.
 ECHO_DEV uint32_t codes4(const float *f, float inv) {
     uint32_t b[4];
 #pragma unroll
@@ -96,7 +97,12 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
                 if (c >= C) continue;
                 const bool bad = a >= 0x7F800000u;
                 const float amax = __uint_as_float(a);
-                const float inv = !bad && amax > 0.f ? __fdiv_rn(127.f, amax) : 0.f;
+                float inv = !bad && amax > 0.f ? __fdiv_rn(127.f, amax) : 0.f;
+                if (inv == INFINITY) {          // amax below 3.7e-37: +-127 by the clamp, and 0
+                    inv = 127.f;
+#pragma unroll
+                    for (int i = 0; i < EP; ++i) f[i] = f[i] == 0.f ? 0.f : copysignf(1.f, f[i]);
+                }
                 uint8_t *dst = pool.pages + vec * D + (ch % LPH) * GE;
 #pragma unroll
                 for (int h = 0; h < NG; ++h) {

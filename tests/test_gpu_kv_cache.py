@@ -169,3 +169,34 @@ def test_another_stream_and_empty_calls(ec):
     ec.echo_kv_write(pool, none, k[:0], v[:0])
     ec.echo_kv_read(pool, none)
     assert ec.echo_launch_count() == n and ec.echo_get_device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_heads_of_the_smallest_values(ec, dtype):
+    """Below 127 / FLT_MAX (3.7e-37) 127 / a is infinite in fp32, and the rule's clamp gives
+    +-127 to every value but 0, which stays 0."""
+    import torch
+    largest = [1e-36, 3.8e-37, 3.7e-37, 1e-37, 1.2e-38, 3e-39, 1e-40, 1.0]
+    H, d, n = len(largest), 64, 5
+    x = np.random.default_rng(9).uniform(-1, 1, (n, H, d)) * np.array(largest)[:, None]
+    x[:, :, 3] = largest
+    x[:, :, 10:14], x[:, :, 11] = 0, -0.0
+    t = torch.from_numpy(x.astype(F32).reshape(n, H * d)).cuda()
+    k = t.to(torch.bfloat16) if dtype == "bf16" else t
+    c = kv_case.make("int8", 16, H, d, [n], [n])
+    pool, batch = c.device(ec)
+    ec.echo_kv_write(pool, batch, k, -k)
+    v = host(k).reshape(n, H, d)
+    a = np.abs(v).max(axis=2, keepdims=True)
+    with np.errstate(over="ignore", invalid="ignore"):
+        inv = F32(127) / a
+        q = np.where(v == 0, 0, np.clip(np.rint(v * inv), -127, 127)).astype(np.int8)
+    assert np.isinf(inv[:, 2:7]).all() and np.isfinite(inv[:, :2]).all()
+    assert (np.abs(q[:, 2:7]) == np.where(v[:, 2:7] == 0, 0, 127)).all()
+    page = c.table[0, 0]
+    for i, codes in ((0, q), (1, -q)):
+        assert same(host(pool.pages)[page, i, :, :n].transpose(1, 0, 2), codes)
+        assert same(host(pool.scale)[page, i, :, :n].T, (a / F32(127))[..., 0])
+    back, _ = ec.echo_kv_read(pool, batch, dtype=torch.float32)
+    assert same(host(back).reshape(n, H, d), q.astype(F32) * (a / F32(127)))
+    assert ec.echo_get_device_error() == 0
