@@ -442,6 +442,15 @@ class PageTable:
             self.pages[c].extend(self.free.pop() for _ in range(need[c]))
             self.lens[c] += n
 
+    def shorten(self, rows: dict[int, int]):
+        """Take back the last rows[clip] tokens of each clip, and the pages that only they
+        needed."""
+        for c, n in rows.items():
+            self.lens[c] -= n
+            keep = -(-self.lens[c] // self.page_tokens)
+            self.free.extend(reversed(self.pages[c][keep:]))
+            del self.pages[c][keep:]
+
     def batch(self, rows: dict[int, int], device="cuda") -> ec.KVBatch:
         """The clips of one call with their new rows (rows[clip] each, in the dict's order),
         copied to the device."""
@@ -501,26 +510,38 @@ class ChunkStream:
         self.cond_table.close(clip)
 
     def step(self, chunks: dict[int, torch.Tensor]) -> dict[int, torch.Tensor]:
-        """chunks: bf16 [n, D] per clip; returns bf16 [n, D] per clip."""
+        """chunks: bf16 [n, D] per clip; returns bf16 [n, D] per clip.  After an exception the
+        clips are as they were before the call."""
         rows = {c: x.shape[0] for c, x in chunks.items()}
         if any(c not in self.self_table.lens for c in rows):
             raise ValueError("a clip is not open")
         D = self.H * self.d
-        x = torch.cat(list(chunks.values())) if len(chunks) > 1 else next(iter(chunks.values()))
+        for x in chunks.values():
+            if x.dim() != 2 or x.shape[1] != D or x.device.type != self.device.type:
+                raise ValueError(f"a chunk must be [n, {D}] on {self.device.type}")
+            if x.dtype not in (torch.bfloat16, torch.float32):
+                raise TypeError(f"unsupported dtype {x.dtype}")
+        if not sum(rows.values()):
+            return {c: x.to(torch.bfloat16) for c, x in chunks.items()}
+        x = torch.cat(list(chunks.values())) if len(chunks) > 1 else next(iter(chunks.values())).contiguous()
         self.self_table.extend(rows)
-        batch = self.self_table.batch(rows, self.device)
-        cond = self.cond_table.batch(rows, self.device)   # the same rows, over the audio's pages
-        for blk, pool, cond_pool in zip(self.blocks, self.self_pools, self.cond_pools):
-            w = blk.tensors
-            n1 = ec.echo_layernorm(x)
-            kv = ec.echo_linear(n1, w["Wkv"], w["bkv"])
-            ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
-            a = ec.echo_kv_attention(pool, batch, ec.echo_linear(n1, w["Wq"], w["bq"]),
-                                     causal_block=self.frame_tokens)
-            h1 = ec.echo_linear(a, w["Wo"], w["bo"], resid=x, out_dtype=torch.float32)
-            q = ec.echo_linear(ec.echo_layernorm(h1), w["Wqc"], w["bqc"])
-            a = ec.echo_kv_attention(cond_pool, cond, q)
-            h2 = ec.echo_linear(a, w["Woc"], w["boc"], resid=h1, out_dtype=torch.float32)
-            u = ec.echo_linear(ec.echo_layernorm(h2), w["W1"], w["b1"], act=1)
-            x = ec.echo_linear(u, w["W2"], w["b2"], resid=h2)
+        try:
+            batch = self.self_table.batch(rows, self.device)
+            cond = self.cond_table.batch(rows, self.device)   # the same rows, over the audio's pages
+            for blk, pool, cond_pool in zip(self.blocks, self.self_pools, self.cond_pools):
+                w = blk.tensors
+                n1 = ec.echo_layernorm(x)
+                kv = ec.echo_linear(n1, w["Wkv"], w["bkv"])
+                ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
+                a = ec.echo_kv_attention(pool, batch, ec.echo_linear(n1, w["Wq"], w["bq"]),
+                                         causal_block=self.frame_tokens)
+                h1 = ec.echo_linear(a, w["Wo"], w["bo"], resid=x, out_dtype=torch.float32)
+                q = ec.echo_linear(ec.echo_layernorm(h1), w["Wqc"], w["bqc"])
+                a = ec.echo_kv_attention(cond_pool, cond, q)
+                h2 = ec.echo_linear(a, w["Woc"], w["boc"], resid=h1, out_dtype=torch.float32)
+                u = ec.echo_linear(ec.echo_layernorm(h2), w["W1"], w["b1"], act=1)
+                x = ec.echo_linear(u, w["W2"], w["b2"], resid=h2)
+        except BaseException:
+            self.self_table.shorten(rows)
+            raise
         return dict(zip(rows, x.split(list(rows.values()))))
