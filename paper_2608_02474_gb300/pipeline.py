@@ -493,17 +493,22 @@ class ChunkStream:
     def open(self, clip: int, cond_kv: list):
         """A new clip with its audio condition: per layer the keys and values bf16 [Lc, 2 D]
         of echo_precompute_cross_kv."""
-        Lc, D = cond_kv[0].shape[0], self.H * self.d
+        D = self.H * self.d
+        if len(cond_kv) != len(self.blocks):
+            raise ValueError(f"{len(cond_kv)} layers' keys and values for {len(self.blocks)} blocks")
+        Lc = cond_kv[0].shape[0] if cond_kv else 0
+        if any(tuple(kv.shape) != (Lc, 2 * D) for kv in cond_kv):
+            raise ValueError(f"every layer's keys and values must be [{Lc}, {2 * D}]")
         self.cond_table.open(clip)
         try:
             self.cond_table.extend({clip: Lc})
-        except MemoryError:
+            batch = self.cond_table.batch({clip: Lc}, self.device)
+            for pool, kv in zip(self.cond_pools, cond_kv):
+                ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
+            self.self_table.open(clip)
+        except BaseException:
             self.cond_table.close(clip)
             raise
-        self.self_table.open(clip)
-        batch = self.cond_table.batch({clip: Lc}, self.device)
-        for pool, kv in zip(self.cond_pools, cond_kv):
-            ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
 
     def close(self, clip: int):
         self.self_table.close(clip)

@@ -103,6 +103,32 @@ def test_no_chunks_and_chunks_of_no_rows(stream):
     assert y[0].shape == (0, D) and y[0].dtype == torch.bfloat16 and stream.self_table.lens == {0: 0}
 
 
+def test_opening_looks_at_every_layer(stream):
+    st = stream
+    st.open(7, cond(5))
+    before = state(st)
+    for bad in (cond(5, 1), cond(5, 3), [], [cond(5, 1)[0], cond(6, 1)[0]], [cond(5, 1)[0], rows(5)]):
+        st.calls.clear()
+        with pytest.raises(ValueError):
+            st.open(1, bad)
+        assert state(st) == before and not st.calls
+    with pytest.raises(MemoryError):
+        st.open(1, cond(33))
+    with pytest.raises(ValueError):
+        st.open(7, cond(5))
+    assert state(st) == before
+
+
+def test_an_opening_that_fails_leaves_the_clip_closed(stream):
+    st = stream
+    before = state(st)
+    for fail in (0, 1, 2):
+        steps_after(st, fail, lambda: st.open(1, cond(20)))
+        assert state(st) == before, fail
+    st.open(1, cond(20))
+    assert st.cond_table.lens == {1: 20} and st.self_table.lens == {1: 0}
+
+
 def test_pages_are_given_back_by_the_tokens_that_needed_them():
     t = pipeline.PageTable(6, 16)
     t.open(1)
