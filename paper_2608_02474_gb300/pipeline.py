@@ -474,7 +474,9 @@ class ChunkStream:
     step({clip: x}) takes the new latent tokens of each clip (any number of frames, or a
     single token), appends their keys and values to the clip's pages, and returns the last
     layer's outputs.  Self-attention is causal frame by frame (frame_tokens = 1: token by
-    token): a token sees its own frame and all earlier ones.  The audio condition of a clip,
+    token): a token sees all earlier frames and its own, as far as the clip's chunks have
+    come: the tokens of a frame that comes in parts see the parts up to their own, and their
+    outputs stand when the rest arrives.  The audio condition of a clip,
     of any length, is written into pages of its own when the clip is opened, and the
     cross-attention reads it from there.  The block is that of echo_block_step on these rows:
       h1 = x + MHA(LN(x)) Wo + bo,  h2 = h1 + MHA(LN(h1) Wqc; audio) Woc + boc,

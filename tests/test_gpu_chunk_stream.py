@@ -118,3 +118,27 @@ def test_chunks_of_several_clips(ec, int8, frame):
         rel = np.abs(y - ref).max(axis=1) / np.abs(ref).max(axis=1)
         mean = np.abs(y - ref).sum() / np.abs(ref).sum()
         assert rel.max() <= 2e-2 and mean <= 5e-3, (c, rel.max(), mean)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_frame_that_comes_in_parts(ec, int8):
+    """Tokens see their frame as far as it has come.  One block, whose keys and values do not
+    depend on what earlier tokens saw: each chunk's rows are those of the clip up to it."""
+    import torch
+    from paper_2608_02474_gb300.pipeline import ChunkStream
+    w = G.block_weights(W, 0)
+    cond, x = G.random_rows(19, W.D, seed=61), G.random_rows(90, W.D, seed=62)
+    bf = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda", torch.bfloat16)   # noqa: E731
+    kv = ec.echo_precompute_cross_kv(bf(cond), torch.cat([bf(w["Wkc"]), bf(w["Wvc"])]),
+                                     torch.cat([bf(w["bkc"]), bf(w["bvc"])]))
+    st = ChunkStream([ec.DeviceBlock.from_host(w, np.zeros((1, W.D), F32))], W.H, W.d, 24, n_pages=6, cond_pages=2,
+                     page_tokens=16, kind=ec.CACHE_INT8 if int8 else ec.CACHE_BF16)
+    st.open(0, [kv])
+    lo = 0
+    for n in (17, 1, 30, 24, 18):                      # up to 17, 18, 48, 72, 90 of frames of 24
+        y = st.step({0: bf(x[lo:lo + n])})[0].float().cpu().numpy()
+        lo += n
+        ref = reference(G.to_bf16_values(x[:lo]), [w], [G.to_bf16_values(cond)], 24, int8)[-n:]
+        rel = np.abs(y - ref).max(axis=1) / np.abs(ref).max(axis=1)
+        assert rel.max() <= 2e-2 and np.abs(y - ref).sum() / np.abs(ref).sum() <= 5e-3, (lo, rel.max())
+    assert ec.echo_get_device_error() == 0
