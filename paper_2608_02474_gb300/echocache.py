@@ -578,7 +578,9 @@ class KVPool:
             _dev(scale, "scale")
             if scale.dtype != torch.float32 or scale.shape != pages.shape[:4]:
                 raise ValueError("scale must be f32 [n_pages, 2, H, page_tokens]")
-        self.pages, self.scale = pages, scale
+            if scale.get_device() != pages.get_device():
+                raise ValueError("pages and scale must be on one device")
+        self.pages, self.scale, self._gpu = pages, scale, pages.get_device()
         self.n_pages, _, self.H, self.page_tokens, self.d = pages.shape
         self.cstruct = KVPoolC(CACHE_INT8 if int8 else CACHE_BF16, self.n_pages, self.page_tokens,
                                self.H, self.d, _p(pages), _p(scale))
@@ -612,6 +614,9 @@ class KVBatch:
         B = lens.numel()
         if table.dim() != 2 or table.shape[0] != B or row0.numel() != B + 1:
             raise ValueError("table must be [n_seqs, max_pages] and row0 [n_seqs + 1]")
+        self._gpu = table.get_device()
+        if lens.get_device() != self._gpu or row0.get_device() != self._gpu:
+            raise ValueError("table, lens and row0 must be on one device")
         self.table, self.lens, self.row0 = table, lens, row0
         self.n_seqs, self.n_rows = B, int(n_rows)
         self.max_rows = self.n_rows if max_rows is None else int(max_rows)
@@ -620,22 +625,31 @@ class KVBatch:
         self._ref = _c.byref(self.cstruct)
 
 
-def _rows_of(t, name, n_rows, cols):
-    """Row stride of a CUDA tensor of n_rows rows and at least cols contiguous columns (those
-    of a wider tensor, too).  The stride of a single row means nothing, and may be anything."""
+def _rows_of(t, name, n_rows, cols, gpu):
+    """Row stride of a tensor on device `gpu` of n_rows rows and at least cols contiguous
+    columns (those of a wider tensor, too).  The stride of a single row means nothing, and may
+    be anything."""
     shape, stride = t.shape, t.stride()
-    if not t.is_cuda or len(shape) != 2 or shape[0] != n_rows or shape[1] < cols:
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} must be a CUDA tensor on the pool's device")
+    if len(shape) != 2 or shape[0] != n_rows or shape[1] < cols:
         raise ValueError(f"{name} must be a CUDA tensor of {n_rows} rows and {cols} columns")
     if stride[1] != 1:
         raise ValueError(f"{name}'s columns must be contiguous")
     return stride[0] if n_rows > 1 else (shape[1] + 7) // 8 * 8
 
 
+def _one_gpu(pool: KVPool, batch: KVBatch):
+    if batch._gpu != pool._gpu:
+        raise ValueError("pool and batch must be on one device")
+    return pool._gpu
+
+
 def _kv_rows(pool: KVPool, batch: KVBatch, k, v):
     """Row stride of k and v, [n_rows, >= H d] each."""
-    n, cols = batch.n_rows, pool.H * pool.d
-    ld = _rows_of(k, "k", n, cols)
-    if _rows_of(v, "v", n, cols) != ld and n > 1 or k.dtype != v.dtype:
+    n, cols, gpu = batch.n_rows, pool.H * pool.d, _one_gpu(pool, batch)
+    ld = _rows_of(k, "k", n, cols, gpu)
+    if _rows_of(v, "v", n, cols, gpu) != ld and n > 1 or k.dtype != v.dtype:
         raise ValueError("k and v must share dtype and row stride")
     return ld if n > 1 else (cols + 7) // 8 * 8
 
@@ -674,17 +688,19 @@ def echo_kv_attention(pool: KVPool, batch: KVBatch, q, Hq: int | None = None, ca
                       out=None, workspace=None, stream=None):
     """Attention of the batch's rows, q bf16 [n_rows, Hq d], over their sequences' pages;
     Hq is q's columns over d when not given."""
-    n, bf16 = batch.n_rows, torch.bfloat16
-    Hq = q.shape[1] // pool.d if Hq is None else Hq
-    ldq = _rows_of(q, "q", n, Hq * pool.d)
+    n, bf16, gpu = batch.n_rows, torch.bfloat16, _one_gpu(pool, batch)
+    Hq = q.shape[-1] // pool.d if Hq is None else Hq
+    ldq = _rows_of(q, "q", n, Hq * pool.d, gpu)
     if out is None:
         out = _empty((n, Hq * pool.d), bf16, q.device, stream)
-    ldo = _rows_of(out, "out", n, Hq * pool.d)
+    ldo = _rows_of(out, "out", n, Hq * pool.d, gpu)
     if q.dtype != bf16 or out.dtype != bf16:
         raise TypeError(f"unsupported dtype {q.dtype if q.dtype != bf16 else out.dtype}")
     if workspace is None:
         workspace = _empty(echo_kv_attention_workspace_size(pool, batch, Hq), torch.uint8, q.device,
                            stream)
+    elif workspace.get_device() != gpu or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor on the pool's device")
     _check("echo_kv_attention", lib().echo_kv_attention(
         pool._ref, batch._ref, q.data_ptr(), ldq, Hq, causal_block, out.data_ptr(), ldo,
         workspace.data_ptr(), workspace.nbytes, _stream(stream)))
