@@ -1,10 +1,19 @@
 // Attention of new rows over the paged key/value cache: the entry point.
 #include "kv_pages.cuh"
 
+namespace {
+echo_status check_sizes(const echo_kv_pool *pool, const echo_kv_batch *batch, int32_t Hq, bool *empty) {
+    const echo_status s = echo::kv_check(pool, batch, empty);
+    if (s != ECHO_OK) return s;
+    if (Hq < pool->H || Hq % pool->H || Hq / pool->H > 128) return ECHO_ERR_SHAPE;
+    return (int64_t)batch->n_rows * Hq > INT32_MAX ? ECHO_ERR_SHAPE : ECHO_OK;
+}
+}  // namespace
+
 extern "C" size_t echo_kv_attention_workspace_size(const echo_kv_pool *pool, const echo_kv_batch *batch,
                                                    int32_t Hq) {
     bool empty;
-    if (Hq < 1 || echo::kv_check(pool, batch, &empty) != ECHO_OK) return 0;
+    if (check_sizes(pool, batch, Hq, &empty) != ECHO_OK) return 0;
     const size_t few = echo::kv_decode_workspace(*pool), many = echo::kv_chunk_workspace(*pool);
     return few > many ? few : many;
 }
@@ -15,12 +24,11 @@ extern "C" echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv
                                          echo_stream_t stream) {
     using namespace echo;
     bool empty;
-    const echo_status s = kv_check(pool, batch, &empty);
+    const echo_status s = check_sizes(pool, batch, Hq, &empty);
     if (s != ECHO_OK) return s;
-    if (Hq < pool->H || Hq % pool->H || Hq / pool->H > 128 || causal_block < 0) return ECHO_ERR_SHAPE;
+    if (causal_block < 0) return ECHO_ERR_SHAPE;
     if (ldq < (int64_t)Hq * pool->d || ldo < (int64_t)Hq * pool->d || ldq % 8 || ldo % 8)
         return ECHO_ERR_SHAPE;
-    if ((int64_t)batch->n_rows * Hq > INT32_MAX) return ECHO_ERR_SHAPE;
     if (empty) return ECHO_OK;
     if (!q || !out || !workspace || !aligned16(q) || !aligned16(out)) return ECHO_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ECHO_ERR_INVALID_ARG;

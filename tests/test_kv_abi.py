@@ -106,3 +106,13 @@ def test_binding_checks(ec):
                    torch.zeros(2, dtype=torch.int32), 1)
     with pytest.raises(ValueError, match="INT8 or"):
         ec.KVPool.empty(ec.CACHE_REF, 1, 16, 1, 64)
+
+
+def test_workspace_size_of_sizes_that_the_attention_refuses(ec):
+    def size(Hq, **batch):
+        p, b = ec.KVPoolC(**POOL), ec.KVBatchC(**{**BATCH, **batch})
+        return ec.lib().echo_kv_attention_workspace_size(ctypes.byref(p), ctypes.byref(b), Hq)
+
+    assert size(2) > 0 and size(256) > 0 and size(0, n_seqs=0) == 0
+    assert [size(Hq) for Hq in (-2, 0, 1, 3, 258)] == [0] * 5
+    assert size(2, n_rows=2 ** 30 - 1) > 0 and size(2, n_rows=2 ** 30) == 0
