@@ -507,6 +507,7 @@ echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, v
  *   workspace >= echo_kv_attention_workspace_size bytes, 256-byte aligned; it holds
  *   nothing between calls, and calls that may overlap each need their own.
  * A page that sets the PAGE flag is read as page 0: its sequence's result means nothing.
+ * A sequence longer than its table covers, or than 2^31 - 128 tokens, sets the flag, too.
  * The same call gives the same bits every time.
  * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA, UNSUPPORTED; TIMEOUT, PAGE device flags. */
 echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *q,

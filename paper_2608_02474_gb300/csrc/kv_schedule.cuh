@@ -55,6 +55,7 @@ struct KvWork {
 
 constexpr int kFixedUnits = 2;   // set-up and end of a piece, in key-block times
 constexpr int kLeast = 4;        // the fewest units for a worker
+constexpr int kMostKeys = INT32_MAX / 128 * 128;   // of a sequence: whole blocks and pages in 31 bits
 
 struct KvSeq {             // one sequence of the batch
     int row, packed, len;  // its first row, its packed rows, its length
@@ -447,7 +448,7 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
     w.by_tile = KvDiv(tile);
     w.by_block = KvDiv(a.causal_block > 0 ? a.causal_block : 1);
     w.slot_rows = slot_rows;
-    w.cap = (int)(cap < INT32_MAX ? cap : INT32_MAX);
+    w.cap = (int)(cap < kMostKeys ? cap : kMostKeys);
     w.block_shift = block_shift;
     w.workers = workers;
     w.split = cap > whole_keys;

@@ -99,3 +99,25 @@ def test_items_without_keys_among_rounds(ec, form, chunks):
         rows += [1, 1 + i % 2, 0]
     c = kv_case.make(form, 32, H, 64, lens, rows, seed=3)
     check(ec, c, 1, 1, 1000 if chunks else None)
+
+
+@FORMS
+@pytest.mark.parametrize("chunks", [False, True])
+def test_tables_that_pass_31_bits(ec, form, chunks):
+    """A table of 2^31 positions, one page over and over: the longest sequence is taken as far
+    as 31 bits go, and the one beside it is as ever."""
+    import torch
+    c = kv_case.make(form, 128, 1, 64, [200, 128], [2, 1], seed=4)
+    q = kv_case.queries(3, 64, 4)
+    want, mass = P.attend(c.pages, c.scale, c.table, c.lens, c.row0, q, 1, 1)
+    pool, batch = c.device(ec)
+    table = torch.full((2, 2 ** 24), int(c.table[1, 0]), dtype=torch.int32, device="cuda")
+    table[0, :2] = batch.table[0]
+    for n, status in ((128, 0), (2 ** 31 - 128, 0), (2 ** 31 - 127, 8), (2 ** 31 - 1, 8)):
+        lens = torch.tensor([200, n], dtype=torch.int32, device="cuda")
+        wide = ec.KVBatch(table, lens, batch.row0, 3, 1000 if chunks else 2)
+        out = ec.echo_kv_attention(pool, wide, torch.from_numpy(q).to("cuda", torch.bfloat16), causal_block=1)
+        out = out.float().cpu().numpy()
+        assert ec.echo_get_device_error() == status and np.isfinite(out).all()
+        rows = 3 if n == 128 else 2
+        assert (np.abs(out - want)[:rows] <= TOL * mass[:rows] + 1e-30).all()
