@@ -169,6 +169,16 @@ ECHO_DEV bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort, int
     }
 }
 
+// Wait for what is under way towards a barrier (copies, matrix products) before the memory that
+// it uses is given up: bounded, but whatever the other roles of the CTA have given up.
+ECHO_DEV void mbar_land(uint64_t *bar, uint32_t parity, uint64_t limit_ns = 100000000ull) {
+    const uint32_t a = smem_u32(bar);
+    if (mbar_try_wait(a, parity)) return;
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait(a, parity) && globaltimer_ns() - t0 <= limit_ns) {
+    }
+}
+
 // ---------------------------------------------------------------------------
 // TMA
 // ---------------------------------------------------------------------------

@@ -224,9 +224,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
                 ++loads;
             }
-            if (*abort_v)   // let this CTA's copies land before it exits
-                for (int i = max(0, loads - C::Q_BUFS); i < loads; ++i)
-                    mbar_wait(&sh.q_full[i % C::Q_BUFS], (i / C::Q_BUFS) & 1, abort_v, nullptr, 100000000ull);
+            // copies land before this CTA exits, whoever gives up, and when
+            for (int i = max(0, loads - C::Q_BUFS); i < loads; ++i)
+                mbar_land(&sh.q_full[i % C::Q_BUFS], (i / C::Q_BUFS) & 1);
         } else if (warp == 0) {
             // ---------------- keys and values, a page at a time ----------------
             const int shift = p.pool.shift, per_block = BN >> shift;
@@ -298,15 +298,12 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             // the last V has no K after it
             if (!INT8 && li > 0 && lane == 0) mbar_arrive(&sh.pair[((li - 1) >> 1) % PAIRS]);
-            if (*abort_v && lane == 0) {   // let this CTA's copies land before it exits
-                if (INT8) {
-                    for (int i = max(0, li - RING); i < li; ++i)
-                        mbar_wait(&sh.raw_full[i % RING], (i / RING) & 1, abort_v, nullptr, 100000000ull);
-                } else if (li > 0) {
-                    mbar_wait(&sh.k_first, 0, abort_v, nullptr, 100000000ull);
-                    for (int i = max(0, (li - 1) / 2 - PAIRS); i < (li - 1) / 2; ++i)
-                        mbar_wait(&sh.pair[i % PAIRS], (i / PAIRS) & 1, abort_v, nullptr, 100000000ull);
-                }
+            // copies land before this CTA exits, whoever gives up, and when
+            if (INT8) {
+                for (int i = max(0, li - RING); i < li; ++i) mbar_land(&sh.raw_full[i % RING], (i / RING) & 1);
+            } else if (li > 0) {
+                mbar_land(&sh.k_first, 0);
+                for (int i = max(0, li / 2 - PAIRS); i < li / 2; ++i) mbar_land(&sh.pair[i % PAIRS], (i / PAIRS) & 1);
             }
         } else if (warp == 1) {
             // ---------------- products of both tiles ----------------
@@ -621,7 +618,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             if (!ok && leader) {   // the MMAs already issued, before tensor memory is freed
                 tc_commit(&sh.drain);
-                mbar_wait(&sh.drain, 0, abort_v, nullptr, 100000000ull);
+                mbar_land(&sh.drain, 0);
             }
             __syncwarp();
         }

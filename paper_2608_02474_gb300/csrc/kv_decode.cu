@@ -193,9 +193,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 }
             }
         }
-        if (*abort_v && lane == 0)   // let this CTA's copies land before it exits
-            for (int i = max(0, g - C::RING); i < g; ++i)
-                mbar_wait(&full[i % C::RING], (i / C::RING) & 1, abort_v, nullptr, 100000000ull);
+        // copies land before this CTA exits, whoever gives up, and when
+        for (int i = max(0, g - C::RING); i < g; ++i) mbar_land(&full[i % C::RING], (i / C::RING) & 1);
         return;
     }
 
