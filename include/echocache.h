@@ -460,7 +460,8 @@ typedef struct {
  * row0[b] .. row0[b + 1] - 1 of the call's tensors are sequence b's new rows, n_b of
  * them (none is allowed), at its last positions: row row0[b] + i at position
  * len[b] - n_b + i, len counting the new rows.  row0 ascends from 0; rows at or past
- * row0[n_seqs] belong to no sequence and are neither read nor written. */
+ * row0[n_seqs] belong to no sequence: they are not written, and what they hold has no
+ * effect (it may be read). */
 typedef struct {
     const int32_t *table;  /* [n_seqs, max_pages]; read up to the page of len[b] - 1 */
     const int32_t *len;    /* [n_seqs], >= 0 */
@@ -499,6 +500,8 @@ echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, v
  * rows of any number).  A row that sees no key gives zeros.  A key that a row does not see
  * changes nothing in it, whatever its page holds there; NaN in a key, or a value that is not
  * finite, makes the rows that see it not finite.
+ * Values above 2^64 / len[b] may overflow: a row's running maximum moves only when a later
+ * weight passes 2^64.
  *   q bf16 [n_rows, ldq], out bf16 [n_rows, ldo]; Hq a multiple of H, Hq / H <= 128;
  *   n_rows Hq < 2^31; ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
  *   scales multiply scores and weights in fp32); sums, maxima and rescaling are fp32; the

@@ -47,7 +47,7 @@ ECHO_DEV uint32_t codes4(const float *f, float inv) {
 // rows' keys and values into the pages: piece c of a row is EP values of its keys first and
 // then of its values.  int8: 16, so that a division and the head's maximum (by shuffles) are
 // few beside the values; with 8, rintf and casts, 32760 rows of 40 heads of 128 took 272 us,
-// now 180.  A lane's values are 16-byte groups apart by the head's lanes, so that a warp
+// now 182.  A lane's values are 16-byte groups apart by the head's lanes, so that a warp
 // reads and writes whole stretches.
 template <typename T, bool INT8, int D>
 __global__ void __launch_bounds__(kThreads)

@@ -56,7 +56,7 @@ struct Cfg {
     // registers of warps 0-3, of four helpers and of four softmax warps: together at most
     // what the launch gives; the splits that were fastest.  4864 rows, 8 heads, bf16: 32768
     // keys of 128 354 us (72, 24, 208: 358), 8192 keys of 64 70 us (96, 48, 184: 73); int8
-    // 464 and 98 us (88, 40, 192: 524 and 114; 56, 56, 200: 472 and 101)
+    // 464 and 98 us (88, 40, 192: 524 and 114; 56, 56, 200: 472 and 101), since then 472 and 97
     static constexpr int REGS[3] = {INT8 ? 64 : 88, INT8 ? 64 : 40, 192};
     static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
                   "setmaxnreg takes from the launch's registers");
@@ -364,8 +364,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 // S(k + 3) goes over P(k) right after P V of item k has been issued, and
                 // S(k + 2), the tile's next block, is done while its softmax still works on
                 // item k.  With two buffers each tile's softmax waited for its products
-                // (4864 rows, 8192 keys, 8 heads of 64: 82 us, so 70); d 128, whose products
-                // take twice as long, has them at the tensor cores' rate with two.  S runs
+                // (4864 rows, 8192 keys, 8 heads of 64: 82 us, so 69); d 128, whose products
+                // take twice as long, has room for two only (tensor pipe 66 % active).  S runs
                 // ahead across pieces, whose queries have two buffers.  Issuing must not cost
                 // more than the 1024 cycles of a block's products: a commit takes about 80
                 // cycles and a wait 130, so V_f and K_{f+1} are freed by one commit, and
