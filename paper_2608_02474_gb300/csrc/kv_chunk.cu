@@ -365,7 +365,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 // S(k + 2), the tile's next block, is done while its softmax still works on
                 // item k.  With two buffers each tile's softmax waited for its products
                 // (4864 rows, 8192 keys, 8 heads of 64: 82 us, so 69); d 128, whose products
-                // take twice as long, has room for two only (tensor pipe 66 % active).  S runs
+                // take twice as long, has room for two only (tensor pipe 65 % active).  S runs
                 // ahead across pieces, whose queries have two buffers.  Issuing must not cost
                 // more than the 1024 cycles of a block's products: a commit takes about 80
                 // cycles and a wait 130, so V_f and K_{f+1} are freed by one commit, and
