@@ -23,8 +23,9 @@ rotary  the first 2 pairs columns of each head turned by the angle pos f: column
 int4    keys and values held in 4 bits in the pages (echo_kv_write_at, echo_kv_read,
         echo_kv_attention): 32 neighbouring values u of a head, in bf16, share a scale s, the
         least number of 5 significant bits at or above max |u| / 7 (at least 2^-112); a value's
-        code is the nearest whole number to u / s, halves away from zero, stored as code + 8,
-        the even column's in a byte's low half.  code s is exact in bf16.
+        code is the nearest whole number to u / s, halves away from zero, stored as code + 8.
+        Four bytes, a little-endian word, hold 8 columns: column 2 i in bits 4 i and up, column
+        2 i + 1 in bits 16 + 4 i and up.  code s is exact in bf16.
           pages uint8 [n_pages, 2, H, page, d / 2], scale bf16 [n_pages, 2, H, page, d / 32]
         A row at position p sees the keys below min(len, (p // cb + 1) cb), all where cb is 0.
 
@@ -515,19 +516,20 @@ def _store(s):
         step = (u.abs().amax(3) / torch.full((1,), 7.0, device=DEV)).clamp(min=2.0 ** -112)
         step = ((step.view(I32) + 0x7FFFF) & ~0x7FFFF).view(F32)
         x = u / step[..., None]
-        code = (torch.sign(x) * torch.floor(x.abs() + 0.5) + 8).to(torch.uint8).view(s["n"], c["H"], c["d"] // 2, 2)
+        code = (torch.sign(x) * torch.floor(x.abs() + 0.5) + 8).to(torch.uint8)
+        code = code.view(s["n"], c["H"], -1, 4, 2).transpose(3, 4).reshape(s["n"], c["H"], c["d"] // 2, 2)
         s["pages"][pg, i, :, at] = code[..., 0] | code[..., 1] << 4
         s["scale"][pg, i, :, at] = step.to(BF16)
 
 
+def _value(w, scale):
+    """What bytes and scales stand for, in 32 bits."""
+    code = torch.stack((w & 15, w >> 4), -1).view(*w.shape[:-1], -1, 2, 4).transpose(-1, -2).float() - 8
+    return (code.reshape(*w.shape[:-1], -1, 32) * scale.float()[..., None]).flatten(-2)
+
+
 def _values(s, pg, at):
-    """Keys and values at places of the pool, in 32 bits."""
-    out = []
-    for i in range(2):
-        w = s["pages"][pg, i, :, at]
-        code = torch.stack((w & 15, w >> 4), -1).float() - 8
-        out.append((code.view(*w.shape[:-1], -1, 32) * s["scale"][pg, i, :, at].float()[..., None]).flatten(-2))
-    return out
+    return [_value(s["pages"][pg, i, :, at], s["scale"][pg, i, :, at]) for i in range(2)]
 
 
 def _attend(s):
@@ -536,10 +538,8 @@ def _attend(s):
     H, d, B = c["H"], c["d"], c["seqs"]
     G, R, n = c["Hq"] // H, s["rows"], s["n"]
     ids = s["table"].clamp(min=0).long()
-    w = s["pages"][ids]                                            # [B, pages, 2, H, page, d / 2]
-    x = torch.stack((w & 15, w >> 4), -1).float() - 8
-    x = x.view(*w.shape[:-1], d // 32, 32) * s["scale"][ids].float()[..., None]
-    kv = x.view(*w.shape[:-1], d).permute(2, 0, 3, 1, 4, 5).reshape(2, B, H, -1, d)
+    kv = _value(s["pages"][ids], s["scale"][ids])                  # [B, pages, 2, H, page, d]
+    kv = kv.permute(2, 0, 3, 1, 4, 5).reshape(2, B, H, -1, d)
     L = kv.shape[3]
     r = torch.arange(n, device=DEV)
     b = torch.bucketize(r, s["row0"][1:], right=True)
@@ -635,9 +635,11 @@ def _exact_attend(c, s):
         ids = s["table"][b, :-(-n // page)].long()
         kv = []
         for i in range(2):
-            w = s["pages"][ids, i].transpose(1, 2).flatten(0, 1)[:n]            # [n, H, d / 2]
+            w = s["pages"][ids, i].transpose(1, 2).flatten(0, 1)[:n].to(I64)    # [n, H, d / 2]
+            word = w[..., 0::4] + 256 * w[..., 1::4] + 65536 * w[..., 2::4] + 16777216 * w[..., 3::4]
             x = torch.empty(n, H, d, dtype=F64, device=DEV)
-            x[..., 0::2], x[..., 1::2] = (w % 16).to(F64) - 8, torch.div(w, 16, rounding_mode="floor").to(F64) - 8
+            for col in range(8):
+                x[..., col::8] = ((word >> (4 * (col // 2) + 16 * (col % 2))) % 16 - 8).to(F64)
             sc = s["scale"][ids, i].transpose(1, 2).flatten(0, 1)[:n].to(F64)
             kv.append(x * sc.repeat_interleave(32, dim=2))
         at = slice(first, first + rows[b])
