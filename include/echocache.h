@@ -220,7 +220,10 @@ echo_status echo_select_static(const void *x, echo_dtype xt, const int8_t *cache
  *                    size; seg_len = W' makes a segment one spatial row of a
  *                    latent frame ("adjacent latents").
  * All buffers are device memory owned by the caller, 16-byte aligned. */
-typedef enum { ECHO_CACHE_INT8 = 0, ECHO_CACHE_BF16 = 1, ECHO_CACHE_REF = 2 } echo_cache_kind;
+/* ECHO_CACHE_INT4: pages of keys and values only (echo_kv_pool) */
+typedef enum {
+    ECHO_CACHE_INT8 = 0, ECHO_CACHE_BF16 = 1, ECHO_CACHE_REF = 2, ECHO_CACHE_INT4 = 3
+} echo_cache_kind;
 
 typedef struct {
     int32_t kind;       /* echo_cache_kind */
@@ -445,15 +448,23 @@ echo_status echo_cache_dequant(const int8_t *q, const float *scale, const int32_
  * so that a head's tokens lie side by side.  kind ECHO_CACHE_BF16 keeps the values;
  * ECHO_CACHE_INT8 keeps codes with one scale per token and head (Q of
  * echo_cache_quant over a head's d values; a value of 0 has code 0 where 127 / a is
- * infinite, too), for keys and values apart.
+ * infinite, too), for keys and values apart.  ECHO_CACHE_INT4 keeps 4-bit codes with one
+ * scale per 32 neighbouring values u of a head, taken in bf16:
+ *   s = the least number of 5 significant bits at or above max |u| / 7, and 2^-112 at least,
+ *   code = the whole number nearest to u / s, halves away from zero: -7 .. 7,
+ * stored as code + 8: four bytes, a little-endian word, hold 8 columns, column 2 i in bits 4 i
+ * and up, column 2 i + 1 in bits 16 + 4 i and up.  The value code s is exact in bf16.
  * Pages need no initial contents: nothing at or past a sequence's length is used. */
 typedef struct {
-    int32_t kind;          /* ECHO_CACHE_INT8 or ECHO_CACHE_BF16 */
+    int32_t kind;          /* ECHO_CACHE_INT8, ECHO_CACHE_BF16 or ECHO_CACHE_INT4 */
     int32_t n_pages;       /* >= 1; 2 n_pages H < 2^31 - 1 */
     int32_t page_tokens;   /* 16, 32, 64 or 128 */
     int32_t H, d;          /* key/value heads; d 64 or 128 */
-    void *pages;           /* int8 or bf16 [n_pages, 2, H, page_tokens, d], 16-byte aligned */
-    float *scale;          /* INT8: f32 [n_pages, 2, H, page_tokens], 16-byte aligned; else unused */
+    void *pages;           /* int8 or bf16 [n_pages, 2, H, page_tokens, d], INT4: uint8 [.., d / 2],
+                            * 16-byte aligned */
+    void *scale;           /* INT8: f32 [n_pages, 2, H, page_tokens], INT4: bf16 [n_pages, 2, H,
+                            * page_tokens, d / 32] of at most 5 significant bits; 16-byte aligned;
+                            * BF16: unused */
 } echo_kv_pool;
 
 /* The sequences of one call, in device memory (int32, 4-byte aligned).  Rows
@@ -473,8 +484,9 @@ typedef struct {
 } echo_kv_batch;
 
 /* The new rows' keys and values into the pages: k, v [n_rows, ld] of dtype t (head h at
- * columns h d ..; ld a multiple of 8), rounded to bf16 (BF16) or quantised (INT8).
- * Rows at a position below 0 are left out.  A non-finite head's row of an INT8 pool gets
+ * columns h d ..; ld a multiple of 8), rounded to bf16 (BF16) or quantised (INT8, INT4).
+ * Rows at a position below 0 are left out.  A non-finite head's row of an INT8 pool, or a
+ * non-finite group of 32 of an INT4 pool, gets
  * codes 0 and its |maximum| as scale, and sets the NONFINITE device flag; a position
  * whose table entry is no page of the pool, or lies past max_pages, sets the PAGE flag
  * and is left out.  No two sequences write the same page slot.
@@ -482,9 +494,19 @@ typedef struct {
 echo_status echo_kv_write(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *k,
                           const void *v, int64_t ld, echo_dtype t, echo_stream_t stream);
 
+/* echo_kv_write by a slot map: row r's keys and values go to token place[r] mod page_tokens
+ * of page place[r] / page_tokens.  place int64 [n_rows], 8-byte aligned, as echo_kv_extend
+ * makes it; any rows of any sequences, so that tokens which are refreshed go over their old
+ * values.  A negative place leaves its row out; one past the pool does, too, and sets the
+ * PAGE flag.  No two rows have the same place.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED; NONFINITE, PAGE device flags. */
+echo_status echo_kv_write_at(const echo_kv_pool *pool, const int64_t *place, int32_t n_rows,
+                             const void *k, const void *v, int64_t ld, echo_dtype t,
+                             echo_stream_t stream);
+
 /* The cached keys and values of the positions that the batch's rows stand at, into
  * k, v [n_rows, ld] of dtype t: the bf16 values, or float(code) * scale in fp32, rounded
- * to nearest even for BF16.  Whole sequences: n_b = len[b].  Rows at a position below 0,
+ * to nearest even for BF16 (INT4: exact in both).  Whole sequences: n_b = len[b].  Rows at a position below 0,
  * or at one that sets the PAGE flag (echo_kv_write), are zeros.
  * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
 echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, void *k, void *v,
@@ -504,7 +526,7 @@ echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, v
  * weight passes 2^64.
  *   q bf16 [n_rows, ldq], out bf16 [n_rows, ldo]; Hq a multiple of H, Hq / H <= 128;
  *   n_rows Hq < 2^31; ldq, ldo multiples of 8.  Codes and scales enter unrounded (codes are exact in bf16,
- *   scales multiply scores and weights in fp32); sums, maxima and rescaling are fp32; the
+ *   INT8 scales multiply scores and weights in fp32, INT4 values are exact in bf16); sums, maxima and rescaling are fp32; the
  *   softmax weights (INT8: times the value's scale) are rounded to bf16 for the product
  *   with the values.
  *   workspace >= echo_kv_attention_workspace_size bytes, 256-byte aligned; it holds
@@ -521,6 +543,165 @@ echo_status echo_kv_attention(const echo_kv_pool *pool, const echo_kv_batch *bat
  * their sizes alone); 0 for sizes that it refuses. */
 size_t echo_kv_attention_workspace_size(const echo_kv_pool *pool, const echo_kv_batch *batch,
                                         int32_t Hq);
+
+/* ---- page tables and slot maps on the device (this build's addition) ----
+ *
+ * The bookkeeping of a pool in device memory, so that a step whose sequences grow needs
+ * nothing from the host and can be captured in a graph: each sequence that is kept has a
+ * slot, a row of `table`, and pages are taken from and given back to a stack.  The caller owns the four
+ * arrays (4-byte aligned); echo_kv_tables_reset makes them those of an empty pool. */
+typedef struct {
+    int32_t n_pages;       /* of the pools that the tables serve, >= 1 */
+    int32_t page_tokens;   /* 16, 32, 64 or 128 */
+    int32_t n_slots;       /* 1 .. 262144 */
+    int32_t max_pages;     /* of one slot, >= 1; n_slots max_pages < 2^31 */
+    int32_t *table;        /* [n_slots, max_pages]: a slot's pages in order, the first
+                            * ceil(len / page_tokens) of them */
+    int32_t *len;          /* [n_slots]: tokens of each */
+    int32_t *free_pages;   /* [n_pages]: the free pages are entries 0 .. *n_free - 1 */
+    int32_t *n_free;       /* [1] */
+} echo_kv_tables;
+
+/* No tokens in any slot, all pages free, page 0 the first to be taken.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
+echo_status echo_kv_tables_reset(const echo_kv_tables *t, echo_stream_t stream);
+
+/* Room for rows[b] >= 0 more tokens in slot slots[b] (slots NULL: b) for b < n_seqs, and the
+ * batch and slot map of these new rows.  With have = ceil(len / page_tokens) before and want
+ * after, page j of sequence b, have_b <= j < want_b, becomes
+ *   free_pages[*n_free - 1 - (before_b + j - have_b)],   before_b: pages of the sequences before.
+ *   table   [n_seqs, max_pages] or NULL: each sequence's pages, the entries that it uses (the
+ *           others are left as they were); len [n_seqs] with the new rows and row0 [n_seqs + 1]:
+ *           an echo_kv_batch.  Without slots, t->table itself may serve as the batch's table.
+ *   place   int64 [n_rows] (8-byte aligned), pos int32 [n_rows], seq int32 [n_rows], each or NULL:
+ *           for row r of sequence b, at position p = len_b - rows_b + r - row0[b]: the page times
+ *           page_tokens plus p mod page_tokens; p; b.  -1 for rows behind the last sequence's.
+ * n_rows: the most rows in all.  One launch; slots, rows, len, row0, table, pos, seq 4-byte aligned.
+ * A call that cannot be served (not enough pages, more than n_rows rows or max_pages pages or 2^31 - 128
+ * tokens, rows below 0, a slot that does not exist or comes twice, tables that are no tables) changes
+ * nothing in t and sets the PAGE flag; its row0, then, is 0 throughout, its place, pos and seq
+ * are -1 and its table is left as it was, so that what follows writes no row.
+ * Calls on the same tables run in order (one stream, or events between streams).
+ * Errors: INVALID_ARG, SHAPE (n_seqs not in 0 .. 8192), CUDA, UNSUPPORTED; PAGE device flag. */
+echo_status echo_kv_extend(const echo_kv_tables *t, const int32_t *slots, const int32_t *rows,
+                           int32_t n_seqs, int32_t n_rows, int32_t *table, int32_t *len,
+                           int32_t *row0, int64_t *place, int32_t *pos, int32_t *seq,
+                           echo_stream_t stream);
+
+/* The last rows[b] >= 0 tokens of slot slots[b] (slots NULL: b) are given up, all of them where it has
+ * fewer, and with them the pages that nothing else needs.  They go onto the stack in the order that undoes an
+ * echo_kv_extend of the same rows.  Rejected drafts, a step that failed, a clip that ends.
+ * A call that cannot be served (rows below 0, a slot that does not exist or comes twice,
+ * tables that are no tables) changes nothing and sets the PAGE flag.
+ * Errors: INVALID_ARG, SHAPE (n_seqs not in 0 .. 8192), CUDA, UNSUPPORTED; PAGE device flag. */
+echo_status echo_kv_shorten(const echo_kv_tables *t, const int32_t *slots, const int32_t *rows,
+                            int32_t n_seqs, echo_stream_t stream);
+
+/* ---- rotary positions (this build's addition) ---- */
+
+typedef enum { ECHO_ROTARY_PAIRS = 0, ECHO_ROTARY_HALVES = 1 } echo_rotary_layout;
+typedef enum {
+    ECHO_SCALING_NONE = 0,
+    ECHO_SCALING_LINEAR = 1,   /* positions divided by factor */
+    ECHO_SCALING_NTK = 2,      /* theta times factor^(n / (n - 1)), n pairs of the axis: the slowest pair
+                                * turns factor times more slowly, the fastest as before */
+    ECHO_SCALING_YARN = 3      /* "NTK by parts" (arXiv 2309.00071): a pair that turns beta_fast
+                                * times or more within `original` positions keeps its frequency, one that turns
+                                * beta_slow times or less gets it divided by factor, between them linearly in
+                                * the turns; the turned columns times 0.1 ln(factor) + 1 */
+} echo_scaling;
+
+/* Which columns of a head turn with which position.  Pair i of axis a (its n_a pairs come after those
+ * of the axes before) turns by the angle p_a f_i, f_i = theta^(-i / n_a) before scaling. */
+typedef struct {
+    int32_t layout;          /* echo_rotary_layout: columns 2 i and 2 i + 1, or i and i + pairs */
+    int32_t axes;            /* 1 .. 4 */
+    int32_t axis_pairs[4];   /* pairs of each axis, >= 0; `pairs`, their sum, >= 1 and <= d / 2 */
+    int32_t frame_tokens;    /* > 0: a row has one position, a token index t, and three axes:
+                              * t / frame_tokens, t mod frame_tokens / row_tokens, and
+                              * the rest; frame_tokens a multiple of row_tokens */
+    int32_t row_tokens;
+    float size;              /* factor of the turned columns, finite */
+    const uint64_t *turn;    /* device, [pairs], 8-byte aligned: f_i / (2 pi) as a fraction of
+                              * 2^64, from echo_rotary_turns */
+} echo_rotary_plan;
+
+typedef struct {
+    double theta;                 /* >= 1 */
+    int32_t scaling;              /* echo_scaling */
+    double factor;                /* >= 1 */
+    double original;              /* YARN: positions of the context before scaling, > 0 */
+    double beta_fast, beta_slow;  /* YARN: turns, fast > slow >= 0; 32 and 1 in the paper */
+} echo_rotary_params;
+
+/* Host function: the turns per position of all pairs of `axis_pairs` (axes of them), into host memory
+ * turn[pairs], and the factor of the turned columns (1 but for YARN).  fp64, so that an angle is off by
+ * 2^-52 turns per position at most.  Errors: INVALID_ARG (parameters), SHAPE (axes, pairs). */
+echo_status echo_rotary_turns(const echo_rotary_params *p, int32_t axes, const int32_t *axis_pairs,
+                              uint64_t *turn, float *size);
+
+/* Queries and keys turned by their rows' positions:
+ *   (y1, y2) = size (x1 cos a - x2 sin a, x2 cos a + x1 sin a),  a = sum of the pair's axis: p f,
+ * for each pair (x1, x2) of each head; the columns past 2 pairs stay as they are.  inverse != 0:
+ * with -a, size unchanged, which is the transposed map, and so the gradient of the map itself.
+ * Angles are taken as p times the 64-bit fraction of a turn, modulo 1: exact for any position.
+ *   pos  int32 [n_rows, axes] (frame_tokens > 0: [n_rows]), 4-byte aligned.  A row with a negative position is left
+ *        as it was, in q_out and k_out, too: rows behind the last sequence.
+ *   q [n_rows, ldq] with Hq heads of d columns, k [n_rows, ldk] with Hk, dtype t; d a multiple of 8, at most 256;
+ *   q_out and k_out may be q and k, or share nothing with either input.  k and k_out NULL, Hk 0: queries only.
+ *   Strides multiples of 8, at least heads times d; base addresses 16-byte aligned.
+ * fp32 arithmetic, one rounding to t at the end.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
+echo_status echo_rotary(const echo_rotary_plan *plan, const int32_t *pos, int32_t n_rows, int32_t d,
+                        echo_dtype t, int32_t inverse, const void *q, int64_t ldq, int32_t Hq,
+                        void *q_out, int64_t ldqo, const void *k, int64_t ldk, int32_t Hk,
+                        void *k_out, int64_t ldko, echo_stream_t stream);
+
+/* ---- norms around a gated residual (this build's addition) ---- */
+
+typedef enum { ECHO_NORM_NONE = 0, ECHO_NORM_LAYER = 1, ECHO_NORM_RMS = 2 } echo_norm_kind;
+
+/* One norm over a row of D values: LAYER (v - mean) / sqrt(variance + eps), the biased variance; RMS
+ * v / sqrt(mean of squares + eps); then times weight, plus bias, where there are any. */
+typedef struct {
+    int32_t kind;            /* echo_norm_kind */
+    float eps;               /* >= 0, finite */
+    const float *weight;     /* f32 [D], 16-byte aligned, or NULL */
+    const float *bias;       /* f32 [D], 16-byte aligned, or NULL */
+} echo_norm;
+
+typedef struct {
+    int32_t D;               /* multiple of 8, 8 .. 16384 */
+    echo_norm after;         /* of the branch's output y */
+    echo_norm before;        /* of the new residual, for the next branch */
+    float alpha, beta;       /* finite */
+} echo_gated_norm_plan;
+
+/* The modulations of a call: rows of `dtype`, each or NULL.  Row r takes row m = rows[r] of the
+ * three, or r / rows_per_mod where rows is NULL.  A row whose m is not in 0 .. n_mods - 1 belongs to
+ * no sequence: h and n are left as they were there. */
+typedef struct {
+    const void *gate, *scale, *shift;   /* [n_mods, ld], 16-byte aligned */
+    int64_t ld;                         /* multiple of 8, >= D */
+    int32_t n_mods, rows_per_mod;       /* rows_per_mod >= 1 where rows is NULL */
+    const int32_t *rows;                /* [n_rows], 4-byte aligned, or NULL */
+    echo_dtype t;
+} echo_modulation;
+
+/* The end of one branch of a block and the beginning of the next in one pass over the rows:
+ *   h = alpha x + beta gate * N_after(y)        (y NULL: h = alpha x; gate NULL: ones)
+ *   n = N_before(h) * (1 + scale) + shift       (scale NULL: zeros; shift NULL: zeros)
+ * x [n_rows, ldx] of xt, y [n_rows, ldy] of yt, h [n_rows, ldh] of ht, n [n_rows, ldn] of nt; h or n may
+ * be NULL.  h may be x or y, and n may be x or y (of the same type and stride), but not one another.  n is
+ * made from h as it is before its rounding.  mod NULL: no modulations, every row.
+ * Mean first, then the centred squares, in fp32 in an order that depends on D and n_rows only.
+ * Strides multiples of 8; base addresses 16-byte aligned.
+ * Errors: INVALID_ARG, SHAPE, CUDA, UNSUPPORTED. */
+echo_status echo_gated_norm(const echo_gated_norm_plan *plan, const echo_modulation *mod,
+                            int32_t n_rows, const void *x, int64_t ldx, echo_dtype xt,
+                            const void *y, int64_t ldy, echo_dtype yt, void *h, int64_t ldh,
+                            echo_dtype ht, void *n, int64_t ldn, echo_dtype nt,
+                            echo_stream_t stream);
 
 /* ---- single kernels of echo_block_step, exported so that each can be
  *      checked and timed on its own ---- */
@@ -571,7 +752,8 @@ typedef enum {
     ECHO_K_DEQUANT = 8, ECHO_K_MERGE = 9, ECHO_K_STEP_DELTA = 10, ECHO_K_UNIFORM = 11,
     ECHO_K_REF_SCAN = 12, ECHO_K_REF_ALLOC = 13, ECHO_K_REF_STORE = 14, ECHO_K_CACHE_COPY = 15,
     ECHO_K_MERGE_QUANT = 16, ECHO_K_KV_WRITE = 17, ECHO_K_KV_READ = 18,
-    ECHO_K_KV_ATTENTION = 19, ECHO_K_KV_JOIN = 20, ECHO_K_COUNT = 21
+    ECHO_K_KV_ATTENTION = 19, ECHO_K_KV_JOIN = 20, ECHO_K_KV_TABLES = 21, ECHO_K_ROTARY = 22,
+    ECHO_K_GATED_NORM = 23, ECHO_K_COUNT = 24
 } echo_kernel_kind;
 
 /* Number of kernels this library has launched in this process (all devices). */
@@ -592,7 +774,8 @@ echo_status echo_profile_enable(int32_t on);
  * for the reduction and (0, 0, blocks) for its final combine; UNIFORM (NT, K, 0);
  * REF_SCAN, REF_ALLOC, REF_STORE, CACHE_COPY (rows, D, 0); MERGE_QUANT (NT, D, K active
  * rows); KV_WRITE, KV_READ (rows, H d, 0); KV_ATTENTION (rows, Hq d, sequences),
- * KV_JOIN (rows, Hq d, CTAs that shared the work). */
+ * KV_JOIN (rows, Hq d, CTAs that shared the work); KV_TABLES (rows, sequences, 0 extend, 1
+ * shorten, 2 reset); ROTARY (rows, (Hq + Hk) d, 2 pairs); GATED_NORM (rows, D, mods). */
 int32_t echo_profile_read(int32_t max, int32_t *kinds, int64_t *m, int64_t *n, int64_t *k,
                           float *ms);
 

@@ -95,15 +95,16 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
 bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows) {
     const EncodeTiledFn encode = encode_fn();
     if (!encode) return false;
-    const bool int8 = pool.kind == ECHO_CACHE_INT8;
-    const cuuint64_t d = (cuuint64_t)pool.d, row = int8 ? d : 2 * d;
-    cuuint64_t gdim[3] = {d, (cuuint64_t)pool.page_tokens, 2ull * (cuuint64_t)pool.n_pages * (cuuint64_t)pool.H};
+    const bool bf16 = pool.kind == ECHO_CACHE_BF16;
+    const cuuint64_t d = (cuuint64_t)pool.d, row = bf16 ? 2 * d : pool.kind == ECHO_CACHE_INT8 ? d : d / 2;
+    cuuint64_t gdim[3] = {bf16 ? d : row, (cuuint64_t)pool.page_tokens, 2ull * (cuuint64_t)pool.n_pages * (cuuint64_t)pool.H};
     cuuint64_t gstride[2] = {row, row * (cuuint64_t)pool.page_tokens};
-    cuuint32_t box[3] = {int8 ? (cuuint32_t)d : 64u, box_rows, 1};
+    cuuint32_t box[3] = {bf16 ? 64u : (cuuint32_t)row, box_rows, 1};
     cuuint32_t estride[3] = {1, 1, 1};
-    CUresult r = encode(m, int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+    CUresult r = encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
                         pool.pages, gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        int8 && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                        row >= 128 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                   : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
 }
@@ -224,7 +225,7 @@ extern "C" const char *echo_kernel_name(int32_t kind) {
         "dequant_gather",     "dequant_merge", "step_delta",   "uniform_select",
         "ref_scan",           "ref_alloc",     "ref_store",    "cache_copy",
         "merge_quant",        "kv_write",      "kv_read",      "kv_attention",
-        "kv_join"};
+        "kv_join",           "kv_tables",     "rotary",        "gated_norm"};
     if (kind < 0 || kind >= ECHO_K_COUNT) return "unknown";
     return names[kind];
 }

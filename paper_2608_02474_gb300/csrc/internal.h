@@ -74,7 +74,7 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
                     uint32_t box_rows);
 
 // a pool of key/value pages as [z, page_tokens, d], z = (page, keys or values, head): bf16 in
-// boxes of 64 columns, int8 codes in whole rows, box_rows tokens; swizzled by the box's width
+// boxes of 64 columns, int8 and 4-bit codes in whole rows, box_rows tokens; swizzled by the box's width
 bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
 
 // bf16 rows of heads [n_rows, H, d] (row stride ld elements) in boxes of box_rows rows and

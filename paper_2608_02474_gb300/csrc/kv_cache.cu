@@ -44,16 +44,29 @@ ECHO_DEV uint32_t codes4(const float *f, float inv) {
     return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
 }
 
+// place of row r in the pool, as kv_place: by the slot map where there is one; -1: none
+ECHO_DEV int64_t row_place(const KvPool &pool, const KvBatch &b, const int64_t *place, int r, int *err) {
+    if (place) {
+        const int64_t at = place[r];
+        if (at >> pool.shift < pool.n_pages) return at;      // -1 .. : left out
+        echo_flag_error(err, ECHO_ERR_PAGE);
+        return -1;
+    }
+    const KvRow row = kv_find_row(b, r);
+    return row.seq < 0 || row.p < 0 ? -1 : kv_place(pool, b, row.seq, row.p, err);
+}
+
 // rows' keys and values into the pages: piece c of a row is EP values of its keys first and
 // then of its values.  int8: 16, so that a division and the head's maximum (by shuffles) are
 // few beside the values; with 8, rintf and casts, 32760 rows of 40 heads of 128 took 272 us,
 // now 182.  A lane's values are 16-byte groups apart by the head's lanes, so that a warp
 // reads and writes whole stretches.
-template <typename T, bool INT8, int D>
+template <typename T, int FORM, int D>
 __global__ void __launch_bounds__(kThreads)
-kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, const T *__restrict__ v,
-                int64_t ld, int *err) {
+kv_write_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ place, const T *__restrict__ k,
+                const T *__restrict__ v, int64_t ld, int *err) {
     pdl_enter();
+    constexpr bool INT8 = FORM == kInt8;
     constexpr int GE = kPer16<T>, EP = INT8 ? 16 : 8, NG = EP / GE, LPH = D / EP;   // lanes of a head
     constexpr int U = kLoads / NG;
     const int lane = threadIdx.x & 31;
@@ -72,9 +85,7 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
                 for (int h = 0; h < NG; ++h) in[u][h] = __ldcs(reinterpret_cast<const uint4 *>(src + h * (D / NG)));
             }
         }
-        const KvRow row = kv_find_row(b, r);
-        if (row.seq < 0 || row.p < 0) continue;
-        const int64_t at = kv_place(pool, b, row.seq, row.p, err);
+        const int64_t at = row_place(pool, b, place, r, err);
         if (at < 0) continue;
         const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
 #pragma unroll
@@ -115,7 +126,7 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
                     }
                 }
                 if (ch % LPH == 0) {
-                    pool.scale[vec] = !bad ? __fdiv_rn(amax, 127.f)
+                    static_cast<float *>(pool.scale)[vec] = !bad ? __fdiv_rn(amax, 127.f)
                                            : a > 0x7F800000u ? __int_as_float(0x7fc00000) : INFINITY;
                     if (bad) echo_flag_error(err, ECHO_ERR_NONFINITE);
                 }
@@ -135,14 +146,95 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const T *__restrict__ k, con
     }
 }
 
+// The same into 4-bit pages: 8 neighbouring columns of a lane, four lanes to a scale.  Values are
+// taken in bf16 first, so that max |u| / 7, rounded up to 5 significant bits, and u / s have few bits:
+// with 1 / s a little too large (2^-22), the halves between two codes, and nothing else, pass
+// over to the larger one, and one fused multiply-add rounds the quotient (codes4).
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ place, const T *__restrict__ k,
+                 const T *__restrict__ v, int64_t ld, int *err) {
+    pdl_enter();
+    constexpr int NG = 8 / kPer16<T>, LPH = D / 8, U = kLoads / NG;
+    const int lane = threadIdx.x & 31;
+    const int half = pool.H * LPH, C = 2 * half;      // pieces of a row
+    const int tasks = (C + 32 * U - 1) / (32 * U);
+    PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
+    for (; walk.below(b.n_rows); walk.next()) {
+        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
+        uint4 in[U][NG];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + 32 * u;
+#pragma unroll
+            for (int h = 0; h < NG; ++h) {
+                in[u][h] = make_uint4(0u, 0u, 0u, 0u);
+                if (c < C)
+                    in[u][h] = __ldcs(reinterpret_cast<const uint4 *>((c < half ? k : v) + r * ld +
+                                                                      (int64_t)(c < half ? c : c - half) * 8) + h);
+            }
+        }
+        const int64_t at = row_place(pool, b, place, r, err);
+        if (at < 0) continue;
+        const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + 32 * u;
+            uint4 w = in[u][0];                       // 8 values in bf16
+            if constexpr (NG == 2) {
+                float f[8];
+                values16<T>(in[u][0], f);
+                values16<T>(in[u][NG - 1], f + 4);
+                w = pack8_bf16(f);
+            }
+            uint32_t lo = 0, hi = 0;                  // the largest |value|, as warp_amax_bf16
+            const uint32_t pair[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo = max(lo, pair[i] & 0x7FFFu);
+                hi = max(hi, pair[i] & 0x7FFF0000u);
+            }
+            uint32_t a = max(lo << 16, hi);
+            a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+            a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+            if (c >= C) continue;
+            const bool bad = a >= 0x7F800000u;
+            const float s = fmaxf(__uint_as_float((__float_as_uint(__fdiv_rn(__uint_as_float(a), 7.f)) + 0x7FFFFu) & ~0x7FFFFu),
+                                  1.92592994438723585e-34f);          // 2^-112
+            const float inv = __fmul_rn(__frcp_rn(s), 1.f + 0x1p-22f);
+            uint32_t codes = 0x88888888u;             // zeros
+            if (!bad) {
+                codes = 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // 1.5 2^23 + 8 + code: the code, plus 8, in its low bits
+                    const uint32_t even = __float_as_uint(__fmaf_rn(bf16lo(pair[i]), inv, 12582920.f)) & 15u;
+                    const uint32_t odd = __float_as_uint(__fmaf_rn(bf16hi(pair[i]), inv, 12582920.f)) & 15u;
+                    codes |= even << (4 * i) | odd << (16 + 4 * i);
+                }
+            }
+            const int kv = c >= half, ch = kv ? c - half : c;
+            const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
+            *reinterpret_cast<uint32_t *>(pool.pages + vec * (D / 2) + ch % LPH * 4) = codes;
+            if ((lane & 3) == 0) {
+                // the scale's low 16 bits are zeros; what is not finite stands as it is
+                static_cast<uint16_t *>(pool.scale)[vec * (D / 32) + ch % LPH / 4] = (uint16_t)((bad ? a : __float_as_uint(s)) >> 16);
+                if (bad) echo_flag_error(err, ECHO_ERR_NONFINITE);
+            }
+        }
+    }
+}
+
 // cached rows back: piece c of a row is 16 bytes of what is stored, so that a warp stores
 // whole stretches
-template <typename T, bool INT8, int D>
+template <typename T, int FORM, int D>
 __global__ void __launch_bounds__(kThreads)
 kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restrict__ v, int64_t ld,
                int *err) {
     pdl_enter();
-    constexpr int EP = kPer16<T>, BYTES = EP * (INT8 ? 1 : 2), LPH = D / EP, U = BYTES == 16 ? kLoads : 2 * kLoads;
+    constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4;
+    constexpr int EP = kPer16<T>, BYTES = kv_bytes(FORM, EP), LPH = D / EP, U = BYTES == 16 ? kLoads : 2 * kLoads;
+    constexpr int WORDS = (BYTES + 3) / 4;
     const int lane = threadIdx.x & 31;
     const int half = pool.H * LPH, C = 2 * half;
     const int tasks = (C + 32 * U - 1) / (32 * U);
@@ -153,18 +245,18 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
         if (row.seq < 0) continue;
         const int64_t at = row.p < 0 ? -1 : kv_place(pool, b, row.seq, row.p, err);   // -1: zeros
         const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
-        uint32_t in[U][BYTES / 4];
+        uint32_t in[U][WORDS];
         float sc[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
 #pragma unroll
-            for (int i = 0; i < BYTES / 4; ++i) in[u][i] = 0u;
+            for (int i = 0; i < WORDS; ++i) in[u][i] = 0u;
             sc[u] = 0.f;
             if (c >= C || at < 0) continue;
             const int kv = c >= half, ch = kv ? c - half : c;
             const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            const uint8_t *src = pool.pages + vec * D * (INT8 ? 1 : 2) + ch % LPH * BYTES;
+            const uint8_t *src = pool.pages + vec * kv_bytes(FORM, D) + (INT4 ? ch % LPH * EP / 8 * 4 : ch % LPH * BYTES);
             if constexpr (BYTES == 16) {
                 const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(src));
                 in[u][0] = w.x, in[u][1] = w.y, in[u][2] = w.z, in[u][3] = w.w;
@@ -174,7 +266,9 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
             } else {
                 in[u][0] = __ldcs(reinterpret_cast<const uint32_t *>(src));
             }
-            if constexpr (INT8) sc[u] = pool.scale[vec];
+            if constexpr (INT8) sc[u] = static_cast<const float *>(pool.scale)[vec];
+            if constexpr (INT4)
+                sc[u] = __uint_as_float((uint32_t)static_cast<const uint16_t *>(pool.scale)[vec * (D / 32) + ch % LPH * EP / 32] << 16);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -183,7 +277,12 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
             float f[EP];
 #pragma unroll
             for (int i = 0; i < EP; ++i) {
-                if constexpr (INT8) f[i] = __fmul_rn((float)(int8_t)(in[u][i >> 2] >> (8 * (i & 3))), sc[u]);
+                if constexpr (INT4) {
+                    // columns 2 i and 2 i + 1 of 8 in bits 4 i and 16 + 4 i; fp32: four of them a lane
+                    const int col = EP == 8 ? i : i + 4 * (c & 1);
+                    f[i] = __fmul_rn((float)((int)(in[u][0] >> (4 * (col >> 1) + 16 * (col & 1)) & 15u) - 8), sc[u]);
+                    if (at < 0) f[i] = 0.f;
+                } else if constexpr (INT8) f[i] = __fmul_rn((float)(int8_t)(in[u][i >> 2] >> (8 * (i & 3))), sc[u]);
                 else f[i] = i & 1 ? bf16hi(in[u][i >> 1]) : bf16lo(in[u][i >> 1]);
             }
             store16<T>((c >= half ? v : k) + r * ld + (int64_t)(c >= half ? c - half : c) * EP, f);
@@ -198,52 +297,88 @@ int grid_for(const echo_kv_pool &p, int n_rows, int values, int unroll) {
     return (int)(blocks < 16384 ? blocks : 16384);
 }
 
-template <typename T, bool INT8>
-void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const void *k, const void *v,
-                  int64_t ld, cudaStream_t st) {
-    constexpr int EP = INT8 ? 16 : 8;
+template <typename T, int FORM>
+void launch_write(const echo_kv_pool &p, const echo_kv_batch &b, const int64_t *place, const void *k,
+                  const void *v, int64_t ld, cudaStream_t st) {
+    constexpr int EP = FORM == kInt8 ? 16 : 8;
     const int grid = grid_for(p, b.n_rows, EP, kLoads * kPer16<T> / EP);
-    echo::launch_chained(p.d == 64 ? kv_write_kernel<T, INT8, 64> : kv_write_kernel<T, INT8, 128>,
-                         dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
-                         static_cast<const T *>(k), static_cast<const T *>(v), ld,
-                         echo::device_error_ptr());
+    auto go = [&](auto *kernel) {
+        echo::launch_chained(kernel, dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b), place,
+                             static_cast<const T *>(k), static_cast<const T *>(v), ld, echo::device_error_ptr());
+    };
+    if constexpr (FORM == kInt4) go(p.d == 64 ? kv_write4_kernel<T, 64> : kv_write4_kernel<T, 128>);
+    else go(p.d == 64 ? kv_write_kernel<T, FORM, 64> : kv_write_kernel<T, FORM, 128>);
 }
 
-template <typename T, bool INT8>
+template <typename T>
+echo_status write_rows(const echo_kv_pool &p, const echo_kv_batch &b, const int64_t *place, const void *k,
+                       const void *v, int64_t ld, cudaStream_t st) {
+    echo::LaunchScope ls(ECHO_K_KV_WRITE, b.n_rows, (int64_t)p.H * p.d, 0, st);
+    if (p.kind == kInt4) launch_write<T, kInt4>(p, b, place, k, v, ld, st);
+    else if (p.kind == kInt8) launch_write<T, kInt8>(p, b, place, k, v, ld, st);
+    else launch_write<T, kBf16>(p, b, place, k, v, ld, st);
+    return echo::last_launch_status();
+}
+
+template <typename T, int FORM>
 void launch_read(const echo_kv_pool &p, const echo_kv_batch &b, void *k, void *v, int64_t ld,
                  cudaStream_t st) {
-    const int grid = grid_for(p, b.n_rows, kPer16<T>, !INT8 && sizeof(T) == 2 ? kLoads : 2 * kLoads);
-    echo::launch_chained(p.d == 64 ? kv_read_kernel<T, INT8, 64> : kv_read_kernel<T, INT8, 128>,
+    const int grid = grid_for(p, b.n_rows, kPer16<T>, FORM == kBf16 && sizeof(T) == 2 ? kLoads : 2 * kLoads);
+    echo::launch_chained(p.d == 64 ? kv_read_kernel<T, FORM, 64> : kv_read_kernel<T, FORM, 128>,
                          dim3(grid), dim3(kThreads), 0, st, echo::kv_pool(p), echo::kv_batch(b),
                          static_cast<T *>(k), static_cast<T *>(v), ld, echo::device_error_ptr());
 }
 
-echo_status check_rows(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *k,
-                       const void *v, int64_t ld, echo_dtype t, bool *empty) {
-    const echo_status s = echo::kv_check(pool, batch, empty);
-    if (s != ECHO_OK) return s;
+template <typename T>
+echo_status read_rows(const echo_kv_pool &p, const echo_kv_batch &b, void *k, void *v, int64_t ld, cudaStream_t st) {
+    echo::LaunchScope ls(ECHO_K_KV_READ, b.n_rows, (int64_t)p.H * p.d, 0, st);
+    if (p.kind == kInt4) launch_read<T, kInt4>(p, b, k, v, ld, st);
+    else if (p.kind == kInt8) launch_read<T, kInt8>(p, b, k, v, ld, st);
+    else launch_read<T, kBf16>(p, b, k, v, ld, st);
+    return echo::last_launch_status();
+}
+
+echo_status check_tensors(const echo_kv_pool *pool, const void *k, const void *v, int64_t ld, echo_dtype t,
+                          bool empty) {
     if (t != ECHO_BF16 && t != ECHO_F32) return ECHO_ERR_INVALID_ARG;
     if (ld < (int64_t)pool->H * pool->d || ld % 8) return ECHO_ERR_SHAPE;
-    if (*empty) return ECHO_OK;
+    if (empty) return ECHO_OK;
     if (!k || !v || !echo::aligned16(k) || !echo::aligned16(v)) return ECHO_ERR_INVALID_ARG;
     return echo::device_supported() ? ECHO_OK : ECHO_ERR_UNSUPPORTED;
+}
+
+echo_status check_rows(const echo_kv_pool *pool, const echo_kv_batch *batch, const void *k,
+                       const void *v, int64_t ld, echo_dtype t, bool *empty) {
+    echo_status s = echo::kv_check(pool, batch, empty);
+    if (s != ECHO_OK) return s;
+    return check_tensors(pool, k, v, ld, t, *empty);
 }
 
 }  // namespace
 
 namespace echo {
 
-echo_status kv_check(const echo_kv_pool *p, const echo_kv_batch *b, bool *empty) {
-    if (!p || !b) return ECHO_ERR_INVALID_ARG;
-    if (p->kind != ECHO_CACHE_INT8 && p->kind != ECHO_CACHE_BF16) return ECHO_ERR_INVALID_ARG;
+static echo_status pool_sizes(const echo_kv_pool *p) {
+    if (p->kind != kInt8 && p->kind != kBf16 && p->kind != kInt4) return ECHO_ERR_INVALID_ARG;
     if (p->n_pages < 1 || p->H < 1 || (p->d != 64 && p->d != 128)) return ECHO_ERR_SHAPE;
     if (p->page_tokens != 16 && p->page_tokens != 32 && p->page_tokens != 64 && p->page_tokens != 128)
         return ECHO_ERR_SHAPE;
     // a (page, keys or values, head) is one 32-bit coordinate of the tensor maps
-    if (2ll * p->n_pages * p->H > INT32_MAX - 1) return ECHO_ERR_SHAPE;
-    if (b->n_seqs < 0 || b->max_pages < 0 || b->n_rows < 0 || b->max_rows < 0) return ECHO_ERR_SHAPE;
+    return 2ll * p->n_pages * p->H > INT32_MAX - 1 ? ECHO_ERR_SHAPE : ECHO_OK;
+}
+
+static echo_status pool_memory(const echo_kv_pool *p) {
     if (!p->pages || !aligned16(p->pages)) return ECHO_ERR_INVALID_ARG;
-    if (p->kind == ECHO_CACHE_INT8 && (!p->scale || !aligned16(p->scale))) return ECHO_ERR_INVALID_ARG;
+    if (p->kind != kBf16 && (!p->scale || !aligned16(p->scale))) return ECHO_ERR_INVALID_ARG;
+    return ECHO_OK;
+}
+
+echo_status kv_check(const echo_kv_pool *p, const echo_kv_batch *b, bool *empty) {
+    if (!p || !b) return ECHO_ERR_INVALID_ARG;
+    echo_status s = pool_sizes(p);
+    if (s != ECHO_OK) return s;
+    if (b->n_seqs < 0 || b->max_pages < 0 || b->n_rows < 0 || b->max_rows < 0) return ECHO_ERR_SHAPE;
+    if ((s = pool_memory(p)) != ECHO_OK) return s;
     *empty = b->n_seqs == 0 || b->n_rows == 0;
     if (*empty) return ECHO_OK;
     auto aligned4 = [](const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3u) == 0; };
@@ -261,15 +396,26 @@ extern "C" echo_status echo_kv_write(const echo_kv_pool *pool, const echo_kv_bat
     const echo_status s = check_rows(pool, batch, k, v, ld, t, &empty);
     if (s != ECHO_OK || empty) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    echo::LaunchScope ls(ECHO_K_KV_WRITE, batch->n_rows, (int64_t)pool->H * pool->d, 0, st);
-    const bool q = pool->kind == ECHO_CACHE_INT8;
-    if (t == ECHO_BF16)
-        q ? launch_write<__nv_bfloat16, true>(*pool, *batch, k, v, ld, st)
-          : launch_write<__nv_bfloat16, false>(*pool, *batch, k, v, ld, st);
-    else
-        q ? launch_write<float, true>(*pool, *batch, k, v, ld, st)
-          : launch_write<float, false>(*pool, *batch, k, v, ld, st);
-    return echo::last_launch_status();
+    return t == ECHO_BF16 ? write_rows<__nv_bfloat16>(*pool, *batch, nullptr, k, v, ld, st)
+                          : write_rows<float>(*pool, *batch, nullptr, k, v, ld, st);
+}
+
+extern "C" echo_status echo_kv_write_at(const echo_kv_pool *pool, const int64_t *place, int32_t n_rows,
+                                        const void *k, const void *v, int64_t ld, echo_dtype t,
+                                        echo_stream_t stream) {
+    if (!pool) return ECHO_ERR_INVALID_ARG;
+    echo_status s = echo::pool_sizes(pool);
+    if (s != ECHO_OK) return s;
+    if (n_rows < 0) return ECHO_ERR_SHAPE;
+    if ((s = echo::pool_memory(pool)) != ECHO_OK) return s;
+    if (n_rows > 0 && (!place || (reinterpret_cast<uintptr_t>(place) & 7u))) return ECHO_ERR_INVALID_ARG;
+    s = check_tensors(pool, k, v, ld, t, n_rows == 0);
+    if (s != ECHO_OK || n_rows == 0) return s;
+    echo_kv_batch b = {};
+    b.n_rows = n_rows;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return t == ECHO_BF16 ? write_rows<__nv_bfloat16>(*pool, b, place, k, v, ld, st)
+                          : write_rows<float>(*pool, b, place, k, v, ld, st);
 }
 
 extern "C" echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batch *batch, void *k,
@@ -278,13 +424,6 @@ extern "C" echo_status echo_kv_read(const echo_kv_pool *pool, const echo_kv_batc
     const echo_status s = check_rows(pool, batch, k, v, ld, t, &empty);
     if (s != ECHO_OK || empty) return s;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    echo::LaunchScope ls(ECHO_K_KV_READ, batch->n_rows, (int64_t)pool->H * pool->d, 0, st);
-    const bool q = pool->kind == ECHO_CACHE_INT8;
-    if (t == ECHO_BF16)
-        q ? launch_read<__nv_bfloat16, true>(*pool, *batch, k, v, ld, st)
-          : launch_read<__nv_bfloat16, false>(*pool, *batch, k, v, ld, st);
-    else
-        q ? launch_read<float, true>(*pool, *batch, k, v, ld, st)
-          : launch_read<float, false>(*pool, *batch, k, v, ld, st);
-    return echo::last_launch_status();
+    return t == ECHO_BF16 ? read_rows<__nv_bfloat16>(*pool, *batch, k, v, ld, st)
+                          : read_rows<float>(*pool, *batch, k, v, ld, st);
 }

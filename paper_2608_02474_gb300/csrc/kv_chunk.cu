@@ -11,7 +11,9 @@
 //   warp 3      walks the pieces, hands them to the other warps, copies the queries;
 //   four warps  int8: codes to bf16, a key per thread: the copy leaves a row of codes where
 //               the second half of the row's bf16 values goes, so that each thread
-//               overwrites only its own.  bf16: clear values that no row may use (below);
+//               overwrites only its own.  4 bits: the same with the scales in the values, exactly, so
+//               that the rest is as for bf16; a warp's codes lie where its own rows go.
+//               bf16: clear values that no row may use (below);
 //   eight warps softmax of the two tiles: a row's running maximum comes from
 //               the piece's first block and moves only when a block's weights sum to more
 //               than 2^64 (exact after the division by the row sum).
@@ -20,7 +22,8 @@
 // values too.  In the blocks that some row does not see whole, four warps therefore clear
 // values past the end, clear those that are not finite and name their keys; a row that
 // sees such a key becomes NaN.  For int8 pages only a scale can be non-finite: it then
-// spoils the key's score, and stands as 0 among the values' scales.
+// spoils the key's score, and stands as 0 among the values' scales; for 4-bit pages it makes
+// the key NaN, and its values 0.
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
 #include <cfloat>
 #include <type_traits>
@@ -37,9 +40,11 @@ constexpr int SLOT_ROWS = TILES * BM;
 constexpr int kWholeKeys = 1024;                // 64 bf16 rows, 8 heads of 128: whole 512 keys 16.5 us, 1024 21.5; divided 19.8, 21.8
 constexpr int PAIRS = 3;                        // (V_f, K_{f+1}) on their way or in use
 constexpr int SPOILT = 2;                       // blocks whose spoilt keys are kept
+constexpr int SCALES_AT = 2048;                 // 4 bits: of 32 keys' scales, from where their rows will be
 
-template <bool INT8, int D>
+template <int FORM, int D>
 struct Cfg {
+    static constexpr bool INT8 = FORM == kInt8, CODES = FORM != kBf16;
     // warps 0-3, helpers from 4 on, softmax
     static constexpr int HELP = 4, SOFT0 = 4 + HELP, THREADS = 32 * (SOFT0 + 8);
     static constexpr int ATOMS = D / 64;
@@ -57,7 +62,7 @@ struct Cfg {
     // what the launch gives; the splits that were fastest.  4864 rows, 8 heads, bf16: 32768
     // keys of 128 354 us (72, 24, 208: 358), 8192 keys of 64 70 us (96, 48, 184: 73); int8
     // 464 and 98 us (88, 40, 192: 524 and 114; 56, 56, 200: 472 and 101), since then 472 and 97
-    static constexpr int REGS[3] = {INT8 ? 64 : 88, INT8 ? 64 : 40, 192};
+    static constexpr int REGS[3] = {CODES ? 64 : 88, CODES ? 64 : 40, 192};
     static_assert(REGS[0] + HELP / 4 * REGS[1] + 2 * REGS[2] <= THREADS / 128 * (65536 / THREADS / 8 * 8),
                   "setmaxnreg takes from the launch's registers");
     static constexpr uint32_t IDESC_S = idesc_bf16_f32(BM, BN);
@@ -79,10 +84,11 @@ struct ChunkParams {
 ECHO_DEV int kv_clear(const KvPiece &pc) { return min(max(pc.low / BN - pc.kb0, 0), max(pc.blocks, 0)); }
 
 // what shared memory holds beside the tiles
-template <bool INT8, int D>
+template <int FORM, int D>
 struct Side {
-    static constexpr int RING = Cfg<INT8, D>::RING;
-    using C = Cfg<INT8, D>;
+    static constexpr int RING = Cfg<FORM, D>::RING;
+    using C = Cfg<FORM, D>;
+    static constexpr bool INT8 = C::INT8;
     uint64_t q_full[C::Q_BUFS], q_empty[C::Q_BUFS], k_first, pair[PAIRS], empty[RING], raw_full[RING], edge_go, v_ok;
     uint64_t s_full[C::S_BARS], p_full[C::S_BUFS], pv_done[TILES], drain;
     uint64_t piece_full[PIECES], piece_empty[PIECES], sc_full[2], sc_empty[2];
@@ -96,15 +102,16 @@ struct Side {
     };
 };
 
-template <bool INT8, int D>
-__global__ void __launch_bounds__((Cfg<INT8, D>::THREADS), 1)
+template <int FORM, int D>
+__global__ void __launch_bounds__((Cfg<FORM, D>::THREADS), 1)
 kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
                 const ChunkParams p) {
-    using C = Cfg<INT8, D>;
+    using C = Cfg<FORM, D>;
+    constexpr bool INT8 = C::INT8, INT4 = FORM == kInt4, CODES = C::CODES;
     constexpr int RING = C::RING;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t *Qs = smem, *Ring = smem + C::Q_BUFS * C::Q_BUF;
-    Side<INT8, D> &sh = *reinterpret_cast<Side<INT8, D> *>(smem + C::TILES_BYTES);
+    Side<FORM, D> &sh = *reinterpret_cast<Side<FORM, D> *>(smem + C::TILES_BYTES);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -115,8 +122,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             mbar_init(&sh.q_empty[i], 1);
         }
         // V_f and K_{f+1} share a barrier: two copies, or two tiles from four warps
-        mbar_init(&sh.k_first, INT8 ? 4 : 1);
-        for (int i = 0; i < PAIRS; ++i) mbar_init(&sh.pair[i], INT8 ? 8 : 2);
+        mbar_init(&sh.k_first, CODES ? 4 : 1);
+        for (int i = 0; i < PAIRS; ++i) mbar_init(&sh.pair[i], CODES ? 8 : 2);
         for (int i = 0; i < RING; ++i) {
             mbar_init(&sh.empty[i], 1);
             mbar_init(&sh.raw_full[i], 1);
@@ -264,15 +271,32 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         if (D == 128) ok = wait_all(&sh.empty[slot], ((li / RING) & 1) ^ 1);
                         else if (kv == 1) ok = wait_all(&sh.empty[((li >> 1) + 1) % 3], ((((li >> 1) + 1) / 3) & 1) ^ 1);
                         if (!ok) break;
-                        uint64_t *bar = INT8 ? &sh.raw_full[slot] : li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS];
+                        uint64_t *bar = CODES ? &sh.raw_full[slot] : li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS];
                         uint8_t *dst = Ring + slot * C::SLOT;
-                        // int8: both scales come with the keys
+                        // codes: both scales come with the keys
+                        constexpr int SCALES = INT4 ? D / 8 : INT8 ? 8 : 0;     // bytes of a token's
                         if (lane == 0)
-                            mbar_arrive_expect_tx(bar, (uint32_t)(some << shift) * (INT8 ? D + (kv ? 0 : 8) : 2 * D));
+                            mbar_arrive_expect_tx(bar, (uint32_t)(some << shift) * (kv_bytes(FORM, D) + (kv ? 0 : SCALES)));
                         __syncwarp();
                         if (lane < some) {
                             const int z = (page * 2 + kv) * p.pool.H + head, r0 = lane << shift;
-                            if constexpr (INT8) {
+                            if constexpr (INT4) {
+                                // codes and scales of 32 keys where their own warp's rows will be
+                                const int step = min(shift, 5);
+                                for (int r = 0; r < 1 << shift; r += 1 << step) {
+                                    uint8_t *at = dst + ((r0 + r) & ~31) * 128;
+                                    const int in32 = (r0 + r) & 31;
+                                    tma_load_3d(at + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
+                                    if (kv == 0) {
+                                        const uint8_t *src = static_cast<const uint8_t *>(p.pool.scale) +
+                                                             (((int64_t)z << shift) + r) * (D / 16);
+                                        at += SCALES_AT + in32 * (D / 16);
+                                        bulk_load_1d(at, src, (uint32_t)(D / 16) << step, bar);
+                                        bulk_load_1d(at + 2 * D, src + ((int64_t)p.pool.H << shift) * (D / 16),
+                                                     (uint32_t)(D / 16) << step, bar);
+                                    }
+                                }
+                            } else if constexpr (INT8) {
                                 tma_load_3d(dst + ATOM + r0 * D, &tm_kv, bar, 0, 0, z);
                                 if (kv == 0) {
                                     // the scales of 32 keys where their own warp's rows will be:
@@ -280,7 +304,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                     const int step = min(shift, 5);
                                     for (int r = 0; r < 1 << shift; r += 1 << step) {
                                         uint8_t *at = dst + ((r0 + r) & ~31) * 128 + ((r0 + r) & 31) * 4;
-                                        const float *src = p.pool.scale + (((int64_t)z << shift) + r);
+                                        const float *src = static_cast<const float *>(p.pool.scale) + (((int64_t)z << shift) + r);
                                         bulk_load_1d(at, src, 4u << step, bar);
                                         bulk_load_1d(at + 128, src + ((int64_t)p.pool.H << shift), 4u << step, bar);
                                     }
@@ -297,9 +321,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 }
             }
             // the last V has no K after it
-            if (!INT8 && li > 0 && lane == 0) mbar_arrive(&sh.pair[((li - 1) >> 1) % PAIRS]);
+            if (!CODES && li > 0 && lane == 0) mbar_arrive(&sh.pair[((li - 1) >> 1) % PAIRS]);
             // copies land before this CTA exits, whoever gives up, and when
-            if (INT8) {
+            if (CODES) {
                 for (int i = max(0, li - RING); i < li; ++i) mbar_land(&sh.raw_full[i % RING], (i / RING) & 1);
             } else if (li > 0) {
                 mbar_land(&sh.k_first, 0);
@@ -351,9 +375,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 if (++pr == PAIRS) { pr = 0; pph ^= 1u; }
                 return there;
             };
-            auto edge_go = [&]() { if (!INT8 && lane == 0) mbar_arrive(&sh.edge_go); };
+            auto edge_go = [&]() { if (!CODES && lane == 0) mbar_arrive(&sh.edge_go); };
             auto edge_wait = [&]() -> bool {
-                if (INT8) return true;
+                if (CODES) return true;
                 const bool there = wait_all(&sh.v_ok, eph);
                 eph ^= 1u;
                 return there;
@@ -626,7 +650,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS[1]) : "memory");
         bool ok = true;
         int f = 0;                                            // block
-        if constexpr (!INT8) {
+        if constexpr (!CODES) {
             // ---------------- values that no row may use, cleared ----------------
             int edge = 0;
             for (int n = 0; ok; ++n) {
@@ -679,6 +703,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks, keys = pc.keys;
             piece_done(n);
             for (int kb = kb0; ok && kb < kb1; ++kb, ++f) {
+                [[maybe_unused]] uint32_t vw[D / 64];         // 4 bits: the values' scales, two groups a word
 #pragma unroll 1
                 for (int kv = 0; kv < 2; ++kv) {
                     const int li = 2 * f + kv, slot = li % RING;
@@ -686,6 +711,54 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     if (!ok) break;
                     uint8_t *tile = Ring + slot * C::SLOT;
                     float ks = 0.f, vs = 0.f;
+                    if constexpr (INT4) {
+                        constexpr int CHUNKS = D / 32;        // groups of 32 codes, 16 bytes each
+                        uint8_t *mine = tile + (r & ~31) * 128;
+                        uint4 in[CHUNKS];
+                        uint32_t sw[D / 64];
+#pragma unroll
+                        for (int c = 0; c < CHUNKS; ++c) {
+                            const int at = D == 128 ? lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)
+                                                    : lane * 32 + ((c ^ ((lane >> 2) & 1)) << 4);
+                            in[c] = *reinterpret_cast<const uint4 *>(mine + (C::ATOMS - 1) * ATOM + at);
+                        }
+                        const uint8_t *sc = mine + SCALES_AT + lane * (D / 16);
+                        if (kv == 0) {
+                            // a value's scale that is not finite stands as 0, and spoils the key instead
+                            uint32_t bad = 0;
+                            const bool past = kb * BN + r >= keys;    // slots past the end: anything
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i) {
+                                sw[i] = reinterpret_cast<const uint32_t *>(sc)[i];
+                                vw[i] = reinterpret_cast<const uint32_t *>(sc + 2 * D)[i];
+                                const uint32_t off = kv_not_finite2(vw[i]);
+                                bad |= off;
+                                vw[i] = past ? 0u : vw[i] & ~off;
+                            }
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i) sw[i] = past ? 0u : bad ? 0x7FC07FC0u : sw[i];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i) sw[i] = vw[i];
+                        }
+                        __syncwarp();                         // read before the rows are written
+#pragma unroll
+                        for (int c = 0; c < CHUNKS; ++c) {
+                            const KvScale2 s = kv_scale2(__byte_perm(sw[c / 2], 0u, c & 1 ? 0x3232u : 0x1010u));
+                            const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {     // 8 values
+                                const uint4 v = make_uint4(kv_nibbles2<0>(w[h], s), kv_nibbles2<1>(w[h], s),
+                                                           kv_nibbles2<2>(w[h], s), kv_nibbles2<3>(w[h], s));
+                                const int out = 4 * (c & 1) + h;
+                                *reinterpret_cast<uint4 *>(tile + (c / 2) * ATOM + r * 128 + ((out ^ (r & 7)) << 4)) = v;
+                            }
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(li == 0 ? &sh.k_first : &sh.pair[((li - 1) >> 1) % PAIRS]);
+                        continue;
+                    }
                     if (kv == 0) {
                         const float *sc = reinterpret_cast<const float *>(tile + (r & ~31) * 128) + lane;
                         ks = sc[0];
@@ -949,7 +1022,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     tmem_st32(s_at + 32, pk + 32);
                 }
                 tmem_st_wait();
-                if (!INT8 && j >= clear) {                      // keys whose values are not finite
+                if (!CODES && j >= clear) {                     // keys whose values are not finite
                     ok = wait_all(&sh.v_ok, edge & 1);
                     if (!ok) break;
 #pragma unroll
@@ -983,6 +1056,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
                 }
             }
+            if constexpr (INT4) l[0] *= 1.f / kNibbleUnit;       // as the values in O
             const bool whole = pc.whole;
             const float m_row = own(m), l_row = own(l);
             const float inv = l_row == 0.f ? 0.f : 1.f / l_row;  // no key: zeros
@@ -1031,24 +1105,24 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
 }
 
-template <bool INT8, int D>
+template <int FORM, int D>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
-    using C = Cfg<INT8, D>;
-    constexpr int SMEM = C::TILES_BYTES + (int)sizeof(Side<INT8, D>);
-    using S = Side<INT8, D>;
+    using C = Cfg<FORM, D>;
+    constexpr int SMEM = C::TILES_BYTES + (int)sizeof(Side<FORM, D>);
+    using S = Side<FORM, D>;
     static_assert(SMEM <= 232448 && C::TILES_BYTES % 16 == 0 && offsetof(S, scales) % 16 == 0, "");
     static int attr_done[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(kv_chunk_kernel<INT8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        cudaFuncSetAttribute(kv_chunk_kernel<FORM, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
         attr_done[dev] = 1;
     }
     const int group = a.Hq / a.pool->H, tokens = BM / group;
     CUtensorMap tq, tk;
     if (!echo::make_tmap_rows(&tq, a.q, (uint64_t)a.batch->n_rows, (uint64_t)a.Hq, (uint64_t)D, (uint64_t)a.ldq,
                               (uint32_t)group, (uint32_t)tokens) ||
-        !echo::make_tmap_pages(&tk, *a.pool, (uint32_t)a.pool->page_tokens))
+        !echo::make_tmap_pages(&tk, *a.pool, (uint32_t)(FORM == kInt4 && a.pool->page_tokens > 32 ? 32 : a.pool->page_tokens)))
         return ECHO_ERR_CUDA;
     ChunkParams p;
     p.pool = echo::kv_pool(*a.pool);
@@ -1057,12 +1131,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.out = static_cast<__nv_bfloat16 *>(a.out);
     p.ws = static_cast<float *>(a.ws);
     p.ldo = a.ldo;
-    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (FORM == kInt4 ? kNibbleUnit : FORM == kInt8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
     cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        launched = echo::launch_chained(kv_chunk_kernel<INT8, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
+        launched = echo::launch_chained(kv_chunk_kernel<FORM, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
     }
     if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
@@ -1077,9 +1151,10 @@ size_t kv_chunk_workspace(const echo_kv_pool &pool) {
 }
 
 echo_status launch_kv_chunk(const KvAttention &a, cudaStream_t st) {
-    const bool i8 = a.pool->kind == ECHO_CACHE_INT8;
-    if (a.pool->d == 64) return i8 ? launch<true, 64>(a, st) : launch<false, 64>(a, st);
-    return i8 ? launch<true, 128>(a, st) : launch<false, 128>(a, st);
+    const int form = a.pool->kind;
+    if (a.pool->d == 64)
+        return form == kInt4 ? launch<kInt4, 64>(a, st) : form == kInt8 ? launch<kInt8, 64>(a, st) : launch<kBf16, 64>(a, st);
+    return form == kInt4 ? launch<kInt4, 128>(a, st) : form == kInt8 ? launch<kInt8, 128>(a, st) : launch<kBf16, 128>(a, st);
 }
 
 }  // namespace echo

@@ -28,17 +28,19 @@ namespace {
 constexpr int PIECES = 4;                      // handed out ahead
 constexpr int kWholeKeys = 768;     // 16 heads of 64, one bf16 token: whole 256 keys 9.2 us, 1024 13.4; divided 11.6, 12.1
 
-template <bool INT8, int D, int NR>
+template <int FORM, int D, int NR>
 struct Cfg {
+    static constexpr bool CODES = FORM != kBf16;
     static constexpr int ROWS = 8 * NR;
-    static constexpr int GROUPS = NR * D <= (INT8 ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
+    static constexpr int GROUPS = NR * D <= (CODES ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
     static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
-    static constexpr int KPW = INT8 ? 32 : 16;             // keys of a warp
+    static constexpr int KPW = CODES ? 32 : 16;            // keys of a warp
     static constexpr int BK = 4 * KPW;                     // keys of a block
-    static constexpr int BSHIFT = INT8 ? 7 : 6;
-    static constexpr int ROW_BYTES = INT8 ? D : 2 * D;
+    static constexpr int BSHIFT = CODES ? 7 : 6;
+    static constexpr int ROW_BYTES = kv_bytes(FORM, D);
     static constexpr int HALF = BK * ROW_BYTES;            // K or V of a block
-    static constexpr int SCALES = INT8 ? 2 * BK * 4 : 0;
+    static constexpr int TOKEN_SCALES = FORM == kInt8 ? 4 : FORM == kInt4 ? D / 16 : 0;   // bytes, of K or V
+    static constexpr int SCALES = 2 * BK * TOKEN_SCALES;
     static constexpr int STAGE = 2 * HALF + SCALES;        // a multiple of 1024
     static constexpr int JOIN = WARPS / 4 * ROWS * D * 4;  // half of the warps' half of O
     static constexpr bool Q_SMEM = NR * D >= 192 && D == 64;          // the queries' registers do not suffice
@@ -83,17 +85,31 @@ ECHO_DEV void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// neighbouring words of shared memory, read at once
+template <int N>
+ECHO_DEV void load_words(const uint8_t *from, uint32_t (&to)[N]) {
+    if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(from);
+        to[0] = v.x;
+        to[1] = v.y;
+    } else {
+        to[0] = *reinterpret_cast<const uint32_t *>(from);
+    }
+}
+
 // byte offset of 16-byte chunk c of row r of a block's K or V, as the tensor maps lay it out
-template <bool INT8, int D, int BK>
+template <int FORM, int D, int BK>
 ECHO_DEV uint32_t chunk_at(int r, int c) {
-    if constexpr (INT8 && D == 64) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+    if constexpr (kv_bytes(FORM, D) == 32) return (uint32_t)(r * 32 + ((c ^ ((r >> 2) & 1)) << 4));
+    else if constexpr (kv_bytes(FORM, D) == 64) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
     else return (uint32_t)((c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-template <bool INT8, int D, int NR>
-__global__ void __launch_bounds__((Cfg<INT8, D, NR>::THREADS), 2)
+template <int FORM, int D, int NR>
+__global__ void __launch_bounds__((Cfg<FORM, D, NR>::THREADS), 2)
 kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
-    using C = Cfg<INT8, D, NR>;
+    using C = Cfg<FORM, D, NR>;
+    constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4, CODES = C::CODES;
     constexpr int KPW = C::KPW, BK = C::BK, KG = KPW / 16, MT = D / 16, ROWS = C::ROWS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -170,7 +186,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&empty[stage], ((g / C::RING) & 1) ^ 1, abort_v, p.err));
                 if (!ok) break;
                 const int n = min(per_block, copies - first);
-                if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(n << cs) * (2 * C::ROW_BYTES + (INT8 ? 8 : 0)));
+                if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(n << cs) * 2 * (C::ROW_BYTES + C::TOKEN_SCALES));
                 const int page = __shfl_sync(0xffffffffu, now, (first - c0 + lane) & 31);
                 __syncwarp();
                 if (lane < n) {
@@ -179,10 +195,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         const int z = (page * 2 + kv) * p.pool.H + walk.head;
-                        if constexpr (INT8) {
-                            tma_load_3d(dst + kv * C::HALF + r0 * D, &tm, &full[stage], 0, y, z);
-                            bulk_load_1d(dst + 2 * C::HALF + (kv * BK + r0) * 4,
-                                         p.pool.scale + (((int64_t)z << shift) + y), 4u << cs, &full[stage]);
+                        if constexpr (CODES) {
+                            tma_load_3d(dst + kv * C::HALF + r0 * C::ROW_BYTES, &tm, &full[stage], 0, y, z);
+                            bulk_load_1d(dst + 2 * C::HALF + (kv * BK + r0) * C::TOKEN_SCALES,
+                                         static_cast<const uint8_t *>(p.pool.scale) +
+                                             (((int64_t)z << shift) + y) * C::TOKEN_SCALES,
+                                         (uint32_t)C::TOKEN_SCALES << cs, &full[stage]);
                         } else {
 #pragma unroll
                             for (int a = 0; a < D / 64; ++a)
@@ -224,7 +242,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             if (pr < s.packed) {
                 const int r = p.work.by_group(pr);
                 const __nv_bfloat16 *src = p.q + (int64_t)(s.row + r) * p.ldq + (head * group + pr - r * group) * D + 16 * kk;
-                if constexpr (INT8) {
+                if constexpr (INT4) {          // a lane's word of 32 columns: 8 of them, 4 a product
+                    v = *reinterpret_cast<const uint2 *>(src - 16 * (kk & 1) + 8 * tq + 4 * (kk & 1));
+                } else if constexpr (INT8) {
                     v = *reinterpret_cast<const uint2 *>(src + 4 * tq);
                 } else {
                     v.x = *reinterpret_cast<const uint32_t *>(src + 2 * tq);
@@ -276,16 +296,42 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             if (key0 < keys && (C::GROUPS == 1 || (g & 1) == warp >> 2)) {
                 // S^T = K Q^T, 16 keys at a time
                 float sc[KG][NR][4] = {};
+                const uint8_t *token_scales = smem + stage * C::STAGE + 2 * C::HALF;
+                constexpr int STEPS = INT4 ? 4 : INT8 ? 2 : 1;   // products of what four matrices hold
 #pragma unroll
-                for (int kg = 0; kg < KG; ++kg)
+                for (int kg = 0; kg < KG; ++kg) {
+                    uint32_t ks[2][D / 64];          // 4 bits: the scales of keys gq and gq + 8, two groups a word
+                    if constexpr (INT4) {
 #pragma unroll
-                    for (int kk = 0; kk < MT; kk += INT8 ? 2 : 1) {
+                        for (int h = 0; h < 2; ++h)
+                            load_words(token_scales + (wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES, ks[h]);
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < MT; kk += STEPS) {
                         uint32_t r[4];
                         const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
-                        ldsm4(kbase + chunk_at<INT8, D, BK>(row, INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
+                        ldsm4(kbase + chunk_at<FORM, D, BK>(row, INT4 ? kk / 2 + (mi >> 1) : INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
+                        KvScale2 f0, f1;
 #pragma unroll
-                        for (int i = 0; i < (INT8 ? 2 : 1); ++i) {
+                        for (int i = 0; i < STEPS; ++i) {
                             uint32_t a[4] = {r[0], r[1], r[2], r[3]};
+                            if constexpr (INT4) {
+                                const uint32_t w0 = r[2 * (i / 2)], w1 = r[2 * (i / 2) + 1];
+                                if (i % 2 == 0) {
+                                    const uint32_t both = i / 2 ? 0x3232u : 0x1010u;
+                                    f0 = kv_scale2(__byte_perm(ks[0][kk / 4], 0u, both));
+                                    f1 = kv_scale2(__byte_perm(ks[1][kk / 4], 0u, both));
+                                    a[0] = kv_nibbles2<0>(w0, f0);
+                                    a[1] = kv_nibbles2<0>(w1, f1);
+                                    a[2] = kv_nibbles2<1>(w0, f0);
+                                    a[3] = kv_nibbles2<1>(w1, f1);
+                                } else {
+                                    a[0] = kv_nibbles2<2>(w0, f0);
+                                    a[1] = kv_nibbles2<2>(w1, f1);
+                                    a[2] = kv_nibbles2<3>(w0, f0);
+                                    a[3] = kv_nibbles2<3>(w1, f1);
+                                }
+                            }
                             if constexpr (INT8) {
                                 const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
                                 a[0] = kv_codes2(w0, 0x4140);
@@ -304,8 +350,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                             }
                         }
                     }
+                }
                 // in the exponent of two: keys gq and gq + 8 of each 16, rows 2 tq and 2 tq + 1
-                const float *scales = reinterpret_cast<const float *>(smem + stage * C::STAGE + 2 * C::HALF) + wk + gq;
+                const float *scales = reinterpret_cast<const float *>(token_scales) + wk + gq;
                 const bool edge = key0 + KPW > low;      // some row does not see all of these keys
                 float vs[KG][2];
 #pragma unroll
@@ -324,8 +371,17 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         }
                         if (edge) {
                             const int j = key0 + kg * 16 + 8 * h + gq;
-                            const bool bad = INT8 && !(fabsf(vs[kg][h]) < INFINITY);   // spoils the rows that see it
-                            if (bad) vs[kg][h] = 0.f;
+                            bool bad = false;        // a value's scale is not finite: it spoils the rows that see it
+                            if constexpr (INT8) {
+                                bad = !(fabsf(vs[kg][h]) < INFINITY);
+                                if (bad) vs[kg][h] = 0.f;
+                            }
+                            if constexpr (INT4) {
+                                uint32_t w[D / 64];
+                                load_words(token_scales + (BK + wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES, w);
+#pragma unroll
+                                for (int i = 0; i < D / 64; ++i) bad |= kv_not_finite2(w[i]) != 0u;
+                            }
 #pragma unroll
                             for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
@@ -400,18 +456,18 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         b[nt][0] = turn8x8(pb[kg][nt][0]);
                         b[nt][1] = turn8x8(pb[kg][nt][1]);
                     }
-                    // a matrix of 8 keys and 16 bytes: bf16 keys, then columns; int8 the other way
-                    const int row = wk + kg * 16 + (INT8 ? (mi & 1) : (mi >> 1)) * 8 + mr;
-                    const int col = INT8 ? mi >> 1 : mi & 1;
+                    // a matrix of 8 keys and 16 bytes: bf16 keys, then columns; codes the other way
+                    const int row = wk + kg * 16 + (CODES ? (mi & 1) : (mi >> 1)) * 8 + mr;
+                    const int col = CODES ? mi >> 1 : mi & 1;
                     uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
-                    if (!INT8 && edge && low < keys) {
+                    if (!CODES && edge && low < keys) {
                         // rows that do not see all of these keys: values that are not finite
                         // become 0, and spoil the rows that do see them (0 times infinity)
                         uint32_t bad = 0;                    // of the 16 keys
 #pragma unroll
                         for (int t = 0; t < MT; ++t) {
                             uint32_t r[4];
-                            ldsm4_t(vbase + chunk_at<INT8, D, BK>(row, 2 * t + col), r);
+                            ldsm4_t(vbase + chunk_at<FORM, D, BK>(row, 2 * t + col), r);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 if ((r[i] & 0x7F80u) == 0x7F80u) bad |= 1u << (8 * (i >> 1) + 2 * tq);
@@ -431,18 +487,47 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                             keep[h] = ((bad >> (8 * h + 2 * tq)) & 1 ? 0u : 0xffffu) |
                                       ((bad >> (8 * h + 2 * tq)) & 2 ? 0u : 0xffff0000u);
                     }
-                    if (!INT8 && tail) {
+                    if (!CODES && tail) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const int j = key0 + kg * 16 + 8 * h + 2 * tq;
                             keep[h] &= (j < keys ? 0xffffu : 0u) | (j + 1 < keys ? 0xffff0000u : 0u);
                         }
                     }
+                    // 4 bits: the scales of keys 2 tq, 2 tq + 1 and of 8 keys further on, as the weights lie
+                    uint32_t vw[2][2][D / 64];
+                    if constexpr (INT4) {
 #pragma unroll
-                    for (int t = 0; t < MT; t += INT8 ? 2 : 1) {
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                load_words(token_scales + (BK + wk + kg * 16 + 8 * h + 2 * tq + e) * C::TOKEN_SCALES, vw[h][e]);
+                    }
+#pragma unroll
+                    for (int t = 0; t < MT; t += STEPS) {
                         uint32_t r[4];
-                        ldsm4_t(vbase + chunk_at<INT8, D, BK>(row, INT8 ? t + col : 2 * t + col), r);
-                        if constexpr (INT8) {
+                        ldsm4_t(vbase + chunk_at<FORM, D, BK>(row, INT4 ? t / 2 + col : INT8 ? t + col : 2 * t + col), r);
+                        if constexpr (INT4) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {            // a group of 32 columns
+                                KvScale2 f[2];
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    uint32_t s2 = __byte_perm(vw[h][0][t / 4], vw[h][1][t / 4], i ? 0x7632u : 0x5410u);
+                                    if (edge) s2 &= ~kv_not_finite2(s2);   // spoilt above; or past the end, anything
+                                    f[h] = kv_scale2(s2);
+                                }
+                                const uint32_t a[4] = {kv_nibbles2<0>(r[2 * i], f[0]), kv_nibbles2<1>(r[2 * i], f[0]),
+                                                       kv_nibbles2<0>(r[2 * i + 1], f[1]), kv_nibbles2<1>(r[2 * i + 1], f[1])};
+                                const uint32_t c[4] = {kv_nibbles2<2>(r[2 * i], f[0]), kv_nibbles2<3>(r[2 * i], f[0]),
+                                                       kv_nibbles2<2>(r[2 * i + 1], f[1]), kv_nibbles2<3>(r[2 * i + 1], f[1])};
+#pragma unroll
+                                for (int nt = 0; nt < NR; ++nt) {
+                                    mma16816(o[nt][t + 2 * i], a, b[nt][0], b[nt][1]);
+                                    mma16816(o[nt][t + 2 * i + 1], c, b[nt][0], b[nt][1]);
+                                }
+                            }
+                        } else if constexpr (INT8) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
                                 const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
@@ -477,6 +562,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], x);
+                if constexpr (INT4) l[nt][e] *= 1.f / kNibbleUnit;   // as the values in O
                 if (gq == 0) row_ml[warp][nt * 8 + 2 * tq + e] = make_float2(m[nt][e], l[nt][e]);
             }
         named_bar_sync(1, 32 * C::WARPS);
@@ -527,7 +613,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         if (lane == 0) mbar_arrive(&piece_empty[n % PIECES]);
         if (warp != 0) continue;
         // Columns in pairs: int8 has 2 gq and 2 gq + 1 of each 16.  bf16 has gq and gq + 8:
-        // lanes of even gq trade row 2 tq + 1 for row 2 tq of the lane after them.
+        // lanes of even gq trade row 2 tq + 1 for row 2 tq of the lane after them.  So do 4
+        // bits, whose columns are 8 (gq / 2) + gq mod 2 of each 32, plus 4 (t mod 2), and 2 more.
 #pragma unroll
         for (int nt = 0; nt < NR; ++nt) {
             float inv[2];
@@ -555,7 +642,8 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         b = e ? x1 : got;
                     }
                     const int row = nt * 8 + 2 * tq + e, pr = tile * ROWS + row;
-                    const int col = 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
+                    const int col = INT4 ? 32 * (t >> 1) + 8 * (gq >> 1) + 4 * (t & 1) + 2 * u
+                                         : 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
                     if (pr >= s.packed) continue;
                     const int r = pr / group;
                     if (whole)
@@ -568,14 +656,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     }
 }
 
-template <bool INT8, int D, int NR>
+template <int FORM, int D, int NR>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
-    using C = Cfg<INT8, D, NR>;
+    using C = Cfg<FORM, D, NR>;
     static int attr_done[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(kv_decode_kernel<INT8, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        cudaFuncSetAttribute(kv_decode_kernel<FORM, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         attr_done[dev] = 1;
     }
     CUtensorMap tm;
@@ -589,12 +677,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     p.ws = static_cast<float *>(a.ws);
     p.ldq = a.ldq;
     p.ldo = a.ldo;
-    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (INT8 ? kCodeUnit : 1.f);
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)D) * (FORM == kInt4 ? kNibbleUnit : FORM == kInt8 ? kCodeUnit : 1.f);
     p.err = echo::device_error_ptr();
     cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        launched = echo::launch_chained(kv_decode_kernel<INT8, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
+        launched = echo::launch_chained(kv_decode_kernel<FORM, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
     }
     if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
@@ -608,19 +696,19 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
 //          32760 tokens, 40 heads: 32 in 16s 190, 133)
 //          int8 8 rows 56, 16 60, 24 in 16s 89, 32 90 (128), 48 131 (129); three CTAs of an
 //          SM, with two thirds of the registers, are slower: d 64 int8 24 rows 60
-int tile_rows(bool i8, int d, int64_t rows) {
-    if (d == 128) return rows <= 8 ? 8 : rows <= (i8 ? 32 : 16) ? 16 : 0;
+int tile_rows(bool codes, int d, int64_t rows) {
+    if (d == 128) return rows <= 8 ? 8 : rows <= (codes ? 32 : 16) ? 16 : 0;
     if (rows <= 32) return (int)(rows + 7) / 8 * 8 + (rows == 0 ? 8 : 0);
-    return i8 && rows <= 64 ? (rows <= 48 ? 24 : 32) : 0;
+    return codes && rows <= 64 ? (rows <= 48 ? 24 : 32) : 0;
 }
 
-template <bool INT8, int D>
+template <int FORM, int D>
 echo_status launch_rows(const echo::KvAttention &a, int tile, cudaStream_t st) {
-    if (tile == 8) return launch<INT8, D, 1>(a, st);
-    if (tile == 16) return launch<INT8, D, 2>(a, st);
+    if (tile == 8) return launch<FORM, D, 1>(a, st);
+    if (tile == 16) return launch<FORM, D, 2>(a, st);
     if constexpr (D == 64) {
-        if (tile == 24) return launch<INT8, D, 3>(a, st);
-        return launch<INT8, D, 4>(a, st);
+        if (tile == 24) return launch<FORM, D, 3>(a, st);
+        return launch<FORM, D, 4>(a, st);
     }
     return ECHO_ERR_SHAPE;
 }
@@ -634,14 +722,16 @@ size_t kv_decode_workspace(const echo_kv_pool &pool) {
 }
 
 bool kv_few_rows(const echo_kv_pool &pool, int64_t rows) {
-    return tile_rows(pool.kind == ECHO_CACHE_INT8, pool.d, rows) > 0;
+    return tile_rows(pool.kind != kBf16, pool.d, rows) > 0;
 }
 
 echo_status launch_kv_decode(const KvAttention &a, int64_t rows, cudaStream_t st) {
-    const bool i8 = a.pool->kind == ECHO_CACHE_INT8;
-    const int tile = tile_rows(i8, a.pool->d, rows);
-    if (a.pool->d == 64) return i8 ? launch_rows<true, 64>(a, tile, st) : launch_rows<false, 64>(a, tile, st);
-    return i8 ? launch_rows<true, 128>(a, tile, st) : launch_rows<false, 128>(a, tile, st);
+    const int form = a.pool->kind, tile = tile_rows(form != kBf16, a.pool->d, rows);
+    if (a.pool->d == 64)
+        return form == kInt4 ? launch_rows<kInt4, 64>(a, tile, st)
+               : form == kInt8 ? launch_rows<kInt8, 64>(a, tile, st) : launch_rows<kBf16, 64>(a, tile, st);
+    return form == kInt4 ? launch_rows<kInt4, 128>(a, tile, st)
+           : form == kInt8 ? launch_rows<kInt8, 128>(a, tile, st) : launch_rows<kBf16, 128>(a, tile, st);
 }
 
 }  // namespace echo

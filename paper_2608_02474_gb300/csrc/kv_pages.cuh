@@ -5,12 +5,19 @@
 #include "common.cuh"
 #include "internal.h"
 
-// a pool by value: pages [n_pages, 2, H, 1 << shift, d], scale [n_pages, 2, H, 1 << shift]
+// a pool by value: pages [n_pages, 2, H, 1 << shift, d], scale [n_pages, 2, H, 1 << shift]; for
+// 4-bit codes pages [.., d / 2] bytes, scale bf16 [.., 1 << shift, d / 32]
 struct KvPool {
     uint8_t *pages;
-    float *scale;
+    void *scale;
     int n_pages, shift, H;
 };
+
+// What pages hold, as a constant of the kernels: an echo_cache_kind.
+constexpr int kBf16 = ECHO_CACHE_BF16, kInt8 = ECHO_CACHE_INT8, kInt4 = ECHO_CACHE_INT4;
+constexpr int kv_bytes(int form, int values) {
+    return form == kInt4 ? values / 2 : form == kInt8 ? values : 2 * values;
+}
 
 struct KvBatch {
     const int32_t *table, *len, *row0;
@@ -66,6 +73,36 @@ ECHO_DEV uint32_t kv_codes2(uint32_t flipped, uint32_t sel) {
         : "r"(__byte_perm(flipped, 0u, sel)), "r"(0x7F007F00u), "r"(0xC000C000u));   // 2^127, -2
     return r;
 }
+
+// Four-bit codes of two columns in bits 4 i .. 4 i + 3 of w's halves, as a bf16 pair of
+// code s / 32, exactly.  The four bits go below a bf16 exponent of 0, which is 1 + (code + 8) / 16, and
+// (1 + (code + 8) / 16) s / 2 - 3 / 4 s = code s / 32: s of 5 significant bits leaves s / 2 and 3 / 4 s
+// (7 bits) and the result (8) without rounding, and nothing overflows that code s does not.  Whoever
+// multiplies takes the factor kNibbleUnit back.
+constexpr float kNibbleUnit = 32.f;
+struct KvScale2 {
+    uint32_t half, less;   // s / 2 and -3 / 4 s of two columns or keys
+};
+ECHO_DEV uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+ECHO_DEV KvScale2 kv_scale2(uint32_t s2) {
+    return {bf16x2_mul(s2, 0x3F003F00u), bf16x2_mul(s2, 0xBF40BF40u)};
+}
+template <int I>
+ECHO_DEV uint32_t kv_nibbles2(uint32_t w, const KvScale2 &s) {
+    const uint32_t x = ((I == 0 ? w << 3 : w >> (4 * I - 3)) & 0x00780078u) | 0x3F803F80u;
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(s.half), "r"(s.less));
+    return r;
+}
+// the halves of a pair of bf16 that are not finite: all ones there
+ECHO_DEV uint32_t kv_not_finite2(uint32_t v) {
+    return ((v & 0x7F80u) == 0x7F80u ? 0xffffu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0xffff0000u : 0u);
+}
+
 namespace echo {
 // argument checks of the entry points; ECHO_OK with *empty set: there is nothing to do
 echo_status kv_check(const echo_kv_pool *pool, const echo_kv_batch *batch, bool *empty);

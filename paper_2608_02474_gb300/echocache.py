@@ -40,7 +40,7 @@ class RateParams(_c.Structure):
     _fields_ = [("r_min", _f64), ("r_max", _f64), ("alpha", _f64)]
 
 
-CACHE_INT8, CACHE_BF16, CACHE_REF = 0, 1, 2
+CACHE_INT8, CACHE_BF16, CACHE_REF, CACHE_INT4 = 0, 1, 2, 3
 
 
 class CacheC(_c.Structure):
@@ -67,6 +67,34 @@ class KVPoolC(_c.Structure):
 class KVBatchC(_c.Structure):
     _fields_ = [("table", _vp), ("len", _vp), ("row0", _vp), ("n_seqs", _i32), ("max_pages", _i32),
                 ("n_rows", _i32), ("max_rows", _i32)]
+
+
+class KVTablesC(_c.Structure):
+    _fields_ = [("n_pages", _i32), ("page_tokens", _i32), ("n_slots", _i32), ("max_pages", _i32),
+                ("table", _vp), ("len", _vp), ("free_pages", _vp), ("n_free", _vp)]
+
+
+class RotaryPlanC(_c.Structure):
+    _fields_ = [("layout", _i32), ("axes", _i32), ("axis_pairs", _i32 * 4), ("frame_tokens", _i32),
+                ("row_tokens", _i32), ("size", _f32), ("turn", _vp)]
+
+
+class RotaryParams(_c.Structure):
+    _fields_ = [("theta", _f64), ("scaling", _i32), ("factor", _f64), ("original", _f64),
+                ("beta_fast", _f64), ("beta_slow", _f64)]
+
+
+class NormC(_c.Structure):
+    _fields_ = [("kind", _i32), ("eps", _f32), ("weight", _vp), ("bias", _vp)]
+
+
+class GatedNormPlanC(_c.Structure):
+    _fields_ = [("D", _i32), ("after", NormC), ("before", NormC), ("alpha", _f32), ("beta", _f32)]
+
+
+class ModulationC(_c.Structure):
+    _fields_ = [("gate", _vp), ("scale", _vp), ("shift", _vp), ("ld", _i64), ("n_mods", _i32),
+                ("rows_per_mod", _i32), ("rows", _vp), ("t", _i32)]
 
 
 _SIGS = {
@@ -107,6 +135,17 @@ _SIGS = {
     "echo_cache_dequant": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp, _i32, _vp]),
     "echo_kv_write": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _vp, _i64, _i32, _vp]),
     "echo_kv_read": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _vp, _i64, _i32, _vp]),
+    "echo_kv_write_at": (_i32, [_c.POINTER(KVPoolC), _vp, _i32, _vp, _vp, _i64, _i32, _vp]),
+    "echo_kv_tables_reset": (_i32, [_c.POINTER(KVTablesC), _vp]),
+    "echo_kv_extend": (_i32, [_c.POINTER(KVTablesC), _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                              _vp, _vp]),
+    "echo_kv_shorten": (_i32, [_c.POINTER(KVTablesC), _vp, _vp, _i32, _vp]),
+    "echo_rotary_turns": (_i32, [_c.POINTER(RotaryParams), _i32, _c.POINTER(_i32), _vp,
+                                 _c.POINTER(_f32)]),
+    "echo_rotary": (_i32, [_c.POINTER(RotaryPlanC), _vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32,
+                           _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp]),
+    "echo_gated_norm": (_i32, [_c.POINTER(GatedNormPlanC), _c.POINTER(ModulationC), _i32, _vp, _i64,
+                               _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp]),
     "echo_kv_attention_workspace_size": (_sz, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _i32]),
     "echo_kv_attention": (_i32, [_c.POINTER(KVPoolC), _c.POINTER(KVBatchC), _vp, _i64, _i32, _i32,
                                  _vp, _i64, _vp, _sz, _vp]),
@@ -166,6 +205,16 @@ _cur_device = torch.cuda.current_device
 
 def _stream(stream=None):
     return _raw_stream(_cur_device()) if stream is None else stream.cuda_stream
+
+
+def _stream_on(gpu: int, stream=None):
+    """The stream's handle for tensors on device `gpu`: without a stream, that device's current one, and
+    the device has to be the current one, since that is where kernels go."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _cur_device() != gpu:
+        raise ValueError(f"the tensors are on device {gpu}, which is not the current one")
+    return _raw_stream(gpu)
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -563,37 +612,45 @@ def echo_block_step_cache(weights: DeviceBlock, dims: BlockDims, x, idx, K: int,
 class KVPool:
     """A pool of key/value pages (echo_kv_pool) over the caller's tensors: pages int8 or
     bf16 [n_pages, 2, H, page_tokens, d] (keys, then values), with scale f32 [n_pages, 2,
-    H, page_tokens] where the pages hold int8 codes.  Pages need no initial contents."""
+    H, page_tokens] where the pages hold int8 codes; uint8 [.., d / 2] with scale bf16 [..,
+    page_tokens, d / 32] for 4-bit codes.  Pages need no initial contents."""
 
     def __init__(self, pages: torch.Tensor, scale: torch.Tensor | None = None):
         _dev(pages, "pages")
         if pages.dim() != 5 or pages.shape[1] != 2:
             raise ValueError("pages must be [n_pages, 2, H, page_tokens, d]")
-        if pages.dtype not in (torch.int8, torch.bfloat16):
+        if pages.dtype not in (torch.int8, torch.bfloat16, torch.uint8):
             raise TypeError(f"unsupported page dtype {pages.dtype}")
-        int8 = pages.dtype == torch.int8
-        if int8 != (scale is not None):
-            raise ValueError("int8 pages need scales, and bf16 pages have none")
-        if int8:
+        kind = {torch.int8: CACHE_INT8, torch.bfloat16: CACHE_BF16}.get(pages.dtype, CACHE_INT4)
+        if (kind != CACHE_BF16) != (scale is not None):
+            raise ValueError("int8 pages and those of 4 bits need scales, and bf16 pages have none")
+        d = 2 * pages.shape[4] if kind == CACHE_INT4 else pages.shape[4]
+        if kind != CACHE_BF16:
             _dev(scale, "scale")
-            if scale.dtype != torch.float32 or scale.shape != pages.shape[:4]:
+            if kind == CACHE_INT8 and (scale.dtype != torch.float32 or scale.shape != pages.shape[:4]):
                 raise ValueError("scale must be f32 [n_pages, 2, H, page_tokens]")
+            if kind == CACHE_INT4 and (scale.dtype != torch.bfloat16
+                                       or tuple(scale.shape) != (*pages.shape[:4], d // 32)):
+                raise ValueError("scale must be bf16 [n_pages, 2, H, page_tokens, d / 32]")
             if scale.get_device() != pages.get_device():
                 raise ValueError("pages and scale must be on one device")
         self.pages, self.scale, self._gpu = pages, scale, pages.get_device()
-        self.n_pages, _, self.H, self.page_tokens, self.d = pages.shape
-        self.cstruct = KVPoolC(CACHE_INT8 if int8 else CACHE_BF16, self.n_pages, self.page_tokens,
-                               self.H, self.d, _p(pages), _p(scale))
+        self.n_pages, _, self.H, self.page_tokens = pages.shape[:4]
+        self.kind, self.d = kind, d
+        self.cstruct = KVPoolC(kind, self.n_pages, self.page_tokens, self.H, self.d, _p(pages), _p(scale))
         self._ref = _c.byref(self.cstruct)
 
     @staticmethod
     def empty(kind: int, n_pages: int, page_tokens: int, H: int, d: int,
               device="cuda") -> "KVPool":
-        """A new pool of CACHE_INT8 or CACHE_BF16 pages."""
-        if kind not in (CACHE_INT8, CACHE_BF16):
-            raise ValueError("a pool holds CACHE_INT8 or CACHE_BF16 pages")
+        """A new pool of CACHE_INT8, CACHE_BF16 or CACHE_INT4 pages."""
+        if kind not in (CACHE_INT8, CACHE_BF16, CACHE_INT4):
+            raise ValueError("a pool holds CACHE_INT8 or CACHE_BF16 or CACHE_INT4 pages")
         int8 = kind == CACHE_INT8
         shape = (n_pages, 2, H, page_tokens, d)
+        if kind == CACHE_INT4:
+            return KVPool(torch.empty(*shape[:4], d // 2, dtype=torch.uint8, device=device),
+                          torch.empty(*shape[:4], d // 32, dtype=torch.bfloat16, device=device))
         return KVPool(torch.empty(shape, dtype=torch.int8 if int8 else torch.bfloat16, device=device),
                       torch.empty(shape[:4], dtype=torch.float32, device=device) if int8 else None)
 
@@ -669,6 +726,22 @@ def echo_kv_write(pool: KVPool, batch: KVBatch, k, v, stream=None):
                                                 _stream(stream)))
 
 
+def echo_kv_write_at(pool: KVPool, place, k, v, stream=None):
+    """Keys and values, [n, H d] bf16 or f32, into the places of a slot map, int64 [n]: page *
+    page_tokens + token of the page, as echo_kv_extend makes it; negative ones are left out."""
+    n, cols = place.numel(), pool.H * pool.d
+    if place.dtype != torch.int64:
+        raise TypeError("place must be int64")
+    if place.get_device() != pool._gpu or not place.is_contiguous():
+        raise ValueError("place must be a contiguous CUDA tensor on the pool's device")
+    ld = _rows_of(k, "k", n, cols, pool._gpu)
+    if _rows_of(v, "v", n, cols, pool._gpu) != ld and n > 1 or k.dtype != v.dtype:
+        raise ValueError("k and v must share dtype and row stride")
+    _check("echo_kv_write_at", lib().echo_kv_write_at(pool._ref, place.data_ptr(), n, k.data_ptr(), v.data_ptr(),
+                                                      ld if n > 1 else (cols + 7) // 8 * 8, _dtype(k),
+                                                      _stream_on(pool._gpu, stream)))
+
+
 def echo_kv_read(pool: KVPool, batch: KVBatch, dtype=torch.bfloat16, k=None, v=None, stream=None):
     """(k, v), [n_rows, H d] each: the cached rows at the positions of the batch's rows."""
     dev, shape = pool.pages.device, (batch.n_rows, pool.H * pool.d)
@@ -705,3 +778,237 @@ def echo_kv_attention(pool: KVPool, batch: KVBatch, q, Hq: int | None = None, ca
         pool._ref, batch._ref, q.data_ptr(), ldq, Hq, causal_block, out.data_ptr(), ldo,
         workspace.data_ptr(), workspace.nbytes, _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------------------
+def _ints(t, name, gpu, n=None, dtype=torch.int32):
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.get_device() != gpu or gpu < 0 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the device of the others")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return t.data_ptr()
+
+
+class KVTables:
+    """Page tables on the device (echo_kv_tables) over the caller's int32 tensors: table
+    [n_slots, max_pages], lens [n_slots], free_pages [n_pages], n_free [1].  Serves the pools of every layer."""
+
+    def __init__(self, table, lens, free_pages, n_free, page_tokens: int):
+        self._gpu = table.get_device()
+        if table.dim() != 2:
+            raise ValueError("table must be [n_slots, max_pages]")
+        ptr = (_ints(table, "table", self._gpu), _ints(lens, "lens", self._gpu, table.shape[0]),
+               _ints(free_pages, "free_pages", self._gpu), _ints(n_free, "n_free", self._gpu, 1))
+        self.table, self.lens, self.free_pages, self.n_free = table, lens, free_pages, n_free
+        self.n_slots, self.max_pages = table.shape
+        self.n_pages, self.page_tokens = free_pages.numel(), page_tokens
+        self.cstruct = KVTablesC(self.n_pages, page_tokens, self.n_slots, self.max_pages, *ptr)
+        self._ref = _c.byref(self.cstruct)
+
+    @staticmethod
+    def empty(n_pages: int, page_tokens: int, n_slots: int, max_pages: int, device="cuda",
+              stream=None) -> "KVTables":
+        """Tables of a new pool: all pages free, no tokens in any slot."""
+        new = lambda *n: _empty(n, torch.int32, device, stream)   # noqa: E731
+        t = KVTables(new(n_slots, max_pages), new(n_slots), new(n_pages), new(1), page_tokens)
+        t.reset(stream)
+        return t
+
+    def reset(self, stream=None):
+        _check("echo_kv_tables_reset", lib().echo_kv_tables_reset(self._ref, _stream_on(self._gpu, stream)))
+
+
+class KVStep:
+    """What echo_kv_extend makes of a step, in the caller's tensors: the batch's table int32
+    [n_seqs, max_pages], lens [n_seqs] and row0 [n_seqs + 1], and per row of the step its place in the pool
+    (int64), position and sequence (int32), -1 behind the last sequence's.  max_rows as for KVBatch."""
+
+    def __init__(self, table, lens, row0, place, pos, seq, max_rows: int | None = None):
+        self._gpu = table.get_device()
+        self.n_seqs, self.n_rows = lens.numel(), place.numel()
+        self.batch = KVBatch(table, lens, row0, self.n_rows, max_rows)
+        self._ptr = (table.data_ptr(), lens.data_ptr(), row0.data_ptr(),
+                     _ints(place, "place", self._gpu, dtype=torch.int64),
+                     _ints(pos, "pos", self._gpu, self.n_rows), _ints(seq, "seq", self._gpu, self.n_rows))
+        self.place, self.pos, self.seq = place, pos, seq
+
+    @staticmethod
+    def empty(tables: KVTables, n_seqs: int, n_rows: int, max_rows: int | None = None, stream=None) -> "KVStep":
+        """For steps of n_seqs sequences and up to n_rows rows over these tables."""
+        dev = tables.table.device
+        new = lambda *n, dtype=torch.int32: _empty(n, dtype, dev, stream)   # noqa: E731
+        return KVStep(new(n_seqs, tables.max_pages), new(n_seqs), new(n_seqs + 1), new(n_rows, dtype=torch.int64),
+                      new(n_rows), new(n_rows), max_rows)
+
+
+def echo_kv_extend(tables: KVTables, rows, step: KVStep, slots=None, stream=None) -> KVStep:
+    """Room for rows[b] more tokens in slot slots[b] (b itself without slots), rows and slots int32
+    on the device; the batch and the slot map of these rows go into `step`.  All or nothing: a call that
+    cannot be served sets the PAGE device flag and makes a step without rows."""
+    gpu = tables._gpu
+    if step._gpu != gpu or step.batch.cstruct.max_pages != tables.max_pages:
+        raise ValueError("step must be one of these tables: max_pages wide, on their device")
+    rows_p = _ints(rows, "rows", gpu, step.n_seqs)
+    slots_p = None if slots is None else _ints(slots, "slots", gpu, step.n_seqs)
+    table, lens, row0, place, pos, seq = step._ptr
+    _check("echo_kv_extend", lib().echo_kv_extend(tables._ref, slots_p, rows_p, step.n_seqs, step.n_rows, table, lens,
+                                                  row0, place, pos, seq, _stream_on(gpu, stream)))
+    return step
+
+
+def echo_kv_shorten(tables: KVTables, rows, slots=None, stream=None):
+    """The last rows[b] tokens of slot slots[b] given up, all where it has fewer, and the pages that
+    only they needed."""
+    n = rows.numel()
+    rows_p = _ints(rows, "rows", tables._gpu)
+    slots_p = None if slots is None else _ints(slots, "slots", tables._gpu, n)
+    _check("echo_kv_shorten", lib().echo_kv_shorten(tables._ref, slots_p, rows_p, n, _stream_on(tables._gpu, stream)))
+
+
+# ---------------------------------------------------------------------------
+_LAYOUTS = {"pairs": 0, "halves": 1}
+_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class Rotary:
+    """Rotary positions of heads of d columns (echo_rotary_plan): axis_pairs, how many pairs of columns
+    turn with each of a row's positions (one number: a single position); layout "pairs" (columns 2 i, 2 i + 1) or
+    "halves" (i, i + pairs); scaling "none", "linear", "ntk" or "yarn" by `factor` for contexts longer than
+    `original` positions.  frame = (tokens of a frame, of one of its rows): a row has one position, its
+    token index, and turns with frame, row and column."""
+
+    def __init__(self, d: int, axis_pairs, layout: str = "pairs", theta: float = 10000.0, scaling: str = "none",
+                 factor: float = 1.0, original: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                 frame: tuple[int, int] | None = None, device="cuda"):
+        pairs = [axis_pairs] if isinstance(axis_pairs, int) else list(axis_pairs)
+        if layout not in _LAYOUTS or scaling not in _SCALINGS:
+            raise ValueError(f"layout is one of {list(_LAYOUTS)}, scaling one of {list(_SCALINGS)}")
+        if not 1 <= len(pairs) <= 4 or min(pairs) < 0 or not 1 <= sum(pairs) <= d // 2:
+            raise ValueError("1 to 4 axes, with 1 to d / 2 pairs together")
+        self.d, self.pairs = d, sum(pairs)
+        self.columns = 1 if frame else len(pairs)           # positions of a row
+        host, size = np.zeros(self.pairs, dtype=np.uint64), _f32(0.0)
+        prm = RotaryParams(theta, _SCALINGS[scaling], factor, original, beta_fast, beta_slow)
+        _check("echo_rotary_turns", lib().echo_rotary_turns(_c.byref(prm), len(pairs), (_i32 * 4)(*pairs),
+                                                            host.ctypes.data, _c.byref(size)))
+        self.turn = torch.from_numpy(host.view(np.int64)).to(device)
+        self.size = size.value
+        self._gpu = self.turn.get_device()
+        self.cstruct = RotaryPlanC(_LAYOUTS[layout], len(pairs), (_i32 * 4)(*pairs), *(frame or (0, 0)), self.size,
+                                   self.turn.data_ptr())
+        self._ref = _c.byref(self.cstruct)
+
+
+def echo_rotary(plan: Rotary, pos, q, k=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """(q, k) turned by their rows' positions, or q alone: [n_rows, heads * d] bf16 or f32, pos
+    int32 [n_rows] (or [n_rows, axes]); rows of negative positions are left as they were in q_out and k_out.
+    q_out, k_out: new tensors when not given; q and k themselves turn in place.  inverse: back, which is the gradient."""
+    n, gpu, d = q.shape[0], plan._gpu, plan.d
+    t = _dtype(q)
+
+    def rows(x, out, name):
+        if x.dim() != 2 or x.shape[1] % d:
+            raise ValueError(f"{name} must be [n_rows, heads * {d}]")
+        ld = _rows_of(x, name, n, x.shape[1], gpu)
+        if out is None:
+            out = _empty(tuple(x.shape), x.dtype, x.device, stream)
+        elif out.shape != x.shape:
+            raise ValueError(f"{name} and {name}_out must have one shape")
+        if x.dtype != q.dtype or out.dtype != q.dtype:
+            raise TypeError("q, k and their outputs must share a dtype")
+        ldo = _rows_of(out, name + "_out", n, x.shape[1], gpu)
+        # strides of a single row mean nothing: what its columns take
+        return out, (ld, ldo) if n > 1 else ((x.shape[1] + 7) // 8 * 8,) * 2, x.shape[1] // d
+
+    q_out, (ldq, ldqo), Hq = rows(q, q_out, "q")
+    pos_p = _ints(pos, "pos", gpu, n * plan.columns)
+    if k is None:
+        args = (None, 0, 0, None, 0)
+    else:
+        k_out, (ldk, ldko), Hk = rows(k, k_out, "k")
+        args = (k.data_ptr(), ldk, Hk, k_out.data_ptr(), ldko)
+    _check("echo_rotary", lib().echo_rotary(plan._ref, pos_p, n, d, t, inverse, q.data_ptr(), ldq, Hq,
+                                            q_out.data_ptr(), ldqo, *args, _stream_on(gpu, stream)))
+    return q_out if k is None else (q_out, k_out)
+
+
+# ---------------------------------------------------------------------------
+_NORMS = {"none": 0, "layer": 1, "rms": 2}
+
+
+class GatedNorm:
+    """The norms around a gated residual over rows of D values (echo_gated_norm_plan): `before` of the new
+    residual ("layer", "rms" or "none") with weight and bias f32 [D] or none, `after` of the branch's output
+    with its own, and h = alpha x + beta gate * N_after(y)."""
+
+    def __init__(self, D: int, before: str = "layer", weight=None, bias=None, after: str = "none", after_weight=None,
+                 after_bias=None, eps: float = 1e-6, alpha: float = 1.0, beta: float = 1.0):
+        if before not in _NORMS or after not in _NORMS:
+            raise ValueError(f"a norm is one of {list(_NORMS)}")
+        self.D, self._keep = D, (weight, bias, after_weight, after_bias)
+        self._gpu = None
+        for name, v in zip(("weight", "bias", "after_weight", "after_bias"), self._keep):
+            if v is None:
+                continue
+            _dev(v, name)
+            if v.dtype != torch.float32 or v.numel() != D:
+                raise ValueError(f"{name} must be f32 [{D}]")
+            if self._gpu not in (None, v.get_device()):
+                raise ValueError("weights and biases must be on one device")
+            self._gpu = v.get_device()
+        self.cstruct = GatedNormPlanC(D, NormC(_NORMS[after], eps, _p(after_weight), _p(after_bias)),
+                                      NormC(_NORMS[before], eps, _p(weight), _p(bias)), alpha, beta)
+        self._ref = _c.byref(self.cstruct)
+
+
+def echo_gated_norm(plan: GatedNorm, x, y=None, gate=None, scale=None, shift=None, mod_rows=None,
+                    rows_per_mod: int = 0, h=None, n=None, want_h: bool = True, want_n: bool = True, stream=None):
+    """(h, n): h = alpha x + beta gate * N_after(y) and n = N_before(h) * (1 + scale) + shift, for x and y
+    [n_rows, D] bf16 or f32.  gate, scale and shift: [n_mods, D] of one dtype and row stride, each or none;
+    row r takes row mod_rows[r] (int32) of them, or r // rows_per_mod; rows whose number is no row are left out.
+    h has x's dtype and n is bf16 where they are not given; want_h, want_n: None instead."""
+    N, D, gpu = x.shape[0], plan.D, x.get_device()
+    if plan._gpu not in (None, gpu):
+        raise ValueError("x must be on the device of the weights")
+
+    def rows(t, name):
+        if t is None:
+            return None, 0, 0
+        ld = _rows_of(t, name, N, D, gpu)
+        if t.shape[1] != D:
+            raise ValueError(f"{name} must be [{N}, {D}]")
+        return t.data_ptr(), ld if N > 1 else (D + 7) // 8 * 8, _dtype(t)
+
+    xs, ys = rows(x, "x"), rows(y, "y")
+    if gpu < 0:
+        raise ValueError("x must be a CUDA tensor")
+    if not want_h:
+        h = None
+    elif h is None:
+        h = _empty((N, D), x.dtype, x.device, stream)
+    if not want_n:
+        n = None
+    elif n is None:
+        n = _empty((N, D), torch.bfloat16, x.device, stream)
+    mod = None
+    first = gate if gate is not None else scale if scale is not None else shift
+    if first is not None:
+        mods, ld, dtype, ptr = first.shape[0], first.stride(0), first.dtype, []
+        if mods == 1:                    # a single row's stride means nothing
+            ld = (D + 7) // 8 * 8
+        for name, v in (("gate", gate), ("scale", scale), ("shift", shift)):
+            if v is None:
+                ptr.append(None)
+                continue
+            if _rows_of(v, name, mods, D, gpu) != ld and mods > 1 or v.dtype != dtype or v.shape[1] != D:
+                raise ValueError(f"gate, scale and shift must be [n_mods, {D}] of one dtype and row stride")
+            ptr.append(v.data_ptr())
+        rows_p = None if mod_rows is None else _ints(mod_rows, "mod_rows", gpu, N)
+        mod = _c.byref(ModulationC(*ptr, ld, mods, rows_per_mod, rows_p, _dtype(first)))
+    elif mod_rows is not None:
+        raise ValueError("mod_rows without gate, scale or shift")
+    _check("echo_gated_norm", lib().echo_gated_norm(plan._ref, mod, N, *xs, *ys, *rows(h, "h"), *rows(n, "n"),
+                                                    _stream_on(gpu, stream)))
+    return h, n
