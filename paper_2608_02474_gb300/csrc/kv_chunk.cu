@@ -744,7 +744,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         __syncwarp();                         // read before the rows are written
 #pragma unroll
                         for (int c = 0; c < CHUNKS; ++c) {
-                            const KvScale2 s = kv_scale2(__byte_perm(sw[c / 2], 0u, c & 1 ? 0x3232u : 0x1010u));
+                            const uint32_t s = __byte_perm(sw[c / 2], 0u, c & 1 ? 0x3232u : 0x1010u);
                             const uint32_t w[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
 #pragma unroll
                             for (int h = 0; h < 4; ++h) {     // 8 values

@@ -311,25 +311,26 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         uint32_t r[4];
                         const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
                         ldsm4(kbase + chunk_at<FORM, D, BK>(row, INT4 ? kk / 2 + (mi >> 1) : INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
-                        KvScale2 f0, f1;
+                        // 4 bits, 8 packed rows: a group's scores by themselves, times the keys' scales; more
+                        // rows: the scales go into the keys
+                        constexpr bool APART = INT4 && NR == 1;
+                        float part[4];
 #pragma unroll
                         for (int i = 0; i < STEPS; ++i) {
                             uint32_t a[4] = {r[0], r[1], r[2], r[3]};
                             if constexpr (INT4) {
                                 const uint32_t w0 = r[2 * (i / 2)], w1 = r[2 * (i / 2) + 1];
-                                if (i % 2 == 0) {
+                                a[0] = i % 2 ? kv_nibbles2<2>(w0) : kv_nibbles2<0>(w0);
+                                a[1] = i % 2 ? kv_nibbles2<2>(w1) : kv_nibbles2<0>(w1);
+                                a[2] = i % 2 ? kv_nibbles2<3>(w0) : kv_nibbles2<1>(w0);
+                                a[3] = i % 2 ? kv_nibbles2<3>(w1) : kv_nibbles2<1>(w1);
+                                if constexpr (!APART) {
                                     const uint32_t both = i / 2 ? 0x3232u : 0x1010u;
-                                    f0 = kv_scale2(__byte_perm(ks[0][kk / 4], 0u, both));
-                                    f1 = kv_scale2(__byte_perm(ks[1][kk / 4], 0u, both));
-                                    a[0] = kv_nibbles2<0>(w0, f0);
-                                    a[1] = kv_nibbles2<0>(w1, f1);
-                                    a[2] = kv_nibbles2<1>(w0, f0);
-                                    a[3] = kv_nibbles2<1>(w1, f1);
-                                } else {
-                                    a[0] = kv_nibbles2<2>(w0, f0);
-                                    a[1] = kv_nibbles2<2>(w1, f1);
-                                    a[2] = kv_nibbles2<3>(w0, f0);
-                                    a[3] = kv_nibbles2<3>(w1, f1);
+                                    const uint32_t s0 = __byte_perm(ks[0][kk / 4], 0u, both), s1 = __byte_perm(ks[1][kk / 4], 0u, both);
+                                    a[0] = bf16x2_mul(a[0], s0);
+                                    a[1] = bf16x2_mul(a[1], s1);
+                                    a[2] = bf16x2_mul(a[2], s0);
+                                    a[3] = bf16x2_mul(a[3], s1);
                                 }
                             }
                             if constexpr (INT8) {
@@ -344,6 +345,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                                 if constexpr (C::Q_SMEM) {
                                     const uint2 b = q_smem[(nt * MT + kk + i) * 32 + lane];
                                     mma16816(sc[kg][nt], a, b.x, b.y);
+                                } else if constexpr (APART) {
+                                    if (i % 2 == 0) part[0] = part[1] = part[2] = part[3] = 0.f;
+                                    mma16816(part, a, qb[nt][kk + i][0], qb[nt][kk + i][1]);
+                                    if (i % 2) {
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e)
+                                            sc[kg][nt][e] = fmaf(part[e], i / 2 ? bf16hi(ks[e / 2][kk / 4]) : bf16lo(ks[e / 2][kk / 4]), sc[kg][nt][e]);
+                                    }
                                 } else {
                                     mma16816(sc[kg][nt], a, qb[nt][kk + i][0], qb[nt][kk + i][1]);
                                 }
@@ -354,6 +363,21 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 // in the exponent of two: keys gq and gq + 8 of each 16, rows 2 tq and 2 tq + 1
                 const float *scales = reinterpret_cast<const float *>(token_scales) + wk + gq;
                 const bool edge = key0 + KPW > low;      // some row does not see all of these keys
+                uint32_t spoilt = 0;                     // 4 bits: of this lane's key, and of all
+                if (INT4 && edge) {
+                    // values' scales that are not finite, or anything past the end: 0, and what is
+                    // spoilt spoils the rows that see it.  This warp's keys alone.
+                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + lane) * C::TOKEN_SCALES);
+#pragma unroll
+                    for (int i = 0; i < C::TOKEN_SCALES / 4; ++i) {
+                        const uint32_t off = kv_not_finite2(at[i]);
+                        spoilt |= off;
+                        if (off) at[i] &= ~off;
+                    }
+                    spoilt = __ballot_sync(0xffffffffu, spoilt != 0u);
+                    fence_proxy_async_smem();            // before the copies of a later block
+                    __syncwarp();
+                }
                 float vs[KG][2];
 #pragma unroll
                 for (int kg = 0; kg < KG; ++kg)
@@ -376,12 +400,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                                 bad = !(fabsf(vs[kg][h]) < INFINITY);
                                 if (bad) vs[kg][h] = 0.f;
                             }
-                            if constexpr (INT4) {
-                                uint32_t w[D / 64];
-                                load_words(token_scales + (BK + wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES, w);
-#pragma unroll
-                                for (int i = 0; i < D / 64; ++i) bad |= kv_not_finite2(w[i]) != 0u;
-                            }
+                            if constexpr (INT4) bad = (spoilt >> (kg * 16 + 8 * h + gq)) & 1u;
 #pragma unroll
                             for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
@@ -510,17 +529,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         if constexpr (INT4) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {            // a group of 32 columns
-                                KvScale2 f[2];
+                                uint32_t s2[2];
 #pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    uint32_t s2 = __byte_perm(vw[h][0][t / 4], vw[h][1][t / 4], i ? 0x7632u : 0x5410u);
-                                    if (edge) s2 &= ~kv_not_finite2(s2);   // spoilt above; or past the end, anything
-                                    f[h] = kv_scale2(s2);
-                                }
-                                const uint32_t a[4] = {kv_nibbles2<0>(r[2 * i], f[0]), kv_nibbles2<1>(r[2 * i], f[0]),
-                                                       kv_nibbles2<0>(r[2 * i + 1], f[1]), kv_nibbles2<1>(r[2 * i + 1], f[1])};
-                                const uint32_t c[4] = {kv_nibbles2<2>(r[2 * i], f[0]), kv_nibbles2<3>(r[2 * i], f[0]),
-                                                       kv_nibbles2<2>(r[2 * i + 1], f[1]), kv_nibbles2<3>(r[2 * i + 1], f[1])};
+                                for (int h = 0; h < 2; ++h)
+                                    s2[h] = __byte_perm(vw[h][0][t / 4], vw[h][1][t / 4], i ? 0x7632u : 0x5410u);
+                                const uint32_t a[4] = {kv_nibbles2<0>(r[2 * i], s2[0]), kv_nibbles2<1>(r[2 * i], s2[0]),
+                                                       kv_nibbles2<0>(r[2 * i + 1], s2[1]), kv_nibbles2<1>(r[2 * i + 1], s2[1])};
+                                const uint32_t c[4] = {kv_nibbles2<2>(r[2 * i], s2[0]), kv_nibbles2<3>(r[2 * i], s2[0]),
+                                                       kv_nibbles2<2>(r[2 * i + 1], s2[1]), kv_nibbles2<3>(r[2 * i + 1], s2[1])};
 #pragma unroll
                                 for (int nt = 0; nt < NR; ++nt) {
                                     mma16816(o[nt][t + 2 * i], a, b[nt][0], b[nt][1]);

@@ -74,30 +74,28 @@ ECHO_DEV uint32_t kv_codes2(uint32_t flipped, uint32_t sel) {
     return r;
 }
 
-// Four-bit codes of two columns in bits 4 i .. 4 i + 3 of w's halves, as a bf16 pair of
-// code s / 32, exactly.  The four bits go below a bf16 exponent of 0, which is 1 + (code + 8) / 16, and
-// (1 + (code + 8) / 16) s / 2 - 3 / 4 s = code s / 32: s of 5 significant bits leaves s / 2 and 3 / 4 s
-// (7 bits) and the result (8) without rounding, and nothing overflows that code s does not.  Whoever
-// multiplies takes the factor kNibbleUnit back.
-constexpr float kNibbleUnit = 32.f;
-struct KvScale2 {
-    uint32_t half, less;   // s / 2 and -3 / 4 s of two columns or keys
-};
+// Four-bit codes of two columns, nibble I of w's halves, as a bf16 pair of code / 64, exactly: as
+// for int8, the nibbles stand alone in the halves as numbers of 2^-133 (the higher one of a byte as 16
+// times that, bit 7 being the first of the exponents'), and a fused multiply-add makes (n - 8) / 64 of
+// them.  A shift serves two nibbles: the integer pipe, of half the rate, is the one that fills up.
+constexpr float kNibbleUnit = 64.f;   // what scores and sums are multiplied by in return
+template <int I>
+ECHO_DEV uint32_t kv_nibbles2(uint32_t w) {
+    const uint32_t x = (I < 2 ? w : w >> 8) & (I % 2 ? 0x00F000F0u : 0x000F000Fu);
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;"
+        : "=r"(r)
+        : "r"(x), "r"(I % 2 ? 0x7D007D00u : 0x7F007F00u), "r"(0xBE00BE00u));   // 2^123 or 2^127, -1 / 8
+    return r;
+}
+// times the scales of two columns or keys: code s / 64, exact for s of 5 significant bits
 ECHO_DEV uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-ECHO_DEV KvScale2 kv_scale2(uint32_t s2) {
-    return {bf16x2_mul(s2, 0x3F003F00u), bf16x2_mul(s2, 0xBF40BF40u)};
-}
 template <int I>
-ECHO_DEV uint32_t kv_nibbles2(uint32_t w, const KvScale2 &s) {
-    const uint32_t x = ((I == 0 ? w << 3 : w >> (4 * I - 3)) & 0x00780078u) | 0x3F803F80u;
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(s.half), "r"(s.less));
-    return r;
-}
+ECHO_DEV uint32_t kv_nibbles2(uint32_t w, uint32_t s2) { return bf16x2_mul(kv_nibbles2<I>(w), s2); }
 // the halves of a pair of bf16 that are not finite: all ones there
 ECHO_DEV uint32_t kv_not_finite2(uint32_t v) {
     return ((v & 0x7F80u) == 0x7F80u ? 0xffffu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0xffff0000u : 0u);
