@@ -229,6 +229,264 @@ gated_norm_kernel(const NormParams p) {
     }
 }
 
+// Many rows of more than 1024 values: a chunk of 8 columns to a thread, so that its gate, scale and
+// shift stay in registers while the rows' modulation is the same, and R rows at a time, whose sums
+// share their barriers.  Rows come by bulk copies into two buffers of R rows; a buffer is
+// filled again as soon as its rows are in registers, while the sums of these are under way.
+#ifndef STREAM_ROWS
+#define STREAM_ROWS 8
+#endif
+
+// R sums over the block, in all threads.  A lane passes on half of what it holds at a time, so
+// that R = 4 sums take 6 exchanges and not 20.
+template <int R>
+ECHO_DEV void block_sums(float (&v)[R], float4 (*part)[32], int &turn) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    auto reduce = [&](float a, float b, float c, float d) -> float {   // of row lane / 8
+        const bool high = lane & 16;
+        const float x = high ? c : a, y = high ? d : b;
+        float s0 = x + __shfl_xor_sync(0xffffffffu, high ? a : c, 16), s1 = y + __shfl_xor_sync(0xffffffffu, high ? b : d, 16);
+        const bool odd = lane & 8;
+        float s = (odd ? s1 : s0) + __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, 8);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    };
+    float4 *at = part[turn & 1];
+    ++turn;
+    const float s = reduce(v[0], v[1 % R], R > 2 ? v[2 % R] : 0.f, R > 2 ? v[3 % R] : 0.f);
+    if ((lane & 7) == 0) reinterpret_cast<float *>(&at[warp])[lane >> 3] = s;
+    __syncthreads();
+    const float4 w = lane < warps ? at[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float all = reduce(w.x, w.y, w.z, w.w);
+#pragma unroll
+    for (int k = 0; k < R; ++k) v[k] = __shfl_sync(0xffffffffu, all, 8 * k);
+}
+
+// Values in pairs: one instruction for two of them.
+struct Pairs {
+    uint64_t v[4];
+};
+ECHO_DEV Pairs splat(float x) { return {{f2_pack(x, x), f2_pack(x, x), f2_pack(x, x), f2_pack(x, x)}}; }
+ECHO_DEV Pairs pairs_of(const float *f) {
+    return {{f2_pack(f[0], f[1]), f2_pack(f[2], f[3]), f2_pack(f[4], f[5]), f2_pack(f[6], f[7])}};
+}
+ECHO_DEV void floats_of(const Pairs &p, float *f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f2_unpack(p.v[i], f[2 * i], f[2 * i + 1]);
+}
+ECHO_DEV Pairs fma8(const Pairs &a, const Pairs &b, const Pairs &c) {
+    return {{f2_fma(a.v[0], b.v[0], c.v[0]), f2_fma(a.v[1], b.v[1], c.v[1]), f2_fma(a.v[2], b.v[2], c.v[2]), f2_fma(a.v[3], b.v[3], c.v[3])}};
+}
+ECHO_DEV Pairs mul8(const Pairs &a, const Pairs &b) {
+    return {{f2_mul(a.v[0], b.v[0]), f2_mul(a.v[1], b.v[1]), f2_mul(a.v[2], b.v[2]), f2_mul(a.v[3], b.v[3])}};
+}
+ECHO_DEV Pairs add8(const Pairs &a, const Pairs &b) {
+    return {{f2_add(a.v[0], b.v[0]), f2_add(a.v[1], b.v[1]), f2_add(a.v[2], b.v[2]), f2_add(a.v[3], b.v[3])}};
+}
+ECHO_DEV float sum8(const Pairs &a) {
+    float x, y;
+    f2_unpack(f2_add(f2_add(a.v[0], a.v[1]), f2_add(a.v[2], a.v[3])), x, y);
+    return x + y;
+}
+ECHO_DEV float square8(const Pairs &a) {
+    float x, y;
+    f2_unpack(f2_add(f2_fma(a.v[0], a.v[0], f2_mul(a.v[1], a.v[1])), f2_fma(a.v[2], a.v[2], f2_mul(a.v[3], a.v[3]))), x, y);
+    return x + y;
+}
+ECHO_DEV Pairs shared_pairs(const void *p, int64_t at, bool f32) {
+    float f[8];
+    shared8(p, at, f32, f);
+    return pairs_of(f);
+}
+
+// R rows' chunks from shared memory; zeros past the row's end and the last row
+template <int R, int N>
+ECHO_DEV void staged(const uint8_t *rows, uint32_t row_bytes, bool f32, int t, int n, Pairs (&v)[N]) {
+    if (f32) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            float f[8] = {};
+            if (k < n) {
+                floats4(reinterpret_cast<const uint4 *>(rows + k * row_bytes)[2 * t], f);
+                floats4(reinterpret_cast<const uint4 *>(rows + k * row_bytes)[2 * t + 1], f + 4);
+            }
+            v[k] = pairs_of(f);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (k < n) w = reinterpret_cast<const uint4 *>(rows + k * row_bytes)[t];
+            float f[8];
+            unpack8_bf16(w, f);
+            v[k] = pairs_of(f);
+        }
+    }
+}
+template <int R>
+ECHO_DEV void store_rows(uint8_t *to, int64_t stride, bool f32, const int (&m)[R], const Pairs (&v)[R]) {
+#pragma unroll
+    for (int k = 0; k < R; ++k, to += stride) {
+        float f[8];
+        floats_of(v[k], f);
+        if (m[k] >= 0) store8(to, 0, f32, f);
+    }
+}
+
+// 1 / root of the rows' spread, v centred (LAYER); between(): after the first barrier
+template <int R, typename F>
+ECHO_DEV void spreads(const Norm &n, float inv_d, bool live, Pairs (&v)[R], float (&f)[R], float4 (*part)[32], int &turn, F between) {
+    if (n.kind == ECHO_NORM_LAYER) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) f[k] = sum8(v[k]);
+        block_sums<R>(f, part, turn);
+        between();
+        const float less = live ? -inv_d : 0.f;      // threads past the row's end keep their zeros
+#pragma unroll
+        for (int k = 0; k < R; ++k) v[k] = add8(v[k], splat(f[k] * less));
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) f[k] = square8(v[k]);
+    block_sums<R>(f, part, turn);
+    if (n.kind != ECHO_NORM_LAYER) between();
+#pragma unroll
+    for (int k = 0; k < R; ++k) f[k] = rsqrtf(f[k] * inv_d + n.eps);
+}
+ECHO_DEV Pairs affine8(const Norm &n, int c, Pairs v) {
+    if (n.weight) v = mul8(v, shared_pairs(n.weight, 8 * c, true));
+    if (n.bias) v = add8(v, shared_pairs(n.bias, 8 * c, true));
+    return v;
+}
+
+template <int R, bool AFTER, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+gated_norm_rows_kernel(const NormParams p, int *err) {
+    extern __shared__ __align__(128) uint8_t buf[];
+    __shared__ __align__(8) uint64_t full[2];
+    __shared__ float4 part[2][32];
+    __shared__ int abort_flag;
+    const int t = threadIdx.x;
+    const bool live = t < p.chunks;
+    const uint32_t xb = (uint32_t)p.chunks * (p.xf ? 32u : 16u), yb = p.y ? (uint32_t)p.chunks * (p.yf ? 32u : 16u) : 0u;
+    const uint32_t row_bytes = xb + yb;
+    if (t == 0) {
+        mbar_init(&full[0], 1);
+        mbar_init(&full[1], 1);
+        abort_flag = 0;
+        fence_barrier_init();
+    }
+    __syncthreads();
+    pdl_enter();
+    const int first = (int)((int64_t)p.n_rows * blockIdx.x / gridDim.x);
+    const int last = (int)((int64_t)p.n_rows * (blockIdx.x + 1) / gridDim.x);
+    const int batches = (last - first + R - 1) / R;
+    auto fetch = [&](int i) {            // one thread
+        const int r0 = first + i * R, n = min(R, last - r0);
+        uint8_t *dst = buf + (i & 1) * (R * row_bytes);
+        mbar_arrive_expect_tx(&full[i & 1], n * row_bytes);
+        for (int k = 0; k < n; ++k, dst += row_bytes) {
+            const int64_t r = r0 + k;
+            bulk_load_1d(dst, static_cast<const uint8_t *>(p.x) + r * p.ldx * (p.xf ? 4 : 2), xb, &full[i & 1]);
+            if (p.y) bulk_load_1d(dst + xb, static_cast<const uint8_t *>(p.y) + r * p.ldy * (p.yf ? 4 : 2), yb, &full[i & 1]);
+        }
+    };
+    if (t == 0) {
+        if (batches > 0) fetch(0);
+        if (batches > 1) fetch(1);
+    }
+    // the modulation's row of the batch's rows; -1: the row is left as it is
+    auto mods = [&](int i, int (&m)[R]) {
+        const int r0 = first + i * R;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            m[k] = 0;
+            if (p.n_mods >= 0 && r0 + k < last) m[k] = p.mod_rows ? p.mod_rows[r0 + k] : (r0 + k) / p.rows_per_mod;
+        }
+    };
+    int m[R], next[R], turn = 0, gate_m = -1, out_m = -1;
+    const Pairs alpha = splat(p.alpha);
+    Pairs gate = splat(p.beta), scale = splat(1.f), shift = splat(0.f);   // beta gate, 1 + scale
+    uint8_t *h_to = static_cast<uint8_t *>(p.h) + (first * p.ldh + 8 * t) * (p.hf ? 4 : 2);
+    uint8_t *n_to = static_cast<uint8_t *>(p.n) + (first * p.ldn + 8 * t) * (p.nf ? 4 : 2);
+    const int64_t h_row = p.ldh * (p.hf ? 4 : 2), n_row = p.ldn * (p.nf ? 4 : 2);
+    mods(0, next);
+    bool ok = true;
+    for (int i = 0; i < batches; ++i) {
+        const int n = min(R, last - first - i * R);
+#pragma unroll
+        for (int k = 0; k < R; ++k) m[k] = k < n && live && (p.n_mods < 0 || (unsigned)next[k] < (unsigned)p.n_mods) ? next[k] : -1;
+        if (i + 1 < batches) mods(i + 1, next);
+        // a wait that gives up lets the others give up; nothing is stored from then on
+        ok = ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err);
+        const uint8_t *rows = buf + (i & 1) * (R * row_bytes);
+        auto refill = [&]() {            // the rows are in registers, behind a barrier
+            if (t == 0 && ok && i + 2 < batches) fetch(i + 2);
+        };
+        Pairs h[R];
+        float f[R];
+        staged<R>(rows, row_bytes, p.xf, t, live ? n : 0, h);
+#pragma unroll
+        for (int k = 0; k < R; ++k) h[k] = mul8(h[k], alpha);
+        if (p.y) {
+            Pairs y[AFTER ? R : 1];
+            if constexpr (AFTER) {
+                staged<R>(rows + xb, row_bytes, p.yf, t, live ? n : 0, y);
+                spreads<R>(p.after, p.inv_d, live, y, f, part, turn, [] {});
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                constexpr int ONE = AFTER ? R : 1;           // AFTER: y[k], else a row at a time
+                Pairs &yk = y[k % ONE];
+                if constexpr (!AFTER) staged<1>(rows + k * row_bytes + xb, row_bytes, p.yf, t, live ? n - k : 0, y);
+                if (p.gate && m[k] != gate_m && m[k] >= 0) {
+                    gate = mul8(shared_pairs(p.gate, m[k] * p.ldm + 8 * t, p.mf), splat(p.beta));
+                    gate_m = m[k];
+                }
+                if constexpr (AFTER) {
+                    yk = mul8(yk, splat(f[k]));
+                    if (live) yk = affine8(p.after, t, yk);
+                }
+                h[k] = fma8(gate, yk, h[k]);
+            }
+        }
+        if (!ok) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) m[k] = -1;
+        }
+        if (p.h) store_rows<R>(h_to, h_row, p.hf, m, h);
+        const bool normed = p.n && p.before.kind != ECHO_NORM_NONE;
+        if (normed) {
+            spreads<R>(p.before, p.inv_d, live, h, f, part, turn, refill);
+        } else {
+            __syncthreads();
+            refill();
+        }
+        if (p.n) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (m[k] != out_m && m[k] >= 0) {
+                    if (p.scale) scale = add8(shared_pairs(p.scale, m[k] * p.ldm + 8 * t, p.mf), splat(1.f));
+                    if (p.shift) shift = shared_pairs(p.shift, m[k] * p.ldm + 8 * t, p.mf);
+                    out_m = m[k];
+                }
+                if (normed) {
+                    h[k] = mul8(h[k], splat(f[k]));
+                    if (live) h[k] = affine8(p.before, t, h[k]);
+                }
+                h[k] = fma8(h[k], scale, shift);
+            }
+            store_rows<R>(n_to, n_row, p.nf, m, h);
+        }
+        h_to += R * h_row;
+        n_to += R * n_row;
+    }
+    // copies land before this block exits
+    if (!ok && t == 0) {
+        for (int i = 0; i < 4; ++i) mbar_land(&full[i & 1], i >> 1);
+    }
+}
+
 template <int TPR, int CH>
 void launch(const NormParams &p, cudaStream_t st) {
     constexpr int RPB = TPR == 32 ? 8 : 1, THREADS = TPR == 32 ? 256 : TPR;
@@ -247,8 +505,35 @@ void launch(const NormParams &p, cudaStream_t st) {
     echo::launch_chained(gated_norm_kernel<TPR, CH>, dim3(grid), dim3(THREADS), 0, st, p);
 }
 
+template <int R, bool AFTER, int THREADS>
+void launch_rows(const NormParams &p, cudaStream_t st) {
+    const int threads = (p.chunks + 31) / 32 * 32;
+    const size_t smem = 2ull * R * p.chunks * ((p.xf ? 32 : 16) + (p.y ? (p.yf ? 32 : 16) : 0));
+    static int attr_done[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 0 && dev < 64 && !attr_done[dev]) {
+        cudaFuncSetAttribute(gated_norm_rows_kernel<R, AFTER, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+        attr_done[dev] = 1;
+    }
+    int blocks = 1;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, gated_norm_rows_kernel<R, AFTER, THREADS>, threads, smem) != cudaSuccess || blocks < 1)
+        blocks = 1;
+    const int64_t all = ((int64_t)p.n_rows + R - 1) / R, most = (int64_t)echo::num_sms() * blocks;
+    const int grid = (int)(all < most ? all : most);
+    echo::launch_chained(gated_norm_rows_kernel<R, AFTER, THREADS>, dim3(grid), dim3(threads), smem, st, p, echo::device_error_ptr());
+}
+
 void launch_width(const NormParams &p, cudaStream_t st) {
     const int c = p.chunks;
+    const int row_bytes = c * ((p.xf ? 32 : 16) + (p.y ? (p.yf ? 32 : 16) : 0));
+    if (c > 128 && p.n_rows >= 152 * STREAM_ROWS) {
+        const bool after = p.y && p.after.kind != ECHO_NORM_NONE;
+        if (!after && c <= 640 && 8 * row_bytes <= 200 * 1024) return launch_rows<4, false, 640>(p, st);
+        if (after && c <= 640 && 4 * row_bytes <= 200 * 1024) return launch_rows<2, true, 640>(p, st);
+        if (!after && c <= 1024 && 4 * row_bytes <= 200 * 1024) return launch_rows<2, false, 1024>(p, st);
+        if (after && c <= 1024 && 2 * row_bytes <= 200 * 1024) return launch_rows<1, true, 1024>(p, st);
+    }
     if (c <= 32) return launch<32, 1>(p, st);
     if (c <= 64) return launch<32, 2>(p, st);
     if (c <= 128) return launch<32, 4>(p, st);

@@ -35,6 +35,7 @@ struct Cfg {
     static constexpr int GROUPS = NR * D <= (CODES ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
     static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
     static constexpr int KPW = CODES ? 32 : 16;            // keys of a warp
+    static constexpr int KG = KPW / 16;                    // 16 keys of a warp, this many at once
     static constexpr int BK = 4 * KPW;                     // keys of a block
     static constexpr int BSHIFT = CODES ? 7 : 6;
     static constexpr int ROW_BYTES = kv_bytes(FORM, D);
@@ -88,7 +89,13 @@ ECHO_DEV void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
 // neighbouring words of shared memory, read at once
 template <int N>
 ECHO_DEV void load_words(const uint8_t *from, uint32_t (&to)[N]) {
-    if constexpr (N == 2) {
+    if constexpr (N == 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(from);
+        to[0] = v.x;
+        to[1] = v.y;
+        to[2] = v.z;
+        to[3] = v.w;
+    } else if constexpr (N == 2) {
         const uint2 v = *reinterpret_cast<const uint2 *>(from);
         to[0] = v.x;
         to[1] = v.y;
@@ -110,7 +117,7 @@ __global__ void __launch_bounds__((Cfg<FORM, D, NR>::THREADS), 2)
 kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     using C = Cfg<FORM, D, NR>;
     constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4, CODES = C::CODES;
-    constexpr int KPW = C::KPW, BK = C::BK, KG = KPW / 16, MT = D / 16, ROWS = C::ROWS;
+    constexpr int KG = C::KG, STEP = 16 * KG, BK = C::BK, MT = D / 16, ROWS = C::ROWS;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                 ~static_cast<uintptr_t>(1023));
@@ -219,7 +226,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     // ---------------- groups of four warps, a quarter of each block's keys each ----------------
     // a fragment's row group and column pair; lane's row and chunk in four 8x8 matrices
     const int gq = lane >> 2, tq = lane & 3, mi = lane >> 3, mr = lane & 7;
-    const int wk = (warp & 3) * KPW;                 // this warp's first key of a block
+    const int wk0 = (warp & 3) * C::KPW;             // this warp's first key of a block
     const uint32_t ring = smem_u32(smem);
     int g = 0;
     bool ok = true;
@@ -291,9 +298,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             const int stage = g % C::RING;
             ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (g / C::RING) & 1, abort_v, p.err));
             if (!ok) break;
-            const int key0 = kb * BK + wk;               // this warp's first key
             const uint32_t kbase = ring + stage * C::STAGE, vbase = kbase + C::HALF;
-            if (key0 < keys && (C::GROUPS == 1 || (g & 1) == warp >> 2)) {
+            if (C::GROUPS == 1 || (g & 1) == warp >> 2)
+#pragma unroll 1
+            for (int k0 = 0; k0 < C::KPW; k0 += STEP) {
+                const int wk = wk0 + k0, key0 = kb * BK + wk;    // the first key of this step
+                if (key0 >= keys) break;
                 // S^T = K Q^T, 16 keys at a time
                 float sc[KG][NR][4] = {};
                 const uint8_t *token_scales = smem + stage * C::STAGE + 2 * C::HALF;
@@ -362,12 +372,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 }
                 // in the exponent of two: keys gq and gq + 8 of each 16, rows 2 tq and 2 tq + 1
                 const float *scales = reinterpret_cast<const float *>(token_scales) + wk + gq;
-                const bool edge = key0 + KPW > low;      // some row does not see all of these keys
+                const bool edge = key0 + STEP > low;      // some row does not see all of these keys
                 uint32_t spoilt = 0;                     // 4 bits: of this lane's key, and of all
                 if (INT4 && edge) {
                     // values' scales that are not finite, or anything past the end: 0, and what is
                     // spoilt spoils the rows that see it.  This warp's keys alone.
-                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + lane) * C::TOKEN_SCALES);
+                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + (lane & (STEP - 1))) * C::TOKEN_SCALES);
 #pragma unroll
                     for (int i = 0; i < C::TOKEN_SCALES / 4; ++i) {
                         const uint32_t off = kv_not_finite2(at[i]);
@@ -466,7 +476,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) l[nt][e] += add[nt][e];
                 // O^T += V^T P^T
-                const bool tail = key0 + KPW > keys;     // V rows past the last key: not copied
+                const bool tail = key0 + STEP > keys;     // V rows past the last key: not copied
 #pragma unroll
                 for (int kg = 0; kg < KG; ++kg) {
                     uint32_t b[NR][2];
@@ -514,13 +524,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         }
                     }
                     // 4 bits: the scales of keys 2 tq, 2 tq + 1 and of 8 keys further on, as the weights lie
-                    uint32_t vw[2][2][D / 64];
+                    uint32_t vw[2][2 * (D / 64)];
                     if constexpr (INT4) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                load_words(token_scales + (BK + wk + kg * 16 + 8 * h + 2 * tq + e) * C::TOKEN_SCALES, vw[h][e]);
+                            load_words(token_scales + (BK + wk + kg * 16 + 8 * h + 2 * tq) * C::TOKEN_SCALES, vw[h]);
                     }
 #pragma unroll
                     for (int t = 0; t < MT; t += STEPS) {
@@ -532,7 +540,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                                 uint32_t s2[2];
 #pragma unroll
                                 for (int h = 0; h < 2; ++h)
-                                    s2[h] = __byte_perm(vw[h][0][t / 4], vw[h][1][t / 4], i ? 0x7632u : 0x5410u);
+                                    s2[h] = __byte_perm(vw[h][t / 4], vw[h][D / 64 + t / 4], i ? 0x7632u : 0x5410u);
                                 const uint32_t a[4] = {kv_nibbles2<0>(r[2 * i], s2[0]), kv_nibbles2<1>(r[2 * i], s2[0]),
                                                        kv_nibbles2<0>(r[2 * i + 1], s2[1]), kv_nibbles2<1>(r[2 * i + 1], s2[1])};
                                 const uint32_t c[4] = {kv_nibbles2<2>(r[2 * i], s2[0]), kv_nibbles2<3>(r[2 * i], s2[0]),

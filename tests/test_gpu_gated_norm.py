@@ -121,6 +121,49 @@ def test_numbers_of_rows(ec, n, D):
     assert all((a[n // 2] == b[0]).all() for a, b in zip(got, one))
 
 
+@pytest.mark.parametrize("D", [1032, 2048, 5120, 5128, 8192])
+@pytest.mark.parametrize("after,before", [("none", "layer"), ("none", "none"), ("layer", "rms"), ("rms", "layer")])
+@pytest.mark.parametrize("xt,yt", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
+def test_many_rows(ec, D, after, before, xt, yt):
+    """Rows that are copied ahead: sequences of modulations that change within and between
+    batches, rows of none among them, in place, and the last rows of a block."""
+    import torch
+    n, mods = 4001, 9
+    x, y = rows(n, D, xt, D), rows(n, D, yt, D + 1, wide=True)
+    table = rows(mods, 3 * D, "f32", 5) / 4
+    gate, scale, shift = (table[:, i * D:(i + 1) * D] for i in range(3))
+    g = np.random.default_rng(D)
+    m = np.sort(g.integers(0, mods, n))
+    m[1000:1100] = g.integers(0, mods, 100)
+    m[[5, 2000, 2001, 4000]] = [-1, mods, 2 ** 30, -2 ** 31]
+    live = (m >= 0) & (m < mods)
+    w, b = (torch.from_numpy(g.standard_normal(D).astype(F32)).cuda() for _ in range(2))
+    plan = ec.GatedNorm(D, before, *((w, b) if before != "none" else (None, None)), after=after,
+                        after_weight=b if after != "none" else None, alpha=1.5, beta=0.5)
+    k = torch.full((n, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    xx = x.clone()
+    mod = torch.from_numpy(m.astype(np.int32)).cuda()
+    ec.echo_gated_norm(plan, xx, y, gate, scale, shift, mod_rows=mod, h=xx, n=k)
+    again = ec.echo_gated_norm(plan, x, y, gate, scale, shift, mod_rows=mod)
+    ok = torch.from_numpy(live)
+    assert (xx[ok] == again[0][ok]).all() and (k[ok] == again[1][ok]).all()
+    assert (xx[~ok] == x[~ok]).all() and (k[~ok] == 7.0).all()
+    some = np.unique(np.concatenate([np.arange(30), np.arange(1000, 1100), np.arange(3950, n), g.integers(0, n, 60)]))
+    at = torch.from_numpy(some).cuda()
+    pick = lambda a: host(a)[np.where(live, m, 0)[some]]      # noqa: E731
+    check((xx[at], k[at]), host(x[at]), host(y[at]), pick(gate), pick(scale), pick(shift), live[some], before,
+          *((host(w), host(b)) if before != "none" else (None, None)), after, host(b) if after != "none" else None, None,
+          1.5, 0.5)
+    # without a branch, n or h alone, rows by number
+    h, k = ec.echo_gated_norm(plan, x, scale=scale, shift=shift, rows_per_mod=500)
+    mm = (some // 500)
+    check((h[at], k[at]), host(x[at]), None, None, host(scale)[mm], host(shift)[mm], slice(None), before,
+          *((host(w), host(b)) if before != "none" else (None, None)), "none", None, None, 1.5, 0.5)
+    assert (ec.echo_gated_norm(plan, x, scale=scale, shift=shift, rows_per_mod=500, want_h=False)[1] == k).all()
+    assert (ec.echo_gated_norm(plan, x, want_n=False)[0] == h).all()
+    assert ec.echo_get_device_error() == 0
+
+
 def test_parts(ec):
     """Without a branch, without gate, scale, shift; h or n alone; a norm alone is the layer norm."""
     import torch
