@@ -6,6 +6,8 @@
 // centred squares.  A thread block takes neighbouring rows, which mostly share their modulation,
 // so that gate, scale and shift (for fp32 as many bytes as a row's x, y, h and n, and half as many again)
 // come from the L1; the rows themselves pass it by.
+#include <type_traits>
+
 #include "common.cuh"
 #include "internal.h"
 
@@ -324,13 +326,13 @@ ECHO_DEV void staged(const uint8_t *rows, uint32_t row_bytes, bool f32, int t, i
         }
     }
 }
-template <int R>
+template <int R, bool ALL>
 ECHO_DEV void store_rows(uint8_t *to, int64_t stride, bool f32, const int (&m)[R], const Pairs (&v)[R]) {
 #pragma unroll
     for (int k = 0; k < R; ++k, to += stride) {
         float f[8];
         floats_of(v[k], f);
-        if (m[k] >= 0) store8(to, 0, f32, f);
+        if (ALL || m[k] >= 0) store8(to, 0, f32, f);
     }
 }
 
@@ -412,37 +414,35 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
     const int64_t h_row = p.ldh * (p.hf ? 4 : 2), n_row = p.ldn * (p.nf ? 4 : 2);
     mods(0, next);
     bool ok = true;
-    for (int i = 0; i < batches; ++i) {
-        const int n = min(R, last - first - i * R);
-#pragma unroll
-        for (int k = 0; k < R; ++k) m[k] = k < n && live && (p.n_mods < 0 || (unsigned)next[k] < (unsigned)p.n_mods) ? next[k] : -1;
-        if (i + 1 < batches) mods(i + 1, next);
-        // a wait that gives up lets the others give up; nothing is stored from then on
-        ok = ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err);
+    int i = 0;
+    // a batch of rows; SAME: R rows, all of the modulation that is in registers
+    auto batch = [&](auto SAME, int n) {
         const uint8_t *rows = buf + (i & 1) * (R * row_bytes);
         auto refill = [&]() {            // the rows are in registers, behind a barrier
             if (t == 0 && ok && i + 2 < batches) fetch(i + 2);
         };
         Pairs h[R];
         float f[R];
-        staged<R>(rows, row_bytes, p.xf, t, live ? n : 0, h);
+        const int there = !live ? 0 : SAME ? R : n;
+        staged<R>(rows, row_bytes, p.xf, t, there, h);
 #pragma unroll
         for (int k = 0; k < R; ++k) h[k] = mul8(h[k], alpha);
         if (p.y) {
             Pairs y[AFTER ? R : 1];
             if constexpr (AFTER) {
-                staged<R>(rows + xb, row_bytes, p.yf, t, live ? n : 0, y);
+                staged<R>(rows + xb, row_bytes, p.yf, t, there, y);
                 spreads<R>(p.after, p.inv_d, live, y, f, part, turn, [] {});
             }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 constexpr int ONE = AFTER ? R : 1;           // AFTER: y[k], else a row at a time
                 Pairs &yk = y[k % ONE];
-                if constexpr (!AFTER) staged<1>(rows + k * row_bytes + xb, row_bytes, p.yf, t, live ? n - k : 0, y);
-                if (p.gate && m[k] != gate_m && m[k] >= 0) {
-                    gate = mul8(shared_pairs(p.gate, m[k] * p.ldm + 8 * t, p.mf), splat(p.beta));
-                    gate_m = m[k];
-                }
+                if constexpr (!AFTER) staged<1>(rows + k * row_bytes + xb, row_bytes, p.yf, t, there - k, y);
+                if constexpr (!SAME)
+                    if (p.gate && m[k] != gate_m && m[k] >= 0) {
+                        if (live) gate = mul8(shared_pairs(p.gate, m[k] * p.ldm + 8 * t, p.mf), splat(p.beta));
+                        gate_m = m[k];
+                    }
                 if constexpr (AFTER) {
                     yk = mul8(yk, splat(f[k]));
                     if (live) yk = affine8(p.after, t, yk);
@@ -450,11 +450,7 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
                 h[k] = fma8(gate, yk, h[k]);
             }
         }
-        if (!ok) {
-#pragma unroll
-            for (int k = 0; k < R; ++k) m[k] = -1;
-        }
-        if (p.h) store_rows<R>(h_to, h_row, p.hf, m, h);
+        if (p.h && live) store_rows<R, SAME>(h_to, h_row, p.hf, m, h);
         const bool normed = p.n && p.before.kind != ECHO_NORM_NONE;
         if (normed) {
             spreads<R>(p.before, p.inv_d, live, h, f, part, turn, refill);
@@ -462,22 +458,41 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
             __syncthreads();
             refill();
         }
-        if (p.n) {
+        if (p.n && live) {
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                if (m[k] != out_m && m[k] >= 0) {
-                    if (p.scale) scale = add8(shared_pairs(p.scale, m[k] * p.ldm + 8 * t, p.mf), splat(1.f));
-                    if (p.shift) shift = shared_pairs(p.shift, m[k] * p.ldm + 8 * t, p.mf);
-                    out_m = m[k];
-                }
-                if (normed) {
-                    h[k] = mul8(h[k], splat(f[k]));
-                    if (live) h[k] = affine8(p.before, t, h[k]);
-                }
+                if constexpr (!SAME)
+                    if (m[k] != out_m && m[k] >= 0) {
+                        if (p.scale) scale = add8(shared_pairs(p.scale, m[k] * p.ldm + 8 * t, p.mf), splat(1.f));
+                        if (p.shift) shift = shared_pairs(p.shift, m[k] * p.ldm + 8 * t, p.mf);
+                        out_m = m[k];
+                    }
+                if (normed) h[k] = affine8(p.before, t, mul8(h[k], splat(f[k])));
                 h[k] = fma8(h[k], scale, shift);
             }
-            store_rows<R>(n_to, n_row, p.nf, m, h);
+            store_rows<R, SAME>(n_to, n_row, p.nf, m, h);
         }
+        if (!live) out_m = m[R - 1];     // as the threads that have columns
+    };
+    for (; i < batches; ++i) {
+        const int n = min(R, last - first - i * R);
+        bool same = n == R;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            m[k] = k < n && (p.n_mods < 0 || (unsigned)next[k] < (unsigned)p.n_mods) ? next[k] : -1;
+            same = same && m[k] >= 0 && m[k] == out_m && (m[k] == gate_m || !p.gate || !p.y);
+        }
+        if (i + 1 < batches) mods(i + 1, next);
+        // a wait that gives up lets the others give up; nothing is stored from then on
+        ok = ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err);
+        if (!ok) {
+            same = false;
+#pragma unroll
+            for (int k = 0; k < R; ++k) m[k] = -1;
+        }
+        // the whole warp takes one way: a barrier lies on both
+        if (__all_sync(0xffffffffu, same)) batch(std::true_type(), R);
+        else batch(std::false_type(), n);
         h_to += R * h_row;
         n_to += R * n_row;
     }

@@ -2,7 +2,8 @@
 // frequency, for queries and keys in one launch.
 //
 // (y1, y2) = size (x1 cos a - x2 sin a, x2 cos a + x1 sin a).  A value is read once and
-// written once and the time is that of the bytes, if the angles cost little: a frequency is held
+// written once and the time is that of the bytes (32760 rows of 80 heads of 128, bf16, neighbouring
+// columns: 197 us, 6.8 TB/s, as a plain copy), if the angles cost little: a frequency is held
 // in turns, as a 64-bit fraction, so that position x frequency modulo one turn is an integer
 // product whose high part is left over - exact for every position, without fp64 - and a thread
 // takes the same columns of several heads, whose angles are the same.
@@ -20,7 +21,7 @@ struct RotaryParams {
     const void *in[2];            // queries, keys
     void *out[2];
     int64_t ld_in[2], ld_out[2];
-    int heads, first_key;         // of both; the keys' first
+    int Hq, Hk, key_chunk;        // heads; the first of a row's chunks that are the keys'
     int n_rows, d, pairs, units, turned, chunks, per;   // units of a head, `turned` of them with pairs; heads a thread
     int axes, end[3];             // pairs before the second, third and fourth axis
     int frame, row;
@@ -39,126 +40,219 @@ ECHO_DEV float value(const float &x) { return x; }
 ECHO_DEV void put(__nv_bfloat16 &to, float x) { to = __float2bfloat16_rn(x); }
 ECHO_DEV void put(float &to, float x) { to = x; }
 
-// W neighbouring values of T, read and written at once
-template <typename T, int W>
-struct Vec {
+// neighbouring values of T, read and written at once
+template <typename T, int N>
+struct Some {
     union {
-        typename Raw<W * (int)sizeof(T)>::type raw;
-        T v[W];
+        typename Raw<N * (int)sizeof(T)>::type raw;
+        T v[N];
     };
-    ECHO_DEV Vec() {}
+    ECHO_DEV Some() {}
+};
+template <typename T>
+using Vec = Some<T, 16 / (int)sizeof(T)>;
+
+// the heads of a row's chunk, of the queries or of the keys
+template <typename T>
+struct Heads {
+    const T *src;
+    T *dst;
+    int n;
+    ECHO_DEV Heads(const RotaryParams &p, int r, int chunk) {
+        const int kv = chunk >= p.key_chunk, h0 = (chunk - (kv ? p.key_chunk : 0)) * p.per;
+        src = static_cast<const T *>(p.in[kv]) + r * p.ld_in[kv] + (int64_t)h0 * p.d;
+        dst = static_cast<T *>(p.out[kv]) + r * p.ld_out[kv] + (int64_t)h0 * p.d;
+        n = min(p.per, (kv ? p.Hk : p.Hq) - h0);
+    }
 };
 
-// A unit is W neighbouring columns: W / 2 pairs (PAIRS), or W columns of the first half and the
-// same of the second (HALVES); beyond the turned ones, W columns that are copied.
-template <typename T, bool HALVES, int W>
-__global__ void __launch_bounds__(kThreads)
-rotary_kernel(const RotaryParams p) {
+// A row's positions on its axes; false: the row is left as it is
+ECHO_DEV bool positions(const RotaryParams &p, int r, int (&at)[4]) {
+    at[0] = at[1] = at[2] = at[3] = 0;
+    if (p.frame > 0) {
+        const int t = p.pos[r];
+        at[0] = t / p.frame;
+        at[1] = (t - at[0] * p.frame) / p.row;
+        at[2] = t - at[0] * p.frame - at[1] * p.row;
+        return t >= 0;
+    }
+    bool in = true;
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+        if (a < p.axes) {
+            at[a] = p.pos[(int64_t)r * p.axes + a];
+            in &= at[a] >= 0;
+        }
+    return in;
+}
+// size times cosine and sine of a pair's angle; size and 0 for pairs that there are none of
+ECHO_DEV void angle(const RotaryParams &p, int pair, bool there, const int (&at)[4], float &c, float &s) {
+    const uint64_t turn = there ? __ldg(p.turn + pair) : 0ull;
+    const int q = pair < p.end[0] ? at[0] : pair < p.end[1] ? at[1] : pair < p.end[2] ? at[2] : at[3];
+    // the fraction of a turn, -1/2 .. 1/2, in half turns
+    const int32_t f = (int32_t)((turn * (uint64_t)(uint32_t)q) >> 32);
+    sincospif((float)f * 4.656612873077393e-10f, &s, &c);
+    c *= p.size;
+    s *= p.inverse ? -p.size : p.size;
+}
+
+// Pairs of neighbouring columns.  Four blocks of an SM, and two pairs to an instruction: three
+// blocks and single pairs took 250 us where this takes 197.  A unit of a head is 16 bytes: W values, W / 2 pairs, or beyond the
+// turned ones W columns that are copied.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 4)
+rotary_pairs_kernel(const RotaryParams p) {
     pdl_enter();
-    constexpr int NP = HALVES ? W : W / 2;            // pairs of a unit
+    constexpr int W = 16 / (int)sizeof(T), NP = W / 2;
     const int per_block = kThreads / p.units;         // (row, some heads) of a block
     const int slot = threadIdx.x / p.units, u = threadIdx.x - slot * p.units;
     if (slot >= per_block) return;
-    PieceWalk walk(blockIdx.x * per_block + slot, gridDim.x * per_block, p.chunks);
     const bool turned = u < p.turned;
-    uint64_t turn[NP];
-    int axis[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int pair = u * NP + i;
-        turn[i] = turned && pair < p.pairs ? p.turn[pair] : 0ull;
-        axis[i] = (pair >= p.end[0]) + (pair >= p.end[1]) + (pair >= p.end[2]);
-    }
+    PieceWalk walk(blockIdx.x * per_block + slot, gridDim.x * per_block, p.chunks);
     for (; walk.below(p.n_rows); walk.next()) {
         const int r = (int)walk.row;
-        int at[4] = {0, 0, 0, 0};
-        if (p.frame > 0) {
-            const int t = p.pos[r];
-            at[0] = t / p.frame;
-            at[1] = (t - at[0] * p.frame) / p.row;
-            at[2] = t - at[0] * p.frame - at[1] * p.row;
-            if (t < 0) continue;
-        } else {
-            bool out = false;
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-                if (a < p.axes) {
-                    at[a] = p.pos[(int64_t)r * p.axes + a];
-                    out |= at[a] < 0;
-                }
-            if (out) continue;
-        }
+        int at[4];
+        if (!positions(p, r, at)) continue;
         float c[NP], s[NP];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int q = axis[i] == 0 ? at[0] : axis[i] == 1 ? at[1] : axis[i] == 2 ? at[2] : at[3];
-            // the fraction of a turn, -1/2 .. 1/2, in half turns
-            const int32_t f = (int32_t)((turn[i] * (uint64_t)(uint32_t)q) >> 32);
-            sincospif((float)f * 4.656612873077393e-10f, &s[i], &c[i]);
-            c[i] *= p.size;
-            s[i] *= p.inverse ? -p.size : p.size;
-        }
-        const int h0 = (int)walk.piece * p.per, h1 = min(h0 + p.per, p.heads);
-        for (int h = h0; h < h1; h += kAtOnce) {
-            Vec<T, W> x[kAtOnce][HALVES ? 2 : 1];
-            T *dst[kAtOnce];
+        for (int i = 0; i < NP; ++i) angle(p, u * NP + i, turned && u * NP + i < p.pairs, at, c[i], s[i]);
+        const Heads<T> hd(p, r, (int)walk.piece);
+        const T *src = hd.src + u * W;
+        T *dst = hd.dst + u * W;
+        if (!turned && src == dst) continue;                  // stays as it is
+        for (int h = 0; h < hd.n; h += kAtOnce, src += kAtOnce * p.d, dst += kAtOnce * p.d) {
+            Vec<T> x[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (h + k < hd.n) x[k].raw = *reinterpret_cast<const uint4 *>(src + k * p.d);
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
-                const int kv = h + k >= p.first_key, hh = h + k - (kv ? p.first_key : 0);
-                const T *src = static_cast<const T *>(p.in[kv]) + r * p.ld_in[kv] + hh * p.d;
-                dst[k] = static_cast<T *>(p.out[kv]) + r * p.ld_out[kv] + hh * p.d;
-                if (h + k >= h1) dst[k] = nullptr;
-                if (!turned && src == dst[k]) dst[k] = nullptr;       // stays as it is
-                const int col = HALVES && !turned ? 2 * p.pairs + (u - p.turned) * W : u * W;
-                src += col;
-                if (!dst[k]) continue;
-                dst[k] += col;
-                x[k][0].raw = *reinterpret_cast<const decltype(x[k][0].raw) *>(src);
-                if (HALVES && turned) x[k][HALVES].raw = *reinterpret_cast<const decltype(x[k][0].raw) *>(src + p.pairs);
-            }
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                if (!dst[k]) continue;
+                if (h + k >= hd.n) continue;
                 if (turned) {
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) {
-                        T &e1 = HALVES ? x[k][0].v[i] : x[k][0].v[2 * i], &e2 = HALVES ? x[k][HALVES].v[i] : x[k][0].v[2 * i + 1];
-                        if (!HALVES && u * NP + i >= p.pairs) continue;
-                        const float x1 = value(e1), x2 = value(e2);
-                        put(e1, x1 * c[i] - x2 * s[i]);
-                        put(e2, x2 * c[i] + x1 * s[i]);
+                    for (int i = 0; i < NP; i += 2) {         // two pairs at once
+                        T *v = x[k].v + 2 * i;
+                        const uint64_t x1 = f2_pack(value(v[0]), value(v[2])), x2 = f2_pack(value(v[1]), value(v[3]));
+                        const uint64_t cc = f2_pack(c[i], c[i + 1]), ss = f2_pack(s[i], s[i + 1]), less = f2_pack(-s[i], -s[i + 1]);
+                        float y1[2], y2[2];
+                        f2_unpack(f2_fma(x1, cc, f2_mul(x2, less)), y1[0], y1[1]);
+                        f2_unpack(f2_fma(x2, cc, f2_mul(x1, ss)), y2[0], y2[1]);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (u * NP + i + e >= p.pairs) continue;
+                            put(v[2 * e], y1[e]);
+                            put(v[2 * e + 1], y2[e]);
+                        }
                     }
                 }
-                *reinterpret_cast<decltype(x[k][0].raw) *>(dst[k]) = x[k][0].raw;
-                if (HALVES && turned) *reinterpret_cast<decltype(x[k][0].raw) *>(dst[k] + p.pairs) = x[k][HALVES].raw;
+                *reinterpret_cast<uint4 *>(dst + k * p.d) = x[k].raw;
             }
         }
     }
 }
 
-template <typename T, bool HALVES, int W>
-void launch(RotaryParams &p, bool tail, cudaStream_t st) {
-    p.turned = HALVES ? p.pairs / W : (2 * p.pairs + W - 1) / W;
-    p.units = HALVES ? p.turned + (tail ? (p.d - 2 * p.pairs) / W : 0) : tail ? p.d / W : p.turned;
-    const int per_block = kThreads / p.units;
-    // heads a thread: one angle for many values where there are threads enough
-    p.per = 8;
-    while (p.per > 1 && (int64_t)p.n_rows * ((p.heads + p.per - 1) / p.per) * p.units < 152ll * 4096) p.per /= 2;
-    p.chunks = (p.heads + p.per - 1) / p.per;
+// Halves: column i and column i + pairs lie apart, and the second may begin anywhere.  A warp
+// takes some heads through shared memory, whole stretches in and out, and PW neighbouring pairs (2 where
+// that fills the lanes) in between, the next heads on their way meanwhile.  32760 rows of 80 heads of 128,
+// bf16, 64 pairs: 222 us, 7 pairs 212; with 16 bytes of either half in a thread's registers 64 pairs
+// took 222, but 32 pairs 283 and 7, whose halves are not aligned, 890.
+template <typename T, int PW>
+__global__ void __launch_bounds__(kThreads)
+rotary_halves_kernel(const RotaryParams p) {
+    constexpr int kBytes = 1024, NP = 4 / PW;         // bytes of a warp; times 32 PW pairs: 128 at most
+    __shared__ __align__(16) uint8_t stage[kThreads / 32][kBytes];
+    pdl_enter();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    T *mine = reinterpret_cast<T *>(stage[warp]);
+    const int head_bytes = p.d * (int)sizeof(T), at_once = min(kBytes / head_bytes, p.per);
+    PieceWalk walk(blockIdx.x * (kThreads / 32) + warp, gridDim.x * (kThreads / 32), p.chunks);
+    for (; walk.below(p.n_rows); walk.next()) {
+        const int r = (int)walk.row;
+        int at[4];
+        if (!positions(p, r, at)) continue;
+        float c[NP][PW], s[NP][PW];
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int e = 0; e < PW; ++e) {
+                const int pair = PW * (lane + 32 * i) + e;
+                if (32 * PW * i < p.pairs) angle(p, pair, pair < p.pairs, at, c[i][e], s[i][e]);
+            }
+        const Heads<T> hd(p, r, (int)walk.piece);
+        const uint8_t *src = reinterpret_cast<const uint8_t *>(hd.src);
+        uint8_t *dst = reinterpret_cast<uint8_t *>(hd.dst);
+        uint4 next[kBytes / 512];                     // the heads after these are on their way
+        auto fetch = [&](const uint8_t *from, int heads) {
+#pragma unroll
+            for (int i = 0; i < kBytes / 512; ++i)
+                if ((lane + 32 * i) * 16 < min(heads, at_once) * head_bytes) next[i] = reinterpret_cast<const uint4 *>(from)[lane + 32 * i];
+        };
+        fetch(src, hd.n);
+        for (int h = 0; h < hd.n; h += at_once, dst += at_once * head_bytes) {
+            const int some = min(at_once, hd.n - h), bytes = some * head_bytes;
+#pragma unroll
+            for (int i = 0; i < kBytes / 512; ++i)
+                if ((lane + 32 * i) * 16 < bytes) reinterpret_cast<uint4 *>(mine)[lane + 32 * i] = next[i];
+            src += at_once * head_bytes;
+            if (h + at_once < hd.n) fetch(src, hd.n - h - at_once);
+            __syncwarp();
+#pragma unroll 4
+            for (int k = 0; k < some; ++k) {
+                T *head = mine + k * p.d;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const int pair = PW * (lane + 32 * i);
+                    if (pair >= p.pairs) continue;            // PW divides pairs
+                    Some<T, PW> a, b;
+                    a.raw = *reinterpret_cast<decltype(a.raw) *>(head + pair);
+                    b.raw = *reinterpret_cast<decltype(b.raw) *>(head + pair + p.pairs);
+#pragma unroll
+                    for (int e = 0; e < PW; ++e) {
+                        const float x1 = value(a.v[e]), x2 = value(b.v[e]);
+                        put(a.v[e], fmaf(x1, c[i][e], -x2 * s[i][e]));
+                        put(b.v[e], fmaf(x2, c[i][e], x1 * s[i][e]));
+                    }
+                    *reinterpret_cast<decltype(a.raw) *>(head + pair) = a.raw;
+                    *reinterpret_cast<decltype(b.raw) *>(head + pair + p.pairs) = b.raw;
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kBytes / 512; ++i)
+                if ((lane + 32 * i) * 16 < bytes)
+                    reinterpret_cast<uint4 *>(dst)[lane + 32 * i] = reinterpret_cast<const uint4 *>(mine)[lane + 32 * i];
+            __syncwarp();
+        }
+    }
+}
+
+// `lanes` lanes work on some heads of a row: as many heads, up to `most`, as leave work for every SM, since
+// their angles are the same
+void divide(RotaryParams &p, int lanes, int most) {
+    auto chunks = [&](int heads) { return (heads + p.per - 1) / p.per; };
+    p.per = most;
+    while (p.per > 1 && (int64_t)p.n_rows * (chunks(p.Hq) + chunks(p.Hk)) * lanes < 152ll * 4096) p.per /= 2;
+    p.key_chunk = chunks(p.Hq);
+    p.chunks = p.key_chunk + chunks(p.Hk);
+}
+int blocks_of(const RotaryParams &p, int per_block) {
     const int64_t blocks = ((int64_t)p.n_rows * p.chunks + per_block - 1) / per_block;
-    const int grid = (int)(blocks < 65536 ? blocks : 65536);
-    echo::launch_chained(rotary_kernel<T, HALVES, W>, dim3(grid), dim3(kThreads), 0, st, p);
+    return (int)(blocks < 65536 ? blocks : 65536);
 }
 
 template <typename T>
-void launch_layout(RotaryParams &p, bool halves, bool tail, cudaStream_t st) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (!halves) return launch<T, false, V>(p, tail, st);
-    // the second half begins at column `pairs`: as wide as its alignment allows
-    if (p.pairs % V == 0) return launch<T, true, V>(p, tail, st);
-    if (V == 8 && p.pairs % 4 == 0) return launch<T, true, 4>(p, tail, st);
-    if (p.pairs % 2 == 0) return launch<T, true, 2>(p, tail, st);
-    launch<T, true, 1>(p, tail, st);
+void launch(RotaryParams &p, bool halves, bool tail, cudaStream_t st) {
+    if (!halves) {
+        constexpr int W = 16 / (int)sizeof(T);
+        p.turned = (2 * p.pairs + W - 1) / W;
+        p.units = tail ? p.d / W : p.turned;
+        divide(p, p.units, 8);
+        echo::launch_chained(rotary_pairs_kernel<T>, dim3(blocks_of(p, kThreads / p.units)), dim3(kThreads), 0, st, p);
+        return;
+    }
+    divide(p, 32, 16);
+    echo::launch_chained(p.pairs % 2 || p.pairs < 64 ? rotary_halves_kernel<T, 1> : rotary_halves_kernel<T, 2>,
+                         dim3(blocks_of(p, kThreads / 32)), dim3(kThreads), 0, st, p);
 }
 
 }  // namespace
@@ -245,8 +339,8 @@ extern "C" echo_status echo_rotary(const echo_rotary_plan *plan, const int32_t *
     p.ld_in[1] = ldk;
     p.ld_out[0] = ldqo;
     p.ld_out[1] = ldko;
-    p.heads = Hq + Hk;
-    p.first_key = Hq;
+    p.Hq = Hq;
+    p.Hk = Hk;
     p.n_rows = n_rows;
     p.d = d;
     p.pairs = total;
@@ -258,8 +352,8 @@ extern "C" echo_status echo_rotary(const echo_rotary_plan *plan, const int32_t *
     p.inverse = inverse != 0;
     const bool tail = 2 * total < d && (q != q_out || (Hk > 0 && k != k_out));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    echo::LaunchScope ls(ECHO_K_ROTARY, n_rows, (int64_t)p.heads * d, 2 * total, st);
-    if (t == ECHO_BF16) launch_layout<__nv_bfloat16>(p, plan->layout == ECHO_ROTARY_HALVES, tail, st);
-    else launch_layout<float>(p, plan->layout == ECHO_ROTARY_HALVES, tail, st);
+    echo::LaunchScope ls(ECHO_K_ROTARY, n_rows, ((int64_t)Hq + Hk) * d, 2 * total, st);
+    if (t == ECHO_BF16) launch<__nv_bfloat16>(p, plan->layout == ECHO_ROTARY_HALVES, tail, st);
+    else launch<float>(p, plan->layout == ECHO_ROTARY_HALVES, tail, st);
     return echo::last_launch_status();
 }
