@@ -99,15 +99,13 @@ template <int TPR>
 ECHO_DEV float row_sum(float v, float (*red)[TPR / 32], int &turn) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (TPR > 32) {
-        float *at = red[turn & 1];
-        ++turn;
-        if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.f;
+    float *at = red[turn & 1];
+    ++turn;
+    if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.f;
 #pragma unroll
-        for (int w = 0; w < TPR / 32; ++w) v += at[w];
-    }
+    for (int w = 0; w < TPR / 32; ++w) v += at[w];
     return v;
 }
 
@@ -149,16 +147,15 @@ ECHO_DEV void affine(const Norm &n, int c, float *v) {
     }
 }
 
-// TPR threads to a row, the whole block but for a warp's rows; CH chunks of 8 values a thread
+// Rows of more than 8192 values: a block to a row, CH chunks of 8 values a thread.
 template <int TPR, int CH>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
+__global__ void __launch_bounds__(TPR)
 gated_norm_kernel(const NormParams p) {
     pdl_enter();
     __shared__ float red[2][TPR / 32];
-    constexpr int RPB = TPR == 32 ? 8 : 1;
-    const int t = threadIdx.x % TPR;
-    const int64_t workers = (int64_t)gridDim.x * RPB, me = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    const int first = (int)(p.n_rows * me / workers), last = (int)(p.n_rows * (me + 1) / workers);
+    const int t = threadIdx.x;
+    const int first = (int)((int64_t)p.n_rows * blockIdx.x / gridDim.x);
+    const int last = (int)((int64_t)p.n_rows * (blockIdx.x + 1) / gridDim.x);
     int turn = 0;
     for (int r = first; r < last; ++r) {
         int m = 0;
@@ -231,13 +228,12 @@ gated_norm_kernel(const NormParams p) {
     }
 }
 
-// Many rows of more than 1024 values: a chunk of 8 columns to a thread, so that its gate, scale and
-// shift stay in registers while the rows' modulation is the same, and R rows at a time, whose sums
-// share their barriers.  Rows come by bulk copies into two buffers of R rows; a buffer is
-// filled again as soon as its rows are in registers, while the sums of these are under way.
-#ifndef STREAM_ROWS
-#define STREAM_ROWS 8
-#endif
+// Many rows: a chunk of 8 columns to a thread, so that its gate, scale and
+// shift stay in registers while the rows' modulation is the same (the norms' weights in them), and R rows at
+// a time, whose sums share their barriers.  Rows come by bulk copies into two buffers of R rows; a buffer
+// is filled again as soon as its rows are in registers, while the sums of these are under way.
+// A block takes neighbouring rows (in turn with the others, 264 us for 211: the modulation comes again and again).
+constexpr int kBufferBytes = 100 * 1024;
 
 // R sums over the block, in all threads.  A lane passes on half of what it holds at a time, so
 // that R = 4 sums take 6 exchanges and not 20.
@@ -256,6 +252,18 @@ ECHO_DEV void block_sums(float (&v)[R], float4 (*part)[32], int &turn) {
     };
     float4 *at = part[turn & 1];
     ++turn;
+    if constexpr (R == 1) {
+        float s = v[0];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) at[warp].x = s;
+        __syncthreads();
+        s = lane < warps ? at[lane].x : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        v[0] = s;
+        return;
+    }
     const float s = reduce(v[0], v[1 % R], R > 2 ? v[2 % R] : 0.f, R > 2 ? v[3 % R] : 0.f);
     if ((lane & 7) == 0) reinterpret_cast<float *>(&at[warp])[lane >> 3] = s;
     __syncthreads();
@@ -355,12 +363,6 @@ ECHO_DEV void spreads(const Norm &n, float inv_d, bool live, Pairs (&v)[R], floa
 #pragma unroll
     for (int k = 0; k < R; ++k) f[k] = rsqrtf(f[k] * inv_d + n.eps);
 }
-ECHO_DEV Pairs affine8(const Norm &n, int c, Pairs v) {
-    if (n.weight) v = mul8(v, shared_pairs(n.weight, 8 * c, true));
-    if (n.bias) v = add8(v, shared_pairs(n.bias, 8 * c, true));
-    return v;
-}
-
 template <int R, bool AFTER, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 gated_norm_rows_kernel(const NormParams p, int *err) {
@@ -397,22 +399,46 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         if (batches > 0) fetch(0);
         if (batches > 1) fetch(1);
     }
-    // the modulation's row of the batch's rows; -1: the row is left as it is
-    auto mods = [&](int i, int (&m)[R]) {
-        const int r0 = first + i * R;
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            m[k] = 0;
-            if (p.n_mods >= 0 && r0 + k < last) m[k] = p.mod_rows ? p.mod_rows[r0 + k] : (r0 + k) / p.rows_per_mod;
+    // the modulation's row, for the lanes of a batch's rows; -1: the row is left as it is
+    const int lane = t & 31;
+    auto mod_of = [&](int i) {
+        const int r = first + i * R + lane;
+        int m = 0;
+        if (lane >= R || r >= last) return -1;
+        if (p.n_mods >= 0) {
+            m = p.mod_rows ? p.mod_rows[r] : r / p.rows_per_mod;
+            if ((unsigned)m >= (unsigned)p.n_mods) m = -1;
+        }
+        return m;
+    };
+    int mod, next, turn = 0, cur = -1, cur_out = -1;
+    const Pairs alpha = splat(p.alpha);
+    // of the modulations `cur` and `cur_out`, the norms' weights and biases in them (but for a bias of the first)
+    Pairs gate = splat(p.beta), scale = splat(1.f), shift = splat(0.f);
+    auto take = [&](int m) {
+        if (m == cur || m < 0) return;
+        cur = m;
+        if (!live) return;
+        gate = splat(p.beta);
+        if (p.gate) gate = mul8(shared_pairs(p.gate, m * p.ldm + 8 * t, p.mf), gate);
+        if constexpr (AFTER) {
+            if (p.after.weight && !p.after.bias) gate = mul8(shared_pairs(p.after.weight, 8 * t, true), gate);
         }
     };
-    int m[R], next[R], turn = 0, gate_m = -1, out_m = -1;
-    const Pairs alpha = splat(p.alpha);
-    Pairs gate = splat(p.beta), scale = splat(1.f), shift = splat(0.f);   // beta gate, 1 + scale
-    uint8_t *h_to = static_cast<uint8_t *>(p.h) + (first * p.ldh + 8 * t) * (p.hf ? 4 : 2);
-    uint8_t *n_to = static_cast<uint8_t *>(p.n) + (first * p.ldn + 8 * t) * (p.nf ? 4 : 2);
+    auto take_out = [&](int m) {
+        if (m == cur_out || m < 0) return;
+        cur_out = m;
+        if (!live) return;
+        scale = splat(1.f);
+        if (p.scale) scale = add8(shared_pairs(p.scale, m * p.ldm + 8 * t, p.mf), scale);
+        if (p.shift) shift = shared_pairs(p.shift, m * p.ldm + 8 * t, p.mf);
+        else shift = splat(0.f);
+        if (p.before.bias) shift = fma8(shared_pairs(p.before.bias, 8 * t, true), scale, shift);
+        if (p.before.weight) scale = mul8(shared_pairs(p.before.weight, 8 * t, true), scale);
+    };
+    uint8_t *h_to, *n_to;                // of the batch
     const int64_t h_row = p.ldh * (p.hf ? 4 : 2), n_row = p.ldn * (p.nf ? 4 : 2);
-    mods(0, next);
+    next = mod_of(0);
     bool ok = true;
     int i = 0;
     // a batch of rows; SAME: R rows, all of the modulation that is in registers
@@ -421,33 +447,36 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         auto refill = [&]() {            // the rows are in registers, behind a barrier
             if (t == 0 && ok && i + 2 < batches) fetch(i + 2);
         };
+        int m[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) m[k] = SAME ? 0 : ok ? __shfl_sync(0xffffffffu, mod, k) : -1;
         Pairs h[R];
         float f[R];
         const int there = !live ? 0 : SAME ? R : n;
-        staged<R>(rows, row_bytes, p.xf, t, there, h);
-#pragma unroll
-        for (int k = 0; k < R; ++k) h[k] = mul8(h[k], alpha);
-        if (p.y) {
-            Pairs y[AFTER ? R : 1];
-            if constexpr (AFTER) {
-                staged<R>(rows + xb, row_bytes, p.yf, t, there, y);
-                spreads<R>(p.after, p.inv_d, live, y, f, part, turn, [] {});
-            }
+        Pairs one[1];                    // the other of x and y, a row at a time
+        if constexpr (AFTER) {
+            staged<R>(rows + xb, row_bytes, p.yf, t, there, h);
+            spreads<R>(p.after, p.inv_d, live, h, f, part, turn, [] {});
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                constexpr int ONE = AFTER ? R : 1;           // AFTER: y[k], else a row at a time
-                Pairs &yk = y[k % ONE];
-                if constexpr (!AFTER) staged<1>(rows + k * row_bytes + xb, row_bytes, p.yf, t, there - k, y);
-                if constexpr (!SAME)
-                    if (p.gate && m[k] != gate_m && m[k] >= 0) {
-                        if (live) gate = mul8(shared_pairs(p.gate, m[k] * p.ldm + 8 * t, p.mf), splat(p.beta));
-                        gate_m = m[k];
-                    }
-                if constexpr (AFTER) {
-                    yk = mul8(yk, splat(f[k]));
-                    if (live) yk = affine8(p.after, t, yk);
+                if constexpr (!SAME) take(m[k]);
+                h[k] = mul8(h[k], splat(f[k]));
+                if (p.after.bias && live) {
+                    if (p.after.weight) h[k] = mul8(h[k], shared_pairs(p.after.weight, 8 * t, true));
+                    h[k] = add8(h[k], shared_pairs(p.after.bias, 8 * t, true));
                 }
-                h[k] = fma8(gate, yk, h[k]);
+                staged<1>(rows + k * row_bytes, row_bytes, p.xf, t, there - k, one);
+                h[k] = fma8(gate, h[k], mul8(one[0], alpha));
+            }
+        } else {
+            staged<R>(rows, row_bytes, p.xf, t, there, h);
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                h[k] = mul8(h[k], alpha);
+                if (!p.y) continue;
+                staged<1>(rows + k * row_bytes + xb, row_bytes, p.yf, t, there - k, one);
+                if constexpr (!SAME) take(m[k]);
+                h[k] = fma8(gate, one[0], h[k]);
             }
         }
         if (p.h && live) store_rows<R, SAME>(h_to, h_row, p.hf, m, h);
@@ -457,44 +486,37 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         } else {
             __syncthreads();
             refill();
+#pragma unroll
+            for (int k = 0; k < R; ++k) f[k] = 1.f;
         }
         if (p.n && live) {
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                if constexpr (!SAME)
-                    if (m[k] != out_m && m[k] >= 0) {
-                        if (p.scale) scale = add8(shared_pairs(p.scale, m[k] * p.ldm + 8 * t, p.mf), splat(1.f));
-                        if (p.shift) shift = shared_pairs(p.shift, m[k] * p.ldm + 8 * t, p.mf);
-                        out_m = m[k];
-                    }
-                if (normed) h[k] = affine8(p.before, t, mul8(h[k], splat(f[k])));
-                h[k] = fma8(h[k], scale, shift);
+                if constexpr (!SAME) take_out(m[k]);
+                h[k] = fma8(mul8(h[k], splat(f[k])), scale, shift);
             }
             store_rows<R, SAME>(n_to, n_row, p.nf, m, h);
         }
-        if (!live) out_m = m[R - 1];     // as the threads that have columns
+        if constexpr (!SAME) {
+            // as the threads that have columns, whatever was asked for
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (!live || !p.y) take(m[k]);
+                if (!live || !p.n) take_out(m[k]);
+            }
+        }
     };
     for (; i < batches; ++i) {
-        const int n = min(R, last - first - i * R);
-        bool same = n == R;
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            m[k] = k < n && (p.n_mods < 0 || (unsigned)next[k] < (unsigned)p.n_mods) ? next[k] : -1;
-            same = same && m[k] >= 0 && m[k] == out_m && (m[k] == gate_m || !p.gate || !p.y);
-        }
-        if (i + 1 < batches) mods(i + 1, next);
+        const int r0 = first + i * R, n = min(R, last - r0);
+        h_to = static_cast<uint8_t *>(p.h) + r0 * h_row + 8 * t * (p.hf ? 4 : 2);
+        n_to = static_cast<uint8_t *>(p.n) + r0 * n_row + 8 * t * (p.nf ? 4 : 2);
+        mod = next;
+        if (i + 1 < batches) next = mod_of(i + 1);
         // a wait that gives up lets the others give up; nothing is stored from then on
         ok = ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err);
-        if (!ok) {
-            same = false;
-#pragma unroll
-            for (int k = 0; k < R; ++k) m[k] = -1;
-        }
         // the whole warp takes one way: a barrier lies on both
-        if (__all_sync(0xffffffffu, same)) batch(std::true_type(), R);
+        if (__all_sync(0xffffffffu, ok && (lane >= R || (mod >= 0 && mod == cur && mod == cur_out)))) batch(std::true_type(), R);
         else batch(std::false_type(), n);
-        h_to += R * h_row;
-        n_to += R * n_row;
     }
     // copies land before this block exits
     if (!ok && t == 0) {
@@ -502,22 +524,85 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
     }
 }
 
+// Few rows: one to a block, a chunk to a thread, and everything that it needs asked for before the first
+// sum, since the time is that of one access after the other.
+ECHO_DEV Pairs chunk_of(const void *p, int64_t at, bool f32) {
+    float f[8];
+    if (f32) {
+        floats4(ld_once(static_cast<const float *>(p) + at), f);
+        floats4(ld_once(static_cast<const float *>(p) + at + 4), f + 4);
+    } else {
+        unpack8_bf16(ld_once(static_cast<const __nv_bfloat16 *>(p) + at), f);
+    }
+    return pairs_of(f);
+}
+__global__ void __launch_bounds__(1024)
+gated_norm_row_kernel(const NormParams p) {
+    __shared__ float4 part[2][32];
+    const int t = threadIdx.x;
+    const bool live = t < p.chunks;
+    int turn = 0;
+    pdl_enter();
+    for (int r = blockIdx.x; r < p.n_rows; r += gridDim.x) {
+        int m = 0;
+        const Pairs none = splat(0.f);
+        Pairs h[1] = {none}, y[1] = {none};
+        if (live) {
+            h[0] = chunk_of(p.x, r * p.ldx + 8 * t, p.xf);
+            if (p.y) y[0] = chunk_of(p.y, r * p.ldy + 8 * t, p.yf);
+        }
+        if (p.n_mods >= 0) {
+            m = p.mod_rows ? p.mod_rows[r] : r / p.rows_per_mod;
+            if ((unsigned)m >= (unsigned)p.n_mods) continue;
+        }
+        Pairs gate = splat(p.beta), scale = splat(1.f), shift = none;
+        if (live) {
+            const int64_t at = m * p.ldm + 8 * t;
+            if (p.gate) gate = mul8(shared_pairs(p.gate, at, p.mf), gate);
+            if (p.scale) scale = add8(shared_pairs(p.scale, at, p.mf), scale);
+            if (p.shift) shift = shared_pairs(p.shift, at, p.mf);
+            if (p.before.bias) shift = fma8(shared_pairs(p.before.bias, 8 * t, true), scale, shift);
+            if (p.before.weight) scale = mul8(shared_pairs(p.before.weight, 8 * t, true), scale);
+        }
+        float f[1] = {1.f};
+        h[0] = mul8(h[0], splat(p.alpha));
+        if (p.y) {
+            if (p.after.kind != ECHO_NORM_NONE) {
+                spreads<1>(p.after, p.inv_d, live, y, f, part, turn, [] {});
+                if (live) {
+                    if (p.after.bias) h[0] = fma8(shared_pairs(p.after.bias, 8 * t, true), gate, h[0]);
+                    if (p.after.weight) gate = mul8(shared_pairs(p.after.weight, 8 * t, true), gate);
+                    h[0] = fma8(mul8(y[0], splat(f[0])), gate, h[0]);
+                }
+            } else {
+                h[0] = fma8(y[0], gate, h[0]);
+            }
+        }
+        const int one[1] = {0};
+        if (p.h && live) store_rows<1, true>(static_cast<uint8_t *>(p.h) + (r * p.ldh + 8 * t) * (p.hf ? 4 : 2), 0, p.hf, one, h);
+        if (!p.n) continue;
+        f[0] = 1.f;
+        if (p.before.kind != ECHO_NORM_NONE) spreads<1>(p.before, p.inv_d, live, h, f, part, turn, [] {});
+        h[0] = fma8(mul8(h[0], splat(f[0])), scale, shift);
+        if (live) store_rows<1, true>(static_cast<uint8_t *>(p.n) + (r * p.ldn + 8 * t) * (p.nf ? 4 : 2), 0, p.nf, one, h);
+    }
+}
+
 template <int TPR, int CH>
 void launch(const NormParams &p, cudaStream_t st) {
-    constexpr int RPB = TPR == 32 ? 8 : 1, THREADS = TPR == 32 ? 256 : TPR;
     static int per_sm[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     int blocks = 1;
     if (dev >= 0 && dev < 64) {
         if (!per_sm[dev] && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm[dev], gated_norm_kernel<TPR, CH>,
-                                                                          THREADS, 0) != cudaSuccess)
+                                                                          TPR, 0) != cudaSuccess)
             per_sm[dev] = 1;
         blocks = per_sm[dev] > 0 ? per_sm[dev] : 1;
     }
-    const int64_t all = ((int64_t)p.n_rows + RPB - 1) / RPB, most = (int64_t)echo::num_sms() * blocks;
-    const int grid = (int)(all < most ? all : most);
-    echo::launch_chained(gated_norm_kernel<TPR, CH>, dim3(grid), dim3(THREADS), 0, st, p);
+    const int64_t most = (int64_t)echo::num_sms() * blocks;
+    const int grid = (int)(p.n_rows < most ? p.n_rows : most);
+    echo::launch_chained(gated_norm_kernel<TPR, CH>, dim3(grid), dim3(TPR), 0, st, p);
 }
 
 template <int R, bool AFTER, int THREADS>
@@ -528,36 +613,39 @@ void launch_rows(const NormParams &p, cudaStream_t st) {
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(gated_norm_rows_kernel<R, AFTER, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+        cudaFuncSetAttribute(gated_norm_rows_kernel<R, AFTER, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * kBufferBytes);
         attr_done[dev] = 1;
     }
     int blocks = 1;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, gated_norm_rows_kernel<R, AFTER, THREADS>, threads, smem) != cudaSuccess || blocks < 1)
         blocks = 1;
-    const int64_t all = ((int64_t)p.n_rows + R - 1) / R, most = (int64_t)echo::num_sms() * blocks;
-    const int grid = (int)(all < most ? all : most);
+    const int64_t most = (int64_t)echo::num_sms() * blocks;
+    const int grid = (int)(p.n_rows < most ? p.n_rows : most);
     echo::launch_chained(gated_norm_rows_kernel<R, AFTER, THREADS>, dim3(grid), dim3(threads), smem, st, p, echo::device_error_ptr());
 }
 
+// Rows of up to 8192 values: up to an SM's worth of them, one to a block; else four at a time where two
+// buffers of four rows fit into shared memory, and fewer otherwise.  us for 32760 rows of 5120, bf16 (198
+// at the rate of a copy): layer norm 211 (two rows at a time 277, three 249); with a norm of y
+// before it 268 (two 338); the root of the mean square, with less to do between its loads and
+// stores, 221 three at a time (four 234).  fp32 and 16380 rows 184; 20000 rows of 8192, one at a time since 1024
+// threads leave few registers, 256 (two 321); 1560 rows 13.6, 48 rows 3.7 (6.1 with the rows kernel's copies).
+// Longer rows: a block to a row.
 void launch_width(const NormParams &p, cudaStream_t st) {
     const int c = p.chunks;
-    const int row_bytes = c * ((p.xf ? 32 : 16) + (p.y ? (p.yf ? 32 : 16) : 0));
-    if (c > 128 && p.n_rows >= 152 * STREAM_ROWS) {
+    if (c <= 1024) {
+        if (p.n_rows <= echo::num_sms()) {
+            echo::launch_chained(gated_norm_row_kernel, dim3(p.n_rows), dim3((c + 31) / 32 * 32), 0, st, p);
+            return;
+        }
         const bool after = p.y && p.after.kind != ECHO_NORM_NONE;
-        if (!after && c <= 640 && 8 * row_bytes <= 200 * 1024) return launch_rows<4, false, 640>(p, st);
-        if (after && c <= 640 && 4 * row_bytes <= 200 * 1024) return launch_rows<2, true, 640>(p, st);
-        if (!after && c <= 1024 && 4 * row_bytes <= 200 * 1024) return launch_rows<2, false, 1024>(p, st);
-        if (after && c <= 1024 && 2 * row_bytes <= 200 * 1024) return launch_rows<1, true, 1024>(p, st);
+        const int row_bytes = c * ((p.xf ? 32 : 16) + (p.y ? (p.yf ? 32 : 16) : 0));
+        const int most = kBufferBytes / row_bytes;     // rows of a buffer
+        if (c > 640) return after ? launch_rows<1, true, 1024>(p, st) : launch_rows<1, false, 1024>(p, st);
+        if (after) return most >= 4 ? launch_rows<4, true, 640>(p, st) : launch_rows<2, true, 640>(p, st);
+        if (most >= 4 && p.before.kind != ECHO_NORM_RMS) return launch_rows<4, false, 640>(p, st);
+        return most >= 3 ? launch_rows<3, false, 640>(p, st) : launch_rows<2, false, 640>(p, st);
     }
-    if (c <= 32) return launch<32, 1>(p, st);
-    if (c <= 64) return launch<32, 2>(p, st);
-    if (c <= 128) return launch<32, 4>(p, st);
-    if (c <= 256) return launch<128, 2>(p, st);
-    if (c <= 384) return launch<128, 3>(p, st);
-    if (c <= 512) return launch<128, 4>(p, st);
-    if (c <= 640) return launch<128, 5>(p, st);
-    if (c <= 768) return launch<256, 3>(p, st);
-    if (c <= 1024) return launch<256, 4>(p, st);
     if (c <= 1536) return launch<512, 3>(p, st);
     launch<512, 4>(p, st);
 }
