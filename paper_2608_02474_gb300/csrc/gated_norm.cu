@@ -436,7 +436,8 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         if (p.before.bias) shift = fma8(shared_pairs(p.before.bias, 8 * t, true), scale, shift);
         if (p.before.weight) scale = mul8(shared_pairs(p.before.weight, 8 * t, true), scale);
     };
-    uint8_t *h_to, *n_to;                // of the batch
+    uint8_t *h_to = static_cast<uint8_t *>(p.h) + (first * p.ldh + 8 * t) * (p.hf ? 4 : 2);
+    uint8_t *n_to = static_cast<uint8_t *>(p.n) + (first * p.ldn + 8 * t) * (p.nf ? 4 : 2);
     const int64_t h_row = p.ldh * (p.hf ? 4 : 2), n_row = p.ldn * (p.nf ? 4 : 2);
     next = mod_of(0);
     bool ok = true;
@@ -507,9 +508,7 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         }
     };
     for (; i < batches; ++i) {
-        const int r0 = first + i * R, n = min(R, last - r0);
-        h_to = static_cast<uint8_t *>(p.h) + r0 * h_row + 8 * t * (p.hf ? 4 : 2);
-        n_to = static_cast<uint8_t *>(p.n) + r0 * n_row + 8 * t * (p.nf ? 4 : 2);
+        const int n = min(R, last - first - i * R);
         mod = next;
         if (i + 1 < batches) next = mod_of(i + 1);
         // a wait that gives up lets the others give up; nothing is stored from then on
@@ -517,6 +516,8 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         // the whole warp takes one way: a barrier lies on both
         if (__all_sync(0xffffffffu, ok && (lane >= R || (mod >= 0 && mod == cur && mod == cur_out)))) batch(std::true_type(), R);
         else batch(std::false_type(), n);
+        h_to += R * h_row;
+        n_to += R * n_row;
     }
     // copies land before this block exits
     if (!ok && t == 0) {
