@@ -217,12 +217,14 @@ def _stream_on(gpu: int, stream=None):
     return _raw_stream(gpu)
 
 
+_DTYPES = {torch.bfloat16: ECHO_BF16, torch.float32: ECHO_F32}
+
+
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return ECHO_BF16
-    if t.dtype == torch.float32:
-        return ECHO_F32
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"unsupported dtype {t.dtype}") from None
 
 
 def _dev(t: torch.Tensor, name: str):
@@ -901,37 +903,43 @@ class Rotary:
         self._ref = _c.byref(self.cstruct)
 
 
+def _turned(x, out, name, n, d, dtype, gpu):
+    """Row strides and heads of a tensor and of what it is turned into."""
+    cols = x.shape[-1]
+    if x.dim() != 2 or cols % d:
+        raise ValueError(f"{name} must be [n_rows, heads * {d}]")
+    ld = _rows_of(x, name, n, cols, gpu)
+    if out is x:
+        ldo = ld
+    else:
+        if out.shape != x.shape:
+            raise ValueError(f"{name} and {name}_out must have one shape")
+        ldo = _rows_of(out, name, n, cols, gpu)
+    if x.dtype != dtype or out.dtype != dtype:
+        raise TypeError("q, k and their outputs must share a dtype")
+    return ld, ldo, cols // d
+
+
 def echo_rotary(plan: Rotary, pos, q, k=None, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """(q, k) turned by their rows' positions, or q alone: [n_rows, heads * d] bf16 or f32, pos
     int32 [n_rows] (or [n_rows, axes]); rows of negative positions are left as they were in q_out and k_out.
     q_out, k_out: new tensors when not given; q and k themselves turn in place.  inverse: back, which is the gradient."""
-    n, gpu, d = q.shape[0], plan._gpu, plan.d
-    t = _dtype(q)
-
-    def rows(x, out, name):
-        if x.dim() != 2 or x.shape[1] % d:
-            raise ValueError(f"{name} must be [n_rows, heads * {d}]")
-        ld = _rows_of(x, name, n, x.shape[1], gpu)
-        if out is None:
-            out = _empty(tuple(x.shape), x.dtype, x.device, stream)
-        elif out.shape != x.shape:
-            raise ValueError(f"{name} and {name}_out must have one shape")
-        if x.dtype != q.dtype or out.dtype != q.dtype:
-            raise TypeError("q, k and their outputs must share a dtype")
-        ldo = _rows_of(out, name + "_out", n, x.shape[1], gpu)
-        # strides of a single row mean nothing: what its columns take
-        return out, (ld, ldo) if n > 1 else ((x.shape[1] + 7) // 8 * 8,) * 2, x.shape[1] // d
-
-    q_out, (ldq, ldqo), Hq = rows(q, q_out, "q")
+    n, gpu, d, t = q.shape[0], plan._gpu, plan.d, q.dtype
+    if q_out is None:
+        q_out = _empty(tuple(q.shape), t, q.device, stream)
+    q_ld, q_ldo, Hq = _turned(q, q_out, "q", n, d, t, gpu)
     pos_p = _ints(pos, "pos", gpu, n * plan.columns)
     if k is None:
-        args = (None, 0, 0, None, 0)
-    else:
-        k_out, (ldk, ldko), Hk = rows(k, k_out, "k")
-        args = (k.data_ptr(), ldk, Hk, k_out.data_ptr(), ldko)
-    _check("echo_rotary", lib().echo_rotary(plan._ref, pos_p, n, d, t, inverse, q.data_ptr(), ldq, Hq,
-                                            q_out.data_ptr(), ldqo, *args, _stream_on(gpu, stream)))
-    return q_out if k is None else (q_out, k_out)
+        _check("echo_rotary", lib().echo_rotary(plan._ref, pos_p, n, d, _dtype(q), inverse, q.data_ptr(), q_ld, Hq,
+                                                q_out.data_ptr(), q_ldo, None, 0, 0, None, 0, _stream_on(gpu, stream)))
+        return q_out
+    if k_out is None:
+        k_out = _empty(tuple(k.shape), t, k.device, stream)
+    k_ld, k_ldo, Hk = _turned(k, k_out, "k", n, d, t, gpu)
+    _check("echo_rotary", lib().echo_rotary(plan._ref, pos_p, n, d, _dtype(q), inverse, q.data_ptr(), q_ld, Hq,
+                                            q_out.data_ptr(), q_ldo, k.data_ptr(), k_ld, Hk, k_out.data_ptr(), k_ldo,
+                                            _stream_on(gpu, stream)))
+    return q_out, k_out
 
 
 # ---------------------------------------------------------------------------
@@ -970,20 +978,10 @@ def echo_gated_norm(plan: GatedNorm, x, y=None, gate=None, scale=None, shift=Non
     row r takes row mod_rows[r] (int32) of them, or r // rows_per_mod; rows whose number is no row are left out.
     h has x's dtype and n is bf16 where they are not given; want_h, want_n: None instead."""
     N, D, gpu = x.shape[0], plan.D, x.get_device()
-    if plan._gpu not in (None, gpu):
-        raise ValueError("x must be on the device of the weights")
-
-    def rows(t, name):
-        if t is None:
-            return None, 0, 0
-        ld = _rows_of(t, name, N, D, gpu)
-        if t.shape[1] != D:
-            raise ValueError(f"{name} must be [{N}, {D}]")
-        return t.data_ptr(), ld if N > 1 else (D + 7) // 8 * 8, _dtype(t)
-
-    xs, ys = rows(x, "x"), rows(y, "y")
     if gpu < 0:
         raise ValueError("x must be a CUDA tensor")
+    if plan._gpu not in (None, gpu):
+        raise ValueError("x must be on the device of the weights")
     if not want_h:
         h = None
     elif h is None:
@@ -992,23 +990,31 @@ def echo_gated_norm(plan: GatedNorm, x, y=None, gate=None, scale=None, shift=Non
         n = None
     elif n is None:
         n = _empty((N, D), torch.bfloat16, x.device, stream)
+    args = []
+    for t, name in ((x, "x"), (y, "y"), (h, "h"), (n, "n")):
+        if t is None:
+            args += (None, 0, 0)
+            continue
+        ld = _rows_of(t, name, N, D, gpu)
+        if t.shape[1] != D:
+            raise ValueError(f"{name} must be [{N}, {D}]")
+        args += (t.data_ptr(), ld, _dtype(t))
     mod = None
     first = gate if gate is not None else scale if scale is not None else shift
     if first is not None:
-        mods, ld, dtype, ptr = first.shape[0], first.stride(0), first.dtype, []
-        if mods == 1:                    # a single row's stride means nothing
-            ld = (D + 7) // 8 * 8
-        for name, v in (("gate", gate), ("scale", scale), ("shift", shift)):
+        mods, dtype, ptr, ld = first.shape[0], first.dtype, [], None
+        for v, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
             if v is None:
                 ptr.append(None)
                 continue
-            if _rows_of(v, name, mods, D, gpu) != ld and mods > 1 or v.dtype != dtype or v.shape[1] != D:
+            own = _rows_of(v, name, mods, D, gpu)
+            if own != (own if ld is None else ld) or v.dtype != dtype or v.shape[1] != D:
                 raise ValueError(f"gate, scale and shift must be [n_mods, {D}] of one dtype and row stride")
+            ld = own
             ptr.append(v.data_ptr())
-        rows_p = None if mod_rows is None else _ints(mod_rows, "mod_rows", gpu, N)
-        mod = _c.byref(ModulationC(*ptr, ld, mods, rows_per_mod, rows_p, _dtype(first)))
+        mod = _c.byref(ModulationC(*ptr, ld, mods, rows_per_mod,
+                                   None if mod_rows is None else _ints(mod_rows, "mod_rows", gpu, N), _dtype(first)))
     elif mod_rows is not None:
         raise ValueError("mod_rows without gate, scale or shift")
-    _check("echo_gated_norm", lib().echo_gated_norm(plan._ref, mod, N, *xs, *ys, *rows(h, "h"), *rows(n, "n"),
-                                                    _stream_on(gpu, stream)))
+    _check("echo_gated_norm", lib().echo_gated_norm(plan._ref, mod, N, *args, _stream_on(gpu, stream)))
     return h, n
