@@ -28,25 +28,30 @@ namespace {
 constexpr int PIECES = 4;                      // handed out ahead
 constexpr int kWholeKeys = 768;     // 16 heads of 64, one bf16 token: whole 256 keys 9.2 us, 1024 13.4; divided 11.6, 12.1
 
-template <int FORM, int D, int NR>
+// LONG: twice as many keys of a block, for 4-bit heads of 64 over much work (48 tokens of 16 heads over
+// up to 8190 keys each 82 us, so 94; one over 2000 18, so 14)
+template <int FORM, int D, int NR, bool LONG>
 struct Cfg {
     static constexpr bool CODES = FORM != kBf16;
     static constexpr int ROWS = 8 * NR;
     static constexpr int GROUPS = NR * D <= (CODES ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
     static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
-    static constexpr int KPW = CODES ? 32 : 16;            // keys of a warp
-    static constexpr int KG = KPW / 16;                    // 16 keys of a warp, this many at once
+    static constexpr int KPW = LONG ? 64 : CODES ? 32 : 16;   // keys of a warp
+    static constexpr int KG = CODES ? 2 : 1;               // 16 keys of them at once
     static constexpr int BK = 4 * KPW;                     // keys of a block
-    static constexpr int BSHIFT = CODES ? 7 : 6;
+    static constexpr int BSHIFT = KPW == 64 ? 8 : CODES ? 7 : 6;
     static constexpr int ROW_BYTES = kv_bytes(FORM, D);
     static constexpr int HALF = BK * ROW_BYTES;            // K or V of a block
     static constexpr int TOKEN_SCALES = FORM == kInt8 ? 4 : FORM == kInt4 ? D / 16 : 0;   // bytes, of K or V
     static constexpr int SCALES = 2 * BK * TOKEN_SCALES;
     static constexpr int STAGE = 2 * HALF + SCALES;        // a multiple of 1024
-    static constexpr int JOIN = WARPS / 4 * ROWS * D * 4;  // half of the warps' half of O
-    static constexpr bool Q_SMEM = NR * D >= 192 && D == 64;          // the queries' registers do not suffice
-    static constexpr int Q_BYTES = Q_SMEM ? ROWS * D * 2 : 0;
-    static constexpr int RING = (110 * 1024 - JOIN - Q_BYTES) / STAGE;   // two CTAs share an SM
+    // half of the warps' half of O; 4 bits: all of it
+    static constexpr int JOIN = (FORM == kInt4 ? WARPS : WARPS / 4) * ROWS * D * 4;
+    static constexpr bool Q_SMEM = (NR * D >= 192 && D == 64) || FORM == kInt4;   // the queries' registers do not suffice
+    static constexpr int Q_BUF = ROWS * D * 2, Q_BYTES = Q_SMEM ? (FORM == kInt4 ? 2 : 1) * Q_BUF : 0;   // this piece's and the next
+    // two CTAs share an SM.  4 bits: a multiple of the groups, so that a stage is always the same group's
+    static constexpr bool OWN = FORM == kInt4;
+    static constexpr int RING = (110 * 1024 - JOIN - Q_BYTES) / STAGE / (OWN ? GROUPS : 1) * (OWN ? GROUPS : 1);
     static constexpr int SMEM = RING * STAGE + JOIN + Q_BYTES + 1024;
     static_assert(STAGE % 1024 == 0 && RING >= 2, "");
 };
@@ -112,10 +117,10 @@ ECHO_DEV uint32_t chunk_at(int r, int c) {
     else return (uint32_t)((c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-template <int FORM, int D, int NR>
-__global__ void __launch_bounds__((Cfg<FORM, D, NR>::THREADS), 2)
+template <int FORM, int D, int NR, bool LONG>
+__global__ void __launch_bounds__((Cfg<FORM, D, NR, LONG>::THREADS), 2)
 kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
-    using C = Cfg<FORM, D, NR>;
+    using C = Cfg<FORM, D, NR, LONG>;
     constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4, CODES = C::CODES;
     constexpr int KG = C::KG, STEP = 16 * KG, BK = C::BK, MT = D / 16, ROWS = C::ROWS;
     extern __shared__ uint8_t smem_raw[];
@@ -133,7 +138,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::RING; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], C::WARPS);
+            mbar_init(&empty[i], C::OWN ? 4 : C::WARPS);
         }
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&piece_full[i], 1);
@@ -244,11 +249,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         const int kb0 = pc.kb0, kb1 = kb0 + pc.blocks;
         // B of the first product: 8 packed rows a fragment, row gq of them in this lane
         uint32_t qb[C::Q_SMEM ? 1 : NR][C::Q_SMEM ? 1 : MT][2];
-        auto query = [&](int pr, int kk) -> uint2 {
+        auto query = [&](const KvPiece &of, int pr, int kk) -> uint2 {
             uint2 v = make_uint2(0u, 0u);
-            if (pr < s.packed) {
+            if (pr < of.packed) {
                 const int r = p.work.by_group(pr);
-                const __nv_bfloat16 *src = p.q + (int64_t)(s.row + r) * p.ldq + (head * group + pr - r * group) * D + 16 * kk;
+                const __nv_bfloat16 *src = p.q + (int64_t)(of.row + r) * p.ldq + (of.head * group + pr - r * group) * D + 16 * kk;
                 if constexpr (INT4) {          // a lane's word of 32 columns: 8 of them, 4 a product
                     v = *reinterpret_cast<const uint2 *>(src - 16 * (kk & 1) + 8 * tq + 4 * (kk & 1));
                 } else if constexpr (INT8) {
@@ -260,11 +265,35 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             }
             return v;
         };
-        if constexpr (C::Q_SMEM) {                   // the fragments as they are, lane by lane
+        // 4 bits: the fragments that this warp fetches for all
+        constexpr int QN = (NR * MT + C::WARPS - 1) / C::WARPS;
+        uint2 qn[INT4 ? QN : 1];
+        auto fetch_queries = [&](const KvPiece &of) {
+#pragma unroll
+            for (int i0 = 0; i0 < QN; ++i0) {
+                const int i = i0 * C::WARPS + warp;
+                if (i < NR * MT) qn[INT4 ? i0 : 0] = query(of, of.tile * ROWS + (i / MT) * 8 + gq, i % MT);
+            }
+        };
+        auto keep_queries = [&](uint2 *to) {
+#pragma unroll
+            for (int i0 = 0; i0 < QN; ++i0) {
+                const int i = i0 * C::WARPS + warp;
+                if (i < NR * MT) to[i * 32 + lane] = qn[INT4 ? i0 : 0];
+            }
+        };
+        const uint2 *q_now = q_smem + (INT4 ? (n & 1) * (C::Q_BUF / 8) : 0);
+        if constexpr (INT4) {
+            if (n == 0) {                            // those of later pieces came meanwhile, below
+                fetch_queries(pc);
+                keep_queries(q_smem);
+                named_bar_sync(1, 32 * C::WARPS);
+            }
+        } else if constexpr (C::Q_SMEM) {            // the fragments as they are, lane by lane
 #pragma unroll
             for (int i0 = 0; i0 < NR * MT; i0 += C::WARPS) {
                 const int i = i0 + warp;             // WARPS divides NR * MT
-                q_smem[i * 32 + lane] = query(tile * ROWS + (i / MT) * 8 + gq, i % MT);
+                q_smem[i * 32 + lane] = query(pc, tile * ROWS + (i / MT) * 8 + gq, i % MT);
             }
             named_bar_sync(1, 32 * C::WARPS);
         } else {
@@ -272,7 +301,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
                 for (int kk = 0; kk < MT; ++kk) {
-                    const uint2 v = query(tile * ROWS + nt * 8 + gq, kk);
+                    const uint2 v = query(pc, tile * ROWS + nt * 8 + gq, kk);
                     qb[nt][kk][0] = v.x;
                     qb[nt][kk][1] = v.y;
                 }
@@ -295,11 +324,13 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         for (int kb = kb0; kb < kb1; ++kb, ++g) {
             // every warp sees every stage fill, its own or not, before the stage is filled again:
             // a barrier's phases are told apart by their parity only
+            const bool own = C::GROUPS == 1 || (g & 1) == warp >> 2;
+            if (C::OWN && !own) continue;
             const int stage = g % C::RING;
             ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (g / C::RING) & 1, abort_v, p.err));
             if (!ok) break;
             const uint32_t kbase = ring + stage * C::STAGE, vbase = kbase + C::HALF;
-            if (C::GROUPS == 1 || (g & 1) == warp >> 2)
+            if (own)
 #pragma unroll 1
             for (int k0 = 0; k0 < C::KPW; k0 += STEP) {
                 const int wk = wk0 + k0, key0 = kb * BK + wk;    // the first key of this step
@@ -308,41 +339,73 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 float sc[KG][NR][4] = {};
                 const uint8_t *token_scales = smem + stage * C::STAGE + 2 * C::HALF;
                 constexpr int STEPS = INT4 ? 4 : INT8 ? 2 : 1;   // products of what four matrices hold
+                if constexpr (INT4) {
+                    // 8 packed rows: a group's scores by themselves, times the keys' scales; more rows: the
+                    // scales go into the keys
+                    constexpr bool APART = NR == 1;
 #pragma unroll
-                for (int kg = 0; kg < KG; ++kg) {
-                    uint32_t ks[2][D / 64];          // 4 bits: the scales of keys gq and gq + 8, two groups a word
-                    if constexpr (INT4) {
+                    for (int kk = 0; kk < MT; kk += STEPS) {
+                        uint2 qf[NR][STEPS];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            load_words(token_scales + (wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES, ks[h]);
+                        for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+                            for (int i = 0; i < STEPS; ++i) {
+                                qf[nt][i] = q_now[(nt * MT + kk + i) * 32 + lane];
+                            }
+#pragma unroll
+                        for (int kg = 0; kg < KG; ++kg) {
+                            uint32_t r[4], ks[2];    // two groups' codes; scales of keys gq and gq + 8
+                            const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
+                            ldsm4(kbase + chunk_at<FORM, D, BK>(row, kk / 2 + (mi >> 1)), r);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                ks[h] = *reinterpret_cast<const uint32_t *>(token_scales + (wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES + kk);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {        // a group of 32 columns
+                                uint32_t a[4], c[4];
+                                a[0] = kv_nibbles2<0>(r[2 * i]);
+                                a[1] = kv_nibbles2<0>(r[2 * i + 1]);
+                                a[2] = kv_nibbles2<1>(r[2 * i]);
+                                a[3] = kv_nibbles2<1>(r[2 * i + 1]);
+                                c[0] = kv_nibbles2<2>(r[2 * i]);
+                                c[1] = kv_nibbles2<2>(r[2 * i + 1]);
+                                c[2] = kv_nibbles2<3>(r[2 * i]);
+                                c[3] = kv_nibbles2<3>(r[2 * i + 1]);
+                                if constexpr (APART) {
+                                    float part[4] = {};
+                                    mma16816(part, a, qf[0][2 * i].x, qf[0][2 * i].y);
+                                    mma16816(part, c, qf[0][2 * i + 1].x, qf[0][2 * i + 1].y);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        sc[kg][0][e] = fmaf(part[e], i ? bf16hi(ks[e / 2]) : bf16lo(ks[e / 2]), sc[kg][0][e]);
+                                } else {
+                                    const uint32_t both = i ? 0x3232u : 0x1010u;
+                                    const uint32_t s0 = __byte_perm(ks[0], 0u, both), s1 = __byte_perm(ks[1], 0u, both);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        a[e] = bf16x2_mul(a[e], e & 1 ? s1 : s0);
+                                        c[e] = bf16x2_mul(c[e], e & 1 ? s1 : s0);
+                                    }
+#pragma unroll
+                                    for (int nt = 0; nt < NR; ++nt) {
+                                        mma16816(sc[kg][nt], a, qf[nt][2 * i].x, qf[nt][2 * i].y);
+                                        mma16816(sc[kg][nt], c, qf[nt][2 * i + 1].x, qf[nt][2 * i + 1].y);
+                                    }
+                                }
+                            }
+                        }
                     }
+                } else {
+#pragma unroll
+                for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
                     for (int kk = 0; kk < MT; kk += STEPS) {
                         uint32_t r[4];
                         const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
-                        ldsm4(kbase + chunk_at<FORM, D, BK>(row, INT4 ? kk / 2 + (mi >> 1) : INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
-                        // 4 bits, 8 packed rows: a group's scores by themselves, times the keys' scales; more
-                        // rows: the scales go into the keys
-                        constexpr bool APART = INT4 && NR == 1;
-                        float part[4];
+                        ldsm4(kbase + chunk_at<FORM, D, BK>(row, INT8 ? kk + (mi >> 1) : 2 * kk + (mi >> 1)), r);
 #pragma unroll
                         for (int i = 0; i < STEPS; ++i) {
                             uint32_t a[4] = {r[0], r[1], r[2], r[3]};
-                            if constexpr (INT4) {
-                                const uint32_t w0 = r[2 * (i / 2)], w1 = r[2 * (i / 2) + 1];
-                                a[0] = i % 2 ? kv_nibbles2<2>(w0) : kv_nibbles2<0>(w0);
-                                a[1] = i % 2 ? kv_nibbles2<2>(w1) : kv_nibbles2<0>(w1);
-                                a[2] = i % 2 ? kv_nibbles2<3>(w0) : kv_nibbles2<1>(w0);
-                                a[3] = i % 2 ? kv_nibbles2<3>(w1) : kv_nibbles2<1>(w1);
-                                if constexpr (!APART) {
-                                    const uint32_t both = i / 2 ? 0x3232u : 0x1010u;
-                                    const uint32_t s0 = __byte_perm(ks[0][kk / 4], 0u, both), s1 = __byte_perm(ks[1][kk / 4], 0u, both);
-                                    a[0] = bf16x2_mul(a[0], s0);
-                                    a[1] = bf16x2_mul(a[1], s1);
-                                    a[2] = bf16x2_mul(a[2], s0);
-                                    a[3] = bf16x2_mul(a[3], s1);
-                                }
-                            }
                             if constexpr (INT8) {
                                 const uint32_t w0 = kv_flip(r[2 * i]), w1 = kv_flip(r[2 * i + 1]);
                                 a[0] = kv_codes2(w0, 0x4140);
@@ -355,14 +418,6 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                                 if constexpr (C::Q_SMEM) {
                                     const uint2 b = q_smem[(nt * MT + kk + i) * 32 + lane];
                                     mma16816(sc[kg][nt], a, b.x, b.y);
-                                } else if constexpr (APART) {
-                                    if (i % 2 == 0) part[0] = part[1] = part[2] = part[3] = 0.f;
-                                    mma16816(part, a, qb[nt][kk + i][0], qb[nt][kk + i][1]);
-                                    if (i % 2) {
-#pragma unroll
-                                        for (int e = 0; e < 4; ++e)
-                                            sc[kg][nt][e] = fmaf(part[e], i / 2 ? bf16hi(ks[e / 2][kk / 4]) : bf16lo(ks[e / 2][kk / 4]), sc[kg][nt][e]);
-                                    }
                                 } else {
                                     mma16816(sc[kg][nt], a, qb[nt][kk + i][0], qb[nt][kk + i][1]);
                                 }
@@ -377,7 +432,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 if (INT4 && edge) {
                     // values' scales that are not finite, or anything past the end: 0, and what is
                     // spoilt spoils the rows that see it.  This warp's keys alone.
-                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + (lane & (STEP - 1))) * C::TOKEN_SCALES);
+                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + lane) * C::TOKEN_SCALES);
 #pragma unroll
                     for (int i = 0; i < C::TOKEN_SCALES / 4; ++i) {
                         const uint32_t off = kv_not_finite2(at[i]);
@@ -580,6 +635,13 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         // a wait that gave up is told to all warps, which leave together
         ok = !named_bar_or(1, 32 * C::WARPS, !ok);
         if (!ok) break;
+        bool more = false;                           // 4 bits: the next piece's queries on their way
+        if constexpr (INT4) {
+            const KvPiece &after = piece[(n + 1) % PIECES];
+            more = __all_sync(0xffffffffu, mbar_wait(&piece_full[(n + 1) % PIECES], ((n + 1) / PIECES) & 1, abort_v, p.err)) &&
+                   after.blocks >= 0;
+            if (more) fetch_queries(after);
+        }
 #pragma unroll
         for (int nt = 0; nt < NR; ++nt)
 #pragma unroll
@@ -611,8 +673,58 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                     o[nt][t][2 + e] *= f;
                 }
             }
-        // warp w takes over warp w + W/2, W/4, ...: half the columns at a time
         float *const flat = &o[0][0][0];
+        if constexpr (INT4) {
+            // every warp puts down what it has, and adds up the warps' pairs of an even share: one barrier
+            constexpr int N = NR * MT * 4, PAIRS = N / 2 / C::WARPS;
+            static_assert(MT * 2 % C::WARPS == 0, "a share's pairs are of known rows");
+#pragma unroll
+            for (int i = 0; i < N; ++i) join[(warp * N + i) * 32 + lane] = flat[i];
+            if (more) keep_queries(q_smem + ((n + 1) & 1) * (C::Q_BUF / 8));
+            named_bar_sync(1, 32 * C::WARPS);
+            const bool whole = pc.whole;
+            float *slot = kv_slot(p.ws, blockIdx.x, pc.tail, ROWS, D);
+            if (!whole && warp == 0 && gq == 0) {
+#pragma unroll
+                for (int nt = 0; nt < NR; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = nt * 8 + 2 * tq + e;
+                        if (tile * ROWS + row < s.packed)
+                            *reinterpret_cast<float2 *>(slot + ROWS * D + 2 * row) = make_float2(mt[nt][e], lt[nt][e]);
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) {
+                const int i = k * C::WARPS + warp, nt = k * C::WARPS / (MT * 2);   // pair i: of tile t, column of gq u
+                const int t = i / 2 % MT, u = i & 1;
+                float x[2] = {0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < C::WARPS; ++w)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x[e] += join[(w * N + 2 * i + e) * 32 + lane];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x[e] *= !whole ? 1.f : lt[nt][e] == 0.f ? 0.f : 1.f / lt[nt][e];   // no key: zeros
+                // columns in pairs, those of lanes gq and gq + 1: even lanes trade row 2 tq + 1 for row 2 tq.
+                // They are 8 (gq / 2) + gq mod 2 of each 32, plus 4 (t mod 2), and 2 u
+                const int e = gq & 1;
+                const float got = __shfl_xor_sync(0xffffffffu, e ? x[0] : x[1], 4);
+                const float a = e ? got : x[0], b = e ? x[1] : got;
+                const int row = nt * 8 + 2 * tq + e, pr = tile * ROWS + row;
+                const int col = 32 * (t >> 1) + 8 * (gq >> 1) + 4 * (t & 1) + 2 * u;
+                if (pr < s.packed) {
+                    const int r = p.work.by_group(pr);
+                    if (whole)
+                        *reinterpret_cast<uint32_t *>(p.out + (int64_t)(s.row + r) * p.ldo +
+                                                      (head * group + pr - r * group) * D + col) = pack_bf16(a, b);
+                    else *reinterpret_cast<float2 *>(slot + row * D + col) = make_float2(a, b);
+                }
+                __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(&piece_empty[n % PIECES]);
+            continue;
+        }
+        // warp w takes over warp w + W/2, W/4, ...: half the columns at a time
         constexpr int HALF_O = NR * MT * 2;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -637,8 +749,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         if (lane == 0) mbar_arrive(&piece_empty[n % PIECES]);
         if (warp != 0) continue;
         // Columns in pairs: int8 has 2 gq and 2 gq + 1 of each 16.  bf16 has gq and gq + 8:
-        // lanes of even gq trade row 2 tq + 1 for row 2 tq of the lane after them.  So do 4
-        // bits, whose columns are 8 (gq / 2) + gq mod 2 of each 32, plus 4 (t mod 2), and 2 more.
+        // lanes of even gq trade row 2 tq + 1 for row 2 tq of the lane after them.
 #pragma unroll
         for (int nt = 0; nt < NR; ++nt) {
             float inv[2];
@@ -666,8 +777,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         b = e ? x1 : got;
                     }
                     const int row = nt * 8 + 2 * tq + e, pr = tile * ROWS + row;
-                    const int col = INT4 ? 32 * (t >> 1) + 8 * (gq >> 1) + 4 * (t & 1) + 2 * u
-                                         : 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
+                    const int col = 16 * t + (INT8 ? 2 * gq : 8 * u + (gq & ~1));
                     if (pr >= s.packed) continue;
                     const int r = pr / group;
                     if (whole)
@@ -680,14 +790,14 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     }
 }
 
-template <int FORM, int D, int NR>
+template <int FORM, int D, int NR, bool LONG = false>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
-    using C = Cfg<FORM, D, NR>;
+    using C = Cfg<FORM, D, NR, LONG>;
     static int attr_done[64] = {};
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(kv_decode_kernel<FORM, D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        cudaFuncSetAttribute(kv_decode_kernel<FORM, D, NR, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         attr_done[dev] = 1;
     }
     CUtensorMap tm;
@@ -706,7 +816,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        launched = echo::launch_chained(kv_decode_kernel<FORM, D, NR>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
+        launched = echo::launch_chained(kv_decode_kernel<FORM, D, NR, LONG>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
     }
     if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
@@ -728,6 +838,12 @@ int tile_rows(bool codes, int d, int64_t rows) {
 
 template <int FORM, int D>
 echo_status launch_rows(const echo::KvAttention &a, int tile, cudaStream_t st) {
+    if constexpr (FORM == kInt4 && D == 64) {
+        // 16 blocks of 256 keys for each worker, if the sequences fill their tables
+        const double keys = (double)a.batch->max_pages * a.pool->page_tokens;
+        if (tile == 8 && (double)a.batch->n_seqs * a.pool->H * keys >= 2.0 * echo::num_sms() * 16 * 256)
+            return launch<FORM, D, 1, true>(a, st);
+    }
     if (tile == 8) return launch<FORM, D, 1>(a, st);
     if (tile == 16) return launch<FORM, D, 2>(a, st);
     if constexpr (D == 64) {
