@@ -12,6 +12,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kLoads = 4;   // 16-byte loads of a lane on their way at once
+constexpr float kSeventh = (float)((1.0 - 1.0 / 1048576) / 7.0);   // 1 / 7, less 2^-20 of it
 
 // 16 bytes of a row: 8 bf16 values, or 4 of fp32
 template <typename T>
@@ -147,9 +148,22 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ 
 }
 
 // The same into 4-bit pages: 8 neighbouring columns of a lane, four lanes to a scale.  Values are
-// taken in bf16 first, so that max |u| / 7, rounded up to 5 significant bits, and u / s have few bits:
-// with 1 / s a little too large (2^-22), the halves between two codes, and nothing else, pass
-// over to the larger one, and one fused multiply-add rounds the quotient (codes4).
+// taken in bf16 first, so that max |u| / 7 and u / s have few bits and no division is needed: a product
+// with 1 / 7 a little too small (2^-20) lies below a number of 5 bits where the quotient is that number, and
+// above no other that the quotient is below; with 1 / s a little too large, the halves between two codes,
+// and nothing else, pass over to the larger one.  (bf16 has 8 bits: other quotients are 2^-9 of
+// themselves away.)  With divisions, and codes put together one by one, 32760 rows of 40 heads of 128 took
+// 205 us, now WRITE4.
+ECHO_DEV uint32_t max_abs2(uint32_t a, uint32_t b) {      // of pairs without signs; NaN where there is one
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+ECHO_DEV float rcp_approx(float x) {                      // to 2^-23
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads)
 kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ place, const T *__restrict__ k,
@@ -187,32 +201,25 @@ kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__
                 values16<T>(in[u][NG - 1], f + 4);
                 w = pack8_bf16(f);
             }
-            uint32_t lo = 0, hi = 0;                  // the largest |value|, as warp_amax_bf16
             const uint32_t pair[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                lo = max(lo, pair[i] & 0x7FFFu);
-                hi = max(hi, pair[i] & 0x7FFF0000u);
-            }
-            uint32_t a = max(lo << 16, hi);
-            a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
-            a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+            uint32_t a2 = max_abs2(max_abs2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu),
+                                   max_abs2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
+            a2 = max_abs2(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
+            a2 = max_abs2(a2, __shfl_xor_sync(0xffffffffu, a2, 2));
             if (c >= C) continue;
+            const uint32_t a = max(a2 << 16, a2 & 0xFFFF0000u);       // fp32 bits; NaN above infinity
             const bool bad = a >= 0x7F800000u;
-            const float s = fmaxf(__uint_as_float((__float_as_uint(__fdiv_rn(__uint_as_float(a), 7.f)) + 0x7FFFFu) & ~0x7FFFFu),
+            const float s = fmaxf(__uint_as_float((__float_as_uint(__fmul_rn(__uint_as_float(a), kSeventh)) + 0x7FFFFu) & ~0x7FFFFu),
                                   1.92592994438723585e-34f);          // 2^-112
-            const float inv = __fmul_rn(__frcp_rn(s), 1.f + 0x1p-22f);
-            uint32_t codes = 0x88888888u;             // zeros
-            if (!bad) {
-                codes = 0u;
+            const float inv = __fmul_rn(rcp_approx(s), 1.f + 0x1p-20f);
+            // 1.5 2^23 + 8 + code has the code, plus 8, in its low bits and nothing else below bit 22
+            uint32_t even = 0, odd = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    // 1.5 2^23 + 8 + code: the code, plus 8, in its low bits
-                    const uint32_t even = __float_as_uint(__fmaf_rn(bf16lo(pair[i]), inv, 12582920.f)) & 15u;
-                    const uint32_t odd = __float_as_uint(__fmaf_rn(bf16hi(pair[i]), inv, 12582920.f)) & 15u;
-                    codes |= even << (4 * i) | odd << (16 + 4 * i);
-                }
+            for (int i = 3; i >= 0; --i) {
+                even = even * 16u + __float_as_uint(__fmaf_rn(bf16lo(pair[i]), inv, 12582920.f));
+                odd = odd * 16u + __float_as_uint(__fmaf_rn(bf16hi(pair[i]), inv, 12582920.f));
             }
+            const uint32_t codes = bad ? 0x88888888u : __byte_perm(even, odd, 0x5410);
             const int kv = c >= half, ch = kv ? c - half : c;
             const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
             *reinterpret_cast<uint32_t *>(pool.pages + vec * (D / 2) + ch % LPH * 4) = codes;
@@ -274,18 +281,32 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
         for (int u = 0; u < U; ++u) {
             const int c = c0 + 32 * u;
             if (c >= C) continue;
+            T *dst = (c >= half ? v : k) + r * ld + (int64_t)(c >= half ? c - half : c) * EP;
             float f[EP];
+            if constexpr (INT4) {
+                // code / 64, times 64, times the scale: exact.  fp32: four of a word's columns a lane
+                const uint32_t s2 = __float_as_uint(sc[u]) | __float_as_uint(sc[u]) >> 16;
+                const uint32_t w0 = EP == 8 ? in[u][0] : in[u][0] >> (8 * (c & 1));
+                auto value2 = [&](uint32_t code) { return at < 0 ? 0u : bf16x2_mul(bf16x2_mul(code, 0x42804280u), s2); };
+                const uint4 w = make_uint4(value2(kv_nibbles2<0>(w0)), value2(kv_nibbles2<1>(w0)),
+                                           value2(kv_nibbles2<2>(w0)), value2(kv_nibbles2<3>(w0)));
+                if constexpr (sizeof(T) == 2) {
+                    __stcs(reinterpret_cast<uint4 *>(dst), w);
+                } else {
+                    f[0] = bf16lo(w.x);
+                    f[1] = bf16hi(w.x);
+                    f[2] = bf16lo(w.y);
+                    f[3] = bf16hi(w.y);
+                    store16<T>(dst, f);
+                }
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < EP; ++i) {
-                if constexpr (INT4) {
-                    // columns 2 i and 2 i + 1 of 8 in bits 4 i and 16 + 4 i; fp32: four of them a lane
-                    const int col = EP == 8 ? i : i + 4 * (c & 1);
-                    f[i] = __fmul_rn((float)((int)(in[u][0] >> (4 * (col >> 1) + 16 * (col & 1)) & 15u) - 8), sc[u]);
-                    if (at < 0) f[i] = 0.f;
-                } else if constexpr (INT8) f[i] = __fmul_rn((float)(int8_t)(in[u][i >> 2] >> (8 * (i & 3))), sc[u]);
+                if constexpr (INT8) f[i] = __fmul_rn((float)(int8_t)(in[u][i >> 2] >> (8 * (i & 3))), sc[u]);
                 else f[i] = i & 1 ? bf16hi(in[u][i >> 1]) : bf16lo(in[u][i >> 1]);
             }
-            store16<T>((c >= half ? v : k) + r * ld + (int64_t)(c >= half ? c - half : c) * EP, f);
+            store16<T>(dst, f);
         }
     }
 }

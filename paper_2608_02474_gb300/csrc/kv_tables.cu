@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kMostSeqs = 8192, kMostSlots = 1 << 18;
+constexpr int kAtOnce = 4;
 constexpr int kMostTokens = INT32_MAX / 128 * 128;   // of a sequence, as the attention takes them
 
 struct Tables {
@@ -143,29 +144,36 @@ kv_tables_kernel(const Tables t, const Step s, int *err) {
         if (EXTEND && tid == 0) s.row0[0] = 0;
     }
     if (EXTEND) {
-        // rows: the last b with row0[b] <= r, over the smem copy
-        const int live = ok ? row0[n] : 0;
-        for (int64_t r0 = (int64_t)rank * kThreads + tid; r0 < s.n_rows; r0 += (int64_t)ranks * kThreads) {
-            const int r = (int)r0;
-            int64_t place = -1;
-            int p = -1, b = -1;
-            if (r < live) {
+        // rows: the last b with row0[b] <= r, over the copy in shared memory.  A page's number is a wait
+        // for the L2: those of kAtOnce rows on their way together
+        const int live = ok ? row0[n] : 0, step = ranks * kThreads;
+        for (int64_t r0 = (int64_t)rank * kThreads + tid; r0 < s.n_rows; r0 += (int64_t)kAtOnce * step) {
+            int id[kAtOnce], p[kAtOnce], b[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                id[k] = p[k] = b[k] = -1;
+                const int64_t r = r0 + (int64_t)k * step;
+                if (r >= live) continue;
                 int lo = 0, width = n;                // the answer is in [lo, lo + width)
                 while (width > 1) {
                     const int half = width >> 1;
-                    if (row0[lo + half] <= r) lo += half, width -= half;
+                    if (row0[lo + half] <= (int)r) lo += half, width -= half;
                     else width = half;
                 }
-                b = lo;
-                p = len[b] + (r - row0[b]);
-                const int j = p >> t.shift;
-                const int id = j < have[b] ? t.table[(int64_t)slot[b] * t.max_pages + j]
-                                           : t.free_pages[n_free - 1 - (before[b] + j - have[b])];
-                place = ((int64_t)id << t.shift) + (p & (page - 1));
+                b[k] = lo;
+                p[k] = len[lo] + ((int)r - row0[lo]);
+                const int j = p[k] >> t.shift;
+                id[k] = j < have[lo] ? t.table[(int64_t)slot[lo] * t.max_pages + j]
+                                     : t.free_pages[n_free - 1 - (before[lo] + j - have[lo])];
             }
-            if (s.place) s.place[r] = place;
-            if (s.pos) s.pos[r] = p;
-            if (s.seq) s.seq[r] = b;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int64_t r = r0 + (int64_t)k * step;
+                if (r >= s.n_rows) continue;
+                if (s.place) s.place[r] = r < live ? ((int64_t)id[k] << t.shift) + (p[k] & (page - 1)) : -1;
+                if (s.pos) s.pos[r] = p[k];
+                if (s.seq) s.seq[r] = b[k];
+            }
         }
     }
     if (!ok) return;
