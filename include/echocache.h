@@ -576,7 +576,7 @@ echo_status echo_kv_tables_reset(const echo_kv_tables *t, echo_stream_t stream);
  *   place   int64 [n_rows] (8-byte aligned), pos int32 [n_rows], seq int32 [n_rows], each or NULL:
  *           for row r of sequence b, at position p = len_b - rows_b + r - row0[b]: the page times
  *           page_tokens plus p mod page_tokens; p; b.  -1 for rows behind the last sequence's.
- * n_rows: the most rows in all.  One launch; slots, rows, len, row0, table, pos, seq 4-byte aligned.
+ * n_rows: the most rows in all.  One launch, two for many rows; slots, rows, len, row0, table, pos, seq 4-byte aligned.
  * A call that cannot be served (not enough pages, more than n_rows rows or max_pages pages or 2^31 - 128
  * tokens, rows below 0, a slot that does not exist or comes twice, tables that are no tables) changes
  * nothing in t and sets the PAGE flag; its row0, then, is 0 throughout, its place, pos and seq

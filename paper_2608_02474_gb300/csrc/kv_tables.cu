@@ -4,8 +4,8 @@
 // Both are sums over the sequences (pages that those before a sequence take, rows that they
 // have) and then independent entries.  One launch: each CTA of a cluster computes the sums of
 // all sequences for itself (8192 of them are 32 KB an array, from the L2), and the cluster
-// shares out the entries; a cluster barrier between the two parts keeps the tables as they
-// were until everybody has read them.  The bytes are few (a row's place, position and sequence
+// shares out the entries (those of many rows are left to a second launch); a cluster barrier between
+// the two parts keeps the tables as they were until everybody has read them.  The bytes are few (a row's place, position and sequence
 // are 16), so what a call takes is its latency: launch, reading lengths, the sums' barriers,
 // and the chain from an entry's search to its page.
 #include "common.cuh"
@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kMostSeqs = 8192, kMostSlots = 1 << 18;
-constexpr int kAtOnce = 4;
+constexpr int kRowsHere = 8192;                       // rows whose maps the first launch makes
 constexpr int kMostTokens = INT32_MAX / 128 * 128;   // of a sequence, as the attention takes them
 
 struct Tables {
@@ -27,6 +27,7 @@ struct Step {
     int32_t *table, *len, *row0, *pos, *seq;
     int64_t *place;
     int n_seqs, n_rows;
+    bool rows_here;              // the row maps, too
 };
 
 // exclusive sums of two numbers over the CTA's threads, and their totals; `part` [2][kWarps]
@@ -144,36 +145,30 @@ kv_tables_kernel(const Tables t, const Step s, int *err) {
         if (EXTEND && tid == 0) s.row0[0] = 0;
     }
     if (EXTEND) {
-        // rows: the last b with row0[b] <= r, over the copy in shared memory.  A page's number is a wait
-        // for the L2: those of kAtOnce rows on their way together
-        const int live = ok ? row0[n] : 0, step = ranks * kThreads;
-        for (int64_t r0 = (int64_t)rank * kThreads + tid; r0 < s.n_rows; r0 += (int64_t)kAtOnce * step) {
-            int id[kAtOnce], p[kAtOnce], b[kAtOnce];
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                id[k] = p[k] = b[k] = -1;
-                const int64_t r = r0 + (int64_t)k * step;
-                if (r >= live) continue;
+        // rows: the last b with row0[b] <= r, over the copy in shared memory; many rows are left
+        // to kv_rows_kernel
+        const int live = ok ? row0[n] : 0;
+        for (int64_t r0 = (int64_t)rank * kThreads + tid; s.rows_here && r0 < s.n_rows; r0 += (int64_t)ranks * kThreads) {
+            const int r = (int)r0;
+            int64_t place = -1;
+            int p = -1, b = -1;
+            if (r < live) {
                 int lo = 0, width = n;                // the answer is in [lo, lo + width)
                 while (width > 1) {
                     const int half = width >> 1;
-                    if (row0[lo + half] <= (int)r) lo += half, width -= half;
+                    if (row0[lo + half] <= r) lo += half, width -= half;
                     else width = half;
                 }
-                b[k] = lo;
-                p[k] = len[lo] + ((int)r - row0[lo]);
-                const int j = p[k] >> t.shift;
-                id[k] = j < have[lo] ? t.table[(int64_t)slot[lo] * t.max_pages + j]
-                                     : t.free_pages[n_free - 1 - (before[lo] + j - have[lo])];
+                b = lo;
+                p = len[b] + (r - row0[b]);
+                const int j = p >> t.shift;
+                const int id = j < have[b] ? t.table[(int64_t)slot[b] * t.max_pages + j]
+                                           : t.free_pages[n_free - 1 - (before[b] + j - have[b])];
+                place = ((int64_t)id << t.shift) + (p & (page - 1));
             }
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const int64_t r = r0 + (int64_t)k * step;
-                if (r >= s.n_rows) continue;
-                if (s.place) s.place[r] = r < live ? ((int64_t)id[k] << t.shift) + (p[k] & (page - 1)) : -1;
-                if (s.pos) s.pos[r] = p[k];
-                if (s.seq) s.seq[r] = b[k];
-            }
+            if (s.place) s.place[r] = place;
+            if (s.pos) s.pos[r] = p;
+            if (s.seq) s.seq[r] = b;
         }
     }
     if (!ok) return;
@@ -200,6 +195,67 @@ kv_tables_kernel(const Tables t, const Step s, int *err) {
             for (int j = have[b] + lane; j < had; j += width)
                 t.free_pages[n_free + moved - 1 - (before[b] + j - have[b])] = own[j];
         }
+    }
+}
+
+// The maps of many rows, four neighbouring ones to a thread, from the tables as they are now: a launch of
+// its own, since a cluster is 8 SMs (240000 rows of five sequences extended and shortened again: in
+// the cluster's own launch 24.5 us, so 11.8).
+template <bool WIDE>
+__global__ void __launch_bounds__(256) kv_rows_kernel(const Tables t, const Step s) {
+    pdl_enter();
+    const int live = s.row0[s.n_seqs];
+    const int64_t first = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+    if (first >= s.n_rows) return;
+    int b = 0, from = 0, to = 0, len = 0, slot = 0, page_at = -1, page = 0;
+    int64_t place[4];
+    int pos[4], seq[4];
+    if (first < live) {
+        int width = s.n_seqs;                         // the answer is in [b, b + width)
+        while (width > 1) {
+            const int half = width >> 1;
+            if (s.row0[b + half] <= first) b += half, width -= half;
+            else width = half;
+        }
+    }
+    auto load = [&]() {
+        from = s.row0[b];
+        to = s.row0[b + 1];
+        len = s.len[b];
+        slot = s.slots ? s.slots[b] : b;
+        page_at = -1;
+    };
+    if (first < live) load();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t r = first + k;
+        place[k] = pos[k] = seq[k] = -1;
+        if (r >= live) continue;
+        while (r >= to) {                             // row0 ends above every live row
+            ++b;
+            load();
+        }
+        seq[k] = b;
+        pos[k] = len - to + (int)r;
+        const int j = pos[k] >> t.shift;
+        if (j != page_at) page = t.table[(int64_t)slot * t.max_pages + (page_at = j)];
+        place[k] = ((int64_t)page << t.shift) + (pos[k] & ((1 << t.shift) - 1));
+    }
+    if (WIDE && first + 3 < s.n_rows) {
+        if (s.place) {
+            reinterpret_cast<longlong2 *>(s.place + first)[0] = make_longlong2(place[0], place[1]);
+            reinterpret_cast<longlong2 *>(s.place + first)[1] = make_longlong2(place[2], place[3]);
+        }
+        if (s.pos) *reinterpret_cast<int4 *>(s.pos + first) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        if (s.seq) *reinterpret_cast<int4 *>(s.seq + first) = make_int4(seq[0], seq[1], seq[2], seq[3]);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (first + k >= s.n_rows) continue;
+        if (s.place) s.place[first + k] = place[k];
+        if (s.pos) s.pos[first + k] = pos[k];
+        if (s.seq) s.seq[first + k] = seq[k];
     }
 }
 
@@ -234,7 +290,7 @@ Tables tables(const echo_kv_tables &t) {
 template <bool EXTEND>
 echo_status launch(const echo_kv_tables &t, const Step &s, cudaStream_t st) {
     // an entry or four a thread; 8 CTAs: the largest cluster that every GPU has
-    const int64_t entries = (int64_t)s.n_rows + (int64_t)s.n_seqs * t.max_pages;
+    const int64_t entries = (s.rows_here ? (int64_t)s.n_rows : 0) + (int64_t)s.n_seqs * t.max_pages;
     unsigned ranks = 1;
     while (ranks < 8 && ranks * 4 * (int64_t)kThreads < entries) ranks *= 2;
     const size_t smem = 4 * (5 * (size_t)s.n_seqs + 1 + ((size_t)t.n_slots + 31) / 32);
@@ -279,8 +335,16 @@ extern "C" echo_status echo_kv_extend(const echo_kv_tables *t, const int32_t *sl
         if (!aligned4(p)) return ECHO_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(place) & 7u) return ECHO_ERR_INVALID_ARG;
     if (!echo::device_supported()) return ECHO_ERR_UNSUPPORTED;
-    return launch<true>(*t, {slots, rows, table, len, row0, pos, seq, place, n_seqs, n_rows},
-                        reinterpret_cast<cudaStream_t>(stream));
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const bool maps = place || pos || seq, apart = maps && n_rows > kRowsHere && n_seqs > 0;
+    const Step s = {slots, rows, table, len, row0, pos, seq, place, n_seqs, n_rows, maps && !apart};
+    const echo_status done = launch<true>(*t, s, st);
+    if (done != ECHO_OK || !apart) return done;
+    const int grid = (int)(((int64_t)n_rows + 1023) / 1024);
+    const bool wide = echo::aligned16(place) && echo::aligned16(pos) && echo::aligned16(seq);
+    echo::LaunchScope ls(ECHO_K_KV_TABLES, n_rows, n_seqs, 0, st);
+    echo::launch_chained(wide ? kv_rows_kernel<true> : kv_rows_kernel<false>, dim3(grid), dim3(256), 0, st, tables(*t), s);
+    return echo::last_launch_status();
 }
 
 extern "C" echo_status echo_kv_shorten(const echo_kv_tables *t, const int32_t *slots, const int32_t *rows,
@@ -291,6 +355,6 @@ extern "C" echo_status echo_kv_shorten(const echo_kv_tables *t, const int32_t *s
     if (n_seqs == 0) return ECHO_OK;
     if (!rows || !aligned4(rows) || !aligned4(slots)) return ECHO_ERR_INVALID_ARG;
     if (!echo::device_supported()) return ECHO_ERR_UNSUPPORTED;
-    return launch<false>(*t, {slots, rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, n_seqs, 0},
+    return launch<false>(*t, {slots, rows, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, n_seqs, 0, false},
                          reinterpret_cast<cudaStream_t>(stream));
 }

@@ -123,6 +123,32 @@ def test_many_sequences(ec):
     assert ec.echo_get_device_error() == 0
 
 
+@pytest.mark.parametrize("rows,pad", [([9000], 1), ([8190, 0, 0, 1, 2], 2), ([3] * 3000, 6), ([0, 0, 20011, 0], 0)])
+def test_many_rows(ec, rows, pad):
+    """Row maps of a launch of their own; refused calls; maps that are not wanted, or lie anywhere."""
+    import ctypes
+    import torch
+    B, n = len(rows), sum(rows)
+    t, o = pair(ec, n // 16 + 2 * B + 5, 16, B + 2, n // 16 + 3, seed=3)
+    slots = [int(s) for s in np.random.default_rng(4).permutation(B + 2)[:B]]
+    extend(ec, t, o, slots, rows, n + pad)
+    extend(ec, t, o, None, [min(r, 1) for r in rows], n + pad)
+    step = ec.KVStep.empty(t, B, n + pad)
+    ec.echo_kv_extend(t, i32([n + pad + 1] + [0] * (B - 1)), step, i32(slots))
+    assert ec.echo_get_device_error() == 8 and bool((step.place == -1).all()) and bool((step.seq == -1).all())
+    same_tables(t, o)
+    # four bytes further on, and without places and sequences
+    wide = torch.full((n + pad + 9,), -9, dtype=torch.int32, device="cuda")
+    few = [min(r, 2) for r in rows]
+    lens, row0 = i32([0] * B), i32([0] * (B + 1))
+    assert ec.lib().echo_kv_extend(ctypes.byref(t.cstruct), i32(slots).data_ptr(), i32(few).data_ptr(), B, n + pad, None,
+                                   lens.data_ptr(), row0.data_ptr(), None, wide.data_ptr() + 4, None,
+                                   torch.cuda.current_stream().cuda_stream) == 0
+    _, _, maps = o.extend(slots, few, n + pad)
+    assert wide.tolist() == [-9] + [m[1] for m in maps] + [-9] * 8
+    same_tables(t, o)
+
+
 def test_tokens_past_31_bits_in_all(ec):
     """Shortening sequences whose lengths sum to more than 2^31 (their tables are only read
     where pages are given back)."""
