@@ -467,6 +467,66 @@ class PageTable:
                           flat[B * width + B:], row0[-1], max(rows.values(), default=0))
 
 
+class DevicePageTable:
+    """PageTable with the pages' numbers on the GPU (ec.KVTables): the host keeps how many pages each
+    clip has, the device which.  extend() enqueues a step's tables, places and positions and copies
+    two numbers a clip; with those in device memory already, echo_kv_extend itself copies nothing and
+    can be captured."""
+
+    def __init__(self, n_pages: int, page_tokens: int, max_clips: int, device="cuda"):
+        self.n_pages, self.page_tokens, self.device = n_pages, page_tokens, torch.device(device)
+        self.tables = ec.KVTables.empty(n_pages, page_tokens, max_clips, n_pages, device)
+        self.free_slots = list(range(max_clips - 1, -1, -1))
+        self.slots: dict[int, int] = {}
+        self.lens: dict[int, int] = {}
+        self.n_free = n_pages
+
+    def _pages(self, tokens: int) -> int:
+        return -(-tokens // self.page_tokens)
+
+    def _numbers(self, rows: dict[int, int]):
+        """(slots, rows) of the clips on the device, from one copy."""
+        host = torch.tensor([[self.slots[c] for c in rows], list(rows.values())], dtype=torch.int32)
+        both = host.pin_memory().to(self.device, non_blocking=True)
+        return both[0], both[1]
+
+    def open(self, clip: int):
+        if clip in self.slots:
+            raise ValueError(f"clip {clip} is open already")
+        if not self.free_slots:
+            raise MemoryError("every slot is taken")
+        self.slots[clip], self.lens[clip] = self.free_slots.pop(), 0
+
+    def close(self, clip: int):
+        """Give the clip's pages back; as for PageTable, to whoever comes next on this stream."""
+        self.shorten({clip: self.lens[clip]})
+        self.free_slots.append(self.slots.pop(clip))
+        del self.lens[clip]
+
+    def extend(self, rows: dict[int, int]) -> ec.KVStep:
+        """Room for rows[clip] more tokens of each clip, all of them or none, and the step that
+        they make, its rows in the dict's order."""
+        need = sum(self._pages(self.lens[c] + n) - self._pages(self.lens[c]) for c, n in rows.items())
+        if need > self.n_free:
+            raise MemoryError(f"{need} pages needed, {self.n_free} free")
+        slots, n = self._numbers(rows)
+        step = ec.KVStep.empty(self.tables, len(rows), sum(rows.values()), max(rows.values(), default=0))
+        ec.echo_kv_extend(self.tables, n, step, slots)
+        self.n_free -= need
+        for c, k in rows.items():
+            self.lens[c] += k
+        return step
+
+    def shorten(self, rows: dict[int, int]):
+        """Take back the last rows[clip] tokens of each clip, and the pages that only they
+        needed."""
+        slots, n = self._numbers(rows)
+        ec.echo_kv_shorten(self.tables, n, slots)
+        for c, k in rows.items():
+            self.n_free += self._pages(self.lens[c]) - self._pages(self.lens[c] - k)
+            self.lens[c] -= k
+
+
 class ChunkStream:
     """Blocks run chunk by chunk over several clips at once, each clip's earlier keys and
     values in pages of one pool per layer.
@@ -481,16 +541,30 @@ class ChunkStream:
     cross-attention reads it from there.  The block is that of echo_block_step on these rows:
       h1 = x + MHA(LN(x)) Wo + bo,  h2 = h1 + MHA(LN(h1) Wqc; audio) Woc + boc,
       y = h2 + GELU(LN(h2) W1 + b1) W2 + b2.
-    kind: ec.CACHE_BF16 or ec.CACHE_INT8 pages."""
+    kind: ec.CACHE_BF16, ec.CACHE_INT8 or ec.CACHE_INT4 pages.
+
+    device_tables: the page tables are kept on the GPU, for up to max_clips clips at a time.  With
+    them, rotary turns each token's queries and keys by its number in the clip before the
+    self-attention, and step() takes modulations: mods[clip], f32 or bf16 [layers, 6, D], the
+    shift, scale and gate of the self-attention and of the FFN,
+      h1 = x + gate_a * (MHA(LN(x) (1 + scale_a) + shift_a) Wo + bo),  h2 as above,
+      y = h2 + gate_f * (GELU((LN(h2) (1 + scale_f) + shift_f) W1 + b1) W2 + b2)."""
 
     def __init__(self, blocks: list, H: int, d: int, frame_tokens: int, n_pages: int,
-                 cond_pages: int, page_tokens: int = 64, kind: int = ec.CACHE_INT8, device="cuda"):
+                 cond_pages: int, page_tokens: int = 64, kind: int = ec.CACHE_INT8, device="cuda",
+                 device_tables: bool = False, max_clips: int = 64, rotary: ec.Rotary | None = None):
+        if rotary is not None and (not device_tables or rotary.columns != 1 or rotary.d != d):
+            raise ValueError("rotary needs device_tables, heads of this size and one position a token")
         self.blocks, self.H, self.d, self.frame_tokens = blocks, H, d, frame_tokens
         self.device = torch.device(device)
         pool = lambda n: [ec.KVPool.empty(kind, n, page_tokens, H, d, device) for _ in blocks]
         self.self_pools, self.cond_pools = pool(n_pages), pool(cond_pages)
-        self.self_table = PageTable(n_pages, page_tokens)
-        self.cond_table = PageTable(cond_pages, page_tokens)
+        self.device_tables, self.rotary = device_tables, rotary
+        table = lambda n: (DevicePageTable(n, page_tokens, max_clips, device) if device_tables   # noqa: E731
+                           else PageTable(n, page_tokens))
+        self.self_table, self.cond_table = table(n_pages), table(cond_pages)
+        if device_tables:
+            self.norm = ec.GatedNorm(H * d)
 
     def open(self, clip: int, cond_kv: list):
         """A new clip with its audio condition: per layer the keys and values bf16 [Lc, 2 D]
@@ -503,10 +577,15 @@ class ChunkStream:
             raise ValueError(f"every layer's keys and values must be [{Lc}, {2 * D}]")
         self.cond_table.open(clip)
         try:
-            self.cond_table.extend({clip: Lc})
-            batch = self.cond_table.batch({clip: Lc}, self.device)
-            for pool, kv in zip(self.cond_pools, cond_kv):
-                ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
+            if self.device_tables:
+                place = self.cond_table.extend({clip: Lc}).place
+                for pool, kv in zip(self.cond_pools, cond_kv):
+                    ec.echo_kv_write_at(pool, place, kv[:, :D], kv[:, D:])
+            else:
+                self.cond_table.extend({clip: Lc})
+                batch = self.cond_table.batch({clip: Lc}, self.device)
+                for pool, kv in zip(self.cond_pools, cond_kv):
+                    ec.echo_kv_write(pool, batch, kv[:, :D], kv[:, D:])
             self.self_table.open(clip)
         except BaseException:
             self.cond_table.close(clip)
@@ -516,7 +595,8 @@ class ChunkStream:
         self.self_table.close(clip)
         self.cond_table.close(clip)
 
-    def step(self, chunks: dict[int, torch.Tensor]) -> dict[int, torch.Tensor]:
+    def step(self, chunks: dict[int, torch.Tensor],
+             mods: dict[int, torch.Tensor] | None = None) -> dict[int, torch.Tensor]:
         """chunks: bf16 [n, D] per clip; returns bf16 [n, D] per clip.  After an exception the
         clips are as they were before the call."""
         rows = {c: x.shape[0] for c, x in chunks.items()}
@@ -528,9 +608,23 @@ class ChunkStream:
                 raise ValueError(f"a chunk must be [n, {D}] on {self.device.type}")
             if x.dtype not in (torch.bfloat16, torch.float32):
                 raise TypeError(f"unsupported dtype {x.dtype}")
+        if mods is not None:
+            if not self.device_tables:
+                raise ValueError("modulations need device_tables")
+            shape = (len(self.blocks), 6, D)
+            if set(mods) != set(rows) or any(tuple(m.shape) != shape for m in mods.values()):
+                raise ValueError(f"modulations are one tensor {list(shape)} per clip of the step")
         if not sum(rows.values()):
             return {c: x.to(torch.bfloat16) for c, x in chunks.items()}
         x = torch.cat(list(chunks.values())) if len(chunks) > 1 else next(iter(chunks.values())).contiguous()
+        if self.device_tables:
+            step = self.self_table.extend(rows)
+            try:
+                x = self._layers(x, rows, step, None if mods is None else torch.stack([mods[c] for c in rows]))
+            except BaseException:
+                self.self_table.shorten(rows)
+                raise
+            return dict(zip(rows, x.split(list(rows.values()))))
         self.self_table.extend(rows)
         try:
             batch = self.self_table.batch(rows, self.device)
@@ -552,3 +646,36 @@ class ChunkStream:
             self.self_table.shorten(rows)
             raise
         return dict(zip(rows, x.split(list(rows.values()))))
+
+    def _layers(self, x, rows, step: ec.KVStep, mods):
+        """The blocks over a step's rows; mods [clips, layers, 6, D] or none."""
+        D, last = self.H * self.d, len(self.blocks) - 1
+        # the same rows over the audio's pages: no more tokens, and these rows' numbers
+        audio = self.cond_table.extend({c: 0 for c in rows}).batch
+        cond = ec.KVBatch(audio.table, audio.lens, step.batch.row0, step.n_rows, step.batch.max_rows)
+
+        def norm(x, y, out=torch.float32, gate=None, scale=None, shift=None, want_h=True, want_n=True):
+            """(h, n) with (layer, row of its modulations) for gate, scale and shift."""
+            part = lambda i: None if mods is None or i is None else mods[:, i[0], i[1]]   # noqa: E731
+            g, s, t = part(gate), part(scale), part(shift)
+            h = torch.empty(x.shape, dtype=out, device=x.device) if want_h else None
+            return ec.echo_gated_norm(self.norm, x, y, g, s, t, h=h, want_h=want_h, want_n=want_n,
+                                      mod_rows=None if g is None and s is None else step.seq)
+
+        n1 = norm(x, None, scale=(0, 1), shift=(0, 0), want_h=False)[1] if self.blocks else None
+        for l, (blk, pool, cond_pool) in enumerate(zip(self.blocks, self.self_pools, self.cond_pools)):
+            w = blk.tensors
+            kv = ec.echo_linear(n1, w["Wkv"], w["bkv"])
+            q, k = ec.echo_linear(n1, w["Wq"], w["bq"]), kv[:, :D]
+            if self.rotary is not None:
+                ec.echo_rotary(self.rotary, step.pos, q, k, q_out=q, k_out=k)
+            ec.echo_kv_write_at(pool, step.place, k, kv[:, D:])
+            a = ec.echo_kv_attention(pool, step.batch, q, causal_block=self.frame_tokens)
+            h1, nq = norm(x, ec.echo_linear(a, w["Wo"], w["bo"]), gate=(l, 2))
+            a = ec.echo_kv_attention(cond_pool, cond, ec.echo_linear(nq, w["Wqc"], w["bqc"]))
+            h2, nf = norm(h1, ec.echo_linear(a, w["Woc"], w["boc"]), scale=(l, 4), shift=(l, 3))
+            y = ec.echo_linear(ec.echo_linear(nf, w["W1"], w["b1"], act=1), w["W2"], w["b2"])
+            after = (l + 1, 1) if l < last else None           # of the next block's first norm
+            x, n1 = norm(h2, y, torch.bfloat16, gate=(l, 5), scale=after,
+                         shift=None if after is None else (l + 1, 0), want_n=l < last)
+        return x
