@@ -506,6 +506,8 @@ class DevicePageTable:
     def extend(self, rows: dict[int, int]) -> ec.KVStep:
         """Room for rows[clip] more tokens of each clip, all of them or none, and the step that
         they make, its rows in the dict's order."""
+        if min(rows.values(), default=0) < 0:
+            raise ValueError("a clip's rows cannot be negative")
         need = sum(self._pages(self.lens[c] + n) - self._pages(self.lens[c]) for c, n in rows.items())
         if need > self.n_free:
             raise MemoryError(f"{need} pages needed, {self.n_free} free")
@@ -518,11 +520,14 @@ class DevicePageTable:
         return step
 
     def shorten(self, rows: dict[int, int]):
-        """Take back the last rows[clip] tokens of each clip, and the pages that only they
-        needed."""
+        """Take back the last rows[clip] tokens of each clip, all where it has fewer, and the pages
+        that only they needed."""
+        if min(rows.values(), default=0) < 0:
+            raise ValueError("a clip's rows cannot be negative")
         slots, n = self._numbers(rows)
         ec.echo_kv_shorten(self.tables, n, slots)
         for c, k in rows.items():
+            k = min(k, self.lens[c])
             self.n_free += self._pages(self.lens[c]) - self._pages(self.lens[c] - k)
             self.lens[c] -= k
 

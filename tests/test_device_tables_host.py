@@ -80,6 +80,20 @@ def test_counts_of_pages_and_slots(calls):
     assert t.slots["c"] == 0 and calls.names.count("echo_kv_shorten") == 2
 
 
+def test_counts_that_the_tables_would_not_follow(calls):
+    """More than a clip has: all of it, as on the device; negative numbers are refused before any call."""
+    t = pipeline.DevicePageTable(10, 16, 2, "cpu")
+    t.open("a")
+    t.extend({"a": 40})
+    made = len(calls.names)
+    for f in (t.extend, t.shorten):
+        with pytest.raises(ValueError):
+            f({"a": -1})
+    assert len(calls.names) == made and t.lens == {"a": 40} and t.n_free == 7
+    t.shorten({"a": 41})
+    assert t.lens == {"a": 0} and t.n_free == 10
+
+
 def stream(**kw):
     return pipeline.ChunkStream([Block(), Block()], H, D // H, 4, n_pages=6, cond_pages=3, page_tokens=16, device="cpu",
                                 device_tables=True, **kw)
