@@ -1,11 +1,11 @@
 // The end of one branch of a block and the beginning of the next, row by row: the branch's
 // output normed, gated and added to the residual stream, the result normed and modulated,
 //   h = alpha x + beta gate * N_after(y),   n = N_before(h) * (1 + scale) + shift.
-// One pass: a row's x and y are read once into registers, h and n written once, and the time is
-// that of those bytes.  Sums are fp32 trees over the row's threads, a mean first and then the
-// centred squares.  A thread block takes neighbouring rows, which mostly share their modulation,
-// so that gate, scale and shift (for fp32 as many bytes as a row's x, y, h and n, and half as many again)
-// come from the L1; the rows themselves pass it by.
+// One pass: a row's x and y are read once, h and n written once, and the time of many rows is
+// that of those bytes (32760 bf16 rows of 5120: 1.34 GB in 211 us, 0.94 of a copy's rate), of few rows
+// that of one access after the other.  Sums are fp32 trees over the row's threads, a mean first and then
+// the centred squares.  gate, scale and shift (for fp32 as many bytes as a row's x, y, h and n, and half
+// as many again) are read again only where the modulation changes.
 #include <type_traits>
 
 #include "common.cuh"
@@ -402,9 +402,9 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
     // the modulation's row, for the lanes of a batch's rows; -1: the row is left as it is
     const int lane = t & 31;
     auto mod_of = [&](int i) {
-        const int r = first + i * R + lane;
+        const int r0 = first + i * R, r = r0 + lane;
         int m = 0;
-        if (lane >= R || r >= last) return -1;
+        if (lane >= min(R, last - r0)) return -1;
         if (p.n_mods >= 0) {
             m = p.mod_rows ? p.mod_rows[r] : r / p.rows_per_mod;
             if ((unsigned)m >= (unsigned)p.n_mods) m = -1;
