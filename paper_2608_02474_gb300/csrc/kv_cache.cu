@@ -153,7 +153,7 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ 
 // above no other that the quotient is below; with 1 / s a little too large, the halves between two codes,
 // and nothing else, pass over to the larger one.  (bf16 has 8 bits: other quotients are 2^-9 of
 // themselves away.)  With divisions, and codes put together one by one, 32760 rows of 40 heads of 128 took
-// 205 us, now WRITE4.
+// 205 us, now 160.
 ECHO_DEV uint32_t max_abs2(uint32_t a, uint32_t b) {      // of pairs without signs; NaN where there is one
     uint32_t r;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));

@@ -24,6 +24,10 @@
 // sees such a key becomes NaN.  For int8 pages only a scale can be non-finite: it then
 // spoils the key's score, and stands as 0 among the values' scales; for 4-bit pages it makes
 // the key NaN, and its values 0.
+// 4 bits: 1560 rows over 31200 keys, 40 heads of 128, 706 to 733 us (bf16 638, int8 860).  The converting
+// warps' stores into shared memory and the softmax's instructions take turns with those that bound bf16; V_f and
+// K_{f+1} converted together, so that twice as many loads are under way, took 785, and scales folded into the
+// conversion 705.
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
 #include <cfloat>
 #include <type_traits>

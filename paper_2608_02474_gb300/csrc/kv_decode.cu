@@ -19,6 +19,16 @@
 // scores, the values' scales the weights.  ldmatrix hands out 16-bit units, so a lane gets
 // neighbouring pairs of codes: Q's columns are taken in the same order, and O's columns
 // come out in it.
+//
+// 4-bit codes become code / 64 in bf16 (kv_nibbles2), and a code times its group's scale is exact
+// in bf16 too, so that keys and values can be multiplied out in registers; for 8 packed rows the
+// scores of a group stand apart and take the keys' scale in fp32, with fewer multiplications.
+// With a quarter of bf16's bytes it is the instructions beside the products that
+// bound it, so: a stage of the ring belongs to one group of warps, whose other group neither waits for it nor frees
+// it; the queries of the next piece are fetched while this one's sums are joined; and the warps join behind one
+// barrier, all of O in shared memory.  48 tokens over up to 8190 keys each, 32/8 heads of 128: 72.9 us (80
+// before the three; int8 89.5), 282 MB at 5.2 TB/s beside some 19 us that do not grow with the
+// keys: launch, finding the work (2.8), the first copies, the ends of pieces, workers that end unevenly.
 #include <cfloat>
 
 #include "kv_schedule.cuh"
@@ -830,6 +840,8 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
 //          32760 tokens, 40 heads: 32 in 16s 190, 133)
 //          int8 8 rows 56, 16 60, 24 in 16s 89, 32 90 (128), 48 131 (129); three CTAs of an
 //          SM, with two thirds of the registers, are slower: d 64 int8 24 rows 60
+// 4 bits like int8: d 64 8 rows 29, 17 in 24s 33, 32 41, 48 in 24s 54, 64 in 32s 69; d 128 16 rows 42, 24 in
+// 16s 69, 32 70, 48 (80).
 int tile_rows(bool codes, int d, int64_t rows) {
     if (d == 128) return rows <= 8 ? 8 : rows <= (codes ? 32 : 16) ? 16 : 0;
     if (rows <= 32) return (int)(rows + 7) / 8 * 8 + (rows == 0 ? 8 : 0);

@@ -8,6 +8,9 @@
     python -m paper_2608_02474_gb300.kernel_bench --kernel block --T 21 --N 1560 --D 5120 --K 6552
     python -m paper_2608_02474_gb300.kernel_bench --kernel kv_attention --M 1560 --L 32760 --H 40 --d 128
     python -m paper_2608_02474_gb300.kernel_bench --kernel kv_attention --M 1 --L 8190 --seqs 48 --H 8 --group 4 --int8
+    python -m paper_2608_02474_gb300.kernel_bench --kernel kv_extend --M 1560 --L 62400 --seqs 5 --page 128
+    python -m paper_2608_02474_gb300.kernel_bench --kernel rotary --T 21 --N 1560 --H 40 --d 128
+    python -m paper_2608_02474_gb300.kernel_bench --kernel gated_norm --T 21 --N 1560 --D 5120
 
 Inputs are seeded random device tensors of the right shapes (values do not
 change the work of these kernels).  Prints the mean time per launch over
@@ -29,7 +32,7 @@ def make_parser() -> argparse.ArgumentParser:
     ap.add_argument("--kernel", required=True,
                     choices=["gemm", "attention", "drift", "select", "merge", "quant", "layernorm",
                              "energy", "step_delta", "ref_write", "block", "kv_write", "kv_read",
-                             "kv_attention"])
+                             "kv_attention", "kv_extend", "rotary", "gated_norm"])
     ap.add_argument("--M", type=int, default=6552)
     ap.add_argument("--N", type=int, default=5120)
     ap.add_argument("--K", type=int, default=5120)
@@ -40,7 +43,7 @@ def make_parser() -> argparse.ArgumentParser:
     ap.add_argument("--D", type=int, default=5120)
     ap.add_argument("--act", type=int, default=0)
     ap.add_argument("--rows", type=int, default=0, help="layernorm: gather this many rows")
-    ap.add_argument("--f32", action="store_true", help="layernorm: fp32 input")
+    ap.add_argument("--f32", action="store_true", help="layernorm, rotary, gated_norm: fp32 input")
     ap.add_argument("--samples", type=int, default=80960, help="energy: audio samples")
     ap.add_argument("--F", type=int, default=13824, help="block: FFN width")
     ap.add_argument("--Lc", type=int, default=672, help="block: audio condition tokens")
@@ -48,6 +51,10 @@ def make_parser() -> argparse.ArgumentParser:
     ap.add_argument("--group", type=int, default=1, help="kv_attention: query heads of a key/value head")
     ap.add_argument("--page", type=int, default=64, help="kv_*: tokens of a page")
     ap.add_argument("--int8", action="store_true", help="kv_*: int8 pages")
+    ap.add_argument("--int4", action="store_true", help="kv_*: 4-bit pages")
+    ap.add_argument("--halves", action="store_true", help="rotary: pairs of columns half a head apart")
+    ap.add_argument("--rms", action="store_true", help="gated_norm: the root of the mean square, not layer norm")
+    ap.add_argument("--after", action="store_true", help="gated_norm: the branch's output normed, too")
     ap.add_argument("--cb", type=int, default=0, help="kv_attention: causal_block")
     ap.add_argument("--iters", type=int, default=3)
     ap.add_argument("--warmup", type=int, default=1)
@@ -135,18 +142,57 @@ def main():
         ws = torch.empty(cache.write_workspace_size(a.K), dtype=torch.uint8, device=dev)
         run = lambda: cache.write(src, rows, workspace=ws)
         work, unit = a.K * (3.0 * D + 8), "GB/s"
+    elif a.kernel == "kv_extend":
+        # M more tokens of every sequence of L, and given back
+        per = -(-(a.L + a.M) // a.page)
+        tables = ec.KVTables.empty(per * a.seqs, a.page, a.seqs, per)
+        count = lambda n: torch.full((a.seqs,), n, dtype=torch.int32, device=dev)   # noqa: E731
+        ec.echo_kv_extend(tables, count(a.L), ec.KVStep.empty(tables, a.seqs, a.seqs * a.L))
+        step, more = ec.KVStep.empty(tables, a.seqs, a.seqs * a.M, a.M), count(a.M)
+
+        def run():
+            ec.echo_kv_extend(tables, more, step)
+            ec.echo_kv_shorten(tables, more)
+        work, unit = 16.0 * a.seqs * a.M + 8.0 * a.seqs * per, "GB/s"
+    elif a.kernel == "rotary":
+        # queries and keys of T frames of N tokens, by frame, row and column, in place
+        NT, t = a.T * a.N, torch.float32 if a.f32 else torch.bfloat16
+        side = next(n for n in range(int(a.N ** 0.5), 0, -1) if a.N % n == 0)
+        third = a.d // 2 // 3
+        plan = ec.Rotary(a.d, (a.d // 2 - 2 * third, third, third), "halves" if a.halves else "pairs",
+                         frame=(a.N, a.N // side))
+        q, k = rn(NT, a.H * a.d).to(t), rn(NT, a.H * a.d).to(t)
+        pos = torch.arange(NT, dtype=torch.int32, device=dev)
+        run = lambda: ec.echo_rotary(plan, pos, q, k, q_out=q, k_out=k)
+        work, unit = 4.0 * q.nbytes, "GB/s"
+    elif a.kernel == "gated_norm":
+        # the residual in fp32 or bf16, one modulation to a frame
+        NT, t = a.T * a.N, torch.float32 if a.f32 else torch.bfloat16
+        plan = ec.GatedNorm(a.D, "rms" if a.rms else "layer", after="rms" if a.after else "none")
+        x, y, m = rn(NT, a.D).to(t), rn(NT, a.D).to(torch.bfloat16), rn(3, a.T, a.D)
+        h, n = torch.empty_like(x), torch.empty_like(y)
+        run = lambda: ec.echo_gated_norm(plan, x, y, m[0], m[1], m[2], rows_per_mod=a.N, h=h, n=n)
+        work, unit = 2.0 * (x.nbytes + y.nbytes), "GB/s"
     elif a.kernel.startswith("kv_"):
         # a batch whose M rows of every sequence are its L tokens' last, pages in random order
         per, n = -(-a.L // a.page), a.seqs * a.M
-        pool = ec.KVPool.empty(ec.CACHE_INT8 if a.int8 else ec.CACHE_BF16, per * a.seqs, a.page, a.H, a.d)
+        kind = ec.CACHE_INT4 if a.int4 else ec.CACHE_INT8 if a.int8 else ec.CACHE_BF16
+        pool = ec.KVPool.empty(kind, per * a.seqs, a.page, a.H, a.d)
         for page in pool.pages:
-            page.copy_(torch.randint(-127, 128, page.shape, generator=g, device=dev) if a.int8 else rn(*page.shape))
-        if a.int8:
+            if a.int4:                                             # codes -7 to 7, plus 8, two to a byte
+                page.copy_(torch.randint(1, 16, page.shape, generator=g, device=dev)
+                           + 16 * torch.randint(1, 16, page.shape, generator=g, device=dev))
+            else:
+                page.copy_(torch.randint(-127, 128, page.shape, generator=g, device=dev) if a.int8 else rn(*page.shape))
+        if a.int4:
+            pool.scale.copy_(torch.randint(16, 32, pool.scale.shape, generator=g, device=dev) / 128)
+        elif a.int8:
             pool.scale.copy_(torch.rand(pool.scale.shape, generator=g, device=dev) / 64)
         batch = ec.KVBatch(torch.randperm(per * a.seqs, generator=g, device=dev).to(torch.int32).view(a.seqs, per),
                            torch.full((a.seqs,), a.L, dtype=torch.int32, device=dev),
                            torch.arange(0, n + 1, a.M, dtype=torch.int32, device=dev), n, a.M)
-        token = 2.0 * a.H * (a.d + 4 if a.int8 else 2 * a.d)       # bytes of a token in the pages
+        # bytes of a token in the pages
+        token = 2.0 * a.H * (a.d / 2 + a.d / 16 if a.int4 else a.d + 4 if a.int8 else 2 * a.d)
         if a.kernel == "kv_attention":
             q = rn(n, a.H * a.group * a.d).to(torch.bfloat16)
             out = torch.empty_like(q)

@@ -261,6 +261,12 @@ def test_scales_far_from_one(ec, d, amplitude):
         check(ec, c, 2, 1)
 
 
+def batch_of_all(ec, batch, n):
+    """The one sequence of the batch, all of its n tokens as rows."""
+    import torch
+    return ec.KVBatch(batch.table, batch.lens, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n)
+
+
 @HEADS
 @pytest.mark.parametrize("rows", [1, 60])
 @pytest.mark.parametrize("kv", [0, 1])
@@ -284,6 +290,40 @@ def test_scales_that_are_not_finite(ec, d, rows, kv, value):
             else:
                 close(got[r], want[r], mass[r])
         assert ec.echo_get_device_error() == 0
+
+
+@HEADS
+@pytest.mark.parametrize("rows", [1, 60])
+@pytest.mark.parametrize("kv", [0, 1])
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+def test_values_that_are_not_finite(ec, d, rows, kv, value):
+    """As echo_kv_write leaves them (codes 0 under a scale that is not finite): the rows that see the
+    key are not finite in the group's columns of this head.  The other head keeps its bits.  Rows that do
+    not see the key may be rounded about another maximum, since a weight that is not finite moves those of all
+    of a tile's rows: both results are within TOL * mass of the exact one, and so within 2 TOL * mass of each other."""
+    n = 300
+    base = int4_case.make(32, 2, d, [n], [rows], seed=9)
+    q = bf(kv_case.queries(rows, 2 * d, 10, 1.5))
+    pool, batch = base.device(ec)
+    every = batch_of_all(ec, batch, n)
+    kept = ec.echo_kv_read(pool, every)
+    ec.echo_kv_write(pool, every, *kept)               # their scales may be smaller now
+    want = host(ec.echo_kv_attention(pool, batch, q, causal_block=1))
+    mass = P.attend(I.values(host(pool.pages), host(pool.scale)), None, base.table, base.lens, base.row0, host(q),
+                    2, 1)[1]
+    for p in (3, n - 1, n - rows):
+        k, v = kept[0].clone(), kept[1].clone()
+        (k, v)[kv][p, d + 32] = float(value)
+        ec.echo_kv_write(pool, every, k, v)
+        assert ec.echo_get_device_error() == 5
+        got = host(ec.echo_kv_attention(pool, batch, q, causal_block=1))
+        for r in range(rows):
+            if n - rows + r >= p:
+                assert not np.isfinite(got[r, d + 32:d + 64]).any()
+                assert same(got[r, :d], want[r, :d])
+            else:
+                assert same(got[r, :d], want[r, :d])
+                assert (np.abs(got[r, d:] - want[r, d:]) <= 2 * TOL * mass[r, d:] + 1e-30).all()
 
 
 def test_pages_that_are_none(ec):
