@@ -153,10 +153,11 @@ kv_write_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ 
 // above no other that the quotient is below; with 1 / s a little too large, the halves between two codes,
 // and nothing else, pass over to the larger one.  (bf16 has 8 bits: other quotients are 2^-9 of
 // themselves away.)  With divisions, and codes put together one by one, 32760 rows of 40 heads of 128 took
-// 205 us, now 160.
-ECHO_DEV uint32_t max_abs2(uint32_t a, uint32_t b) {      // of pairs without signs; NaN where there is one
+// 205 us, with an address made of the page for every store 160, now 140 (134 by a slot map; 127 at the rate of a
+// copy).
+ECHO_DEV uint32_t max_abs2(uint32_t a, uint32_t b) {      // of pairs, but for the signs; NaN where there is one
     uint32_t r;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 ECHO_DEV float rcp_approx(float x) {                      // to 2^-23
@@ -169,31 +170,37 @@ __global__ void __launch_bounds__(kThreads)
 kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__ place, const T *__restrict__ k,
                  const T *__restrict__ v, int64_t ld, int *err) {
     pdl_enter();
-    constexpr int NG = 8 / kPer16<T>, LPH = D / 8, U = kLoads / NG;
-    const int lane = threadIdx.x & 31;
-    const int half = pool.H * LPH, C = 2 * half;      // pieces of a row
-    const int tasks = (C + 32 * U - 1) / (32 * U);
+    constexpr int NG = 8 / kPer16<T>, U = kLoads / NG;
+    constexpr uint32_t LPH = D / 8;
+    const uint32_t lane = threadIdx.x & 31;
+    const uint32_t half = pool.H * LPH, C = 2 * half;      // pieces of a row
+    const uint32_t tasks = (C + 32 * U - 1) / (32 * U);
+    const uint32_t code_step = (uint32_t)(D / 2) << pool.shift, scale_step = (uint32_t)(D / 32) << pool.shift;   // of a head
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
-        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
+        const int r = (int)walk.row;
+        const uint32_t c0 = (uint32_t)walk.piece * 32 * U + lane;
+        const T *const kr = k + r * ld, *const vr = v + r * ld - (int64_t)half * 8;    // piece c: 8 c from either
         uint4 in[U][NG];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + 32 * u;
+            const uint32_t c = c0 + 32 * u;
 #pragma unroll
             for (int h = 0; h < NG; ++h) {
                 in[u][h] = make_uint4(0u, 0u, 0u, 0u);
-                if (c < C)
-                    in[u][h] = __ldcs(reinterpret_cast<const uint4 *>((c < half ? k : v) + r * ld +
-                                                                      (int64_t)(c < half ? c : c - half) * 8) + h);
+                if (c < C) in[u][h] = __ldcs(reinterpret_cast<const uint4 *>((c < half ? kr : vr) + (uint64_t)c * 8) + h);
             }
         }
         const int64_t at = row_place(pool, b, place, r, err);
         if (at < 0) continue;
-        const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
+        // this token of the page's first head; heads, the values' after the keys', lie a step apart
+        const int64_t vec = ((at >> pool.shift) * 2 * pool.H << pool.shift) + (at & ((1 << pool.shift) - 1));
+        uint8_t *const codes_at = pool.pages + vec * (D / 2);
+        uint16_t *const scales_at = static_cast<uint16_t *>(pool.scale) + vec * (D / 32);
+        bool any = false;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + 32 * u;
+            const uint32_t c = c0 + 32 * u;
             uint4 w = in[u][0];                       // 8 values in bf16
             if constexpr (NG == 2) {
                 float f[8];
@@ -202,10 +209,9 @@ kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__
                 w = pack8_bf16(f);
             }
             const uint32_t pair[4] = {w.x, w.y, w.z, w.w};
-            uint32_t a2 = max_abs2(max_abs2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu),
-                                   max_abs2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
+            uint32_t a2 = max_abs2(max_abs2(w.x, w.y), max_abs2(w.z, w.w));
             a2 = max_abs2(a2, __shfl_xor_sync(0xffffffffu, a2, 1));
-            a2 = max_abs2(a2, __shfl_xor_sync(0xffffffffu, a2, 2));
+            a2 = max_abs2(a2, __shfl_xor_sync(0xffffffffu, a2, 2)) & 0x7FFF7FFFu;
             if (c >= C) continue;
             const uint32_t a = max(a2 << 16, a2 & 0xFFFF0000u);       // fp32 bits; NaN above infinity
             const bool bad = a >= 0x7F800000u;
@@ -220,15 +226,14 @@ kv_write4_kernel(const KvPool pool, const KvBatch b, const int64_t *__restrict__
                 odd = odd * 16u + __float_as_uint(__fmaf_rn(bf16hi(pair[i]), inv, 12582920.f));
             }
             const uint32_t codes = bad ? 0x88888888u : __byte_perm(even, odd, 0x5410);
-            const int kv = c >= half, ch = kv ? c - half : c;
-            const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            *reinterpret_cast<uint32_t *>(pool.pages + vec * (D / 2) + ch % LPH * 4) = codes;
-            if ((lane & 3) == 0) {
-                // the scale's low 16 bits are zeros; what is not finite stands as it is
-                static_cast<uint16_t *>(pool.scale)[vec * (D / 32) + ch % LPH / 4] = (uint16_t)((bad ? a : __float_as_uint(s)) >> 16);
-                if (bad) echo_flag_error(err, ECHO_ERR_NONFINITE);
-            }
+            const uint32_t head = c / LPH, piece = c % LPH;
+            *reinterpret_cast<uint32_t *>(codes_at + (uint64_t)head * code_step + piece * 4) = codes;
+            // the scale's low 16 bits are zeros; what is not finite stands as it is
+            if ((lane & 3) == 0)
+                scales_at[(uint64_t)head * scale_step + piece / 4] = (uint16_t)((bad ? a : __float_as_uint(s)) >> 16);
+            any |= bad;
         }
+        if (any) echo_flag_error(err, ECHO_ERR_NONFINITE);
     }
 }
 
@@ -240,30 +245,35 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
                int *err) {
     pdl_enter();
     constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4;
-    constexpr int EP = kPer16<T>, BYTES = kv_bytes(FORM, EP), LPH = D / EP, U = BYTES == 16 ? kLoads : 2 * kLoads;
+    constexpr int EP = kPer16<T>, BYTES = kv_bytes(FORM, EP), U = BYTES == 16 ? kLoads : 2 * kLoads;
     constexpr int WORDS = (BYTES + 3) / 4;
-    const int lane = threadIdx.x & 31;
-    const int half = pool.H * LPH, C = 2 * half;
-    const int tasks = (C + 32 * U - 1) / (32 * U);
+    constexpr uint32_t LPH = D / EP;
+    const uint32_t lane = threadIdx.x & 31;
+    const uint32_t half = pool.H * LPH, C = 2 * half;
+    const uint32_t head_step = (uint32_t)kv_bytes(FORM, D) << pool.shift;
+    const uint32_t tasks = (C + 32 * U - 1) / (32 * U);
     PieceWalk walk(blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, tasks);
     for (; walk.below(b.n_rows); walk.next()) {
-        const int r = (int)walk.row, c0 = (int)walk.piece * 32 * U + lane;
+        const int r = (int)walk.row;
+        const uint32_t c0 = (uint32_t)walk.piece * 32 * U + lane;
         const KvRow row = kv_find_row(b, r);
         if (row.seq < 0) continue;
         const int64_t at = row.p < 0 ? -1 : kv_place(pool, b, row.seq, row.p, err);   // -1: zeros
-        const int64_t page = at >> pool.shift, slot = at & ((1 << pool.shift) - 1);
+        // this token of the page's first head; heads, the values' after the keys', lie a step apart
+        const int64_t vec0 = ((at >> pool.shift) * 2 * pool.H << pool.shift) + (at & ((1 << pool.shift) - 1));
+        const uint8_t *const from = pool.pages + vec0 * kv_bytes(FORM, D);
+        T *const kr = k + r * ld, *const vr = v + r * ld - (int64_t)half * EP;    // piece c: EP c from either
         uint32_t in[U][WORDS];
         float sc[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + 32 * u;
+            const uint32_t c = c0 + 32 * u;
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) in[u][i] = 0u;
+            for (int i = 0; i < WORDS; ++i) in[u][i] = INT4 ? 0x88888888u : 0u;      // codes 0
             sc[u] = 0.f;
             if (c >= C || at < 0) continue;
-            const int kv = c >= half, ch = kv ? c - half : c;
-            const int64_t vec = (((page * 2 + kv) * pool.H + ch / LPH) << pool.shift) + slot;
-            const uint8_t *src = pool.pages + vec * kv_bytes(FORM, D) + (INT4 ? ch % LPH * EP / 8 * 4 : ch % LPH * BYTES);
+            const uint32_t head = c / LPH, piece = c % LPH;
+            const uint8_t *src = from + (uint64_t)head * head_step + (INT4 ? piece * EP / 8 * 4 : piece * BYTES);
             if constexpr (BYTES == 16) {
                 const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(src));
                 in[u][0] = w.x, in[u][1] = w.y, in[u][2] = w.z, in[u][3] = w.w;
@@ -273,21 +283,22 @@ kv_read_kernel(const KvPool pool, const KvBatch b, T *__restrict__ k, T *__restr
             } else {
                 in[u][0] = __ldcs(reinterpret_cast<const uint32_t *>(src));
             }
-            if constexpr (INT8) sc[u] = static_cast<const float *>(pool.scale)[vec];
+            if constexpr (INT8) sc[u] = (static_cast<const float *>(pool.scale) + vec0)[(uint64_t)head << pool.shift];
             if constexpr (INT4)
-                sc[u] = __uint_as_float((uint32_t)static_cast<const uint16_t *>(pool.scale)[vec * (D / 32) + ch % LPH * EP / 32] << 16);
+                sc[u] = __uint_as_float((uint32_t)(static_cast<const uint16_t *>(pool.scale) + vec0 * (D / 32))
+                                            [(uint64_t)head * ((D / 32u) << pool.shift) + piece * EP / 32] << 16);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = c0 + 32 * u;
+            const uint32_t c = c0 + 32 * u;
             if (c >= C) continue;
-            T *dst = (c >= half ? v : k) + r * ld + (int64_t)(c >= half ? c - half : c) * EP;
+            T *dst = (c >= half ? vr : kr) + (uint64_t)c * EP;
             float f[EP];
             if constexpr (INT4) {
                 // code / 64, times 64, times the scale: exact.  fp32: four of a word's columns a lane
                 const uint32_t s2 = __float_as_uint(sc[u]) | __float_as_uint(sc[u]) >> 16;
                 const uint32_t w0 = EP == 8 ? in[u][0] : in[u][0] >> (8 * (c & 1));
-                auto value2 = [&](uint32_t code) { return at < 0 ? 0u : bf16x2_mul(bf16x2_mul(code, 0x42804280u), s2); };
+                auto value2 = [&](uint32_t code) { return bf16x2_mul(bf16x2_mul(code, 0x42804280u), s2); };
                 const uint4 w = make_uint4(value2(kv_nibbles2<0>(w0)), value2(kv_nibbles2<1>(w0)),
                                            value2(kv_nibbles2<2>(w0)), value2(kv_nibbles2<3>(w0)));
                 if constexpr (sizeof(T) == 2) {
