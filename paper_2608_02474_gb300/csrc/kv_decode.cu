@@ -21,7 +21,7 @@
 // come out in it.
 //
 // 4-bit codes become code / 64 in bf16 (kv_nibbles2), and a code times its group's scale is exact
-// in bf16 too, so that keys and values can be multiplied out in registers; for 8 packed rows the
+// in bf16 too, so that keys and values can be multiplied out in registers; the softmax's scale goes into the exponents' multiply-add; for 8 packed rows the
 // scores of a group stand apart and take the keys' scale in fp32, with fewer multiplications.
 // With a quarter of bf16's bytes it is the instructions beside the products that
 // bound it, so: a stage of the ring belongs to one group of warps, whose other group neither waits for it nor frees
@@ -47,7 +47,9 @@ struct Cfg {
     static constexpr int GROUPS = NR * D <= (CODES ? 64 : 128) || NR == 1 ? 2 : 1;   // of four warps
     static constexpr int WARPS = 4 * GROUPS, THREADS = 32 * (WARPS + 1);
     static constexpr int KPW = LONG ? 64 : CODES ? 32 : 16;   // keys of a warp
-    static constexpr int KG = CODES ? 2 : 1;               // 16 keys of them at once
+    // 16 keys of them at once; twice 16 of codes, but for 32 rows of 4-bit ones, whose registers do not suffice
+    // (8 sequences of 7800 tokens, 16 heads of 64: 43.6 us, so 41.6)
+    static constexpr int KG = CODES && !(FORM == kInt4 && NR == 4) ? 2 : 1;
     static constexpr int BK = 4 * KPW;                     // keys of a block
     static constexpr int BSHIFT = KPW == 64 ? 8 : CODES ? 7 : 6;
     static constexpr int ROW_BYTES = kv_bytes(FORM, D);
@@ -444,7 +446,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                     // spoilt spoils the rows that see it.  This warp's keys alone.
                     uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + lane) * C::TOKEN_SCALES);
 #pragma unroll
-                    for (int i = 0; i < C::TOKEN_SCALES / 4; ++i) {
+                    for (int i = 0; i < (lane < STEP ? C::TOKEN_SCALES / 4 : 0); ++i) {
                         const uint32_t off = kv_not_finite2(at[i]);
                         spoilt |= off;
                         if (off) at[i] &= ~off;
@@ -465,6 +467,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         }
 #pragma unroll
                         for (int nt = 0; nt < NR; ++nt) {
+                            if constexpr (INT4) continue;        // below
                             sc[kg][nt][2 * h] *= f;
                             sc[kg][nt][2 * h + 1] *= f;
                         }
@@ -497,6 +500,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                             for (int kg = 0; kg < KG; ++kg) mx = fmax3(mx, sc[kg][nt][e], sc[kg][nt][2 + e]);
 #pragma unroll
                             for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+                            if constexpr (INT4) mx *= p.scale_log2;
                             const float m2 = fmaxf(m[nt][e], mx), a = ex2_approx(m[nt][e] - m2);
                             m[nt][e] = m2;
                             l[nt][e] *= a;
@@ -519,8 +523,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         for (int kg = 0; kg < KG; ++kg)
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                float w0 = ex2_approx(sc[kg][nt][2 * h] - m[nt][0]);
-                                float w1 = ex2_approx(sc[kg][nt][2 * h + 1] - m[nt][1]);
+                                float w0 = ex2_approx(INT4 ? fmaf(sc[kg][nt][2 * h], p.scale_log2, -m[nt][0]) : sc[kg][nt][2 * h] - m[nt][0]);
+                                float w1 = ex2_approx(INT4 ? fmaf(sc[kg][nt][2 * h + 1], p.scale_log2, -m[nt][1])
+                                                           : sc[kg][nt][2 * h + 1] - m[nt][1]);
                                 add[nt][0] += w0;
                                 add[nt][1] += w1;
                                 if constexpr (INT8) w0 *= vs[kg][h], w1 *= vs[kg][h];
@@ -840,12 +845,13 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
 //          32760 tokens, 40 heads: 32 in 16s 190, 133)
 //          int8 8 rows 56, 16 60, 24 in 16s 89, 32 90 (128), 48 131 (129); three CTAs of an
 //          SM, with two thirds of the registers, are slower: d 64 int8 24 rows 60
-// 4 bits like int8: d 64 8 rows 29, 17 in 24s 33, 32 41, 48 in 24s 54, 64 in 32s 69; d 128 16 rows 42, 24 in
-// 16s 69, 32 70, 48 (80).
-int tile_rows(bool codes, int d, int64_t rows) {
-    if (d == 128) return rows <= 8 ? 8 : rows <= (codes ? 32 : 16) ? 16 : 0;
+//   4 bits: d 64 9 rows 29, 24 32 (59), 32 42 (60), 48 in 24s 52 (60), 64 in 32s 69 (60);
+//          d 128 16 41, 24 in 16s 67 (77), 32 68 (79), 48 (81)
+int tile_rows(int form, int d, int64_t rows) {
+    if (d == 128) return rows <= 8 ? 8 : rows <= (form != kBf16 ? 32 : 16) ? 16 : 0;
     if (rows <= 32) return (int)(rows + 7) / 8 * 8 + (rows == 0 ? 8 : 0);
-    return codes && rows <= 64 ? (rows <= 48 ? 24 : 32) : 0;
+    if (form != kBf16 && rows <= 48) return 24;
+    return form == kInt8 && rows <= 64 ? 32 : 0;
 }
 
 template <int FORM, int D>
@@ -874,11 +880,11 @@ size_t kv_decode_workspace(const echo_kv_pool &pool) {
 }
 
 bool kv_few_rows(const echo_kv_pool &pool, int64_t rows) {
-    return tile_rows(pool.kind != kBf16, pool.d, rows) > 0;
+    return tile_rows(pool.kind, pool.d, rows) > 0;
 }
 
 echo_status launch_kv_decode(const KvAttention &a, int64_t rows, cudaStream_t st) {
-    const int form = a.pool->kind, tile = tile_rows(form != kBf16, a.pool->d, rows);
+    const int form = a.pool->kind, tile = tile_rows(form, a.pool->d, rows);
     if (a.pool->d == 64)
         return form == kInt4 ? launch_rows<kInt4, 64>(a, tile, st)
                : form == kInt8 ? launch_rows<kInt8, 64>(a, tile, st) : launch_rows<kBf16, 64>(a, tile, st);
