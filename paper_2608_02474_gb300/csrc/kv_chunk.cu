@@ -241,6 +241,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         } else if (warp == 0) {
             // ---------------- keys and values, a page at a time ----------------
             const int shift = p.pool.shift, per_block = BN >> shift;
+            const int parts = INT4 ? max(shift - 5, 0) : 0;   // 4 bits: a lane copies 32 keys of a page at most (log2)
             int li = 0;                                       // copies into the ring so far
             for (int n = 0; ok; ++n) {
                 const KvPiece &pc = piece(n, ok);
@@ -267,7 +268,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         then = page_of(c0 + 32 + lane);
                     }
                     const int some = min(per_block, pages - first);
-                    const int page = __shfl_sync(0xffffffffu, now, (first - c0 + lane) & 31);
+                    const int page = __shfl_sync(0xffffffffu, now, (first - c0 + (lane >> parts)) & 31);
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv, ++li) {
                         const int slot = li % RING;
@@ -282,23 +283,19 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         if (lane == 0)
                             mbar_arrive_expect_tx(bar, (uint32_t)(some << shift) * (kv_bytes(FORM, D) + (kv ? 0 : SCALES)));
                         __syncwarp();
-                        if (lane < some) {
-                            const int z = (page * 2 + kv) * p.pool.H + head, r0 = lane << shift;
+                        if (lane < some << parts) {
+                            const int z = (page * 2 + kv) * p.pool.H + head, r0 = lane << (shift - parts);
                             if constexpr (INT4) {
                                 // codes and scales of 32 keys where their own warp's rows will be
-                                const int step = min(shift, 5);
-                                for (int r = 0; r < 1 << shift; r += 1 << step) {
-                                    uint8_t *at = dst + ((r0 + r) & ~31) * 128;
-                                    const int in32 = (r0 + r) & 31;
-                                    tma_load_3d(at + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
-                                    if (kv == 0) {
-                                        const uint8_t *src = static_cast<const uint8_t *>(p.pool.scale) +
-                                                             (((int64_t)z << shift) + r) * (D / 16);
-                                        at += SCALES_AT + in32 * (D / 16);
-                                        bulk_load_1d(at, src, (uint32_t)(D / 16) << step, bar);
-                                        bulk_load_1d(at + 2 * D, src + ((int64_t)p.pool.H << shift) * (D / 16),
-                                                     (uint32_t)(D / 16) << step, bar);
-                                    }
+                                const int r = r0 & ((1 << shift) - 1), in32 = r0 & 31, some32 = shift - parts;
+                                uint8_t *at = dst + (r0 & ~31) * 128;
+                                tma_load_3d(at + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
+                                if (kv == 0) {
+                                    const uint8_t *src = static_cast<const uint8_t *>(p.pool.scale) + (((int64_t)z << shift) + r) * (D / 16);
+                                    at += SCALES_AT + in32 * (D / 16);
+                                    bulk_load_1d(at, src, (uint32_t)(D / 16) << some32, bar);
+                                    bulk_load_1d(at + 2 * D, src + ((int64_t)p.pool.H << shift) * (D / 16),
+                                                 (uint32_t)(D / 16) << some32, bar);
                                 }
                             } else if constexpr (INT8) {
                                 tma_load_3d(dst + ATOM + r0 * D, &tm_kv, bar, 0, 0, z);
