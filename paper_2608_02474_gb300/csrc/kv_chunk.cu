@@ -24,10 +24,11 @@
 // sees such a key becomes NaN.  For int8 pages only a scale can be non-finite: it then
 // spoils the key's score, and stands as 0 among the values' scales; for 4-bit pages it makes
 // the key NaN, and its values 0.
-// 4 bits: 1560 rows over 31200 keys, 40 heads of 128, 706 to 733 us (bf16 638, int8 860).  The converting
-// warps' stores into shared memory and the softmax's instructions take turns with those that bound bf16; V_f and
-// K_{f+1} converted together, so that twice as many loads are under way, took 785, and scales folded into the
-// conversion 705.
+// 4 bits: 1560 rows over 31200 keys, 40 heads of 128, 700 to 733 us (bf16 638, int8 860).  A key's codes wait in
+// their slot until they are converted, so that the time from a slot's release to its values counts; the copies of a
+// block are 16 (32 for pages of 16 tokens: 801 us), issued side by side by as many lanes (one lane for all parts of a
+// page: 763).  V_f and K_{f+1} converted together, so that twice as many loads are under way, took 785; scales copied
+// by another warp, behind a barrier, 730 (pages of 16: 742), read by the converting warps 752 (771).
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
 #include <cfloat>
 #include <type_traits>
@@ -269,6 +270,8 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     }
                     const int some = min(per_block, pages - first);
                     const int page = __shfl_sync(0xffffffffu, now, (first - c0 + (lane >> parts)) & 31);
+                    // 4 bits: lane i takes the scales of part i / 2, keys' or values'
+                    const int page2 = INT4 ? __shfl_sync(0xffffffffu, now, (first - c0 + (lane >> (parts + 1))) & 31) : 0;
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv, ++li) {
                         const int slot = li % RING;
@@ -286,17 +289,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         if (lane < some << parts) {
                             const int z = (page * 2 + kv) * p.pool.H + head, r0 = lane << (shift - parts);
                             if constexpr (INT4) {
-                                // codes and scales of 32 keys where their own warp's rows will be
-                                const int r = r0 & ((1 << shift) - 1), in32 = r0 & 31, some32 = shift - parts;
-                                uint8_t *at = dst + (r0 & ~31) * 128;
-                                tma_load_3d(at + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
-                                if (kv == 0) {
-                                    const uint8_t *src = static_cast<const uint8_t *>(p.pool.scale) + (((int64_t)z << shift) + r) * (D / 16);
-                                    at += SCALES_AT + in32 * (D / 16);
-                                    bulk_load_1d(at, src, (uint32_t)(D / 16) << some32, bar);
-                                    bulk_load_1d(at + 2 * D, src + ((int64_t)p.pool.H << shift) * (D / 16),
-                                                 (uint32_t)(D / 16) << some32, bar);
-                                }
+                                // codes of 32 keys where their own warp's rows will be, their scales next to them (below)
+                                const int r = r0 & ((1 << shift) - 1), in32 = r0 & 31;
+                                tma_load_3d(dst + (r0 & ~31) * 128 + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
                             } else if constexpr (INT8) {
                                 tma_load_3d(dst + ATOM + r0 * D, &tm_kv, bar, 0, 0, z);
                                 if (kv == 0) {
@@ -315,6 +310,13 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                 for (int a = 0; a < C::ATOMS; ++a)
                                     tma_load_3d(dst + a * ATOM + r0 * 128, &tm_kv, bar, 64 * a, 0, z);
                             }
+                        }
+                        if (INT4 && kv == 0 && lane < 2 * some << parts) {
+                            const int side = lane & 1, r0 = (lane >> 1) << (shift - parts);
+                            bulk_load_1d(dst + (r0 & ~31) * 128 + SCALES_AT + side * 2 * D + (r0 & 31) * (D / 16),
+                                         static_cast<const uint8_t *>(p.pool.scale) +
+                                             (((((int64_t)page2 * 2 + side) * p.pool.H + head) << shift) + (r0 & ((1 << shift) - 1))) * (D / 16),
+                                         (uint32_t)(D / 16) << (shift - parts), bar);
                         }
                         __syncwarp();
                     }
