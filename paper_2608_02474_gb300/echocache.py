@@ -946,6 +946,19 @@ def echo_rotary(plan: Rotary, pos, q, k=None, inverse: bool = False, q_out=None,
 _NORMS = {"none": 0, "layer": 1, "rms": 2}
 
 
+def _row_stride(t, name, shape, gpu):
+    """Row stride of a tensor of this shape on device `gpu`, columns contiguous.  The stride of a single
+    row means nothing, and may be anything."""
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} must be a CUDA tensor on the device of x")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    row, column = t.stride()
+    if column != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    return row if shape[0] > 1 else (shape[1] + 7) // 8 * 8
+
+
 class GatedNorm:
     """The norms around a gated residual over rows of D values (echo_gated_norm_plan): `before` of the new
     residual ("layer", "rms" or "none") with weight and bias f32 [D] or none, `after` of the branch's output
@@ -977,38 +990,39 @@ def echo_gated_norm(plan: GatedNorm, x, y=None, gate=None, scale=None, shift=Non
     [n_rows, D] bf16 or f32.  gate, scale and shift: [n_mods, D] of one dtype and row stride, each or none;
     row r takes row mod_rows[r] (int32) of them, or r // rows_per_mod; rows whose number is no row are left out.
     h has x's dtype and n is bf16 where they are not given; want_h, want_n: None instead."""
-    N, D, gpu = x.shape[0], plan.D, x.get_device()
+    D, gpu = plan.D, x.get_device()
     if gpu < 0:
         raise ValueError("x must be a CUDA tensor")
     if plan._gpu not in (None, gpu):
         raise ValueError("x must be on the device of the weights")
+    N = x.shape[0]
+    rows = (N, D)
     if not want_h:
         h = None
     elif h is None:
-        h = _empty((N, D), x.dtype, x.device, stream)
+        h = _empty(rows, x.dtype, x.device, stream)
     if not want_n:
         n = None
     elif n is None:
-        n = _empty((N, D), torch.bfloat16, x.device, stream)
+        n = _empty(rows, torch.bfloat16, x.device, stream)
     args = []
     for t, name in ((x, "x"), (y, "y"), (h, "h"), (n, "n")):
         if t is None:
             args += (None, 0, 0)
             continue
-        ld = _rows_of(t, name, N, D, gpu)
-        if t.shape[1] != D:
-            raise ValueError(f"{name} must be [{N}, {D}]")
+        ld = _row_stride(t, name, rows, gpu)
         args += (t.data_ptr(), ld, _dtype(t))
     mod = None
     first = gate if gate is not None else scale if scale is not None else shift
     if first is not None:
         mods, dtype, ptr, ld = first.shape[0], first.dtype, [], None
+        wide = (mods, D)
         for v, name in ((gate, "gate"), (scale, "scale"), (shift, "shift")):
             if v is None:
                 ptr.append(None)
                 continue
-            own = _rows_of(v, name, mods, D, gpu)
-            if own != (own if ld is None else ld) or v.dtype != dtype or v.shape[1] != D:
+            own = _row_stride(v, name, wide, gpu)
+            if own != ld and ld is not None or v.dtype != dtype:
                 raise ValueError(f"gate, scale and shift must be [n_mods, {D}] of one dtype and row stride")
             ld = own
             ptr.append(v.data_ptr())
