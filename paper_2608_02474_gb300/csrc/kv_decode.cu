@@ -21,14 +21,14 @@
 // come out in it.
 //
 // 4-bit codes become code / 64 in bf16 (kv_nibbles2), and a code times its group's scale is exact
-// in bf16 too, so that keys and values can be multiplied out in registers; the softmax's scale goes into the exponents' multiply-add; for 8 packed rows the
+// in bf16 too, so that keys and values can be multiplied out in registers; for 8 packed rows the
 // scores of a group stand apart and take the keys' scale in fp32, with fewer multiplications.
 // With a quarter of bf16's bytes it is the instructions beside the products that
-// bound it, so: a stage of the ring belongs to one group of warps, whose other group neither waits for it nor frees
+// bound it, so: the softmax's scale goes into the exponents' multiply-add; a stage of the ring belongs to one group of warps, whose other group neither waits for it nor frees
 // it; the queries of the next piece are fetched while this one's sums are joined; and the warps join behind one
-// barrier, all of O in shared memory.  48 tokens over up to 8190 keys each, 32/8 heads of 128: 72.9 us (80
-// before the three; int8 89.5), 282 MB at 5.2 TB/s beside some 19 us that do not grow with the
-// keys: launch, finding the work (2.8), the first copies, the ends of pieces, workers that end unevenly.
+// barrier, all of O in shared memory.  48 tokens over up to 8190 keys each, 32/8 heads of 128: 72.6 us (80
+// before these; int8 89.5; pages of 16 tokens 99, whose copies are four times as many), 282 MB at
+// 5.2 TB/s beside some 19 us that do not grow with the keys: launch, finding the work (2.8), the first copies, the ends of pieces, workers that end unevenly.
 #include <cfloat>
 
 #include "kv_schedule.cuh"
@@ -38,8 +38,8 @@ namespace {
 constexpr int PIECES = 4;                      // handed out ahead
 constexpr int kWholeKeys = 768;     // 16 heads of 64, one bf16 token: whole 256 keys 9.2 us, 1024 13.4; divided 11.6, 12.1
 
-// LONG: twice as many keys of a block, for 4-bit heads of 64 over much work (48 tokens of 16 heads over
-// up to 8190 keys each 82 us, so 94; one over 2000 18, so 14)
+// LONG: 256 keys of a block and not 128, for 4-bit heads of 64 over much work (48 tokens of 16 heads over
+// up to 8190 keys each 80 us and not 94; but one over 2000 18 and not 14)
 template <int FORM, int D, int NR, bool LONG>
 struct Cfg {
     static constexpr bool CODES = FORM != kBf16;
@@ -211,26 +211,25 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 if (!ok) break;
                 const int n = min(per_block, copies - first);
                 if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(n << cs) * 2 * (C::ROW_BYTES + C::TOKEN_SCALES));
-                const int page = __shfl_sync(0xffffffffu, now, (first - c0 + lane) & 31);
+                const int i = CODES ? lane >> 1 : lane;      // codes: a lane for keys and one for values
+                const int page = __shfl_sync(0xffffffffu, now, (first - c0 + i) & 31);
                 __syncwarp();
-                if (lane < n) {
+                if (i < n) {
                     uint8_t *dst = smem + stage * C::STAGE;
-                    const int y = ((first + lane) << cs) & ((1 << shift) - 1), r0 = lane << cs;
+                    const int y = ((first + i) << cs) & ((1 << shift) - 1), r0 = i << cs;
+                    if constexpr (CODES) {
+                        const int kv = lane & 1, z = (page * 2 + kv) * p.pool.H + walk.head;
+                        tma_load_3d(dst + kv * C::HALF + r0 * C::ROW_BYTES, &tm, &full[stage], 0, y, z);
+                        bulk_load_1d(dst + 2 * C::HALF + (kv * BK + r0) * C::TOKEN_SCALES,
+                                     static_cast<const uint8_t *>(p.pool.scale) + (((int64_t)z << shift) + y) * C::TOKEN_SCALES,
+                                     (uint32_t)C::TOKEN_SCALES << cs, &full[stage]);
+                    } else {
 #pragma unroll
-                    for (int kv = 0; kv < 2; ++kv) {
-                        const int z = (page * 2 + kv) * p.pool.H + walk.head;
-                        if constexpr (CODES) {
-                            tma_load_3d(dst + kv * C::HALF + r0 * C::ROW_BYTES, &tm, &full[stage], 0, y, z);
-                            bulk_load_1d(dst + 2 * C::HALF + (kv * BK + r0) * C::TOKEN_SCALES,
-                                         static_cast<const uint8_t *>(p.pool.scale) +
-                                             (((int64_t)z << shift) + y) * C::TOKEN_SCALES,
-                                         (uint32_t)C::TOKEN_SCALES << cs, &full[stage]);
-                        } else {
+                        for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
                             for (int a = 0; a < D / 64; ++a)
-                                tma_load_3d(dst + kv * C::HALF + a * (BK * 128) + r0 * 128, &tm, &full[stage],
-                                            64 * a, y, z);
-                        }
+                                tma_load_3d(dst + kv * C::HALF + a * (BK * 128) + r0 * 128, &tm, &full[stage], 64 * a, y,
+                                            (page * 2 + kv) * p.pool.H + walk.head);
                     }
                 }
             }
