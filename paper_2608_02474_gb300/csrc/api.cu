@@ -109,6 +109,34 @@ bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows
     return r == CUDA_SUCCESS;
 }
 
+bool make_tmap_code_pairs(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows) {
+    const EncodeTiledFn encode = encode_fn();
+    if (!encode) return false;
+    const cuuint64_t row = (cuuint64_t)pool.d / 2, page = row * (cuuint64_t)pool.page_tokens;
+    cuuint64_t gdim[4] = {row, (cuuint64_t)pool.page_tokens, (cuuint64_t)pool.H, 2ull * (cuuint64_t)pool.n_pages};
+    cuuint64_t gstride[3] = {row, page, page * (cuuint64_t)pool.H};
+    cuuint32_t box[4] = {(cuuint32_t)row, box_rows, 1, 2};
+    cuuint32_t estride[4] = {1, 1, 1, 1};
+    CUresult r = encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool.pages, gdim, gstride, box, estride,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
+bool make_tmap_scale_pairs(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows) {
+    const EncodeTiledFn encode = encode_fn();
+    if (!encode) return false;
+    const cuuint64_t words = (cuuint64_t)pool.d / 64, head = words * (cuuint64_t)pool.page_tokens;   // of two scales
+    cuuint64_t gdim[3] = {head, (cuuint64_t)pool.H, 2ull * (cuuint64_t)pool.n_pages};
+    cuuint64_t gstride[2] = {4 * head, 4 * head * (cuuint64_t)pool.H};
+    cuuint32_t box[3] = {(cuuint32_t)words * box_rows, 1, 2};
+    cuuint32_t estride[3] = {1, 1, 1};
+    CUresult r = encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, pool.scale, gdim, gstride, box, estride,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 bool make_tmap_rows(CUtensorMap *m, const void *base, uint64_t n_rows, uint64_t H, uint64_t d,
                     uint64_t ld, uint32_t box_heads, uint32_t box_rows) {
     const EncodeTiledFn encode = encode_fn();

@@ -205,6 +205,15 @@ ECHO_DEV void tma_load_3d(void *dst, const CUtensorMap *m, uint64_t *bar, int32_
         : "memory");
 }
 
+ECHO_DEV void tma_load_4d(void *dst, const CUtensorMap *m, uint64_t *bar, int32_t x, int32_t y,
+                          int32_t z, int32_t w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
 // 2D tiled load into this CTA's shared memory that completes its bytes on the
 // mbarrier at `bar_cluster` (a shared::cluster address, here the even CTA's of a
 // CTA pair); x as for tma_load_2d.

@@ -76,6 +76,10 @@ bool make_tmap_bf16(CUtensorMap *m, const void *base, uint64_t rows, uint64_t co
 // a pool of key/value pages as [z, page_tokens, d], z = (page, keys or values, head): bf16 in
 // boxes of 64 columns, int8 and 4-bit codes in whole rows, box_rows tokens; swizzled by the box's width
 bool make_tmap_pages(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
+// 4-bit pages: a box is box_rows tokens of a head's keys and the same of its values behind them, at
+// {0, token, head, 2 page}; of their scales at {token d / 64, head, 2 page}, 32-bit words.
+bool make_tmap_code_pairs(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
+bool make_tmap_scale_pairs(CUtensorMap *m, const echo_kv_pool &pool, uint32_t box_rows);
 
 // bf16 rows of heads [n_rows, H, d] (row stride ld elements) in boxes of box_rows rows and
 // box_heads heads, 64 columns, 128-byte swizzle

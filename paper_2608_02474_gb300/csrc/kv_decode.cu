@@ -129,9 +129,9 @@ ECHO_DEV uint32_t chunk_at(int r, int c) {
     else return (uint32_t)((c >> 3) * (BK * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-template <int FORM, int D, int NR, bool LONG>
+template <int FORM, int D, int NR, bool LONG, bool P16>
 __global__ void __launch_bounds__((Cfg<FORM, D, NR, LONG>::THREADS), 2)
-kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
+kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_scales, const DecodeParams p) {
     using C = Cfg<FORM, D, NR, LONG>;
     constexpr bool INT8 = FORM == kInt8, INT4 = FORM == kInt4, CODES = C::CODES;
     constexpr int KG = C::KG, STEP = 16 * KG, BK = C::BK, MT = D / 16, ROWS = C::ROWS;
@@ -159,6 +159,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
         abort_flag = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tm);
+        if (INT4) tma_prefetch_desc(&tm_scales);
     }
     volatile int *abort_v = &abort_flag;
     pdl_enter();
@@ -167,7 +168,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 
     if (warp == C::WARPS) {
         // ---------------- producer: the pieces' blocks, a page or part of one at a time ----
-        const int shift = p.pool.shift, cs = min(shift, C::BSHIFT);   // tokens of a copy: 1 << cs
+        const int shift = p.pool.shift, cs = min(shift, INT4 ? 5 : C::BSHIFT);   // tokens of a copy: 1 << cs
         const int per_block = BK >> cs;
         int g = 0;
         bool ok = true;
@@ -211,13 +212,17 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 if (!ok) break;
                 const int n = min(per_block, copies - first);
                 if (lane == 0) mbar_arrive_expect_tx(&full[stage], (uint32_t)(n << cs) * 2 * (C::ROW_BYTES + C::TOKEN_SCALES));
-                const int i = CODES ? lane >> 1 : lane;      // codes: a lane for keys and one for values
+                const int i = INT8 ? lane >> 1 : lane;       // int8: a lane for keys and one for values
                 const int page = __shfl_sync(0xffffffffu, now, (first - c0 + i) & 31);
                 __syncwarp();
                 if (i < n) {
                     uint8_t *dst = smem + stage * C::STAGE;
                     const int y = ((first + i) << cs) & ((1 << shift) - 1), r0 = i << cs;
-                    if constexpr (CODES) {
+                    if constexpr (INT4) {                    // a copy's keys, then its values
+                        tma_load_4d(dst + 2 * r0 * C::ROW_BYTES, &tm, &full[stage], 0, y, walk.head, 2 * page);
+                        tma_load_3d(dst + 2 * C::HALF + 2 * r0 * C::TOKEN_SCALES, &tm_scales, &full[stage], y * (D / 64),
+                                    walk.head, 2 * page);
+                    } else if constexpr (INT8) {
                         const int kv = lane & 1, z = (page * 2 + kv) * p.pool.H + walk.head;
                         tma_load_3d(dst + kv * C::HALF + r0 * C::ROW_BYTES, &tm, &full[stage], 0, y, z);
                         bulk_load_1d(dst + 2 * C::HALF + (kv * BK + r0) * C::TOKEN_SCALES,
@@ -243,6 +248,9 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
     // a fragment's row group and column pair; lane's row and chunk in four 8x8 matrices
     const int gq = lane >> 2, tq = lane & 3, mi = lane >> 3, mr = lane & 7;
     const int wk0 = (warp & 3) * C::KPW;             // this warp's first key of a block
+    // 4 bits: a copy is 32 tokens' keys and then their values, or twice 16 (P16: pages of 16).  Where the next
+    // 16 keys lie, and the values
+    constexpr int next16 = P16 ? 32 : 16, values = INT4 ? 48 - next16 : 0;
     const uint32_t ring = smem_u32(smem);
     int g = 0;
     bool ok = true;
@@ -340,11 +348,12 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
             const int stage = g % C::RING;
             ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (g / C::RING) & 1, abort_v, p.err));
             if (!ok) break;
-            const uint32_t kbase = ring + stage * C::STAGE, vbase = kbase + C::HALF;
+            const uint32_t kbase = ring + stage * C::STAGE, vbase = INT4 ? kbase : kbase + C::HALF;
             if (own)
 #pragma unroll 1
             for (int k0 = 0; k0 < C::KPW; k0 += STEP) {
-                const int wk = wk0 + k0, key0 = kb * BK + wk;    // the first key of this step
+                const int wk = wk0 + k0, key0 = kb * BK + wk;    // the first key of this step, and where it lies
+                const int at0 = INT4 ? 2 * (wk & ~31) + (wk & 16 ? next16 : 0) : wk;
                 if (key0 >= keys) break;
                 // S^T = K Q^T, 16 keys at a time
                 float sc[KG][NR][4] = {};
@@ -366,11 +375,11 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 #pragma unroll
                         for (int kg = 0; kg < KG; ++kg) {
                             uint32_t r[4], ks[2];    // two groups' codes; scales of keys gq and gq + 8
-                            const int row = wk + kg * 16 + (mi & 1) * 8 + mr;
+                            const int row = at0 + kg * next16 + (mi & 1) * 8 + mr;
                             ldsm4(kbase + chunk_at<FORM, D, BK>(row, kk / 2 + (mi >> 1)), r);
 #pragma unroll
                             for (int h = 0; h < 2; ++h)
-                                ks[h] = *reinterpret_cast<const uint32_t *>(token_scales + (wk + kg * 16 + 8 * h + gq) * C::TOKEN_SCALES + kk);
+                                ks[h] = *reinterpret_cast<const uint32_t *>(token_scales + (at0 + kg * next16 + 8 * h + gq) * C::TOKEN_SCALES + kk);
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {        // a group of 32 columns
                                 uint32_t a[4], c[4];
@@ -443,7 +452,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                 if (INT4 && edge) {
                     // values' scales that are not finite, or anything past the end: 0, and what is
                     // spoilt spoils the rows that see it.  This warp's keys alone.
-                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (BK + wk + lane) * C::TOKEN_SCALES);
+                    uint32_t *at = reinterpret_cast<uint32_t *>(smem + stage * C::STAGE + 2 * C::HALF + (at0 + values + (lane >> 4) * next16 + (lane & 15)) * C::TOKEN_SCALES);
 #pragma unroll
                     for (int i = 0; i < (lane < STEP ? C::TOKEN_SCALES / 4 : 0); ++i) {
                         const uint32_t off = kv_not_finite2(at[i]);
@@ -555,7 +564,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                         b[nt][1] = turn8x8(pb[kg][nt][1]);
                     }
                     // a matrix of 8 keys and 16 bytes: bf16 keys, then columns; codes the other way
-                    const int row = wk + kg * 16 + (CODES ? (mi & 1) : (mi >> 1)) * 8 + mr;
+                    const int row = at0 + values + kg * next16 + (CODES ? (mi & 1) : (mi >> 1)) * 8 + mr;
                     const int col = CODES ? mi >> 1 : mi & 1;
                     uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
                     if (!CODES && edge && low < keys) {
@@ -597,7 +606,7 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
                     if constexpr (INT4) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
-                            load_words(token_scales + (BK + wk + kg * 16 + 8 * h + 2 * tq) * C::TOKEN_SCALES, vw[h]);
+                            load_words(token_scales + (at0 + values + kg * next16 + 8 * h + 2 * tq) * C::TOKEN_SCALES, vw[h]);
                     }
 #pragma unroll
                     for (int t = 0; t < MT; t += STEPS) {
@@ -807,15 +816,20 @@ kv_decode_kernel(const __grid_constant__ CUtensorMap tm, const DecodeParams p) {
 template <int FORM, int D, int NR, bool LONG = false>
 echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     using C = Cfg<FORM, D, NR, LONG>;
-    static int attr_done[64] = {};
+    const bool p16 = FORM == kInt4 && a.pool->page_tokens == 16;
+    auto *const kernel = p16 ? kv_decode_kernel<FORM, D, NR, LONG, FORM == kInt4> : kv_decode_kernel<FORM, D, NR, LONG, false>;
+    static int attr_done[64][2] = {};
     int dev = 0;
     cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && !attr_done[dev]) {
-        cudaFuncSetAttribute(kv_decode_kernel<FORM, D, NR, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-        attr_done[dev] = 1;
+    if (dev >= 0 && dev < 64 && !attr_done[dev][p16]) {
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        attr_done[dev][p16] = 1;
     }
-    CUtensorMap tm;
-    if (!echo::make_tmap_pages(&tm, *a.pool, (uint32_t)(a.pool->page_tokens < C::BK ? a.pool->page_tokens : C::BK)))
+    CUtensorMap tm, tm_scales = {};
+    constexpr int most = FORM == kInt4 ? 32 : C::BK;
+    const uint32_t tokens = (uint32_t)(a.pool->page_tokens < most ? a.pool->page_tokens : most);
+    if (FORM == kInt4 ? !echo::make_tmap_code_pairs(&tm, *a.pool, tokens) || !echo::make_tmap_scale_pairs(&tm_scales, *a.pool, tokens)
+                      : !echo::make_tmap_pages(&tm, *a.pool, tokens))
         return ECHO_ERR_CUDA;
     DecodeParams p;
     p.pool = echo::kv_pool(*a.pool);
@@ -830,7 +844,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        launched = echo::launch_chained(kv_decode_kernel<FORM, D, NR, LONG>, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, p);
+        launched = echo::launch_chained(kernel, dim3(p.work.workers), dim3(C::THREADS), C::SMEM, st, tm, tm_scales, p);
     }
     if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();
