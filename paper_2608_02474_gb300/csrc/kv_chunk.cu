@@ -24,11 +24,12 @@
 // sees such a key becomes NaN.  For int8 pages only a scale can be non-finite: it then
 // spoils the key's score, and stands as 0 among the values' scales; for 4-bit pages it makes
 // the key NaN, and its values 0.
-// 4 bits: 1560 rows over 31200 keys, 40 heads of 128, 700 to 733 us (bf16 638, int8 860).  A key's codes wait in
-// their slot until they are converted, so that the time from a slot's release to its values counts; the copies of a
-// block are 16 (32 for pages of 16 tokens: 801 us), issued side by side by as many lanes (one lane for all parts of a
-// page: 763).  V_f and K_{f+1} converted together, so that twice as many loads are under way, took 785; scales copied
-// by another warp, behind a barrier, 730 (pages of 16: 742), read by the converting warps 752 (771).
+// 4 bits: 1560 rows over 31200 keys, 40 heads of 128, 700 to 733 us (bf16 638, int8 860), of 64 497.  A key's codes
+// wait in their slot until they are converted, so that the time from a slot's release to its values counts, and the
+// number of copies: 12 of a block, 24 for pages of 16 tokens (741 and 617 us; with 16 and 32, keys' and values' scales
+// apart, 701 and 530, 801 and 700), issued side by side by as many lanes (one lane for all parts of a page: 763).
+// V_f and K_{f+1} converted together, so that twice as many loads are under way, took 785; scales copied by
+// another warp, behind a barrier, 730 (pages of 16: 742), read by the converting warps 752 (771).
 // Every wait is bounded (ECHO_ERR_TIMEOUT).
 #include <cfloat>
 #include <type_traits>
@@ -110,7 +111,7 @@ struct Side {
 template <int FORM, int D>
 __global__ void __launch_bounds__((Cfg<FORM, D>::THREADS), 1)
 kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_kv,
-                const ChunkParams p) {
+                const __grid_constant__ CUtensorMap tm_scales, const ChunkParams p) {
     using C = Cfg<FORM, D>;
     constexpr bool INT8 = C::INT8, INT4 = FORM == kInt4, CODES = C::CODES;
     constexpr int RING = C::RING;
@@ -270,8 +271,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                     }
                     const int some = min(per_block, pages - first);
                     const int page = __shfl_sync(0xffffffffu, now, (first - c0 + (lane >> parts)) & 31);
-                    // 4 bits: lane i takes the scales of part i / 2, keys' or values'
-                    const int page2 = INT4 ? __shfl_sync(0xffffffffu, now, (first - c0 + (lane >> (parts + 1))) & 31) : 0;
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv, ++li) {
                         const int slot = li % RING;
@@ -289,9 +288,12 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         if (lane < some << parts) {
                             const int z = (page * 2 + kv) * p.pool.H + head, r0 = lane << (shift - parts);
                             if constexpr (INT4) {
-                                // codes of 32 keys where their own warp's rows will be, their scales next to them (below)
+                                // codes of 32 keys where their own warp's rows will be, their scales next to them
                                 const int r = r0 & ((1 << shift) - 1), in32 = r0 & 31;
-                                tma_load_3d(dst + (r0 & ~31) * 128 + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
+                                uint8_t *at = dst + (r0 & ~31) * 128;
+                                tma_load_3d(at + (C::ATOMS - 1) * ATOM + in32 * (D / 2), &tm_kv, bar, 0, r, z);
+                                if (kv == 0)                 // keys' and then values'
+                                    tma_load_3d(at + SCALES_AT + in32 * (D / 8), &tm_scales, bar, r * (D / 64), head, 2 * page);
                             } else if constexpr (INT8) {
                                 tma_load_3d(dst + ATOM + r0 * D, &tm_kv, bar, 0, 0, z);
                                 if (kv == 0) {
@@ -310,13 +312,6 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                 for (int a = 0; a < C::ATOMS; ++a)
                                     tma_load_3d(dst + a * ATOM + r0 * 128, &tm_kv, bar, 64 * a, 0, z);
                             }
-                        }
-                        if (INT4 && kv == 0 && lane < 2 * some << parts) {
-                            const int side = lane & 1, r0 = (lane >> 1) << (shift - parts);
-                            bulk_load_1d(dst + (r0 & ~31) * 128 + SCALES_AT + side * 2 * D + (r0 & 31) * (D / 16),
-                                         static_cast<const uint8_t *>(p.pool.scale) +
-                                             (((((int64_t)page2 * 2 + side) * p.pool.H + head) << shift) + (r0 & ((1 << shift) - 1))) * (D / 16),
-                                         (uint32_t)(D / 16) << (shift - parts), bar);
                         }
                         __syncwarp();
                     }
@@ -725,7 +720,9 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                                     : lane * 32 + ((c ^ ((lane >> 2) & 1)) << 4);
                             in[c] = *reinterpret_cast<const uint4 *>(mine + (C::ATOMS - 1) * ATOM + at);
                         }
-                        const uint8_t *sc = mine + SCALES_AT + lane * (D / 16);
+                        // of 32 tokens' keys and then their values, or twice 16 (pages of 16)
+                        const bool p16 = p.pool.shift == 4;
+                        const uint8_t *sc = mine + SCALES_AT + (lane + (p16 ? lane & 16 : 0)) * (D / 16);
                         if (kv == 0) {
                             // a value's scale that is not finite stands as 0, and spoils the key instead
                             uint32_t bad = 0;
@@ -733,7 +730,7 @@ kv_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
                             for (int i = 0; i < D / 64; ++i) {
                                 sw[i] = reinterpret_cast<const uint32_t *>(sc)[i];
-                                vw[i] = reinterpret_cast<const uint32_t *>(sc + 2 * D)[i];
+                                vw[i] = reinterpret_cast<const uint32_t *>(sc + (p16 ? D : 2 * D))[i];
                                 const uint32_t off = kv_not_finite2(vw[i]);
                                 bad |= off;
                                 vw[i] = past ? 0u : vw[i] & ~off;
@@ -1122,10 +1119,12 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
         attr_done[dev] = 1;
     }
     const int group = a.Hq / a.pool->H, tokens = BM / group;
-    CUtensorMap tq, tk;
+    CUtensorMap tq, tk, ts = {};
+    const uint32_t tokens4 = a.pool->page_tokens < 32 ? (uint32_t)a.pool->page_tokens : 32u;   // of a copy of 4-bit pages
     if (!echo::make_tmap_rows(&tq, a.q, (uint64_t)a.batch->n_rows, (uint64_t)a.Hq, (uint64_t)D, (uint64_t)a.ldq,
                               (uint32_t)group, (uint32_t)tokens) ||
-        !echo::make_tmap_pages(&tk, *a.pool, (uint32_t)(FORM == kInt4 && a.pool->page_tokens > 32 ? 32 : a.pool->page_tokens)))
+        !echo::make_tmap_pages(&tk, *a.pool, FORM == kInt4 ? tokens4 : (uint32_t)a.pool->page_tokens) ||
+        (FORM == kInt4 && !echo::make_tmap_scale_pairs(&ts, *a.pool, tokens4)))
         return ECHO_ERR_CUDA;
     ChunkParams p;
     p.pool = echo::kv_pool(*a.pool);
@@ -1139,7 +1138,7 @@ echo_status launch(const echo::KvAttention &a, cudaStream_t st) {
     cudaError_t launched;
     {
         echo::LaunchScope ls(ECHO_K_KV_ATTENTION, a.batch->n_rows, (int64_t)a.Hq * D, a.batch->n_seqs, st);
-        launched = echo::launch_chained(kv_chunk_kernel<FORM, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, p);
+        launched = echo::launch_chained(kv_chunk_kernel<FORM, D>, dim3(p.work.workers), dim3(C::THREADS), SMEM, st, tq, tk, ts, p);
     }
     if (launched == cudaSuccess) echo::launch_kv_join(a, p.work, st);   // it needs what the kernel leaves
     return echo::last_launch_status();

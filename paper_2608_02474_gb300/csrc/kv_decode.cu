@@ -26,9 +26,11 @@
 // With a quarter of bf16's bytes it is the instructions beside the products that
 // bound it, so: the softmax's scale goes into the exponents' multiply-add; a stage of the ring belongs to one group of warps, whose other group neither waits for it nor frees
 // it; the queries of the next piece are fetched while this one's sums are joined; and the warps join behind one
-// barrier, all of O in shared memory.  48 tokens over up to 8190 keys each, 32/8 heads of 128: 72.6 us (80
-// before these; int8 89.5; pages of 16 tokens 99, whose copies are four times as many), 282 MB at
-// 5.2 TB/s beside some 19 us that do not grow with the keys: launch, finding the work (2.8), the first copies, the ends of pieces, workers that end unevenly.
+// barrier, all of O in shared memory.  Copies are few, too: 32 tokens' keys and values are one, and their scales
+// another (pages of 16 tokens: 16 of them; with four copies for the two, up to 128 tokens each, pages of 16 took 98 us
+// and not 77, and one token over 301 keys 9.0 and not 8.1).  48 tokens over up to 8190 keys each, 32/8 heads
+// of 128: 71.9 us (80 before these; int8 89.5), 282 MB at
+// 5.2 TB/s beside some 18 us that do not grow with the keys: launch, finding the work (2.8), the first copies, the ends of pieces, workers that end unevenly.
 #include <cfloat>
 
 #include "kv_schedule.cuh"
@@ -39,7 +41,7 @@ constexpr int PIECES = 4;                      // handed out ahead
 constexpr int kWholeKeys = 768;     // 16 heads of 64, one bf16 token: whole 256 keys 9.2 us, 1024 13.4; divided 11.6, 12.1
 
 // LONG: 256 keys of a block and not 128, for 4-bit heads of 64 over much work (48 tokens of 16 heads over
-// up to 8190 keys each 80 us and not 94; but one over 2000 18 and not 14)
+// up to 8190 keys each 82 us and not 94; but one over 2000 18 and not 14)
 template <int FORM, int D, int NR, bool LONG>
 struct Cfg {
     static constexpr bool CODES = FORM != kBf16;
