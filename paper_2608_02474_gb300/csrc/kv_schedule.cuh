@@ -55,7 +55,9 @@ struct KvWork {
 
 constexpr int kFixedUnits = 2;   // set-up and end of a piece, in key-block times
 constexpr int kLeast = 4;        // the fewest units for a worker
-constexpr int kMostKeys = INT32_MAX / 128 * 128;   // of a sequence: whole blocks and pages in 31 bits
+// Of a sequence: whole pages in 31 bits, so that keys + 127 are, too.  Blocks may have more keys than 128
+// (their count is taken without that sum); any key of the last one, below 2^31, still has a number.
+constexpr int kMostKeys = INT32_MAX / 128 * 128;
 
 struct KvSeq {             // one sequence of the batch
     int row, packed, len;  // its first row, its packed rows, its length
@@ -82,7 +84,7 @@ struct KvSeq {             // one sequence of the batch
         return top(w, row + w.by_group(last));
     }
     ECHO_DEV int blocks(const KvWork &w, int t) const {
-        return (keys(w, t) + (1 << w.block_shift) - 1) >> w.block_shift;
+        return (int)(((unsigned)keys(w, t) + (1u << w.block_shift) - 1u) >> w.block_shift);
     }
 };
 
