@@ -450,7 +450,12 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         };
         int m[R];
 #pragma unroll
-        for (int k = 0; k < R; ++k) m[k] = SAME ? 0 : ok ? __shfl_sync(0xffffffffu, mod, k) : -1;
+        for (int k = 0; k < R; ++k) {
+            m[k] = 0;
+            if constexpr (SAME) continue;
+            m[k] = __shfl_sync(0xffffffffu, mod, k);
+            if (!ok) m[k] = -1;
+        }
         Pairs h[R];
         float f[R];
         const int there = !live ? 0 : SAME ? R : n;
@@ -511,8 +516,9 @@ gated_norm_rows_kernel(const NormParams p, int *err) {
         const int n = min(R, last - first - i * R);
         mod = next;
         if (i + 1 < batches) next = mod_of(i + 1);
-        // a wait that gives up lets the others give up; nothing is stored from then on
-        ok = ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err);
+        // a wait that gives up lets the others give up; nothing is stored from then on.  By whole warps:
+        // its lanes may have seen different things, and they exchange values below
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(&full[i & 1], (i >> 1) & 1, &abort_flag, err));
         // the whole warp takes one way: a barrier lies on both
         if (__all_sync(0xffffffffu, ok && (lane >= R || (mod >= 0 && mod == cur && mod == cur_out)))) batch(std::true_type(), R);
         else batch(std::false_type(), n);
