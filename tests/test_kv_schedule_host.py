@@ -95,3 +95,9 @@ def test_blocks_of_any_length(lib, shift, cb):
                 p = n - rows + min(16 * (t + 1), rows) - 1
                 want = min(n, most) if cb == 0 else 0 if p < 0 else min(n, most, (p // cb + 1) * cb)
                 assert keys.value == want and got == -(-want // 2 ** shift), (n, rows, t)
+
+
+def test_the_rule_for_blocks_of_256_keys():
+    """As test_gpu_int4_division.py, which widens tables to it, has it."""
+    rule = re.search(r"if \(tile == 8 && ([^\n]*)\)\n\s*return launch<FORM, D, 1, true>", source("kv_decode.cu")).group(1)
+    assert rule.replace("(double)", "").startswith("a.batch->n_seqs * a.pool->H * keys >= 2.0 * echo::num_sms() * 16 * 256")
