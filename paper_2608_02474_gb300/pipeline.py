@@ -659,28 +659,37 @@ class ChunkStream:
         audio = self.cond_table.extend({c: 0 for c in rows}).batch
         cond = ec.KVBatch(audio.table, audio.lens, step.batch.row0, step.n_rows, step.batch.max_rows)
 
-        def norm(x, y, out=torch.float32, gate=None, scale=None, shift=None, want_h=True, want_n=True):
-            """(h, n) with (layer, row of its modulations) for gate, scale and shift."""
+        def norm(x, y=None, out=torch.float32, gate=None, scale=None, shift=None, want_n=True):
+            """(h, n) with (layer, row of its modulations) for gate, scale and shift; without y, n alone."""
             part = lambda i: None if mods is None or i is None else mods[:, i[0], i[1]]   # noqa: E731
             g, s, t = part(gate), part(scale), part(shift)
-            h = torch.empty(x.shape, dtype=out, device=x.device) if want_h else None
-            return ec.echo_gated_norm(self.norm, x, y, g, s, t, h=h, want_h=want_h, want_n=want_n,
+            h = None if y is None else torch.empty(x.shape, dtype=out, device=x.device)
+            return ec.echo_gated_norm(self.norm, x, y, g, s, t, h=h, want_h=h is not None, want_n=want_n,
                                       mod_rows=None if g is None and s is None else step.seq)
 
-        n1 = norm(x, None, scale=(0, 1), shift=(0, 0), want_h=False)[1] if self.blocks else None
+        # a branch meets the residual in fp32: in the product's epilogue, or where it has a gate, in the norm
+        n1 = norm(x, scale=(0, 1), shift=(0, 0))[1] if self.blocks else None
         for l, (blk, pool, cond_pool) in enumerate(zip(self.blocks, self.self_pools, self.cond_pools)):
-            w = blk.tensors
+            w, f32 = blk.tensors, torch.float32
             kv = ec.echo_linear(n1, w["Wkv"], w["bkv"])
             q, k = ec.echo_linear(n1, w["Wq"], w["bq"]), kv[:, :D]
             if self.rotary is not None:
                 ec.echo_rotary(self.rotary, step.pos, q, k, q_out=q, k_out=k)
             ec.echo_kv_write_at(pool, step.place, k, kv[:, D:])
             a = ec.echo_kv_attention(pool, step.batch, q, causal_block=self.frame_tokens)
-            h1, nq = norm(x, ec.echo_linear(a, w["Wo"], w["bo"]), gate=(l, 2))
+            if mods is None:
+                h1 = ec.echo_linear(a, w["Wo"], w["bo"], resid=x, out_dtype=f32)
+                nq = norm(h1)[1]
+            else:
+                h1, nq = norm(x, ec.echo_linear(a, w["Wo"], w["bo"], out_dtype=f32), gate=(l, 2))
             a = ec.echo_kv_attention(cond_pool, cond, ec.echo_linear(nq, w["Wqc"], w["bqc"]))
-            h2, nf = norm(h1, ec.echo_linear(a, w["Woc"], w["boc"]), scale=(l, 4), shift=(l, 3))
-            y = ec.echo_linear(ec.echo_linear(nf, w["W1"], w["b1"], act=1), w["W2"], w["b2"])
+            h2 = ec.echo_linear(a, w["Woc"], w["boc"], resid=h1, out_dtype=f32)
+            u = ec.echo_linear(norm(h2, scale=(l, 4), shift=(l, 3))[1], w["W1"], w["b1"], act=1)
             after = (l + 1, 1) if l < last else None           # of the next block's first norm
-            x, n1 = norm(h2, y, torch.bfloat16, gate=(l, 5), scale=after,
-                         shift=None if after is None else (l + 1, 0), want_n=l < last)
+            if mods is None:
+                x = ec.echo_linear(u, w["W2"], w["b2"], resid=h2)
+                n1 = norm(x)[1] if l < last else None
+            else:
+                x, n1 = norm(h2, ec.echo_linear(u, w["W2"], w["b2"], out_dtype=f32), torch.bfloat16, gate=(l, 5),
+                             scale=after, shift=None if after is None else (l + 1, 0), want_n=l < last)
         return x
