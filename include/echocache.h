@@ -481,6 +481,9 @@ typedef struct {
     int32_t n_rows;        /* rows of the call's tensors, >= row0[n_seqs] */
     int32_t max_rows;      /* about the most rows of one sequence: it chooses between kernels
                             * and their orders of sums; the results are right for any value */
+    int32_t max_len;       /* about the most tokens of one sequence, 0: as many as a row of `table`
+                            * covers.  It decides, as max_rows does, how the work of the attention is
+                            * divided; the results are right for any value */
 } echo_kv_batch;
 
 /* The new rows' keys and values into the pages: k, v [n_rows, ld] of dtype t (head h at

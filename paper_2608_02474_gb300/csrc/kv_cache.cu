@@ -409,7 +409,7 @@ echo_status kv_check(const echo_kv_pool *p, const echo_kv_batch *b, bool *empty)
     if (!p || !b) return ECHO_ERR_INVALID_ARG;
     echo_status s = pool_sizes(p);
     if (s != ECHO_OK) return s;
-    if (b->n_seqs < 0 || b->max_pages < 0 || b->n_rows < 0 || b->max_rows < 0) return ECHO_ERR_SHAPE;
+    if (b->n_seqs < 0 || b->max_pages < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_len < 0) return ECHO_ERR_SHAPE;
     if ((s = pool_memory(p)) != ECHO_OK) return s;
     *empty = b->n_seqs == 0 || b->n_rows == 0;
     if (*empty) return ECHO_OK;

@@ -872,8 +872,8 @@ int tile_rows(int form, int d, int64_t rows) {
 template <int FORM, int D>
 echo_status launch_rows(const echo::KvAttention &a, int tile, cudaStream_t st) {
     if constexpr (FORM == kInt4 && D == 64) {
-        // 16 blocks of 256 keys for each worker, if the sequences fill their tables
-        const double keys = (double)a.batch->max_pages * a.pool->page_tokens;
+        // 16 blocks of 256 keys for each worker, if the sequences are all as long as the longest may be
+        const double keys = (double)echo::kv_longest(a);
         if (tile == 8 && (double)a.batch->n_seqs * a.pool->H * keys >= 2.0 * echo::num_sms() * 16 * 256)
             return launch<FORM, D, 1, true>(a, st);
     }

@@ -435,7 +435,15 @@ inline size_t kv_workspace_bytes(int workers, int rows, int D) {
 }
 
 namespace echo {
-// whole_keys: tables that cover no more are not divided, which saves the second launch
+// Keys of the longest sequence, whole pages of them, as far as the host knows.  A table may be as
+// wide as its pool, so that its width alone says little: a condition of 672 tokens over such a table was
+// divided and joined by a second launch.
+inline int64_t kv_longest(const KvAttention &a) {
+    const int64_t page = a.pool->page_tokens, cap = a.batch->max_pages * page;
+    const int64_t most = (a.batch->max_len + page - 1) / page * page;
+    return most > 0 && most < cap ? most : cap;
+}
+// whole_keys: sequences of no more are not divided, which saves the second launch
 inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_shift, int workers,
                       int whole_keys) {
     const echo_kv_pool &p = *a.pool;
@@ -453,7 +461,7 @@ inline KvWork kv_work(const KvAttention &a, int tile, int slot_rows, int block_s
     w.cap = (int)(cap < kMostKeys ? cap : kMostKeys);
     w.block_shift = block_shift;
     w.workers = workers;
-    w.split = cap > whole_keys;
+    w.split = kv_longest(a) > whole_keys;
     return w;
 }
 void launch_kv_join(const KvAttention &a, const KvWork &w, cudaStream_t st);

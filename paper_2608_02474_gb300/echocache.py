@@ -66,7 +66,7 @@ class KVPoolC(_c.Structure):
 
 class KVBatchC(_c.Structure):
     _fields_ = [("table", _vp), ("len", _vp), ("row0", _vp), ("n_seqs", _i32), ("max_pages", _i32),
-                ("n_rows", _i32), ("max_rows", _i32)]
+                ("n_rows", _i32), ("max_rows", _i32), ("max_len", _i32)]
 
 
 class KVTablesC(_c.Structure):
@@ -661,11 +661,12 @@ class KVBatch:
     """The sequences of one call (echo_kv_batch) over the caller's device tensors: table
     int32 [n_seqs, max_pages], lens int32 [n_seqs] (the new rows included), row0 int32
     [n_seqs + 1].  n_rows: rows of the call's tensors; max_rows: about the most rows of one
-    sequence (n_rows when not given), which only chooses between kernels.  Serves the
-    pools of every layer."""
+    sequence (n_rows when not given), which only chooses between kernels; max_len: about the
+    most tokens of one (as many as a row of the table covers when not given), which only
+    decides how the attention's work is divided.  Serves the pools of every layer."""
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, row0: torch.Tensor, n_rows: int,
-                 max_rows: int | None = None):
+                 max_rows: int | None = None, max_len: int | None = None):
         for t, n in ((table, "table"), (lens, "lens"), (row0, "row0")):
             _dev(t, n)
             if t.dtype != torch.int32:
@@ -680,8 +681,19 @@ class KVBatch:
         self.n_seqs, self.n_rows = B, int(n_rows)
         self.max_rows = self.n_rows if max_rows is None else int(max_rows)
         self.cstruct = KVBatchC(_p(table), _p(lens), _p(row0), B, table.shape[1], self.n_rows,
-                                self.max_rows)
+                                self.max_rows, 0)
         self._ref = _c.byref(self.cstruct)
+        self.max_len = max_len
+
+    @property
+    def max_len(self) -> int | None:
+        return self.cstruct.max_len or None
+
+    @max_len.setter
+    def max_len(self, n: int | None):
+        if n is not None and not 0 <= n < 2 ** 31:
+            raise ValueError("max_len is a number of tokens, or None")
+        self.cstruct.max_len = n or 0
 
 
 def _rows_of(t, name, n_rows, cols, gpu):
@@ -825,24 +837,28 @@ class KVTables:
 class KVStep:
     """What echo_kv_extend makes of a step, in the caller's tensors: the batch's table int32
     [n_seqs, max_pages], lens [n_seqs] and row0 [n_seqs + 1], and per row of the step its place in the pool
-    (int64), position and sequence (int32), -1 behind the last sequence's.  max_rows as for KVBatch."""
+    (int64), position and sequence (int32), -1 behind the last sequence's.  max_rows and max_len as for
+    KVBatch: without max_rows a batch of single tokens is taken for a chunk, and without max_len each
+    sequence for as long as max_pages allow."""
 
-    def __init__(self, table, lens, row0, place, pos, seq, max_rows: int | None = None):
+    def __init__(self, table, lens, row0, place, pos, seq, max_rows: int | None = None, max_len: int | None = None):
         self._gpu = table.get_device()
         self.n_seqs, self.n_rows = lens.numel(), place.numel()
-        self.batch = KVBatch(table, lens, row0, self.n_rows, max_rows)
+        self.batch = KVBatch(table, lens, row0, self.n_rows, max_rows, max_len)
         self._ptr = (table.data_ptr(), lens.data_ptr(), row0.data_ptr(),
                      _ints(place, "place", self._gpu, dtype=torch.int64),
                      _ints(pos, "pos", self._gpu, self.n_rows), _ints(seq, "seq", self._gpu, self.n_rows))
         self.place, self.pos, self.seq = place, pos, seq
 
     @staticmethod
-    def empty(tables: KVTables, n_seqs: int, n_rows: int, max_rows: int | None = None, stream=None) -> "KVStep":
-        """For steps of n_seqs sequences and up to n_rows rows over these tables."""
+    def empty(tables: KVTables, n_seqs: int, n_rows: int, max_rows: int | None = None, stream=None,
+              max_len: int | None = None) -> "KVStep":
+        """For steps of n_seqs sequences and up to n_rows rows over these tables, about max_rows of one
+        sequence, whose sequences have about max_len tokens at most."""
         dev = tables.table.device
         new = lambda *n, dtype=torch.int32: _empty(n, dtype, dev, stream)   # noqa: E731
         return KVStep(new(n_seqs, tables.max_pages), new(n_seqs), new(n_seqs + 1), new(n_rows, dtype=torch.int64),
-                      new(n_rows), new(n_rows), max_rows)
+                      new(n_rows), new(n_rows), max_rows, max_len)
 
 
 def echo_kv_extend(tables: KVTables, rows, step: KVStep, slots=None, stream=None) -> KVStep:

@@ -513,6 +513,8 @@ class DevicePageTable:
             raise MemoryError(f"{need} pages needed, {self.n_free} free")
         slots, n = self._numbers(rows)
         step = ec.KVStep.empty(self.tables, len(rows), sum(rows.values()), max(rows.values(), default=0))
+        # the tables are as wide as the pool; the clips are no longer than this
+        step.batch.max_len = max((self.lens[c] + n for c, n in rows.items()), default=0)
         ec.echo_kv_extend(self.tables, n, step, slots)
         self.n_free -= need
         for c, k in rows.items():
@@ -657,7 +659,7 @@ class ChunkStream:
         D, last = self.H * self.d, len(self.blocks) - 1
         # the same rows over the audio's pages: no more tokens, and these rows' numbers
         audio = self.cond_table.extend({c: 0 for c in rows}).batch
-        cond = ec.KVBatch(audio.table, audio.lens, step.batch.row0, step.n_rows, step.batch.max_rows)
+        cond = ec.KVBatch(audio.table, audio.lens, step.batch.row0, step.n_rows, step.batch.max_rows, audio.max_len)
 
         def norm(x, y=None, out=torch.float32, gate=None, scale=None, shift=None, want_n=True):
             """(h, n) with (layer, row of its modulations) for gate, scale and shift; without y, n alone."""
