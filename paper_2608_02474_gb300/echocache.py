@@ -905,6 +905,9 @@ class Rotary:
             raise ValueError(f"layout is one of {list(_LAYOUTS)}, scaling one of {list(_SCALINGS)}")
         if not 1 <= len(pairs) <= 4 or min(pairs) < 0 or not 1 <= sum(pairs) <= d // 2:
             raise ValueError("1 to 4 axes, with 1 to d / 2 pairs together")
+        # a plan with frames has one position a row, and one without as many as axes
+        if frame and (len(frame) != 2 or len(pairs) != 3 or not 0 < frame[1] <= frame[0] < 2 ** 31 or frame[0] % frame[1]):
+            raise ValueError("frame is tokens of a frame, a multiple of those of one of its rows, for three axes")
         self.d, self.pairs = d, sum(pairs)
         self.columns = 1 if frame else len(pairs)           # positions of a row
         host, size = np.zeros(self.pairs, dtype=np.uint64), _f32(0.0)
