@@ -464,7 +464,8 @@ typedef struct {
                             * 16-byte aligned */
     void *scale;           /* INT8: f32 [n_pages, 2, H, page_tokens], INT4: bf16 [n_pages, 2, H,
                             * page_tokens, d / 32] of at most 5 significant bits; 16-byte aligned;
-                            * BF16: unused */
+                            * BF16: unused.  It was a float * before there were INT4 pools: C++ that reads
+                            * it back has to cast it */
 } echo_kv_pool;
 
 /* The sequences of one call, in device memory (int32, 4-byte aligned).  Rows

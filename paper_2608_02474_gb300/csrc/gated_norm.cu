@@ -633,11 +633,14 @@ void launch_rows(const NormParams &p, cudaStream_t st) {
 
 // Rows of up to 8192 values: up to an SM's worth of them, one to a block; else four at a time where two
 // buffers of four rows fit into shared memory, and fewer otherwise.  us for 32760 rows of 5120, bf16 (198
-// at the rate of a copy): layer norm 211 (two rows at a time 277, three 249); with a norm of y
-// before it 268 (two 338); the root of the mean square, with less to do between its loads and
-// stores, 221 three at a time (four 234).  fp32 and 16380 rows 184; 20000 rows of 8192, one at a time since 1024
-// threads leave few registers, 256 (two 321); 1560 rows 13.6, 48 rows 3.7 (6.1 with the rows kernel's copies).
-// Longer rows: a block to a row.
+// at the rate of a copy): layer norm 211 (two rows at a time 277, three 249); the root of the mean square, with
+// less to do between its loads and stores, 223 three at a time (four 234).  With a norm of y before the layer norm:
+// root of the mean square 257, layer norm 283; before the root of the mean square, that of y 231.  fp32 and 16380
+// rows 183 (148); 1560 rows 13.8 (9.4: three batches a block, the last one half empty), 48 rows 3.7 (6.1 with the rows
+// kernel's copies).  From 5128 columns on one row at a time, since 1024 threads leave few registers: 20000 rows of
+// 8192 256 (193; two 321), but rows of 5632 and 6144, which need 704 and 768 threads, take 209 and 213 (133, 145): a bound of
+// their own was not tried.  More than 8192: a block to a row, neither copied ahead nor with their modulation kept:
+// 10000 rows of 8200 260 (97), of 12288 306 (145), of 16384 412 (193).
 void launch_width(const NormParams &p, cudaStream_t st) {
     const int c = p.chunks;
     if (c <= 1024) {
